@@ -211,11 +211,6 @@ bool choose_form(const ConvArgs& a, const fxpq_conv_desc& d, const char* path, i
     return true;
 }
 
-namespace {
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // cuTensorMapEncodeTiled through the runtime's driver entry point (no link-time driver dependency).
 EncodeTiledFn encode_tiled() {
     static EncodeTiledFn fn = nullptr;
@@ -232,7 +227,6 @@ EncodeTiledFn encode_tiled() {
     }
     return fn;
 }
-}  // namespace
 
 fxpq_status launch_conv_tc(const ConvArgs& a, const fxpq_conv_desc& d, cudaStream_t st, bool& launched, void* ws,
                            size_t ws_bytes) {
