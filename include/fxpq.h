@@ -497,6 +497,112 @@ FXPQ_API fxpq_status fxpq_fopt_cost(const double* d_stats, int64_t cand_stride, 
 FXPQ_API fxpq_status fxpq_top1_ties(const void* d_logits, int32_t is_int64, int32_t N, int32_t C,
                                     int32_t* d_counts, void* stream);
 
+/* ---------------------------------------------------------------------------------------- */
+/* Language-model layers in 8 bits.  The quantizer Q and its dynamic fixed-point scales (Sec. IV-B) */
+/* applied to the decoder layers of a transformer: products of 8-bit rows with a scale for each     */
+/* token and each output channel, and a paged cache of 8-bit keys and values in which every block   */
+/* (one page of one head) has its own scale.  Not part of the paper.                                */
+/* ---------------------------------------------------------------------------------------- */
+
+/* Element types of floating tensors. */
+typedef enum { FXPQ_FT_F32 = 0, FXPQ_FT_F16 = 1, FXPQ_FT_BF16 = 2 } fxpq_ftype;
+
+/* Rows to 8-bit codes with a scale each (activations: one row per token; weights: one row per output
+ * channel).  For row m with a = max_k |x[m, k]|, in fp32:
+ *   d_scale[m] = a * (1 / 127),   codes[m, k] = round_half_even(x[m, k] * ((1 / a) * 127)), |code| <= 127.
+ * A row whose largest magnitude is below 2^-100 (zeros included) gets scale 0 and codes 0.
+ * d_x: M rows of K values of type x_type, x_stride elements apart; d_codes: rows codes_stride >= K bytes
+ * apart, codes K .. codes_stride - 1 of a row are zeroed.  Non-finite values get code 0, take no part in
+ * the maximum and latch FXPQ_ERR_NONFINITE.  M and K may be 0. */
+FXPQ_API fxpq_status fxpq_quantize_tokens(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride,
+                                          int8_t* d_codes, int64_t codes_stride, float* d_scale, void* stream);
+
+/* y[m, n] = (sum_k x[m, k] w[n, k]) * d_sx[m] * d_sw[n] + d_bias[n]   (d_bias may be NULL)
+ * d_x: int8 [M, K], rows x_stride bytes apart; d_w: int8 [N, K], rows w_stride bytes apart; both 16-byte
+ * aligned with strides that are multiples of 16 (pad rows; the bytes past K are not used).  d_y: M rows of
+ * N values of type y_type, y_stride elements apart, any alignment of its type.
+ * The sum runs in fp32 over exact products: exact while every partial sum is below 2^24 (always for
+ * K < 1024), else rounded like fp32 sums.  Scales and bias are applied in fp32, one rounding to y_type.
+ * Workspace: fxpq_linear_i8_workspace bytes, 256-byte aligned, scratch (it may be 0: then d_ws may be NULL). */
+FXPQ_API size_t fxpq_linear_i8_workspace(int64_t M, int32_t N, int32_t K);
+FXPQ_API fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const float* d_sx, const int8_t* d_w,
+                                    int64_t w_stride, const float* d_sw, const float* d_bias, int64_t M, int32_t N,
+                                    int32_t K, int32_t y_type, void* d_y, int64_t y_stride, void* d_ws,
+                                    size_t ws_bytes, void* stream);
+
+/* A paged cache of keys and values: int8 codes [n_pages][heads][page][dim] each (16-byte aligned), value =
+ * code * scale with one fp32 scale > 0 for each block, a page of one head: [n_pages][heads].  page is 16,
+ * 32, 64 or 128 tokens; dim is 64 or 128. */
+typedef struct {
+    int8_t* d_k;
+    int8_t* d_v;
+    float* d_k_scale;
+    float* d_v_scale;
+    int32_t n_pages, page, heads, dim;
+} fxpq_kv_cache;
+
+/* A batch of sequences in such a cache.  Sequence b holds d_lens[b] tokens, its new ones included, token p
+ * in slot p % page of page d_pages[b * pages_stride + p / page].  The new tokens of all sequences lie in one
+ * list of n_tokens rows: those of sequence b are rows d_starts[b] .. d_starts[b + 1] - 1 and its last
+ * tokens (d_starts: n_seqs + 1 entries from 0 to n_tokens, ascending), or with d_starts NULL every
+ * sequence has n_tokens / n_seqs of them.  Entries of d_pages past a sequence's pages are not read.
+ * A page id outside the cache, or a sequence longer than max_pages pages, latches FXPQ_ERR_RANGE and the
+ * tokens there are neither written nor attended to.  New rows that would lie before position 0 (a sequence of
+ * fewer tokens than it has new rows, such as the padding of a batch of fixed size: length 0) are not
+ * appended, their rotated queries are zeros, and they attend to nothing. */
+typedef struct {
+    const int32_t* d_pages;
+    const int32_t* d_lens;
+    const int32_t* d_starts;
+    int32_t n_seqs, max_pages, n_tokens, reserved;
+    int64_t pages_stride;
+} fxpq_kv_batch;
+
+/* New rows [n_tokens][heads][dim] of type `type` with strides in elements between tokens and heads (views
+ * of a fused projection need no copy); the dim values of a head are contiguous. */
+typedef struct {
+    const void* d_x;
+    int64_t token_stride, head_stride;
+} fxpq_kv_rows;
+
+/* Appends the batch's new keys and values to the cache.
+ * Rotation: with d_cos, d_sin ([n_positions][rot / 2] fp32, 16-byte aligned; rot a multiple of 8, <= dim) the
+ * first rot values of each key turn by the token's position p, in fp32 with every product and sum rounded:
+ *   (a, b) -> (a cos[p][i] - b sin[p][i], b cos[p][i] + a sin[p][i])
+ * for the pairs (a, b) = (x[i], x[i + rot / 2]), or (x[2 i], x[2 i + 1]) with interleaved.  rot = 0: none.
+ * Queries (q->d_x not NULL) of q_heads heads turn likewise into d_q_out, contiguous [n_tokens][q_heads][dim].
+ * A token at a position >= n_positions latches FXPQ_ERR_RANGE, is not appended, and its queries are zeros.
+ * Blocks: a block's scale is the smallest 2^-FL, FL in [-32, 40], with max |value| <= 127 * 2^-FL over the
+ * values appended to it; a block that already held tokens keeps its scale unless the new values need a
+ * larger one, and its codes are then rounded again: code = round_half_even(code * (old scale / new scale)).
+ * Codes are round_half_even(value / scale), clipped to [-128, 127].  Non-finite values get code 0, do not count for the
+ * scale and latch FXPQ_ERR_NONFINITE.  Appending the same rows again changes nothing.  No page may hold
+ * new tokens of two sequences. */
+FXPQ_API fxpq_status fxpq_kv_append(const fxpq_kv_cache* cache, const fxpq_kv_batch* batch, int32_t type,
+                                    const fxpq_kv_rows* k, const fxpq_kv_rows* v, const fxpq_kv_rows* q, int32_t q_heads,
+                                    void* d_q_out, const float* d_cos, const float* d_sin, int32_t n_positions,
+                                    int32_t rot, int32_t interleaved, void* stream);
+
+/* Values code * scale of the pages d_list[0 .. n - 1], rounded to `type`: d_k_out, d_v_out
+ * [n][heads][page][dim] (16-byte aligned; either may be NULL).  Pages outside the cache read as zeros and
+ * latch FXPQ_ERR_RANGE. */
+FXPQ_API fxpq_status fxpq_kv_values(const fxpq_kv_cache* cache, const int32_t* d_list, int32_t n, int32_t type,
+                                    void* d_k_out, void* d_v_out, void* stream);
+
+/* Softmax attention of the batch's new tokens over the cache (which already holds their keys and values):
+ *   out[t, h] = sum_p softmax_p(scale * q[t, h] . key[p, h / (q_heads / heads)]) value[p, ...]
+ * over the positions p of the token's sequence, with `causal` only those up to its own.  q->d_x: rows of
+ * q_heads heads (a multiple of cache->heads) of type F16 or BF16; d_out: contiguous [n_tokens][q_heads][dim]
+ * of the same type, 16-byte aligned; d_lse (may be NULL): fp32 [n_tokens][q_heads], the natural logarithm of the sum
+ * of exponentials.  A row that sees no key gives zeros and lse -inf.  softmax_scale > 0.
+ * Queries are held in fp16 with a power of two per row (nothing is lost of bf16 or fp16 values within 2^-31
+ * of their row's largest), codes are exact, products sum in fp32; the probabilities are rounded to
+ * fp16.  Workspace: fxpq_kv_attention_workspace bytes, 256-byte aligned, scratch. */
+FXPQ_API size_t fxpq_kv_attention_workspace(const fxpq_kv_cache* cache, const fxpq_kv_batch* batch, int32_t q_heads);
+FXPQ_API fxpq_status fxpq_kv_attention(const fxpq_kv_cache* cache, const fxpq_kv_batch* batch, int32_t type,
+                                       const fxpq_kv_rows* q, int32_t q_heads, float softmax_scale, int32_t causal,
+                                       void* d_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+
 /* Synchronises `stream`, returns and clears the latched device status (FXPQ_OK if none). */
 FXPQ_API fxpq_status fxpq_get_device_status(void* stream);
 

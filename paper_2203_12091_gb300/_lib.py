@@ -70,12 +70,27 @@ class Net(ctypes.Structure):
                 ("fmt_in", Fmt), ("ops", ctypes.POINTER(OpDesc))]
 
 
+class KVCacheDesc(ctypes.Structure):
+    _fields_ = [("d_k", VP), ("d_v", VP), ("d_k_scale", VP), ("d_v_scale", VP),
+                ("n_pages", I32), ("page", I32), ("heads", I32), ("dim", I32)]
+
+
+class KVBatchDesc(ctypes.Structure):
+    _fields_ = [("d_pages", VP), ("d_lens", VP), ("d_starts", VP), ("n_seqs", I32), ("max_pages", I32),
+                ("n_tokens", I32), ("reserved", I32), ("pages_stride", I64)]
+
+
+class KVRows(ctypes.Structure):
+    _fields_ = [("d_x", VP), ("token_stride", I64), ("head_stride", I64)]
+
+
 # status / dtype / mode constants (mirror of include/fxpq.h)
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_NONFINITE, ERR_TIMEOUT, ERR_CUDA, ERR_WORKSPACE, ERR_RANGE = range(8)
 DT_I8, DT_U8, DT_I16, DT_U16, DT_I32, DT_F16 = range(6)
 SCORE_L2, SCORE_L1 = 0, 1
 OUT_CODES, OUT_ACC64, OUT_F32 = range(3)
 QB_ROWS_F16, QB_FLAT_I32 = range(2)
+FT_F32, FT_F16, FT_BF16 = range(3)
 OP_CONV, OP_MAXPOOL, OP_ELTWISE, OP_AVGPOOL = range(4)
 
 _SIGS = {
@@ -119,6 +134,13 @@ _SIGS = {
     "fxpq_qlayer": (I32, [VP, I64, I32, I32, Fmt, VP, VP]),
     "fxpq_net_workspace": (SZ, [ctypes.POINTER(Net), I32]),
     "fxpq_net_forward": (I32, [ctypes.POINTER(Net), VP, I32, VP, ctypes.POINTER(I32), VP, SZ, VP]),
+    "fxpq_quantize_tokens": (I32, [VP, I32, I64, I32, I64, VP, I64, VP, VP]),
+    "fxpq_linear_i8_workspace": (SZ, [I64, I32, I32]),
+    "fxpq_linear_i8": (I32, [VP, I64, VP, VP, I64, VP, VP, I64, I32, I32, I32, VP, I64, VP, SZ, VP]),
+    "fxpq_kv_append": (I32, [VP, VP, I32, VP, VP, VP, I32, VP, VP, VP, I32, I32, I32, VP]),
+    "fxpq_kv_values": (I32, [VP, VP, I32, I32, VP, VP, VP]),
+    "fxpq_kv_attention_workspace": (SZ, [VP, VP, I32]),
+    "fxpq_kv_attention": (I32, [VP, VP, I32, VP, I32, ctypes.c_float, I32, VP, VP, VP, SZ, VP]),
     "fxpq_get_device_status": (I32, [VP]),
     "fxpq_status_string": (ctypes.c_char_p, [I32]),
     "fxpq_launch_count": (I64, []),

@@ -327,6 +327,45 @@ def fxpq_net_forward(net: L.Net, images, batch, logits, ws, stream=None) -> int:
     return scale.value
 
 
+# ------------------------------------------------------------------------------ language-model layers in 8 bits
+def fxpq_quantize_tokens(x, x_type: int, M: int, K: int, x_stride: int, codes, codes_stride: int, scale, stream=None):
+    L.check("fxpq_quantize_tokens", L.lib().fxpq_quantize_tokens(_p(x), x_type, M, K, x_stride, _p(codes), codes_stride,
+                                                                 _p(scale), _s(stream)))
+
+
+def fxpq_linear_i8_workspace(M: int, N: int, K: int) -> int:
+    return L.lib().fxpq_linear_i8_workspace(M, N, K)
+
+
+def fxpq_linear_i8(x, x_stride: int, sx, w, w_stride: int, sw, bias, M: int, N: int, K: int, y_type: int, y, y_stride: int,
+                   ws=None, stream=None):
+    L.check("fxpq_linear_i8", L.lib().fxpq_linear_i8(_p(x), x_stride, _p(sx), _p(w), w_stride, _p(sw), _p(bias), M, N, K,
+                                                     y_type, _p(y), y_stride, _p(ws), 0 if ws is None else ws.nbytes,
+                                                     _s(stream)))
+
+
+def fxpq_kv_append(cache: L.KVCacheDesc, batch: L.KVBatchDesc, ftype: int, k: L.KVRows, v: L.KVRows, q, q_heads: int,
+                   q_out, cos, sin, n_positions: int, rot: int, interleaved: int, stream=None):
+    L.check("fxpq_kv_append", L.lib().fxpq_kv_append(
+        ctypes.byref(cache), ctypes.byref(batch), ftype, ctypes.byref(k), ctypes.byref(v),
+        None if q is None else ctypes.byref(q), q_heads, _p(q_out), _p(cos), _p(sin), n_positions, rot, interleaved, _s(stream)))
+
+
+def fxpq_kv_values(cache: L.KVCacheDesc, pages, n: int, ftype: int, k_out, v_out, stream=None):
+    L.check("fxpq_kv_values", L.lib().fxpq_kv_values(ctypes.byref(cache), _p(pages), n, ftype, _p(k_out), _p(v_out), _s(stream)))
+
+
+def fxpq_kv_attention_workspace(cache: L.KVCacheDesc, batch: L.KVBatchDesc, q_heads: int) -> int:
+    return L.lib().fxpq_kv_attention_workspace(ctypes.byref(cache), ctypes.byref(batch), q_heads)
+
+
+def fxpq_kv_attention(cache: L.KVCacheDesc, batch: L.KVBatchDesc, ftype: int, q: L.KVRows, q_heads: int, scale: float,
+                      causal: int, out, lse=None, ws=None, stream=None):
+    L.check("fxpq_kv_attention", L.lib().fxpq_kv_attention(
+        ctypes.byref(cache), ctypes.byref(batch), ftype, ctypes.byref(q), q_heads, scale, causal, _p(out), _p(lse), _p(ws),
+        0 if ws is None else ws.nbytes, _s(stream)))
+
+
 def fxpq_get_device_status(stream=None) -> int:
     return int(L.lib().fxpq_get_device_status(_s(stream)))
 
