@@ -1,71 +1,43 @@
-// fxpq_attend.cu -- softmax attention over the paged cache of 8-bit keys and values.
-#include <cfloat>
-
-#include "fxpq_llm.cuh"
-
-namespace fxpq {
-namespace llm {
-namespace {
-
-struct AttendArgs {
-    Seqs s;
-    fxpq_kv_cache c;
-    const void* q;
-    long long q_token, q_head;
-    void* out;
-    float* lse;
-    int q_heads, causal;
-    float scale;
-    int* status;
-};
-
-// One warp per new token and query head, one key at a time: the running maximum and sum of the softmax.
-template <typename T>
-__global__ void __launch_bounds__(128) attend_kernel(const AttendArgs A) {
-    pdl_wait();
-    const long long u = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31, D = A.c.dim, E = D / 32;
-    if (u >= (long long)A.s.n_tokens * A.q_heads) return;
-    const int t = (int)(u / A.q_heads), h = (int)(u - (long long)t * A.q_heads), hk = h / (A.q_heads / A.c.heads);
-    int b = A.s.starts ? 0 : t / A.s.each, first = 0, count = 0;
-    if (A.s.starts)
-        while (b < A.s.n_seqs - 1 && A.s.starts[b + 1] <= t) ++b;
-    new_rows(A.s, b, first, count);
-    const int len = A.s.lens[b], pos = len - count + (t - first);
-    const int end = pos < 0 ? 0 : A.causal ? min(pos + 1, len) : len;
-    float q[4], o[4] = {0, 0, 0, 0}, m = -INFINITY, l = 0.0f;
-    for (int e = 0; e < E; ++e) q[e] = to_f32(static_cast<const T*>(A.q)[t * A.q_token + h * A.q_head + E * lane + e]);
-    for (int p = 0; p < end; ++p) {
-        const int pi = p / A.c.page, pid = pi < A.s.max_pages ? A.s.pages[b * A.s.pages_stride + pi] : -1;
-        if ((unsigned)pid >= (unsigned)A.c.n_pages) {
-            if (lane == 0) latch_status(A.status, FXPQ_ERR_RANGE);
-            continue;
-        }
-        const long long block = (long long)pid * A.c.heads + hk, at = (block * A.c.page + p % A.c.page) * D + E * lane;
-        float s = 0.0f;
-        for (int e = 0; e < E; ++e) s += q[e] * (float)A.c.d_k[at + e];
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        s *= A.c.d_k_scale[block] * A.scale;
-        const float top = fmaxf(m, s), f = expf(m - top), w = expf(s - top);
-        l = l * f + w;
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + w * (float)A.c.d_v[at + e] * A.c.d_v_scale[block];
-        m = top;
-    }
-    for (int e = 0; e < E; ++e)
-        static_cast<T*>(A.out)[((long long)t * A.q_heads + h) * D + E * lane + e] = from_f32<T>(m > -INFINITY || !(l == 0.0f) ? o[e] / l : 0.0f);
-    if (A.lse && lane == 0) A.lse[(long long)t * A.q_heads + h] = !(l == 0.0f) ? m + logf(l) : -INFINITY;
-}
-
-}  // namespace
-}  // namespace llm
-}  // namespace fxpq
+// fxpq_attend.cu -- softmax attention over the paged cache of 8-bit keys and values: checks, choice of kernel.
+#include "fxpq_attend.cuh"
 
 using namespace fxpq;
 using namespace fxpq::llm;
 
+namespace {
+
+// Codes as [n_pages * heads][page][dim] bytes, boxes of one page's `rows` rows, swizzled by their row size.
+bool encode_codes(CUtensorMap* map, const fxpq_kv_cache& c, const int8_t* codes, int rows) {
+    EncodeTiledFn enc = encode_tiled();
+    const cuuint64_t dims[3] = {(cuuint64_t)c.dim, (cuuint64_t)c.page, (cuuint64_t)c.n_pages * c.heads};
+    const cuuint64_t strides[2] = {(cuuint64_t)c.dim, (cuuint64_t)c.dim * c.page};
+    const cuuint32_t box[3] = {(cuuint32_t)c.dim, (cuuint32_t)(rows < c.page ? rows : c.page), 1}, es[3] = {1, 1, 1};
+    return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<int8_t*>(codes), dims, strides, box, es,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, c.dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// How a batch is computed.  New tokens per sequence are known on the host only on average.
+struct Plan {
+    int nt;      // 8 nt query rows share a read of the cache
+    bool whole;  // one CTA per unit
+    size_t ws;
+};
+Plan plan(const fxpq_kv_cache& c, const fxpq_kv_batch& b, int q_heads) {
+    Plan p;
+    const long long group = q_heads / c.heads, seqs = b.n_seqs > 0 ? b.n_seqs : 1;
+    p.nt = stream_nt((b.n_tokens * group + seqs - 1) / seqs);
+    // A cache of at most 2048 tokens is one CTA's work; longer ones are cut into equal shares for all CTAs.
+    p.whole = (long long)b.max_pages * c.page <= 2048;
+    p.ws = p.whole ? 0 : (attend_stream_workspace(c.dim, p.nt) + 255) / 256 * 256;
+    return p;
+}
+
+}  // namespace
+
 extern "C" size_t fxpq_kv_attention_workspace(const fxpq_kv_cache* cache, const fxpq_kv_batch* batch, int32_t q_heads) {
-    (void)cache, (void)batch, (void)q_heads;
-    return 0;
+    if (!cache_ok(cache) || !batch_ok(batch) || q_heads <= 0 || q_heads % cache->heads) return 0;
+    return plan(*cache, *batch, q_heads).ws;
 }
 
 extern "C" fxpq_status fxpq_kv_attention(const fxpq_kv_cache* cache, const fxpq_kv_batch* batch, int32_t type, const fxpq_kv_rows* q,
@@ -77,16 +49,22 @@ extern "C" fxpq_status fxpq_kv_attention(const fxpq_kv_cache* cache, const fxpq_
     if (type == FXPQ_FT_F32) return FXPQ_ERR_UNSUPPORTED;
     if (batch->n_tokens == 0) return FXPQ_OK;
     if (!q->d_x || !aligned(q->d_x, 2) || !d_out || !aligned(d_out, 16) || !aligned(d_lse, 4)) return FXPQ_ERR_INVALID_ARG;
-    const size_t need = fxpq_kv_attention_workspace(cache, batch, q_heads);
-    if (need && (!d_ws || ws_bytes < need || !aligned(d_ws, 256))) return FXPQ_ERR_WORKSPACE;
-    const AttendArgs A = {make_seqs(*batch), *cache, q->d_x, (long long)q->token_stride, (long long)q->head_stride, d_out, d_lse,
-                          q_heads, causal, softmax_scale, status_ptr()};
-    const long long units = (long long)batch->n_tokens * q_heads;
-    if ((units + 3) / 4 > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((units + 3) / 4));
-    if (type == FXPQ_FT_F16)
-        launch_pdl(attend_kernel<__half>, grid, dim3(128), 0, as_stream(stream), A);
-    else
-        launch_pdl(attend_kernel<__nv_bfloat16>, grid, dim3(128), 0, as_stream(stream), A);
-    return after_launch("kv_attention");
+    if ((long long)cache->n_pages * cache->heads > INT32_MAX || (long long)batch->n_tokens * q_heads > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
+    const Plan p = plan(*cache, *batch, q_heads);
+    if (p.ws && (!d_ws || ws_bytes < p.ws || !aligned(d_ws, 256))) return FXPQ_ERR_WORKSPACE;
+    AttendArgs A;
+    if (!encode_codes(&A.tk, *cache, cache->d_k, 32) || !encode_codes(&A.tv, *cache, cache->d_v, 32)) return FXPQ_ERR_CUDA;
+    A.s = make_seqs(*batch);
+    A.k_scale = cache->d_k_scale, A.v_scale = cache->d_v_scale;
+    A.q = q->d_x, A.q_token = q->token_stride, A.q_head = q->head_stride;
+    A.out = d_out, A.lse = d_lse, A.part = static_cast<float*>(d_ws);
+    A.n_pages = cache->n_pages, A.page = cache->page, A.heads = cache->heads, A.q_heads = q_heads, A.group = q_heads / cache->heads;
+    A.q_f16 = type == FXPQ_FT_F16;
+    A.q_vec = aligned(q->d_x, 16) && q->token_stride % 8 == 0 && q->head_stride % 8 == 0;
+    A.causal = causal;
+    A.few = INT32_MAX;
+    A.few_only = 0;
+    A.scale = softmax_scale;
+    A.status = status_ptr();
+    return launch_attend_stream(A, cache->dim, p.nt, p.whole, as_stream(stream));
 }

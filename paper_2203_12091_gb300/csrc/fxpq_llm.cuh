@@ -5,6 +5,8 @@
 #include "fxpq_common.cuh"
 
 namespace fxpq {
+int num_sms();  // of the current device (fxpq_conv_tc.cu)
+
 namespace llm {
 
 inline bool ftype_ok(int t) { return t == FXPQ_FT_F32 || t == FXPQ_FT_F16 || t == FXPQ_FT_BF16; }
