@@ -40,14 +40,6 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
-// Two codes (bytes 0, 1 or 2, 3 of x, sign bits flipped) as fp16: 0x6400 + u is 1024 + u, minus 1152.
-__device__ __forceinline__ uint32_t code_pair(uint32_t x, uint32_t sel) {
-    const uint32_t w = __byte_perm(x, 0x64646464u, sel);
-    return h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&w), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480))));
-}
-constexpr uint32_t LOW_PAIR = 0x4140, HIGH_PAIR = 0x4342;
-
 // The power of two that brings a row's largest value into [2^14, 2^15) (rows of zeros or not finite: 1).
 __device__ __forceinline__ int q_exponent(float amax) {
     const int e = (__float_as_int(amax) >> 23) - 127;

@@ -3,6 +3,7 @@
 #include <cfloat>
 
 #include "fxpq_llm.cuh"
+#include "fxpq_ptx.cuh"
 
 namespace fxpq {
 namespace llm {
@@ -86,14 +87,6 @@ __global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __
     for (long long i = K + t; i < c_stride; i += QT_THREADS) out[i] = 0;
 }
 
-struct LinArgs {
-    const int8_t *x, *w;
-    const float *sx, *sw, *bias;
-    void* y;
-    long long xs, ws, ys, M;
-    int N, K, y_type;
-};
-
 __device__ __forceinline__ void store_y(void* y, int type, long long at, float v) {
     if (type == FXPQ_FT_F32)
         static_cast<float*>(y)[at] = v;
@@ -103,41 +96,230 @@ __device__ __forceinline__ void store_y(void* y, int type, long long at, float v
         static_cast<__nv_bfloat16*>(y)[at] = __float2bfloat16_rn(v);
 }
 
-// 64 x 64 outputs per block of 256 threads, 64 codes of the reduction at a time in shared memory.
-__global__ void __launch_bounds__(256) linear_i8_kernel(const LinArgs A) {
-    pdl_wait();
-    __shared__ int sx[64][17], sw[64][17];
-    const long long m0 = (long long)blockIdx.y * 64;
-    const int n0 = blockIdx.x * 64, t = threadIdx.x, tx = t & 15, ty = t >> 4;
-    int acc[4][4] = {};
-    for (int k0 = 0; k0 < A.K; k0 += 64) {
-        for (int i = t; i < 64 * 16; i += 256) {
-            const int r = i / 16, k = k0 + 4 * (i % 16);
-            int a = 0, b = 0;
-            if (k < A.K) {
-                const int mask = A.K - k >= 4 ? -1 : (1 << (8 * (A.K - k))) - 1;
-                if (m0 + r < A.M) a = *reinterpret_cast<const int*>(A.x + (m0 + r) * A.xs + k) & mask;
-                if (n0 + r < A.N) b = *reinterpret_cast<const int*>(A.w + (long long)(n0 + r) * A.ws + k) & mask;
-            }
-            sx[r][i % 16] = a;
-            sw[r][i % 16] = b;
+struct LinArgs {
+    CUtensorMap tw, tx;  // codes as [N][K], [M][K] bytes, boxes of 128 codes x 128 (tw) or `cols` (tx) rows
+    const float *sx, *sw, *bias;
+    void* y;
+    long long ys, M;
+    int N, y_type, n_kb;
+    int cols;  // tokens of a tile: a multiple of 16, at most 128
+    int stages;
+    int* status;
+};
+
+// ------------------------------------------------------------------ few tokens
+// y^T = w x^T on tcgen05 (kind::f16: the 8-bit kind does not exist on sm_103a; products of codes are exact in fp16): 128
+// output channels on the accumulator's lanes, up to 128 tokens on its columns.  The weights are the traffic.  They
+// arrive as codes (TMA, 128 x 128 bytes a block) and go through registers into tensor memory as the fp16 A operand,
+// so that their shared-memory traffic stays at two bytes a code; the tokens' few rows are expanded in shared memory.
+//   warp 0   copies;   warp 1   tensor memory, products;   warps 4-7, 8-11   converters (blocks in turn), then the epilogue.
+// The reduction is shared by the CTAs of a cluster, whose fp32 sums meet through distributed shared memory: one launch, a
+// fixed order.  Up to 64 tokens two CTAs fit an SM.
+constexpr int LS_THREADS = 384, LS_KB = 128, LS_A = 128 * LS_KB;
+
+__host__ __device__ inline int ls_smem(int cols, int stages) {  // raw stages, two expanded token stages
+    const int ring = stages * (LS_A + cols * LS_KB) + 2 * cols * LS_KB * 2, sums = cols * 128 * 4;
+    return 1024 + (ring > sums ? ring : sums);
+}
+
+__global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_constant__ LinArgs P) {
+    using namespace tc;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    __shared__ __align__(8) uint64_t bars[8 + 2 + 2 + 1 + 8];
+    __shared__ int abort_flag;
+    __shared__ uint32_t tmem_slot;
+    volatile int* abort = &abort_flag;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, ST = P.stages, cols = P.cols;
+    const uint32_t raw_full = smem_u32(bars), raw_empty = raw_full + 8 * 8, conv_full = raw_empty + 8 * 8, conv_empty = conv_full + 16,
+                   done = conv_empty + 16;
+    const int raw_bytes = LS_A + cols * LS_KB;
+    const uint32_t raw0 = smem_u32(smem), conv0 = raw0 + ST * raw_bytes;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(raw_full + 8 * i, 1);
+            mbar_init(raw_empty + 8 * i, 4);
         }
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < 16; ++q)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(sx[ty + 16 * i][q], sw[tx + 16 * j][q], acc[i][j]);
-        __syncthreads();
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(conv_full + 8 * i, 4);
+            mbar_init(conv_empty + 8 * i, 1);
+        }
+        mbar_init(done, 1);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (P.n_kb) {
+            prefetch_tmap(&P.tw);
+            prefetch_tmap(&P.tx);
+        }
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const long long m = m0 + ty + 16 * i;
-            const int n = n0 + tx + 16 * j;
-            if (m < A.M && n < A.N)
-                store_y(A.y, A.y_type, m * A.ys + n, (float)acc[i][j] * A.sx[m] * A.sw[n] + (A.bias ? A.bias[n] : 0.0f));
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(256u));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    pdl_wait();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot, tmem_a = tmem + 128;
+    const int rank = blockIdx.x, shares = gridDim.x, n0 = blockIdx.y * 128;
+    const long long m0 = (long long)blockIdx.z * cols;
+    const int kb0 = (int)((long long)P.n_kb * rank / shares), n_kb = (int)((long long)P.n_kb * (rank + 1) / shares) - kb0;
+
+    if (warp == 0) {
+        int i = 0;
+        for (; i < n_kb; ++i) {
+            const int s = i % ST;
+            if (!wait_warp(raw_empty + 8 * s, ((i / ST) & 1) ^ 1, abort, P.status)) break;
+            const uint32_t bar = raw_full + 8 * s, dst = raw0 + s * raw_bytes;
+            mbar_arrive_expect_tx(bar, (uint32_t)raw_bytes);
+            tma_load_2d(dst, &P.tw, (kb0 + i) * LS_KB, n0, bar);
+            tma_load_2d(dst + LS_A, &P.tx, (kb0 + i) * LS_KB, (int)m0, bar);
         }
+        for (int j = max(0, i - ST); j < i; ++j) {  // every copy has landed before this CTA's memory is used again
+            const long long t0 = clock64();
+            while (!mbar_try_wait(raw_full + 8 * (j % ST), (j / ST) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {
+            }
+        }
+    } else if (warp == 1) {
+        const uint32_t idesc = make_idesc(128, cols);
+        const uint64_t bdesc = make_sdesc(conv0);
+        for (int i = 0; i < n_kb; ++i) {
+            const int c = i & 1;
+            if (!wait_warp(conv_full + 8 * c, (i >> 1) & 1, abort, P.status)) break;
+            tc_fence_after();
+#pragma unroll
+            for (int kk = 0; kk < LS_KB / 16; ++kk)
+                tc_mma_ta(tmem, tmem_a + 64 * c + 8 * kk, bdesc + (uint64_t)((c * cols * 256 + (kk >> 2) * cols * 128) >> 4) + 2 * (kk & 3), idesc,
+                          i > 0 || kk > 0);
+            tc_commit(conv_empty + 8 * c);
+        }
+        tc_commit(done);
+        const long long t0 = clock64();
+        while (!mbar_try_wait(done, 0) && clock64() - t0 < TC_WAIT_CYCLES) {
+        }
+    } else if (warp >= 4) {
+        const int grp = (warp - 4) >> 2, quad = warp & 3, t = threadIdx.x & 127, row = quad * 32 + lane;
+        for (int i = grp; i < n_kb; i += 2) {
+            const int s = i % ST;
+            if (!wait_warp(raw_full + 8 * s, (i / ST) & 1, abort, P.status)) break;
+            if (!wait_warp(conv_empty + 8 * grp, ((i >> 1) & 1) ^ 1, abort, P.status)) break;
+            tc_fence_after();
+            const unsigned char* ra = smem + s * raw_bytes;
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {  // 64 codes of this thread's channel
+                uint32_t r[32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(ra + row * 128 + (((4 * hf + q) ^ (row & 7)) << 4));
+                    const uint32_t w[4] = {v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        r[8 * q + 2 * e] = code_pair(w[e], LOW_PAIR);
+                        r[8 * q + 2 * e + 1] = code_pair(w[e], HIGH_PAIR);
+                    }
+                }
+                tmem_st32_nw(tmem_a + ((uint32_t)(quad * 32) << 16) + 64 * grp + 32 * hf, r);
+            }
+            const unsigned char* rb = ra + LS_A;
+            unsigned char* cb = smem + ST * raw_bytes + grp * cols * 256;
+            for (int rr = t >> 3; rr < cols; rr += 16) {  // 16 codes of one token
+                const int c = t & 7, hf = c >> 2;
+                const uint4 v = *reinterpret_cast<const uint4*>(rb + rr * 128 + ((c ^ (rr & 7)) << 4));
+                uint4 o[2];
+                uint32_t x = v.x ^ 0x80808080u, y = v.y ^ 0x80808080u;
+                o[0] = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
+                x = v.z ^ 0x80808080u, y = v.w ^ 0x80808080u;
+                o[1] = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
+                unsigned char* dst = cb + hf * cols * 128 + rr * 128;
+                const int j = 2 * (c & 3);
+                // (the second half's lanes begin with their odd chunk, else the two halves meet in the banks)
+                *reinterpret_cast<uint4*>(dst + (((j + hf) ^ (rr & 7)) << 4)) = hf ? o[1] : o[0];
+                *reinterpret_cast<uint4*>(dst + (((j + 1 - hf) ^ (rr & 7)) << 4)) = hf ? o[0] : o[1];
+            }
+            tmem_wait_st();
+            fence_proxy_async();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(raw_empty + 8 * s);
+                mbar_arrive(conv_full + 8 * grp);
+            }
+        }
+        // ---- this CTA's sums to shared memory: [token][128 channels]
+        float* sums = reinterpret_cast<float*>(smem);
+        if (n_kb > 0) wait_warp(done, 0, abort, P.status);
+        tc_fence_after();
+        for (int c = 16 * grp; c < cols; c += 32) {
+            uint32_t v[16];
+            tmem_ld16_nw(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
+            tmem_wait_ld();
+            reg_fence(v);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sums[(c + e) * 128 + row] = n_kb > 0 ? __uint_as_float(v[e]) : 0.0f;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u));
+    }
+    // ---- four channels of one token per thread and step, summed over the cluster
+    if (shares > 1) cluster_sync();
+    const int c_lo = cols * rank / shares, c_hi = (int)min((long long)(cols * (rank + 1) / shares), P.M - m0);
+    for (int i = c_lo * 32 + threadIdx.x; i < c_hi * 32; i += LS_THREADS) {
+        const int c = i >> 5, ch = n0 + 4 * (i & 31);
+        const uint32_t at = raw0 + (uint32_t)i * 16;
+        float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int r = 0; r < shares; ++r) {
+            const float4 b = ld_cluster_f4(cluster_addr(at, r));
+            a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w;
+        }
+        const float v[4] = {a.x, a.y, a.z, a.w}, sx = __ldg(P.sx + m0 + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (ch + e < P.N)
+                store_y(P.y, P.y_type, (m0 + c) * P.ys + ch + e,
+                        fmaf(v[e] * sx, __ldg(P.sw + ch + e), P.bias ? __ldg(P.bias + ch + e) : 0.0f));
+    }
+    if (shares > 1) cluster_sync();  // (the others have read this CTA's sums)
+}
+
+// Codes as [rows][K] bytes in boxes of 128 codes x `box` rows, 128-byte swizzle.
+bool encode_rows(CUtensorMap* map, const int8_t* codes, long long rows, int K, long long stride, int box) {
+    EncodeTiledFn enc = encode_tiled();
+    const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
+    const cuuint32_t b[2] = {(cuuint32_t)LS_KB, (cuuint32_t)box}, es[2] = {1, 1};
+    return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(codes), dims, strides, b, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+fxpq_status launch_few(LinArgs& P, cudaStream_t st) {
+    static bool set = false;
+    if (!set) {
+        if (cudaFuncSetAttribute(linear_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ls_smem(128, 4)) != cudaSuccess) return FXPQ_ERR_CUDA;
+        set = true;
+    }
+    const long long tn = (P.N + 127) / 128, tm = (P.M + P.cols - 1) / P.cols;
+    if (tn > 65535 || tm > 65535) return FXPQ_ERR_UNSUPPORTED;
+    const int room = (P.cols <= 64 ? 2 : 1) * num_sms();
+    int shares = 1;
+    while (shares < 8 && tn * tm * shares * 2 <= room && P.n_kb >= 4 * shares) shares *= 2;
+    P.stages = P.cols <= 32 ? 4 : 3;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = shares, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3((unsigned)shares, (unsigned)tn, (unsigned)tm);
+    c.blockDim = dim3(LS_THREADS);
+    c.dynamicSmemBytes = ls_smem(P.cols, P.stages);
+    c.stream = st;
+    c.attrs = at;
+    c.numAttrs = shares > 1 ? 2 : 1;
+    (void)cudaLaunchKernelEx(&c, linear_few_kernel, P);
+    return after_launch("linear_few");
 }
 
 }  // namespace
@@ -186,7 +368,11 @@ extern "C" fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const
         return FXPQ_ERR_INVALID_ARG;
     const size_t need = fxpq_linear_i8_workspace(M, N, K);
     if (need && (!d_ws || ws_bytes < need || !aligned(d_ws, 256))) return FXPQ_ERR_WORKSPACE;
-    const LinArgs A = {d_x, d_w, d_sx, d_sw, d_bias, d_y, x_stride, w_stride, y_stride, M, N, K, y_type};
-    launch_pdl(linear_i8_kernel, dim3((unsigned)((N + 63) / 64), (unsigned)((M + 63) / 64)), dim3(256), 0, as_stream(stream), A);
-    return after_launch("linear_i8");
+    LinArgs P;
+    P.cols = M >= 128 ? 128 : (int)(M + 15) / 16 * 16;
+    P.n_kb = (K + LS_KB - 1) / LS_KB;
+    if (K > 0 && (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_rows(&P.tx, d_x, M, K, x_stride, P.cols))) return FXPQ_ERR_CUDA;
+    P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.y_type = y_type;
+    P.status = status_ptr();
+    return launch_few(P, as_stream(stream));
 }

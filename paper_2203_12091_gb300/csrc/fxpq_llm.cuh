@@ -59,6 +59,14 @@ __device__ __forceinline__ void store_f32(T* p, const float (&v)[N]) {  // align
     }
 }
 
+__device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+// Two codes (bytes 0, 1 or 2, 3 of x, sign bits flipped) as fp16: 0x6400 + u is 1024 + u, minus 1152.
+__device__ __forceinline__ uint32_t code_pair(uint32_t x, uint32_t sel) {
+    const uint32_t w = __byte_perm(x, 0x64646464u, sel);
+    return h2_bits(__hsub2(*reinterpret_cast<const __half2*>(&w), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480))));
+}
+constexpr uint32_t LOW_PAIR = 0x4140, HIGH_PAIR = 0x4342;
+
 // Four codes in a word, first one in the low byte.
 __device__ __forceinline__ uint32_t pack_i8(int a, int b, int c, int d) {
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
