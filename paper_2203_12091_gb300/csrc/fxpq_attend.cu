@@ -17,19 +17,36 @@ bool encode_codes(CUtensorMap* map, const fxpq_kv_cache& c, const int8_t* codes,
                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a batch is computed.  New tokens per sequence are known on the host only on average.
+// How a batch is computed.  Sequences of at most FEW rows (new tokens x grouped heads) per key head are the stream
+// kernel's, the others the tile kernel's; where the counts are only on the device (ragged batches) both are launched
+// unless there is but one kind, and each leaves the other's sequences alone.
+constexpr int FEW = 32;
+
 struct Plan {
+    bool stream, tile;
     int nt;      // 8 nt query rows share a read of the cache
     bool whole;  // one CTA per unit
-    size_t ws;
+    int shares;  // CTAs that share the keys of a block of rows
+    size_t ws_stream, ws;
 };
 Plan plan(const fxpq_kv_cache& c, const fxpq_kv_batch& b, int q_heads) {
     Plan p;
     const long long group = q_heads / c.heads, seqs = b.n_seqs > 0 ? b.n_seqs : 1;
-    p.nt = stream_nt((b.n_tokens * group + seqs - 1) / seqs);
+    const long long mean = (b.n_tokens * group + seqs - 1) / seqs;  // rows of a sequence, the same for all without d_starts
+    p.stream = b.d_starts || mean <= FEW;
+    // (a ragged batch has a sequence of more than FEW rows only if it has that many rows)
+    p.tile = b.d_starts ? b.n_tokens * group > FEW : mean > FEW;
+    p.nt = stream_nt(mean);
     // A cache of at most 2048 tokens is one CTA's work; longer ones are cut into equal shares for all CTAs.
-    p.whole = (long long)b.max_pages * c.page <= 2048;
-    p.ws = p.whole ? 0 : (attend_stream_workspace(c.dim, p.nt) + 255) / 256 * 256;
+    const long long tokens = (long long)b.max_pages * c.page;
+    p.whole = tokens <= 2048;
+    p.ws_stream = p.stream && !p.whole ? (attend_stream_workspace(c.dim, p.nt) + 255) / 256 * 256 : 0;
+    p.shares = 1;
+    if (p.tile) {  // as many as fill the SMs, with at least 512 keys each
+        const long long units = tile_blocks(b.n_tokens, b.n_seqs, (int)group, false) * c.heads + (b.d_starts ? c.heads : 0);
+        while (p.shares < 16 && units * (p.shares + 1) <= num_sms() && tokens >= 512LL * (p.shares + 1)) ++p.shares;
+    }
+    p.ws = p.ws_stream + (p.tile ? (attend_tile_workspace(b.n_tokens, q_heads, c.dim, p.shares) + 255) / 256 * 256 : 0);
     return p;
 }
 
@@ -53,18 +70,26 @@ extern "C" fxpq_status fxpq_kv_attention(const fxpq_kv_cache* cache, const fxpq_
     const Plan p = plan(*cache, *batch, q_heads);
     if (p.ws && (!d_ws || ws_bytes < p.ws || !aligned(d_ws, 256))) return FXPQ_ERR_WORKSPACE;
     AttendArgs A;
-    if (!encode_codes(&A.tk, *cache, cache->d_k, 32) || !encode_codes(&A.tv, *cache, cache->d_v, 32)) return FXPQ_ERR_CUDA;
     A.s = make_seqs(*batch);
     A.k_scale = cache->d_k_scale, A.v_scale = cache->d_v_scale;
     A.q = q->d_x, A.q_token = q->token_stride, A.q_head = q->head_stride;
-    A.out = d_out, A.lse = d_lse, A.part = static_cast<float*>(d_ws);
+    A.out = d_out, A.lse = d_lse;
     A.n_pages = cache->n_pages, A.page = cache->page, A.heads = cache->heads, A.q_heads = q_heads, A.group = q_heads / cache->heads;
     A.q_f16 = type == FXPQ_FT_F16;
     A.q_vec = aligned(q->d_x, 16) && q->token_stride % 8 == 0 && q->head_stride % 8 == 0;
     A.causal = causal;
-    A.few = INT32_MAX;
-    A.few_only = 0;
+    A.few = p.tile ? FEW : INT32_MAX;
+    A.few_only = p.stream && p.tile;
     A.scale = softmax_scale;
     A.status = status_ptr();
-    return launch_attend_stream(A, cache->dim, p.nt, p.whole, as_stream(stream));
+    cudaStream_t st = as_stream(stream);
+    if (p.tile) {  // (first: its CTAs run longest)
+        if (!encode_codes(&A.tk, *cache, cache->d_k, 128) || !encode_codes(&A.tv, *cache, cache->d_v, 128)) return FXPQ_ERR_CUDA;
+        A.part = reinterpret_cast<float*>(static_cast<char*>(d_ws) + p.ws_stream);
+        const fxpq_status rc = launch_attend_tile(A, cache->dim, p.shares, st);
+        if (rc != FXPQ_OK || !p.stream) return rc;
+    }
+    if (!encode_codes(&A.tk, *cache, cache->d_k, 32) || !encode_codes(&A.tv, *cache, cache->d_v, 32)) return FXPQ_ERR_CUDA;
+    A.part = static_cast<float*>(d_ws);
+    return launch_attend_stream(A, cache->dim, p.nt, p.whole, st);
 }

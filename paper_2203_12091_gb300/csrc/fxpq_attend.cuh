@@ -30,7 +30,7 @@ struct AttendArgs {
     float* part;  // partial results of units shared by several CTAs
     int n_pages, page, heads, q_heads, group, q_f16, q_vec, causal;
     int share_min, whole;  // see attend_stream_kernel
-    int few, few_only;     // sequences of at most `few` rows per key head belong to the stream kernel
+    int few, few_only;     // sequences of at most `few` rows per key head belong to the stream kernel, where both run
     float scale;
     int* status;
 };
@@ -65,6 +65,9 @@ __device__ __forceinline__ void load_q8(const AttendArgs& A, long long at, float
 fxpq_status launch_attend_stream(AttendArgs& A, int dim, int nt, bool whole, cudaStream_t st);
 size_t attend_stream_workspace(int dim, int nt);
 int stream_nt(long long rows);
+long long tile_blocks(int n_tokens, int n_seqs, int group, bool ragged);  // blocks of 256 rows for each key head
+fxpq_status launch_attend_tile(AttendArgs& A, int dim, int shares, cudaStream_t st);
+size_t attend_tile_workspace(int n_tokens, int q_heads, int dim, int shares);
 
 }  // namespace llm
 }  // namespace fxpq
