@@ -530,6 +530,14 @@ FXPQ_API fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const f
                                     int32_t K, int32_t y_type, void* d_y, int64_t y_stride, void* d_ws,
                                     size_t ws_bytes, void* stream);
 
+/* fxpq_quantize_tokens of d_x (M rows of K values of type x_type, x_stride elements apart) and fxpq_linear_i8 of its
+ * codes in one call: a layer with 8-bit weights on float activations.  The codes and scales live in the workspace:
+ * fxpq_linear_tokens_workspace bytes, 256-byte aligned, scratch. */
+FXPQ_API size_t fxpq_linear_tokens_workspace(int64_t M, int32_t N, int32_t K);
+FXPQ_API fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64_t x_stride, const int8_t* d_w, int64_t w_stride,
+                                        const float* d_sw, const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type,
+                                        void* d_y, int64_t y_stride, void* d_ws, size_t ws_bytes, void* stream);
+
 /* A paged cache of keys and values: int8 codes [n_pages][heads][page][dim] each (16-byte aligned), value =
  * code * scale with one fp32 scale > 0 for each block, a page of one head: [n_pages][heads].  page is 16,
  * 32, 64 or 128 tokens; dim is 64 or 128. */

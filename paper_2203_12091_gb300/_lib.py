@@ -137,6 +137,8 @@ _SIGS = {
     "fxpq_quantize_tokens": (I32, [VP, I32, I64, I32, I64, VP, I64, VP, VP]),
     "fxpq_linear_i8_workspace": (SZ, [I64, I32, I32]),
     "fxpq_linear_i8": (I32, [VP, I64, VP, VP, I64, VP, VP, I64, I32, I32, I32, VP, I64, VP, SZ, VP]),
+    "fxpq_linear_tokens_workspace": (SZ, [I64, I32, I32]),
+    "fxpq_linear_tokens": (I32, [VP, I32, I64, VP, I64, VP, VP, I64, I32, I32, I32, VP, I64, VP, SZ, VP]),
     "fxpq_kv_append": (I32, [VP, VP, I32, VP, VP, VP, I32, VP, VP, VP, I32, I32, I32, VP]),
     "fxpq_kv_values": (I32, [VP, VP, I32, I32, VP, VP, VP]),
     "fxpq_kv_attention_workspace": (SZ, [VP, VP, I32]),

@@ -357,15 +357,25 @@ extern "C" size_t fxpq_linear_i8_workspace(int64_t M, int32_t N, int32_t K) {
     return 0;
 }
 
-extern "C" fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const float* d_sx, const int8_t* d_w, int64_t w_stride,
-                                      const float* d_sw, const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type,
-                                      void* d_y, int64_t y_stride, void* d_ws, size_t ws_bytes, void* stream) {
+namespace {
+fxpq_status check_linear(const int8_t* d_x, int64_t x_stride, const float* d_sx, const int8_t* d_w, int64_t w_stride, const float* d_sw,
+                         const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type, const void* d_y, int64_t y_stride) {
     if (M < 0 || N < 0 || K < 0 || M > INT32_MAX || !ftype_ok(y_type)) return FXPQ_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return FXPQ_OK;
     if (!d_sx || !d_sw || !d_y || (K > 0 && (!d_x || !d_w)) || !aligned(d_x, 16) || !aligned(d_w, 16) || x_stride % 16 || w_stride % 16 ||
         x_stride < K || w_stride < K || y_stride < N || !aligned(d_y, ftype_bytes(y_type)) || !aligned(d_sx, 4) || !aligned(d_sw, 4) ||
         !aligned(d_bias, 4))
         return FXPQ_ERR_INVALID_ARG;
+    return FXPQ_OK;
+}
+}  // namespace
+
+extern "C" fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const float* d_sx, const int8_t* d_w, int64_t w_stride,
+                                      const float* d_sw, const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type,
+                                      void* d_y, int64_t y_stride, void* d_ws, size_t ws_bytes, void* stream) {
+    const fxpq_status bad = check_linear(d_x, x_stride, d_sx, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride);
+    if (bad != FXPQ_OK) return bad;
+    if (M == 0 || N == 0) return FXPQ_OK;
     const size_t need = fxpq_linear_i8_workspace(M, N, K);
     if (need && (!d_ws || ws_bytes < need || !aligned(d_ws, 256))) return FXPQ_ERR_WORKSPACE;
     LinArgs P;
@@ -375,4 +385,33 @@ extern "C" fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const
     P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.y_type = y_type;
     P.status = status_ptr();
     return launch_few(P, as_stream(stream));
+}
+
+namespace {
+// The workspace of fxpq_linear_tokens: codes, scales, then fxpq_linear_i8's.
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+size_t codes_pitch(int32_t K) { return ((size_t)K + 15) / 16 * 16; }
+}  // namespace
+
+extern "C" size_t fxpq_linear_tokens_workspace(int64_t M, int32_t N, int32_t K) {
+    if (M <= 0 || N < 0 || K < 0) return 0;
+    return up256((size_t)M * codes_pitch(K)) + up256((size_t)M * sizeof(float)) + fxpq_linear_i8_workspace(M, N, K);
+}
+
+extern "C" fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64_t x_stride, const int8_t* d_w, int64_t w_stride,
+                                          const float* d_sw, const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type,
+                                          void* d_y, int64_t y_stride, void* d_ws, size_t ws_bytes, void* stream) {
+    if (M < 0 || N < 0 || K < 0 || !ftype_ok(x_type) || !ftype_ok(y_type)) return FXPQ_ERR_INVALID_ARG;
+    if (M == 0 || N == 0) return FXPQ_OK;
+    const size_t need = fxpq_linear_tokens_workspace(M, N, K);
+    if (!d_ws || ws_bytes < need || !aligned(d_ws, 256)) return FXPQ_ERR_WORKSPACE;
+    const size_t pitch = codes_pitch(K), c = up256((size_t)M * pitch), s = up256((size_t)M * sizeof(float));
+    int8_t* codes = static_cast<int8_t*>(d_ws);
+    float* scale = reinterpret_cast<float*>(codes + c);
+    const fxpq_status bad = check_linear(codes, pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride);
+    if (bad != FXPQ_OK) return bad;  // (before anything is launched)
+    const fxpq_status rc = fxpq_quantize_tokens(d_x, x_type, M, K, x_stride, codes, (int64_t)pitch, scale, stream);
+    if (rc != FXPQ_OK) return rc;
+    return fxpq_linear_i8(codes, (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, codes + c + s,
+                          need - c - s, stream);
 }

@@ -344,6 +344,16 @@ def fxpq_linear_i8(x, x_stride: int, sx, w, w_stride: int, sw, bias, M: int, N: 
                                                      _s(stream)))
 
 
+def fxpq_linear_tokens_workspace(M: int, N: int, K: int) -> int:
+    return L.lib().fxpq_linear_tokens_workspace(M, N, K)
+
+
+def fxpq_linear_tokens(x, x_type: int, x_stride: int, w, w_stride: int, sw, bias, M: int, N: int, K: int, y_type: int, y, y_stride: int,
+                       ws, stream=None):
+    L.check("fxpq_linear_tokens", L.lib().fxpq_linear_tokens(_p(x), x_type, x_stride, _p(w), w_stride, _p(sw), _p(bias), M, N, K,
+                                                             y_type, _p(y), y_stride, _p(ws), ws.nbytes, _s(stream)))
+
+
 def fxpq_kv_append(cache: L.KVCacheDesc, batch: L.KVBatchDesc, ftype: int, k: L.KVRows, v: L.KVRows, q, q_heads: int,
                    q_out, cos, sin, n_positions: int, rot: int, interleaved: int, stream=None):
     L.check("fxpq_kv_append", L.lib().fxpq_kv_append(

@@ -10,44 +10,59 @@ page ids outside the cache, positions past the rotation tables) is latched and r
 from __future__ import annotations
 
 import math
+import struct
 
 import torch
 
 from . import _lib as L
 from . import fxpq as F
 
+# Small calls are bound by the host, so arguments are marshalled by hand here: descriptors packed as bytes (0.3 us, a
+# ctypes structure 1.1), no views, one allocation where there were two.  One token through a 4096 x 4096 layer took 25.8 us
+# on the host with two wrapped calls and 11 on the GPU.
 _FT = {torch.float32: L.FT_F32, torch.float16: L.FT_F16, torch.bfloat16: L.FT_BF16}
+_BATCH = struct.Struct("PPPiiiiq").pack  # fxpq_kv_batch
+_ROWS = struct.Struct("Pqq").pack        # fxpq_kv_rows
+_empty, _i8, _i32, _u8, _f32 = torch.empty, torch.int8, torch.int32, torch.uint8, torch.float32
 
 
 def _ftype(name, dtype, types=_FT):
-    if dtype not in types:
+    ft = types.get(dtype)
+    if ft is None:
         raise TypeError(f"{name}: {dtype} is none of {', '.join(str(t) for t in types)}")
-    return types[dtype]
+    return ft
 
 
 def _want(name, t, dtype, dims):
-    if not t.is_cuda or t.dtype != dtype or t.dim() != dims or not t.is_contiguous():
+    if t.dtype != dtype or t.dim() != dims or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dims}-dimensional CUDA tensor of {dtype} is needed, "
                          f"got {tuple(t.shape)} of {t.dtype} on {t.device}, strides {t.stride()}")
+
+
+def _float_rows(name, x):
+    """x [..., K] as [M, K] with contiguous rows."""
+    if not x.is_cuda or x.dim() < 1:
+        raise ValueError(f"{name}: rows on a CUDA device are needed, got {tuple(x.shape)} on {x.device}")
+    rows = x if x.dim() == 2 else x.reshape(math.prod(x.shape[:-1]), x.shape[-1])
+    return rows if rows.stride(1) == 1 or rows.shape[1] <= 1 else rows.contiguous()
 
 
 def quantize_tokens(x):
     """Rows x [..., K] (float32, float16 or bfloat16) -> (codes int8 [..., K], scales float32 [...]), value =
     code * scale.  The codes' rows lie a multiple of 16 bytes apart, as `linear_i8` needs them."""
     ft = _ftype("quantize_tokens", x.dtype)
-    if not x.is_cuda or x.dim() < 1:
-        raise ValueError(f"quantize_tokens: rows on a CUDA device are needed, got {tuple(x.shape)} on {x.device}")
-    K, lead = x.shape[-1], x.shape[:-1]
-    rows = x if x.dim() == 2 else x.reshape(math.prod(lead), K)
-    if K > 1 and rows.stride(1) != 1:
-        rows = rows.contiguous()
-    M, pitch = rows.shape[0], (K + 15) // 16 * 16
-    codes = torch.empty((M, pitch), dtype=torch.int8, device=x.device)
-    scale = torch.empty(M, dtype=torch.float32, device=x.device)
+    rows = _float_rows("quantize_tokens", x)
+    M, K = rows.shape
+    pitch = (K + 15) // 16 * 16
+    codes = _empty((M, pitch), dtype=_i8, device=x.device)
+    scale = _empty(M, dtype=_f32, device=x.device)
     F.fxpq_quantize_tokens(rows, ft, M, K, rows.stride(0), codes, pitch, scale)
     if pitch != K:
         codes = codes[:, :K]
-    return (codes, scale) if x.dim() == 2 else (codes.unflatten(0, lead) if lead else codes[0], scale.view(lead))
+    if x.dim() == 2:
+        return codes, scale
+    lead = x.shape[:-1]
+    return (codes.unflatten(0, lead) if lead else codes[0]), scale.view(lead)
 
 
 def linear_i8(codes, scale, w, w_scale, bias=None, out_dtype=torch.bfloat16):
@@ -56,22 +71,28 @@ def linear_i8(codes, scale, w, w_scale, bias=None, out_dtype=torch.bfloat16):
     ft = _ftype("linear_i8", out_dtype)
     M, K = codes.shape
     N = w.shape[0]
-    if codes.dtype != torch.int8 or w.dtype != torch.int8 or w.dim() != 2 or w.shape[1] != K:
-        raise ValueError(f"linear_i8: int8 rows of one length are needed, got {tuple(codes.shape)} of {codes.dtype} and "
-                         f"{tuple(w.shape)} of {w.dtype}")
-    if (K > 1 and (codes.stride(1) != 1 or w.stride(1) != 1)) or not codes.is_cuda or not w.is_cuda:
-        raise ValueError("linear_i8: the codes of a row must be contiguous and on a CUDA device")
-    _want("linear_i8: scale", scale, torch.float32, 1)
-    _want("linear_i8: w_scale", w_scale, torch.float32, 1)
-    if bias is not None:
-        _want("linear_i8: bias", bias, torch.float32, 1)
-    if scale.shape[0] != M or w_scale.shape[0] != N or (bias is not None and bias.shape[0] != N):
-        raise ValueError("linear_i8: one scale for each token, one scale and bias for each channel are needed")
-    y = torch.empty((M, N), dtype=out_dtype, device=codes.device)
+    if codes.dtype != _i8 or not codes.is_cuda or (K > 1 and codes.stride(1) != 1):
+        raise ValueError(f"linear_i8: int8 rows on a CUDA device are needed, got {tuple(codes.shape)} of {codes.dtype} on {codes.device}")
+    _check_layer("linear_i8", w, w_scale, bias, K)
+    _want("linear_i8: scale", scale, _f32, 1)
+    if scale.shape[0] != M:
+        raise ValueError("linear_i8: one scale for each token is needed")
+    y = _empty((M, N), dtype=out_dtype, device=codes.device)
     need = F.fxpq_linear_i8_workspace(M, N, K)
-    ws = torch.empty(need, dtype=torch.uint8, device=codes.device) if need else None
+    ws = _empty(need, dtype=_u8, device=codes.device) if need else None
     F.fxpq_linear_i8(codes, _pitch(codes, K), scale, w, _pitch(w, K), w_scale, bias, M, N, K, ft, y, N, ws)
     return y
+
+
+def _check_layer(name, w, w_scale, bias, K):
+    if w.dtype != _i8 or w.dim() != 2 or not w.is_cuda or w.shape[1] != K or (K > 1 and w.stride(1) != 1):
+        raise ValueError(f"{name}: weights int8 [N, {K}] with contiguous rows on a CUDA device are needed, got {tuple(w.shape)} of "
+                         f"{w.dtype} on {w.device}")
+    _want(f"{name}: w_scale", w_scale, _f32, 1)
+    if bias is not None:
+        _want(f"{name}: bias", bias, _f32, 1)
+    if w_scale.shape[0] != w.shape[0] or (bias is not None and bias.shape[0] != w.shape[0]):
+        raise ValueError(f"{name}: one scale and bias for each channel are needed")
 
 
 def _pitch(t, K):  # (a single row, or rows of nothing, may have any stride)
@@ -83,28 +104,44 @@ class Linear8:
     are padded once."""
 
     def __init__(self, w, w_scale, bias=None):
-        _want("Linear8: w", w, torch.int8, 2)
+        _want("Linear8: w", w, _i8, 2)
         N, K = w.shape
         if K % 16 or w.data_ptr() % 16:
-            padded = torch.zeros((N, (K + 15) // 16 * 16), dtype=torch.int8, device=w.device)
+            padded = torch.zeros((N, (K + 15) // 16 * 16), dtype=_i8, device=w.device)
             padded[:, :K] = w
             w = padded[:, :K]
+        self._set(w, w_scale, bias)
+
+    def _set(self, w, w_scale, bias):
+        self.N, self.K = w.shape
+        _check_layer("Linear8", w, w_scale, bias, self.K)
         self.w, self.w_scale, self.bias = w, w_scale, bias
 
     @classmethod
     def from_float(cls, w, bias=None):
         """Quantizes float weights [N, K]."""
-        codes, scale = quantize_tokens(w)
         layer = cls.__new__(cls)
-        layer.w, layer.w_scale, layer.bias = codes, scale, None if bias is None else bias.float().contiguous()
+        layer._set(*quantize_tokens(w), None if bias is None else bias.float().contiguous())
         return layer
 
     def __call__(self, x, out_dtype=None):
-        """x [..., K] in a float type -> [..., N] in out_dtype (x's own by default)."""
-        rows = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
-        codes, scale = quantize_tokens(rows)
-        y = linear_i8(codes, scale, self.w, self.w_scale, self.bias, out_dtype or x.dtype)
-        return y if x.dim() == 2 else y.view(*x.shape[:-1], y.shape[-1])
+        """x [..., K] in a float type -> [..., N] in out_dtype (x's own by default): `quantize_tokens` and `linear_i8`
+        as one call."""
+        rows = _float_rows("Linear8", x)
+        M, K = rows.shape
+        if K != self.K:
+            raise ValueError(f"Linear8: rows of {self.K} values are needed, got {tuple(x.shape)}")
+        dtype = out_dtype or x.dtype
+        xt, yt = _ftype("Linear8", x.dtype), _ftype("Linear8", dtype)
+        lib, dev, N, w = L.lib(), x.device, self.N, self.w
+        y = _empty((M, N), dtype=dtype, device=dev)
+        ws = _empty(lib.fxpq_linear_tokens_workspace(M, N, K), dtype=_u8, device=dev)
+        rc = lib.fxpq_linear_tokens(rows.data_ptr(), xt, rows.stride(0), w.data_ptr(), _pitch(w, K), self.w_scale.data_ptr(),
+                                    None if self.bias is None else self.bias.data_ptr(), M, N, K, yt, y.data_ptr(), N, ws.data_ptr(),
+                                    ws.nbytes, F._s(None))
+        if rc:
+            L.check("fxpq_linear_tokens", rc)
+        return y if x.dim() == 2 else y.view(*x.shape[:-1], N)
 
 
 class KVCache:
@@ -122,6 +159,7 @@ class KVCache:
         self.n_pages, self.heads, self.page, self.dim = k.shape
         self.desc = L.KVCacheDesc(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.n_pages, self.page,
                                   self.heads, self.dim)
+        self.packed = bytes(self.desc)  # fxpq_kv_cache
 
     @classmethod
     def empty(cls, n_pages, heads, page, dim, device="cuda"):
@@ -130,28 +168,31 @@ class KVCache:
 
 
 def _batch(name, pages, lens, starts, T):
-    if pages.dtype != torch.int32 or pages.dim() != 2 or (pages.shape[1] > 1 and pages.stride(1) != 1) or not pages.is_cuda:
+    """fxpq_kv_batch"""
+    B, wide = pages.shape if pages.dim() == 2 else (-1, 0)
+    if pages.dtype != _i32 or B < 0 or not pages.is_cuda or (wide > 1 and pages.stride(1) != 1):
         raise ValueError(f"{name}: pages must be int32 [sequences, pages] on a CUDA device")
-    _want(f"{name}: lens", lens, torch.int32, 1)
-    B = lens.shape[0]
-    if pages.shape[0] != B:
-        raise ValueError(f"{name}: {pages.shape[0]} rows of pages and {B} lengths")
+    _want(name + ": lens", lens, _i32, 1)
+    if lens.shape[0] != B:
+        raise ValueError(f"{name}: {B} rows of pages and {lens.shape[0]} lengths")
+    at = 0
     if starts is not None:
-        _want(f"{name}: starts", starts, torch.int32, 1)
+        _want(name + ": starts", starts, _i32, 1)
         if starts.shape[0] != B + 1:
             raise ValueError(f"{name}: starts must have {B + 1} entries")
+        at = starts.data_ptr()
     elif B and T % B:
         raise ValueError(f"{name}: {T} new tokens are not the same number for each of {B} sequences (give starts)")
-    wide = pages.shape[1]
-    return L.KVBatchDesc(pages.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr(), B, wide, T, 0,
-                         pages.stride(0) if B > 1 else max(wide, 1))
+    return _BATCH(pages.data_ptr(), lens.data_ptr(), at, B, wide, T, 0, pages.stride(0) if B > 1 else max(wide, 1))
 
 
 def _rows(name, x, T, heads, dim):
-    if x.dim() != 3 or tuple(x.shape) != (T, heads, dim) or not x.is_cuda or x.stride(2) != 1:
+    """fxpq_kv_rows"""
+    st = x.stride()
+    if x.shape != (T, heads, dim) or st[2] != 1 or not x.is_cuda:
         raise ValueError(f"{name}: rows [{T}, {heads}, {dim}] with contiguous heads are needed, got {tuple(x.shape)} with "
                          f"strides {x.stride()}")
-    return L.KVRows(x.data_ptr(), x.stride(0), x.stride(1))
+    return _ROWS(x.data_ptr(), st[0], st[1])
 
 
 def kv_append(cache, pages, lens, k, v, q=None, starts=None, cos=None, sin=None, interleaved=False):
@@ -164,37 +205,44 @@ def kv_append(cache, pages, lens, k, v, q=None, starts=None, cos=None, sin=None,
     (i, i + rot / 2) or with interleaved (2 i, 2 i + 1).  k, v and q may be views with any token and head strides."""
     if k.dim() != 3:
         raise ValueError(f"kv_append: k must be [tokens, heads, dim], got {tuple(k.shape)}")
-    T = k.shape[0]
-    ft = _ftype("kv_append", k.dtype)
-    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+    dtype = k.dtype
+    ft = _ftype("kv_append", dtype)
+    if v.dtype != dtype or (q is not None and q.dtype != dtype):
         raise TypeError("kv_append: k, v and q must have one type")
+    T = k.shape[0]
     batch = _batch("kv_append", pages, lens, starts, T)
     rk, rv = _rows("kv_append: k", k, T, cache.heads, cache.dim), _rows("kv_append: v", v, T, cache.heads, cache.dim)
     rq = out = None
-    heads = 0
+    heads = n_pos = rot = to = c = s = 0
     if q is not None:
         heads = q.shape[1] if q.dim() == 3 else 0
         rq = _rows("kv_append: q", q, T, heads, cache.dim)
-        out = torch.empty((T, heads, cache.dim), dtype=q.dtype, device=q.device)
-    n_pos = rot = 0
+        out = _empty((T, heads, cache.dim), dtype=dtype, device=q.device)
+        to = out.data_ptr()
     if (cos is None) != (sin is None):
         raise ValueError("kv_append: cos and sin go together")
     if cos is not None:
-        _want("kv_append: cos", cos, torch.float32, 2)
-        _want("kv_append: sin", sin, torch.float32, 2)
-        if cos.shape != sin.shape:
+        _want("kv_append: cos", cos, _f32, 2)
+        _want("kv_append: sin", sin, _f32, 2)
+        n_pos, rot = cos.shape
+        if sin.shape != (n_pos, rot):
             raise ValueError("kv_append: cos and sin must have one shape")
-        n_pos, rot = cos.shape[0], 2 * cos.shape[1]
-    F.fxpq_kv_append(cache.desc, batch, ft, rk, rv, rq, heads, out, cos, sin, n_pos, rot, int(interleaved))
+        rot, c, s = 2 * rot, cos.data_ptr(), sin.data_ptr()
+    rc = L.lib().fxpq_kv_append(cache.packed, batch, ft, rk, rv, rq, heads, to, c, s, n_pos, rot, 1 if interleaved else 0, F._s(None))
+    if rc:
+        L.check("fxpq_kv_append", rc)
     return out
 
 
 def kv_values(cache, pages, dtype=torch.bfloat16):
     """The values code * scale of the pages int32 [n]: keys and values [n, heads, page, dim]."""
-    _want("kv_values: pages", pages, torch.int32, 1)
-    n = pages.shape[0]
-    k, v = (torch.empty((n, cache.heads, cache.page, cache.dim), dtype=dtype, device=pages.device) for _ in range(2))
-    F.fxpq_kv_values(cache.desc, pages, n, _ftype("kv_values", dtype), k, v)
+    _want("kv_values: pages", pages, _i32, 1)
+    n, ft = pages.shape[0], _ftype("kv_values", dtype)
+    k = _empty((n, cache.heads, cache.page, cache.dim), dtype=dtype, device=pages.device)
+    v = torch.empty_like(k)
+    rc = L.lib().fxpq_kv_values(cache.packed, pages.data_ptr(), n, ft, k.data_ptr(), v.data_ptr(), F._s(None))
+    if rc:
+        L.check("fxpq_kv_values", rc)
     return k, v
 
 
@@ -206,18 +254,21 @@ def kv_attention(cache, pages, lens, q, starts=None, scale=None, causal=True, re
     last tokens of each sequence over the cache, which already holds those tokens; q_heads is a multiple of the
     cache's heads.  scale: 1 / sqrt(dim) by default.  Returns [T, q_heads, dim], and with return_lse the logarithms
     float32 [T, q_heads] of the sums of exponentials; rows that see no key are zeros and -inf."""
-    ft = _ftype("kv_attention", q.dtype, _Q_TYPES)
+    dtype, dim = q.dtype, cache.dim
+    ft = _ftype("kv_attention", dtype, _Q_TYPES)
     if q.dim() != 3:
         raise ValueError(f"kv_attention: q must be [tokens, heads, dim], got {tuple(q.shape)}")
-    T, heads = q.shape[0], q.shape[1]
+    T, heads, _ = q.shape
     if heads == 0 or heads % cache.heads:
         raise ValueError(f"kv_attention: {heads} query heads are no multiple of {cache.heads}")
-    batch = _batch("kv_attention", pages, lens, starts, T)
-    rq = _rows("kv_attention: q", q, T, heads, cache.dim)
-    out = torch.empty((T, heads, cache.dim), dtype=q.dtype, device=q.device)
-    lse = torch.empty((T, heads), dtype=torch.float32, device=q.device) if return_lse else None
-    need = F.fxpq_kv_attention_workspace(cache.desc, batch, heads)
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    F.fxpq_kv_attention(cache.desc, batch, ft, rq, heads, 1.0 / math.sqrt(cache.dim) if scale is None else float(scale),
-                        int(bool(causal)), out, lse, ws)
+    batch, rq = _batch("kv_attention", pages, lens, starts, T), _rows("kv_attention: q", q, T, heads, dim)
+    out = _empty((T, heads, dim), dtype=dtype, device=q.device)
+    lse = _empty((T, heads), dtype=_f32, device=q.device) if return_lse else None
+    lib, packed = L.lib(), cache.packed
+    need = lib.fxpq_kv_attention_workspace(packed, batch, heads)
+    ws = _empty(need, dtype=_u8, device=q.device) if need else None
+    rc = lib.fxpq_kv_attention(packed, batch, ft, rq, heads, dim ** -0.5 if scale is None else scale, 1 if causal else 0, out.data_ptr(),
+                               lse.data_ptr() if return_lse else None, ws.data_ptr() if need else None, need, F._s(None))
+    if rc:
+        L.check("fxpq_kv_attention", rc)
     return (out, lse) if return_lse else out

@@ -105,6 +105,21 @@ def test_linear_refuses(lib):
                 assert lib.fxpq_linear_i8(P, K, P, P, K, P, None, M, N, K, L.FT_F16, P, N, ws, nb, None) == L.ERR_WORKSPACE
 
 
+def test_linear_tokens_refuses(lib):
+    ok = dict(x=P, t=L.FT_BF16, xs=64, w=P, ws=64, sw=P, b=None, M=2, N=3, K=60, yt=L.FT_F16, y=P, ys=3)
+
+    def call(work=P, short=0, **kw):
+        a = {**ok, **kw}
+        n = lib.fxpq_linear_tokens_workspace(a["M"], a["N"], a["K"])
+        return lib.fxpq_linear_tokens(a["x"], a["t"], a["xs"], a["w"], a["ws"], a["sw"], a["b"], a["M"], a["N"], a["K"], a["yt"], a["y"],
+                                      a["ys"], work, n - short, None)
+    for b in [dict(x=None), dict(w=None), dict(sw=None), dict(y=None), dict(x=ODD), dict(w=ODD), dict(xs=59), dict(ws=72), dict(ys=2),
+              dict(t=3), dict(yt=-1), dict(M=-1), dict(N=-1), dict(K=-1), dict(b=ODD), dict(y=ODD)]:
+        assert call(**b) == L.ERR_INVALID_ARG, b
+    assert call(work=None) == call(short=1) == call(work=ctypes.c_void_p(4112)) == L.ERR_WORKSPACE
+    assert call(M=0) == L.OK and call(N=0) == L.OK
+
+
 def _cache(**kw):
     a = dict(k=4096, v=4096, ks=4096, vs=4096, n=4, page=16, heads=2, dim=64)
     a.update(kw)
