@@ -201,8 +201,11 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
         const int grp = (warp - 4) >> 2, quad = warp & 3, t = threadIdx.x & 127, row = quad * 32 + lane;
         for (int i = grp; i < n_kb; i += 2) {
             const int s = i % ST;
-            if (!wait_warp(raw_full + 8 * s, (i / ST) & 1, abort, P.status)) break;
+            // In this order: with an odd number of stages the groups take turns on one, and a parity wait on raw_full
+            // tells block i from block i - ST of the other group only once that one has landed.  Block i - 2's products
+            // are complete here, so all before them are, and their blocks were read.
             if (!wait_warp(conv_empty + 8 * grp, ((i >> 1) & 1) ^ 1, abort, P.status)) break;
+            if (!wait_warp(raw_full + 8 * s, (i / ST) & 1, abort, P.status)) break;
             tc_fence_after();
             const unsigned char* ra = smem + s * raw_bytes;
 #pragma unroll
