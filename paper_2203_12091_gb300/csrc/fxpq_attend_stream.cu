@@ -488,9 +488,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_stream_kernel(const __gr
     }
     // every copy that this warp issued has landed before it leaves (it has, unless a wait ran out)
     for (; used < filled; ++used) {
-        const long long t0 = clock64();
-        while (!mbar_try_wait(bar0 + 8 * (used % ST), (used / ST) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {
-        }
+        drain_warp(bar0 + 8 * (used % ST), (used / ST) & 1);
     }
 }
 

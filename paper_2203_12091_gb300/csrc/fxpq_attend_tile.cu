@@ -341,9 +341,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             }
         }
         tc_commit(drained);  // every product issued here has completed once it fires
-        const long long t0 = clock64();
-        while (!mbar_try_wait(drained, 0) && clock64() - t0 < TC_WAIT_CYCLES) {
-        }
+        drain_warp(drained, 0);
     } else if (warp == 13) {
         // ================================================================ pages, scales, copies
         const int* table = A.s.pages + (long long)b * A.s.pages_stride;
@@ -401,9 +399,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             }
         }
         for (int k = max(0, u - 2); k < u; ++k) {  // every copy has landed
-            const long long t0 = clock64();
-            while (!mbar_try_wait(raw_full + 8 * (k & 1), (k >> 1) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {
-            }
+            drain_warp(raw_full + 8 * (k & 1), (k >> 1) & 1);
         }
     }
     tc_fence_before();

@@ -1,6 +1,7 @@
 // fxpq_linear.cu -- rows quantized to 8 bits with a scale each, and the product of 8-bit rows with scales for
 // each token and each output channel.
 #include <cfloat>
+#include <type_traits>
 
 #include "fxpq_llm.cuh"
 #include "fxpq_ptx.cuh"
@@ -13,13 +14,15 @@ namespace {
 // thread; longer rows are read again, from L2).
 constexpr int QT_THREADS = 256, QT_KEEP = 4;
 
-template <typename T>
+// C: int8 codes, or fp16 ones for the tensor-core kernel that takes them so.
+template <typename T, typename C>
 __global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __restrict__ x, int K, long long x_stride, int vec,
-                                                                     int8_t* __restrict__ codes, long long c_stride, int c_vec,
+                                                                     C* __restrict__ codes, long long c_stride, int c_vec,
                                                                      float* __restrict__ scale, int* status) {
+    constexpr bool HALF = sizeof(C) == 2;
     pdl_wait();
     const T* row = x + (long long)blockIdx.x * x_stride;
-    int8_t* out = codes + (long long)blockIdx.x * c_stride;
+    C* out = codes + (long long)blockIdx.x * c_stride;
     const int t = threadIdx.x, groups = K / 8;  // whole groups of eight; the rest of the row one value at a time
     float keep[QT_KEEP][8], tail = 0.0f, top = 0.0f;
     bool bad = false;
@@ -67,11 +70,16 @@ __global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __
         int c[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) c[e] = code(v[e]);
-        if (c_vec)
+        if constexpr (HALF) {  // (always aligned)
+            uint32_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = h2_bits(__halves2half2(__int2half_rn(c[2 * e]), __int2half_rn(c[2 * e + 1])));
+            *reinterpret_cast<uint4*>(out + 8 * g) = make_uint4(h[0], h[1], h[2], h[3]);
+        } else if (c_vec)
             *reinterpret_cast<uint2*>(out + 8 * g) = make_uint2(pack_i8(c[0], c[1], c[2], c[3]), pack_i8(c[4], c[5], c[6], c[7]));
         else
 #pragma unroll
-            for (int e = 0; e < 8; ++e) out[8 * g + e] = (int8_t)c[e];
+            for (int e = 0; e < 8; ++e) out[8 * g + e] = (C)c[e];
     };
 #pragma unroll
     for (int s = 0; s < QT_KEEP; ++s)
@@ -83,8 +91,8 @@ __global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __
         for (int e = 0; e < 8; ++e) v[e] = fabsf(v[e]) <= FLT_MAX ? v[e] : 0.0f;
         put(g, v);
     }
-    if (t < K - 8 * groups) out[8 * groups + t] = (int8_t)code(tail);
-    for (long long i = K + t; i < c_stride; i += QT_THREADS) out[i] = 0;
+    if (t < K - 8 * groups) out[8 * groups + t] = (C)code(tail);
+    for (long long i = K + t; i < c_stride; i += QT_THREADS) out[i] = (C)0;
 }
 
 __device__ __forceinline__ void store_y(void* y, int type, long long at, float v) {
@@ -176,9 +184,7 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
             tma_load_2d(dst + LS_A, &P.tx, (kb0 + i) * LS_KB, (int)m0, bar);
         }
         for (int j = max(0, i - ST); j < i; ++j) {  // every copy has landed before this CTA's memory is used again
-            const long long t0 = clock64();
-            while (!mbar_try_wait(raw_full + 8 * (j % ST), (j / ST) & 1) && clock64() - t0 < TC_WAIT_CYCLES) {
-            }
+            drain_warp(raw_full + 8 * (j % ST), (j / ST) & 1);
         }
     } else if (warp == 1) {
         const uint32_t idesc = make_idesc(128, cols);
@@ -194,9 +200,7 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
             tc_commit(conv_empty + 8 * c);
         }
         tc_commit(done);
-        const long long t0 = clock64();
-        while (!mbar_try_wait(done, 0) && clock64() - t0 < TC_WAIT_CYCLES) {
-        }
+        drain_warp(done, 0);
     } else if (warp >= 4) {
         const int grp = (warp - 4) >> 2, quad = warp & 3, t = threadIdx.x & 127, row = quad * 32 + lane;
         for (int i = grp; i < n_kb; i += 2) {
@@ -288,6 +292,302 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
     if (shares > 1) cluster_sync();  // (the others have read this CTA's sums)
 }
 
+
+// ------------------------------------------------------------------ many tokens
+// The same product, bound by the tensor pipe: pairs of CTAs share tiles of 256 channels x 256 tokens (cta_group::2), so
+// that a CTA reads only half of the tokens' operand from its shared memory.  Per 64 codes of the reduction (512 cycles of
+// products) it moves 8 KB of weight codes in and out and 16 KB of tokens in and once through the tensor core: 384 cycles
+// of shared memory, where one CTA alone would need 640, and both operands as fp16 in shared memory 512.  The tokens arrive
+// as fp16 codes (written so by the quantizer, or expanded before), the weights as bytes, expanded into tensor memory.
+//   warp 0  weights' copies;  1  tokens' copies;  2  tensor memory, products (CTA 0);  4-7  converters;  8-15  epilogue.
+// The accumulators fill half of tensor memory, the weights' four stages the other half.  The epilogue scales and packs the
+// sums into registers first, so that the next tile's products begin while it still stores.
+constexpr int LM_THREADS = 512, LM_RAW = 3, LM_B = 8, LM_A = 4;
+constexpr int LM_SMEM = 1024 + LM_RAW * LS_A + LM_B * 128 * 128;
+
+struct ManyArgs {
+    CUtensorMap tw, tx;  // weights' codes (boxes of 128 codes x 128 rows), tokens' fp16 codes (64 x 128)
+    const float *sx, *sw, *bias;
+    void* y;
+    long long ys, M;
+    int N, K, y_type, y_pair;  // y_pair: two 16-bit outputs in one aligned access
+    int tiles_n, tiles_m, n_tiles;
+    int* status;
+};
+
+// Tile t: groups of 8 token tiles, in a group the channel tiles outermost, so that the tiles of a moment share both operands.
+__device__ __forceinline__ void tile_of(const ManyArgs& P, int t, int& tn, int& tm) {
+    const int per = 8 * P.tiles_n, g = t / per, in = t - g * per, wide = min(8, P.tiles_m - 8 * g);
+    tn = in / wide;
+    tm = 8 * g + in - tn * wide;
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linear_many_kernel(const __grid_constant__ ManyArgs P) {
+    using namespace tc;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    __shared__ __align__(8) uint64_t bars[2 * LM_RAW + 2 * LM_B + 2 * LM_A + 3];
+    __shared__ __align__(16) float s_sx[8][128];
+    __shared__ int abort_flag;
+    __shared__ uint32_t tmem_slot;
+    volatile int* abort = &abort_flag;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const uint32_t raw_full = smem_u32(bars), raw_empty = raw_full + 8 * LM_RAW, b_full = raw_empty + 8 * LM_RAW, b_empty = b_full + 8 * LM_B,
+                   a_full = b_empty + 8 * LM_B, a_empty = a_full + 8 * LM_A, acc_full = a_empty + 8 * LM_A, acc_empty = acc_full + 8,
+                   done = acc_empty + 8;
+    const uint32_t raw0 = smem_u32(smem), b0 = raw0 + LM_RAW * LS_A;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < LM_RAW; ++i) {
+            mbar_init(raw_full + 8 * i, 1);
+            mbar_init(raw_empty + 8 * i, 4);
+        }
+        for (int i = 0; i < LM_B; ++i) {
+            mbar_init(b_full + 8 * i, 1);  // (CTA 0's: its own arrival, the bytes of both)
+            mbar_init(b_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < LM_A; ++i) {
+            mbar_init(a_full + 8 * i, 8);  // (CTA 0's: the converter warps of both)
+            mbar_init(a_empty + 8 * i, 1);
+        }
+        mbar_init(acc_full, 1);
+        mbar_init(acc_empty, 16);  // (CTA 0's: the epilogue warps of both)
+        mbar_init(done, 1);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_tmap(&P.tw);
+        prefetch_tmap(&P.tx);
+    }
+    pdl_wait();
+    __syncthreads();
+    cluster_sync();  // both CTAs' barriers exist
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    cluster_sync();
+    const uint32_t tmem = tmem_slot, tmem_a = tmem + 256;
+    const int n_kb = (P.K + LS_KB - 1) / LS_KB, n_half = (P.K + 63) / 64;
+
+    if (warp == 0) {
+        uint32_t it = 0;
+        bool ok = true;
+        for (int t = pair; t < P.n_tiles && ok; t += pairs) {
+            int tn, tm;
+            tile_of(P, t, tn, tm);
+            for (int kb = 0; kb < n_kb; ++kb, ++it) {
+                const uint32_t s = it % LM_RAW;
+                if (!wait_warp(raw_empty + 8 * s, ((it / LM_RAW) & 1) ^ 1, abort, P.status)) {
+                    ok = false;
+                    break;
+                }
+                mbar_arrive_expect_tx(raw_full + 8 * s, LS_A);
+                tma_load_2d(raw0 + s * LS_A, &P.tw, kb * LS_KB, tn * 256 + rank * 128, raw_full + 8 * s);
+            }
+        }
+        for (uint32_t j = it > LM_RAW ? it - LM_RAW : 0; j < it; ++j) {  // every copy has landed
+            drain_warp(raw_full + 8 * (j % LM_RAW), (j / LM_RAW) & 1);
+        }
+    } else if (warp == 1) {
+        uint32_t it = 0;
+        bool ok = true;
+        const uint32_t lead = cluster_addr(b_full, 0);
+        for (int t = pair; t < P.n_tiles && ok; t += pairs) {
+            int tn, tm;
+            tile_of(P, t, tn, tm);
+            for (int hb = 0; hb < n_half; ++hb, ++it) {
+                const uint32_t s = it % LM_B;
+                if (!wait_warp(b_empty + 8 * s, ((it / LM_B) & 1) ^ 1, abort, P.status)) {
+                    ok = false;
+                    break;
+                }
+                if (rank == 0) mbar_arrive_expect_tx(b_full + 8 * s, 2 * 128 * 128);
+                tma_load_2d_pair(b0 + s * 128 * 128, &P.tx, hb * 64, tm * 256 + rank * 128, lead + 8 * s);
+            }
+        }
+        if (rank == 0)
+            for (uint32_t j = it > LM_B ? it - LM_B : 0; j < it; ++j) {
+                drain_warp(b_full + 8 * (j % LM_B), (j / LM_B) & 1);
+            }
+    } else if (warp == 2) {
+        if (rank == 0) {
+            const uint32_t idesc = make_idesc(256, 256);
+            const uint64_t bd0 = make_sdesc(b0);
+            uint32_t ia = 0, ib = 0, it = 0;
+            bool ok = true;
+            for (int t = pair; t < P.n_tiles && ok; t += pairs, ++it) {
+                if (!wait_warp_cluster(acc_empty, (it & 1) ^ 1, abort, P.status)) break;
+                tc_fence_after();
+                uint32_t acc = 0;
+                for (int kb = 0; kb < n_kb && ok; ++kb, ++ia) {
+                    const uint32_t c = ia % LM_A;
+                    if (!wait_warp_cluster(a_full + 8 * c, (ia / LM_A) & 1, abort, P.status)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    for (int hf = 0; hf < min(2, n_half - 2 * kb); ++hf, ++ib) {
+                        const uint32_t s = ib % LM_B;
+                        if (!wait_warp_cluster(b_full + 8 * s, (ib / LM_B) & 1, abort, P.status)) {
+                            ok = false;
+                            break;
+                        }
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) {
+                            tc_mma_ta_pair(tmem, tmem_a + 64 * c + 32 * hf + 8 * kk, bd0 + s * (128 * 128 >> 4) + 2 * kk, idesc, acc);
+                            acc = 1;
+                        }
+                        tc_commit_pair(b_empty + 8 * s);
+                    }
+                    if (ok) tc_commit_pair(a_empty + 8 * c);
+                }
+                if (ok) tc_commit_pair(acc_full);
+            }
+            tc_commit_pair(done);
+        }
+        drain_warp(done, 0);
+    } else if (warp >= 4 && warp < 8) {
+        const int quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lead = cluster_addr(a_full, 0);
+        uint32_t it = 0;
+        bool ok = true;
+        for (int t = pair; t < P.n_tiles && ok; t += pairs)
+            for (int kb = 0; kb < n_kb; ++kb, ++it) {
+                const uint32_t s = it % LM_RAW, c = it % LM_A;
+                if (!wait_warp(raw_full + 8 * s, (it / LM_RAW) & 1, abort, P.status) ||
+                    !wait_warp_cluster(a_empty + 8 * c, ((it / LM_A) & 1) ^ 1, abort, P.status)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const unsigned char* ra = smem + s * LS_A;
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    uint32_t r[32];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(ra + row * 128 + (((4 * hf + q) ^ (row & 7)) << 4));
+                        const uint32_t w[4] = {v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            r[8 * q + 2 * e] = code_pair(w[e], LOW_PAIR);
+                            r[8 * q + 2 * e + 1] = code_pair(w[e], HIGH_PAIR);
+                        }
+                    }
+                    tmem_st32_nw(tmem_a + ((uint32_t)(quad * 32) << 16) + 64 * c + 32 * hf, r);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(raw_empty + 8 * s);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(lead + 8 * c);
+            }
+    } else if (warp >= 8) {
+        const int quad = warp & 3, half = (warp - 8) >> 2;  // channels 32 quad + lane, tokens 128 half ..
+        const uint32_t lead = cluster_addr(acc_empty, 0), at = tmem + ((uint32_t)(quad * 32) << 16) + 128 * half;
+        float* sxs = s_sx[warp - 8];
+        uint32_t it = 0;
+        for (int t = pair; t < P.n_tiles; t += pairs, ++it) {
+            int tn, tm;
+            tile_of(P, t, tn, tm);
+            const int ch = tn * 256 + rank * 128 + quad * 32 + lane;
+            const long long m0 = (long long)tm * 256 + 128 * half;
+            const float sw = ch < P.N ? __ldg(P.sw + ch) : 0.0f, bias = P.bias && ch < P.N ? __ldg(P.bias + ch) : 0.0f;
+            for (int i = lane; i < 128; i += 32) sxs[i] = m0 + i < P.M ? __ldg(P.sx + m0 + i) : 0.0f;
+            __syncwarp();
+            if (!wait_warp_cluster(acc_full, it & 1, abort, P.status)) break;
+            tc_fence_after();
+            const int cols = (int)min(128LL, P.M - m0);
+            if (P.y_type == FXPQ_FT_F32) {
+                for (int c = 0; c < 128; c += 16) {
+                    uint32_t v[16];
+                    tmem_ld16_nw(at + c, v);
+                    tmem_wait_ld();
+                    reg_fence(v);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (c + e < cols && ch < P.N)
+                            static_cast<float*>(P.y)[(m0 + c + e) * P.ys + ch] = fmaf(__uint_as_float(v[e]) * sxs[c + e], sw, bias);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(lead);
+                continue;
+            }
+            uint32_t y[64];  // tokens 2 i, 2 i + 1 of this thread's channel
+#pragma unroll
+            for (int c = 0; c < 128; c += 16) {
+                uint32_t v[16];
+                tmem_ld16_nw(at + c, v);
+                tmem_wait_ld();
+                reg_fence(v);
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float2 sx = *reinterpret_cast<const float2*>(sxs + c + e);
+                    const float a = fmaf(__uint_as_float(v[e]) * sx.x, sw, bias), b = fmaf(__uint_as_float(v[e + 1]) * sx.y, sw, bias);
+                    if (P.y_type == FXPQ_FT_F16) {
+                        y[(c + e) / 2] = h2_bits(__floats2half2_rn(a, b));
+                    } else {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+                        y[(c + e) / 2] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(lead);  // the accumulators may be overwritten
+            unsigned short* out = static_cast<unsigned short*>(P.y);
+            if (P.y_pair) {  // even lanes store the even token's two channels, odd lanes the odd token's
+                const int odd = lane & 1, c0 = ch - odd;
+#pragma unroll
+                for (int i = 0; i < 64; ++i) {
+                    const uint32_t o = __shfl_xor_sync(0xffffffffu, y[i], 1);
+                    const uint32_t w = odd ? __byte_perm(o, y[i], 0x7632) : __byte_perm(y[i], o, 0x5410);
+                    const long long m = m0 + 2 * i + odd;
+                    if (2 * i + odd < cols && c0 < P.N) {
+                        if (c0 + 1 < P.N)
+                            *reinterpret_cast<uint32_t*>(out + m * P.ys + c0) = w;
+                        else
+                            out[m * P.ys + c0] = (unsigned short)w;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 64; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (2 * i + e < cols && ch < P.N) out[(m0 + 2 * i + e) * P.ys + ch] = (unsigned short)(y[i] >> (16 * e));
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (warp == 2) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+    }
+    cluster_sync();  // (the other CTA may still arrive on this one's barriers until here)
+}
+
+// int8 rows to fp16 codes, 16 per thread.
+__global__ void __launch_bounds__(256) expand_codes_kernel(const int8_t* __restrict__ x, long long x_stride, int chunks, __half* __restrict__ y,
+                                                           long long y_stride) {
+    pdl_wait();
+    const long long m = blockIdx.y;
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= chunks) return;
+    const uint4 v = *reinterpret_cast<const uint4*>(x + m * x_stride + 16 * c);
+    const uint32_t w[4] = {v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u};
+    uint4* dst = reinterpret_cast<uint4*>(y + m * y_stride + 16 * c);
+    dst[0] = make_uint4(code_pair(w[0], LOW_PAIR), code_pair(w[0], HIGH_PAIR), code_pair(w[1], LOW_PAIR), code_pair(w[1], HIGH_PAIR));
+    dst[1] = make_uint4(code_pair(w[2], LOW_PAIR), code_pair(w[2], HIGH_PAIR), code_pair(w[3], LOW_PAIR), code_pair(w[3], HIGH_PAIR));
+}
+
 // Codes as [rows][K] bytes in boxes of 128 codes x `box` rows, 128-byte swizzle.
 bool encode_rows(CUtensorMap* map, const int8_t* codes, long long rows, int K, long long stride, int box) {
     EncodeTiledFn enc = encode_tiled();
@@ -295,6 +595,35 @@ bool encode_rows(CUtensorMap* map, const int8_t* codes, long long rows, int K, l
     const cuuint32_t b[2] = {(cuuint32_t)LS_KB, (cuuint32_t)box}, es[2] = {1, 1};
     return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(codes), dims, strides, b, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tokens' fp16 codes in boxes of 64 codes x 128 rows.
+bool encode_half_rows(CUtensorMap* map, const __half* codes, long long rows, int K, long long pitch) {
+    EncodeTiledFn enc = encode_tiled();
+    const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch * 2};
+    const cuuint32_t b[2] = {64, 128}, es[2] = {1, 1};
+    return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(codes), dims, strides, b, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+size_t codes_pitch(int32_t K) { return ((size_t)K + 15) / 16 * 16; }
+
+// Many tokens go to the pairs of CTAs.
+bool many_tokens(int64_t M, int32_t N, int32_t K) { return M > 256 && N >= 128 && K >= 128; }
+
+fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
+    static bool set = false;
+    if (!set) {
+        if (cudaFuncSetAttribute(linear_many_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LM_SMEM) != cudaSuccess) return FXPQ_ERR_CUDA;
+        set = true;
+    }
+    const long long tn = ((long long)P.N + 255) / 256, tm = (P.M + 255) / 256;
+    if (tn * tm > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
+    P.tiles_n = (int)tn, P.tiles_m = (int)tm, P.n_tiles = (int)(tn * tm);
+    P.y_pair = aligned(P.y, 4) && P.ys % 2 == 0;
+    const int pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
+    launch_pdl(linear_many_kernel, dim3(2 * (unsigned)(P.n_tiles < pairs ? P.n_tiles : pairs)), dim3(LM_THREADS), LM_SMEM, st, P);
+    return after_launch("linear_many");
 }
 
 fxpq_status launch_few(LinArgs& P, cudaStream_t st) {
@@ -332,32 +661,43 @@ fxpq_status launch_few(LinArgs& P, cudaStream_t st) {
 using namespace fxpq;
 using namespace fxpq::llm;
 
-extern "C" fxpq_status fxpq_quantize_tokens(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, int8_t* d_codes,
-                                            int64_t codes_stride, float* d_scale, void* stream) {
-    if (!ftype_ok(x_type) || M < 0 || K < 0 || M > INT32_MAX || codes_stride < K || (M > 0 && !d_scale) ||
-        (M > 0 && K > 0 && (!d_x || !d_codes)) || (M > 1 && x_stride < K) || !aligned(d_x, ftype_bytes(x_type)) || !aligned(d_scale, 4))
-        return FXPQ_ERR_INVALID_ARG;
-    if (M == 0) return FXPQ_OK;
+namespace {
+template <typename C>
+fxpq_status quantize_rows(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, C* d_codes, int64_t codes_stride,
+                          float* d_scale, cudaStream_t st) {
     const int e = ftype_bytes(x_type), vec = aligned(d_x, 16) && x_stride * e % 16 == 0;
     const int c_vec = aligned(d_codes, 8) && codes_stride % 8 == 0;
     const dim3 grid((unsigned)M), block(QT_THREADS);
-    cudaStream_t st = as_stream(stream);
     int* status = status_ptr();
+    auto launch = [&](auto* x) {
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(x)>>;
+        launch_pdl(quantize_tokens_kernel<T, C>, grid, block, 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
+    };
     if (x_type == FXPQ_FT_F32)
-        launch_pdl(quantize_tokens_kernel<float>, grid, block, 0, st, static_cast<const float*>(d_x), K, x_stride, vec, d_codes,
-                   codes_stride, c_vec, d_scale, status);
+        launch(static_cast<const float*>(d_x));
     else if (x_type == FXPQ_FT_F16)
-        launch_pdl(quantize_tokens_kernel<__half>, grid, block, 0, st, static_cast<const __half*>(d_x), K, x_stride, vec, d_codes,
-                   codes_stride, c_vec, d_scale, status);
+        launch(static_cast<const __half*>(d_x));
     else
-        launch_pdl(quantize_tokens_kernel<__nv_bfloat16>, grid, block, 0, st, static_cast<const __nv_bfloat16*>(d_x), K, x_stride, vec,
-                   d_codes, codes_stride, c_vec, d_scale, status);
+        launch(static_cast<const __nv_bfloat16*>(d_x));
     return after_launch("quantize_tokens");
 }
 
+bool rows_ok(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride) {
+    return ftype_ok(x_type) && M >= 0 && K >= 0 && M <= INT32_MAX && (M == 0 || K == 0 || d_x) && (M <= 1 || x_stride >= K) &&
+           aligned(d_x, ftype_bytes(x_type));
+}
+}  // namespace
+
+extern "C" fxpq_status fxpq_quantize_tokens(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, int8_t* d_codes,
+                                            int64_t codes_stride, float* d_scale, void* stream) {
+    if (!rows_ok(d_x, x_type, M, K, x_stride) || codes_stride < K || (M > 0 && !d_scale) || (M > 0 && K > 0 && !d_codes) || !aligned(d_scale, 4))
+        return FXPQ_ERR_INVALID_ARG;
+    if (M == 0) return FXPQ_OK;
+    return quantize_rows(d_x, x_type, M, K, x_stride, d_codes, codes_stride, d_scale, as_stream(stream));
+}
+
 extern "C" size_t fxpq_linear_i8_workspace(int64_t M, int32_t N, int32_t K) {
-    (void)M, (void)N, (void)K;
-    return 0;
+    return M > 0 && many_tokens(M, N, K) ? ((size_t)M * codes_pitch(K) * sizeof(__half) + 255) / 256 * 256 : 0;
 }
 
 namespace {
@@ -371,6 +711,26 @@ fxpq_status check_linear(const int8_t* d_x, int64_t x_stride, const float* d_sx,
         return FXPQ_ERR_INVALID_ARG;
     return FXPQ_OK;
 }
+
+fxpq_status product_few(const int8_t* d_x, int64_t x_stride, const float* d_sx, const int8_t* d_w, int64_t w_stride, const float* d_sw,
+                        const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st) {
+    LinArgs P;
+    P.cols = M >= 128 ? 128 : (int)(M + 15) / 16 * 16;
+    P.n_kb = (K + LS_KB - 1) / LS_KB;
+    if (K > 0 && (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_rows(&P.tx, d_x, M, K, x_stride, P.cols))) return FXPQ_ERR_CUDA;
+    P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.y_type = y_type;
+    P.status = status_ptr();
+    return launch_few(P, st);
+}
+
+fxpq_status product_many(const __half* half, size_t pitch, const float* d_sx, const int8_t* d_w, int64_t w_stride, const float* d_sw,
+                         const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st) {
+    ManyArgs P;
+    if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_half_rows(&P.tx, half, M, K, (long long)pitch)) return FXPQ_ERR_CUDA;
+    P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.K = K, P.y_type = y_type;
+    P.status = status_ptr();
+    return launch_many(P, st);
+}
 }  // namespace
 
 extern "C" fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const float* d_sx, const int8_t* d_w, int64_t w_stride,
@@ -381,40 +741,54 @@ extern "C" fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const
     if (M == 0 || N == 0) return FXPQ_OK;
     const size_t need = fxpq_linear_i8_workspace(M, N, K);
     if (need && (!d_ws || ws_bytes < need || !aligned(d_ws, 256))) return FXPQ_ERR_WORKSPACE;
-    LinArgs P;
-    P.cols = M >= 128 ? 128 : (int)(M + 15) / 16 * 16;
-    P.n_kb = (K + LS_KB - 1) / LS_KB;
-    if (K > 0 && (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_rows(&P.tx, d_x, M, K, x_stride, P.cols))) return FXPQ_ERR_CUDA;
-    P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.y_type = y_type;
-    P.status = status_ptr();
-    return launch_few(P, as_stream(stream));
+    if (many_tokens(M, N, K)) {
+        const size_t pitch = codes_pitch(K);
+        if (pitch > (size_t)INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
+        __half* half = static_cast<__half*>(d_ws);
+        for (int64_t m = 0; m < M; m += 65535) {  // (the grid's second dimension)
+            const int64_t rows = M - m < 65535 ? M - m : 65535;
+            launch_pdl(expand_codes_kernel, dim3((unsigned)((pitch / 16 + 255) / 256), (unsigned)rows), dim3(256), 0, as_stream(stream),
+                       d_x + m * x_stride, x_stride, (int)(pitch / 16), half + m * pitch, (long long)pitch);
+            const fxpq_status rc = after_launch("expand_codes");
+            if (rc != FXPQ_OK) return rc;
+        }
+        return product_many(half, pitch, d_sx, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, as_stream(stream));
+    }
+    return product_few(d_x, x_stride, d_sx, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, as_stream(stream));
 }
 
 namespace {
-// The workspace of fxpq_linear_tokens: codes, scales, then fxpq_linear_i8's.
+// The workspace of fxpq_linear_tokens: codes (fp16 ones for many tokens), then scales.
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-size_t codes_pitch(int32_t K) { return ((size_t)K + 15) / 16 * 16; }
+size_t tokens_codes(int64_t M, int32_t N, int32_t K) {
+    return up256((size_t)M * codes_pitch(K) * (many_tokens(M, N, K) ? sizeof(__half) : 1));
+}
 }  // namespace
 
 extern "C" size_t fxpq_linear_tokens_workspace(int64_t M, int32_t N, int32_t K) {
     if (M <= 0 || N < 0 || K < 0) return 0;
-    return up256((size_t)M * codes_pitch(K)) + up256((size_t)M * sizeof(float)) + fxpq_linear_i8_workspace(M, N, K);
+    return tokens_codes(M, N, K) + up256((size_t)M * sizeof(float));
 }
 
 extern "C" fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64_t x_stride, const int8_t* d_w, int64_t w_stride,
                                           const float* d_sw, const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type,
                                           void* d_y, int64_t y_stride, void* d_ws, size_t ws_bytes, void* stream) {
-    if (M < 0 || N < 0 || K < 0 || !ftype_ok(x_type) || !ftype_ok(y_type)) return FXPQ_ERR_INVALID_ARG;
+    if (M < 0 || N < 0 || K < 0 || !rows_ok(d_x, x_type, M, K, x_stride) || !ftype_ok(y_type)) return FXPQ_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return FXPQ_OK;
-    const size_t need = fxpq_linear_tokens_workspace(M, N, K);
-    if (!d_ws || ws_bytes < need || !aligned(d_ws, 256)) return FXPQ_ERR_WORKSPACE;
-    const size_t pitch = codes_pitch(K), c = up256((size_t)M * pitch), s = up256((size_t)M * sizeof(float));
+    if (!d_ws || ws_bytes < fxpq_linear_tokens_workspace(M, N, K) || !aligned(d_ws, 256)) return FXPQ_ERR_WORKSPACE;
+    const size_t pitch = codes_pitch(K);
+    float* scale = reinterpret_cast<float*>(static_cast<char*>(d_ws) + tokens_codes(M, N, K));
+    cudaStream_t st = as_stream(stream);
     int8_t* codes = static_cast<int8_t*>(d_ws);
-    float* scale = reinterpret_cast<float*>(codes + c);
-    const fxpq_status bad = check_linear(codes, pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride);
+    const fxpq_status bad = check_linear(codes, (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride);
     if (bad != FXPQ_OK) return bad;  // (before anything is launched)
-    const fxpq_status rc = fxpq_quantize_tokens(d_x, x_type, M, K, x_stride, codes, (int64_t)pitch, scale, stream);
+    if (many_tokens(M, N, K)) {
+        __half* half = static_cast<__half*>(d_ws);
+        const fxpq_status rc = quantize_rows(d_x, x_type, M, K, x_stride, half, (int64_t)pitch, scale, st);
+        if (rc != FXPQ_OK) return rc;
+        return product_many(half, pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, st);
+    }
+    const fxpq_status rc = quantize_rows(d_x, x_type, M, K, x_stride, codes, (int64_t)pitch, scale, st);
     if (rc != FXPQ_OK) return rc;
-    return fxpq_linear_i8(codes, (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, codes + c + s,
-                          need - c - s, stream);
+    return product_few(codes, (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, st);
 }
