@@ -7,7 +7,8 @@
 //   warps 0-3, 4-7  a tile's softmax each, a thread per row: maximum, weights to fp16, sums (rescaled when the
 //                   maximum has grown by 2^8, a few times per row); at the end O / l
 //   warps 8-11      converters: codes to fp16 operand tiles, once for both row tiles
-//   warp 12         tensor memory, products;   warp 13   pages, scales, copies
+//   warp 12         tensor memory, products;   warp 13   pages, scales, copies;   14, 15   none
+// Registers are split 184 : 72 between the softmax warps, which keep a row's 128 scores in them, and the others.
 // Codes arrive as they are stored ([keys][dim] bytes, one TMA box per page): K is a K-major operand and V, with the
 // same bytes, an operand whose columns are contiguous, so that neither is transposed.
 #include "fxpq_attend.cuh"
@@ -18,7 +19,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int KEYS = 128, ROWS = 256, THREADS = 14 * 32;
+constexpr int KEYS = 128, ROWS = 256, THREADS = 16 * 32;
 constexpr int TABS = 8;  // scale tables in flight: the copies run at most five steps ahead of the softmax
 
 template <int D>
@@ -33,6 +34,29 @@ static_assert(Smem<128>::bytes + 2048 <= 232448, "shared memory of a CTA");
 __device__ __forceinline__ uint64_t make_sdesc_mn(uint32_t saddr) {
     return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)(16384u >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1u << 46 |
            (uint64_t)2u << 61;
+}
+
+// Two fp32 values in a register pair, with the packed arithmetic of this architecture.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 template <int D>
@@ -98,6 +122,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     const uint32_t base = smem_u32(smem);
+    // (the launch holds 512 x 128 registers: 256 x 184 + 256 x 72 of them)
+    if (warp < 8)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    else
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
 
     if (warp < 8) {
         // ================================================================ softmax: one row per thread
@@ -151,31 +180,28 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 }
                 tc_fence_after();
                 const int k0 = (j0 + i) * KEYS, room = limit - k0;  // keys of this step that the row sees
-                const bool masked = __any_sync(0xffffffffu, live && room < KEYS);
+                uint32_t s[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32_nw(ts + 32 * c, s[c]);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) reg_fence(s[c]);
+                if (__any_sync(0xffffffffu, live && room < KEYS)) {  // the last steps of a row
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) s[c][e] = 32 * c + e < room ? s[c][e] : 0xff800000u;
+                }
                 // ---- the largest t, 16 keys (one scale) at a time
                 float top = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < KEYS / 32; ++c) {
-                    uint32_t s0[16], s1[16];
-                    tmem_ld16_nw(ts + 32 * c, s0);
-                    tmem_ld16_nw(ts + 32 * c + 16, s1);
-                    tmem_wait_ld();
-                    reg_fence(s0);
-                    reg_fence(s1);
+                for (int g = 0; g < 8; ++g) {
+                    const uint32_t* x = s[g >> 1] + 16 * (g & 1);
+                    float mx = __uint_as_float(x[0]);
 #pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-                        const uint32_t(&s)[16] = hf ? s1 : s0;
-                        float mx = -INFINITY;
-                        if (masked) {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, 32 * c + 16 * hf + e < room ? __uint_as_float(s[e]) : -INFINITY);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, __uint_as_float(s[e]));
-                        }
-                        const float lv = tab[slot][1][2 * c + hf];
-                        if (mx > -INFINITY) top = fmaxf(top, fmaf(mx, tab[slot][0][2 * c + hf] * cf, lv));
-                    }
+                    for (int e = 1; e < 15; e += 2) mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                    mx = fmaxf(mx, __uint_as_float(x[15]));
+                    top = fmaxf(top, mx == -INFINITY ? mx : fmaf(mx, tab[slot][0][g] * cf, tab[slot][1][g]));
                 }
                 const bool grow = top > m + LAZY;
                 if (__any_sync(0xffffffffu, grow)) {
@@ -196,34 +222,29 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                         tmem_wait_st();
                     }
                 }
-                // ---- weights, in place of S from its start (32 scores become 16 words)
+                // ---- weights, in place of S
 #pragma unroll
-                for (int c = 0; c < KEYS / 32; ++c) {
-                    uint32_t s0[16], s1[16], w[16];
-                    tmem_ld16_nw(ts + 32 * c, s0);
-                    tmem_ld16_nw(ts + 32 * c + 16, s1);
-                    tmem_wait_ld();
-                    reg_fence(s0);
-                    reg_fence(s1);
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t w[16];
 #pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {
-                        const uint32_t(&s)[16] = hf ? s1 : s0;
-                        const float f = tab[slot][0][2 * c + hf] * cf, lv = tab[slot][1][2 * c + hf] - m;
-                        float sum0 = 0.0f, sum1 = 0.0f;
+                        const int g = 2 * c + hf;
+                        // (FLT_MIN: a page outside the cache has scale 0, which must not meet the -inf of a masked score)
+                        const float f = fmaxf(tab[slot][0][g] * cf, FLT_MIN), lv = tab[slot][1][g] - m;
+                        const uint64_t f2 = pack2(f, f), lv2 = pack2(lv, lv);
+                        uint64_t sum = 0;
 #pragma unroll
                         for (int e = 0; e < 16; e += 2) {
-                            float x = fmaf(__uint_as_float(s[e]), f, lv), y = fmaf(__uint_as_float(s[e + 1]), f, lv);
-                            if (masked) {
-                                x = 32 * c + 16 * hf + e < room ? x : -INFINITY;
-                                y = 32 * c + 16 * hf + e + 1 < room ? y : -INFINITY;
-                            }
+                            float x, y;
+                            unpack2(fma2(pack2(__uint_as_float(s[c][16 * hf + e]), __uint_as_float(s[c][16 * hf + e + 1])), f2, lv2), x, y);
                             x = ex2(x);
                             y = ex2(y);
-                            sum0 += x;
-                            sum1 += y;
+                            sum = add2(sum, pack2(x, y));
                             w[8 * hf + e / 2] = h2_bits(__floats2half2_rn(x, y));
                         }
-                        l = fmaf(sum0 + sum1, tab[slot][2][2 * c + hf], l);
+                        float a, b2;
+                        unpack2(sum, a, b2);
+                        l = fmaf(a + b2, tab[slot][2][g], l);
                     }
                     tmem_st16_nw(ts + 16 * c, w);
                 }
