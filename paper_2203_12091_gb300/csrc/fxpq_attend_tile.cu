@@ -1,16 +1,21 @@
 // fxpq_attend_tile.cu -- attention of many query rows (prompts and chunks) on tcgen05.
 //
 // A CTA takes 256 query rows (tokens x grouped heads) of one sequence and key head as two tiles of 128 rows and walks
-// the keys 128 at a time.  Two products of 128 x 128 x dim per tile and step bound it: S = Q K^T into tensor memory,
-// then O += W V with the weights W as the operand in tensor memory, in place of S.  The two tiles alternate, so that one
-// tile's products run during the other's exponentials.
-//   warps 0-3, 4-7  a tile's softmax each, a thread per row: maximum, weights to fp16, sums (rescaled when the
-//                   maximum has grown by 2^8, a few times per row); at the end O / l
-//   warps 8-11      converters: codes to fp16 operand tiles, once for both row tiles
-//   warp 12         tensor memory, products;   warp 13   pages, scales, copies;   14, 15   none
-// Registers are split 184 : 72 between the softmax warps, which keep a row's 128 scores in them, and the others.
+// the keys 128 at a time.  Two products of 128 x 128 x dim per tile and 128 keys bound it: S = Q K^T into tensor memory, then
+// O += W V with the weights W as the operand in tensor memory, in place of S.  The weights go in two steps of 64 keys, so
+// that the first's product runs while the second's are formed, and the two tiles alternate: one's products run
+// during the other's exponentials.
+//   warps 0-3, 4-7  a tile's softmax each, a thread per row: weights to fp16, sums; at the end O / l
+//   warps 8-11      converters: codes to fp16 operand tiles of 128 keys, once for both row tiles
+//   warp 12         tensor memory, products;   warp 13   pages, scales, copies
+// A step's weights are formed with the maximum as it was; only where some t has passed it by 2^8 (a few times per row) are
+// they formed again, after the sums have been rescaled.  The maximum then moves by whole powers of two, so that
+// rescaling is exact.
 // Codes arrive as they are stored ([keys][dim] bytes, one TMA box per page): K is a K-major operand and V, with the
 // same bytes, an operand whose columns are contiguous, so that neither is transposed.
+// Tried: two buffers of S of 64 keys, so that no softmax waits for a product.  The scores' products of 64 columns read Q twice
+// as often, 3072 cycles of shared memory per 128 keys instead of 2560 (products alone: 2048), and 2 prompts of 8192
+// tokens took 1335 us instead of 1165.
 #include "fxpq_attend.cuh"
 
 namespace fxpq {
@@ -19,13 +24,15 @@ namespace {
 
 using namespace tc;
 
-constexpr int KEYS = 128, ROWS = 256, THREADS = 16 * 32;
-constexpr int TABS = 8;  // scale tables in flight: the copies run at most five steps ahead of the softmax
+constexpr int KEYS = 128, STEP = 64, ROWS = 256, THREADS = 14 * 32;  // keys of an operand tile, of a step
+// Operand tiles K 0, V 0, K 1, .. pass through RAWS stages of codes (copies in flight) and CONVS expanded ones (the products hold V of one step and K of the next, a third is being written).
+constexpr int RAWS = 4, CONVS = 3;
+constexpr int TABS = 8;  // scale tables in flight: the copies run at most five tiles ahead of the softmax
 
 template <int D>
 struct Smem {  // offsets from the 1024-byte aligned base
     static constexpr int Q = 128 * D * 2, CONV = KEYS * D * 2, RAW = KEYS * D;
-    static constexpr int conv0 = 2 * Q, raw0 = conv0 + 4 * CONV, bytes = raw0 + 2 * RAW + 1024;
+    static constexpr int conv0 = 2 * Q, raw0 = conv0 + CONVS * CONV, bytes = raw0 + RAWS * RAW + 1024;
 };
 static_assert(Smem<128>::bytes + 2048 <= 232448, "shared memory of a CTA");
 
@@ -36,23 +43,6 @@ __device__ __forceinline__ uint64_t make_sdesc_mn(uint32_t saddr) {
            (uint64_t)2u << 61;
 }
 
-// Two fp32 values in a register pair, with the packed arithmetic of this architecture.
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
-    return v;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -64,24 +54,27 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     using S = Smem<D>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    __shared__ __align__(8) uint64_t bars[2 + 2 + 4 + 4 + TABS + 2 + 2 + 2 + 1 + 1];
+    __shared__ __align__(8) uint64_t bars[2 * RAWS + 2 * CONVS + TABS + 2 + 4 + 2 + 2 + 1 + 1];
     __shared__ float tab[TABS][3][8];  // per 16 keys: key scale, log2 of the value scale, its inverse
     __shared__ int abort_flag;
     __shared__ uint32_t tmem_slot;
     volatile int* abort = &abort_flag;
-    const uint32_t raw_full = smem_u32(bars), raw_empty = raw_full + 16, conv_full = raw_empty + 16, conv_empty = conv_full + 32,
-                   tab_full = conv_empty + 32, s_full = tab_full + 8 * TABS, p_full = s_full + 16, o_full = p_full + 16,
-                   q_full = o_full + 16, drained = q_full + 8;
+    const uint32_t raw_full = smem_u32(bars), raw_empty = raw_full + 8 * RAWS, conv_full = raw_empty + 8 * RAWS,
+                   conv_empty = conv_full + 8 * CONVS, tab_full = conv_empty + 8 * CONVS, s_full = tab_full + 8 * TABS, p_full = s_full + 16, pv_done = p_full + 32,
+                   o_full = pv_done + 16, q_full = o_full + 16, drained = q_full + 8;  // p_full: [tile][step of two]
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(raw_full + 8 * i, 1);
-            mbar_init(raw_empty + 8 * i, 4);
             mbar_init(s_full + 8 * i, 1);
-            mbar_init(p_full + 8 * i, 4);
+            mbar_init(pv_done + 8 * i, 1);
             mbar_init(o_full + 8 * i, 1);
         }
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; ++i) mbar_init(p_full + 8 * i, 4);
+        for (int i = 0; i < RAWS; ++i) {
+            mbar_init(raw_full + 8 * i, 1);
+            mbar_init(raw_empty + 8 * i, 4);
+        }
+        for (int i = 0; i < CONVS; ++i) {
             mbar_init(conv_full + 8 * i, 4);
             mbar_init(conv_empty + 8 * i, 1);
         }
@@ -112,6 +105,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     const int seen = last_pos < 0 ? 0 : A.causal ? min(last_pos + 1, end) : end;  // keys that any row sees
     const int n_all = (seen + KEYS - 1) / KEYS;
     const int j0 = (int)((long long)n_all * blockIdx.y / gridDim.y), n = (int)((long long)n_all * (blockIdx.y + 1) / gridDim.y) - j0;
+    const int n2 = n == 0 ? 0 : min(2 * n, (seen - j0 * KEYS + STEP - 1) / STEP);  // steps
 
     if (warp == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u));
@@ -122,11 +116,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     const uint32_t base = smem_u32(smem);
-    // (the launch holds 512 x 128 registers: 256 x 184 + 256 x 72 of them)
-    if (warp < 8)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-    else
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
 
     if (warp < 8) {
         // ================================================================ softmax: one row per thread
@@ -135,32 +124,46 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
         const uint32_t lanes = (uint32_t)(quad * 32) << 16, ts = tmem + 128 * t + lanes, to = tmem + 256 + 128 * t + lanes;
         const long long qrow = (long long)(first + tok) * A.q_token + (long long)(h * A.group + rr - tok * A.group) * A.q_head;
         float cf;
-        {
+        {  // the row's values, kept as they come (two to a register) between the maximum and the conversion
+            uint32_t x[D / 2];
+            const bool f16 = A.q_f16;
+            const unsigned short* src = static_cast<const unsigned short*>(A.q) + qrow;
+            if (!live) {
+#pragma unroll
+                for (int i = 0; i < D / 2; ++i) x[i] = 0u;
+            } else if (A.q_vec) {
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(src + 8 * i);
+                    x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 2; ++i) x[i] = src[2 * i] | (uint32_t)src[2 * i + 1] << 16;
+            }
+            auto pair = [&](uint32_t v) {
+                return f16 ? __half22float2(*reinterpret_cast<const __half2*>(&v)) : make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+            };
             float top = 0.0f;
             bool odd = false;
-            if (live)
-#pragma unroll 4
-                for (int d = 0; d < D; d += 8) {
-                    float x[8];
-                    load_q8(A, qrow + d, x);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        odd |= !(fabsf(x[e]) <= FLT_MAX);
-                        top = fmaxf(top, fabsf(x[e]));
-                    }
-                }
+            for (int i = 0; i < D / 2; ++i) {
+                const float2 v = pair(x[i]);
+                odd |= !(fabsf(v.x) <= FLT_MAX) || !(fabsf(v.y) <= FLT_MAX);
+                top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+            }
             const int e = odd ? 0 : q_exponent(top);
             const float up = pow2i(e);
             cf = A.scale * LOG2E * pow2i(-e);
-#pragma unroll 4
-            for (int d = 0; d < D; d += 8) {
-                float x[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-                if (live) load_q8(A, qrow + d, x);
-                *reinterpret_cast<uint4*>(smem + t * S::Q + (d >> 6) * 16384 + r * 128 + ((((d >> 3) & 7) ^ (r & 7)) << 4)) =
-                    make_uint4(h2_bits(__floats2half2_rn(x[0] * up, x[1] * up)), h2_bits(__floats2half2_rn(x[2] * up, x[3] * up)),
-                               h2_bits(__floats2half2_rn(x[4] * up, x[5] * up)), h2_bits(__floats2half2_rn(x[6] * up, x[7] * up)));
+            for (int d = 0; d < D; d += 8) {
+                uint32_t h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 v = pair(x[d / 2 + i]);
+                    h[i] = h2_bits(__floats2half2_rn(v.x * up, v.y * up));
+                }
+                *reinterpret_cast<uint4*>(smem + t * S::Q + (d >> 6) * 16384 + r * 128 + ((((d >> 3) & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
             }
         }
         fence_proxy_async();
@@ -171,44 +174,88 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             const int limit = !live || pos < 0 ? 0 : A.causal ? min(pos + 1, end) : end;
             float m = NO_MAX, l = 0.0f;
             bool ok = true;
-            for (int i = 0; i < n; ++i) {
-                const int slot = i % TABS;
-                if (!wait_warp(tab_full + 8 * slot, (i / TABS) & 1, abort, A.status) ||
-                    !wait_warp(s_full + 8 * t, i & 1, abort, A.status)) {
-                    ok = false;
-                    break;
+            for (int i = 0; i < n2; ++i) {
+                const int slot = (i >> 1) % TABS;
+                if ((i & 1) == 0) {
+                    if (!wait_warp(tab_full + 8 * slot, ((i >> 1) / TABS) & 1, abort, A.status) ||
+                        !wait_warp(s_full + 8 * t, (i >> 1) & 1, abort, A.status)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
                 }
-                tc_fence_after();
-                const int k0 = (j0 + i) * KEYS, room = limit - k0;  // keys of this step that the row sees
-                uint32_t s[4][32];
+                const int room = limit - j0 * KEYS - i * STEP;  // keys of this step that the row sees
+                const uint32_t sb = ts + STEP * (i & 1);
+                const float *kf = tab[slot][0] + 4 * (i & 1), *lg = tab[slot][1] + 4 * (i & 1), *iv = tab[slot][2] + 4 * (i & 1);
+                const bool masked = __any_sync(0xffffffffu, live && room < STEP);  // the last steps of a row
+                uint32_t s[64], w[32];
+                float part, over;  // the step's normaliser, the largest t - m
+                auto load = [&]() {
+                    tmem_ld32_nw(sb, *reinterpret_cast<uint32_t(*)[32]>(s));
+                    tmem_ld32_nw(sb + 32, *reinterpret_cast<uint32_t(*)[32]>(s + 32));
+                    tmem_wait_ld();
+                    reg_fence(s);
+                    if (masked) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32_nw(ts + 32 * c, s[c]);
-                tmem_wait_ld();
+                        for (int e = 0; e < 64; ++e) s[e] = e < room ? s[e] : 0xff800000u;
+                    }
+                };
+                auto weights = [&]() {  // 16 keys of one scale at a time, four independent chains
+                    float top[4], sums[4];
+                    float2 x[32];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) reg_fence(s[c]);
-                if (__any_sync(0xffffffffu, live && room < KEYS)) {  // the last steps of a row
+                    for (int g = 0; g < 4; ++g) {
+                        // (FLT_MIN: a page outside the cache has scale 0, which must not meet the -inf of a masked score)
+                        const float f = fmaxf(kf[g] * cf, FLT_MIN), lv = lg[g] - m;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                        for (int e = 8 * g; e < 8 * g + 8; ++e)
+                            x[e] = __ffma2_rn(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), make_float2(f, f), make_float2(lv, lv));
+                    }
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) s[c][e] = 32 * c + e < room ? s[c][e] : 0xff800000u;
-                }
-                // ---- the largest t, 16 keys (one scale) at a time
-                float top = -INFINITY;
+                    for (int g = 0; g < 4; ++g) {
+                        top[g] = fmaxf(x[8 * g].x, x[8 * g].y);
 #pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const uint32_t* x = s[g >> 1] + 16 * (g & 1);
-                    float mx = __uint_as_float(x[0]);
+                        for (int e = 8 * g + 1; e < 8 * g + 8; ++e) top[g] = max3(top[g], x[e].x, x[e].y);
+                    }
 #pragma unroll
-                    for (int e = 1; e < 15; e += 2) mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-                    mx = fmaxf(mx, __uint_as_float(x[15]));
-                    top = fmaxf(top, mx == -INFINITY ? mx : fmaf(mx, tab[slot][0][g] * cf, tab[slot][1][g]));
-                }
-                const bool grow = top > m + LAZY;
-                if (__any_sync(0xffffffffu, grow)) {
-                    const float f = grow ? ex2(m - top) : 1.0f;
-                    m = grow ? top : m;
+                    for (int e = 0; e < 32; ++e) x[e] = make_float2(ex2(x[e].x), ex2(x[e].y));
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float2 a = __fadd2_rn(x[8 * g], x[8 * g + 1]), b2 = __fadd2_rn(x[8 * g + 2], x[8 * g + 3]);
+                        a = __fadd2_rn(a, __fadd2_rn(x[8 * g + 4], x[8 * g + 5]));
+                        b2 = __fadd2_rn(b2, __fadd2_rn(x[8 * g + 6], x[8 * g + 7]));
+                        a = __fadd2_rn(a, b2);
+                        sums[g] = a.x + a.y;
+#pragma unroll
+                        for (int e = 8 * g; e < 8 * g + 8; ++e) w[e] = h2_bits(__floats2half2_rn(x[e].x, x[e].y));
+                    }
+                    over = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+                    part = fmaf(sums[0], iv[0], sums[1] * iv[1]) + fmaf(sums[2], iv[2], sums[3] * iv[3]);
+                };
+                load();
+                weights();
+                if (__any_sync(0xffffffffu, over > LAZY)) {
+                    load();
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float mx = -INFINITY;
+#pragma unroll
+                        for (int e = 16 * g; e < 16 * g + 16; e += 2) mx = max3(mx, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+                        top = fmaxf(top, mx == -INFINITY ? mx : fmaf(mx, kf[g] * cf, lg[g]));
+                    }
+                    const bool grow = over > LAZY;
+                    const float now = grow ? ceilf(top) : m, f = grow ? ex2(m - now) : 1.0f;
+                    m = now;
                     l *= f;
-                    if (i > 0) {  // (the products that wrote O are complete: S of this step followed them)
+                    if (i > 0) {
+                        // O holds all steps before this one once the last one's product is complete (the one before that
+                        // is: this step's scores, or the scores this step shares, were issued after it)
+                        if (!wait_warp(pv_done + 8 * t, (i - 1) & 1, abort, A.status)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
 #pragma unroll
                         for (int c = 0; c < D / 16; ++c) {
                             uint32_t o[16];
@@ -219,39 +266,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                             for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
                             tmem_st16_nw(to + 16 * c, o);
                         }
-                        tmem_wait_st();
                     }
+                    weights();
                 }
-                // ---- weights, in place of S
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-                        const int g = 2 * c + hf;
-                        // (FLT_MIN: a page outside the cache has scale 0, which must not meet the -inf of a masked score)
-                        const float f = fmaxf(tab[slot][0][g] * cf, FLT_MIN), lv = tab[slot][1][g] - m;
-                        const uint64_t f2 = pack2(f, f), lv2 = pack2(lv, lv);
-                        uint64_t sum = 0;
-#pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            float x, y;
-                            unpack2(fma2(pack2(__uint_as_float(s[c][16 * hf + e]), __uint_as_float(s[c][16 * hf + e + 1])), f2, lv2), x, y);
-                            x = ex2(x);
-                            y = ex2(y);
-                            sum = add2(sum, pack2(x, y));
-                            w[8 * hf + e / 2] = h2_bits(__floats2half2_rn(x, y));
-                        }
-                        float a, b2;
-                        unpack2(sum, a, b2);
-                        l = fmaf(a + b2, tab[slot][2][g], l);
-                    }
-                    tmem_st16_nw(ts + 16 * c, w);
-                }
+                l += part;
+                tmem_st32_nw(sb, w);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 8 * t);
+                if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * (i & 1));
             }
             if (ok && n > 0) ok = wait_warp(o_full + 8 * t, 0, abort, A.status);
             tc_fence_after();
@@ -289,20 +312,25 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
         // ================================================================ converters
         const int t = threadIdx.x - 256;
         for (int u = 0; u < 2 * n; ++u) {  // K 0, V 0, K 1, V 1 ..
-            if (!wait_warp(raw_full + 8 * (u & 1), (u >> 1) & 1, abort, A.status) ||
-                !wait_warp(conv_empty + 8 * (u & 3), ((u >> 2) & 1) ^ 1, abort, A.status))
+            const int rs = u % RAWS, cs = u % CONVS;
+            if (!wait_warp(raw_full + 8 * rs, (u / RAWS) & 1, abort, A.status) ||
+                !wait_warp(conv_empty + 8 * cs, ((u / CONVS) & 1) ^ 1, abort, A.status))
                 break;
-            const unsigned char* src = smem + S::raw0 + (u & 1) * S::RAW;
-            unsigned char* dst = smem + S::conv0 + (u & 3) * S::CONV;
-            constexpr int CH = D / 16;  // 16-code chunks of a row
-#pragma unroll 4
-            for (int it = 0; it < KEYS * CH / 128; ++it) {
+            const unsigned char* src = smem + S::raw0 + rs * S::RAW;
+            unsigned char* dst = smem + S::conv0 + cs * S::CONV;
+            constexpr int CH = D / 16, IT = KEYS * CH / 128;  // 16-code chunks of a row, of a thread
+            uint4 v[IT];  // all loads in flight together
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const int i = it * 128 + t, row = i / CH, c = i % CH;
+                v[it] = *reinterpret_cast<const uint4*>(src + (D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4)));
+            }
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
                 const int i = it * 128 + t, row = i / CH, c = i % CH, hf = c >> 2;
-                const uint32_t at = D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
-                const uint4 v = *reinterpret_cast<const uint4*>(src + at);
-                uint32_t x = v.x ^ 0x80808080u, y = v.y ^ 0x80808080u;
+                uint32_t x = v[it].x ^ 0x80808080u, y = v[it].y ^ 0x80808080u;
                 const uint4 o0 = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
-                x = v.z ^ 0x80808080u, y = v.w ^ 0x80808080u;
+                x = v[it].z ^ 0x80808080u, y = v[it].w ^ 0x80808080u;
                 const uint4 o1 = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
                 unsigned char* d = dst + hf * 16384 + row * 128;
                 const int j = 2 * (c & 3), odd = D == 128 ? hf : 0;  // (lanes that would meet in a bank begin with the other chunk)
@@ -312,52 +340,51 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(raw_empty + 8 * (u & 1));
-                mbar_arrive(conv_full + 8 * (u & 3));
+                mbar_arrive(raw_empty + 8 * rs);
+                mbar_arrive(conv_full + 8 * cs);
             }
         }
     } else if (warp == 12) {
         // ================================================================ products
         const uint32_t id_qk = make_idesc(128, KEYS), id_pv = make_idesc(128, D) | (1u << 16);
-        bool ok = wait_warp(q_full, 0, abort, A.status);
-        auto scores = [&](int t, int i) {
-            const uint64_t qd = make_sdesc(base + t * S::Q), kd = make_sdesc(base + S::conv0 + ((2 * i) & 3) * S::CONV);
+        // operand tile u of the ring (K 0, V 0, K 1, ..)
+        auto have = [&](int u) { return wait_warp(conv_full + 8 * (u % CONVS), (u / CONVS) & 1, abort, A.status); };
+        auto scores = [&](int t, int j) {  // 128 keys
+            const uint64_t qd = make_sdesc(base + t * S::Q), kd = make_sdesc(base + S::conv0 + (2 * j % CONVS) * S::CONV);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
                 tc_mma(tmem + 128 * t, qd + (kk >> 2) * (16384 >> 4) + 2 * (kk & 3), kd + (kk >> 2) * (16384 >> 4) + 2 * (kk & 3), id_qk, kk > 0);
+            tc_commit(s_full + 8 * t);
+            if (t == tiles - 1) tc_commit(conv_empty + 8 * (2 * j % CONVS));
         };
-        if (ok && n > 0 && wait_warp(conv_full, 0, abort, A.status)) {
+        bool ok = wait_warp(q_full, 0, abort, A.status);
+        if (ok && n > 0 && have(0)) {
             tc_fence_after();
-            for (int t = 0; t < tiles; ++t) {
-                scores(t, 0);
-                tc_commit(s_full + 8 * t);
-            }
-            tc_commit(conv_empty);
-            for (int i = 0; i < n && ok; ++i) {
-                const int uv = (2 * i + 1) & 3, uk = (2 * i + 2) & 3;
-                if (!wait_warp(conv_full + 8 * uv, ((2 * i + 1) >> 2) & 1, abort, A.status)) break;
-                const uint64_t vd = make_sdesc_mn(base + S::conv0 + uv * S::CONV);
+            for (int t = 0; t < tiles; ++t) scores(t, 0);
+            for (int i = 0; i < n2 && ok; ++i) {
+                const int j = i >> 1, uv = (2 * j + 1) % CONVS;
+                if ((i & 1) == 0 && !have(2 * j + 1)) break;
+                const uint64_t vd = make_sdesc_mn(base + S::conv0 + uv * S::CONV + (i & 1) * (STEP * 128));
                 for (int t = 0; t < tiles; ++t) {
-                    if (!wait_warp(p_full + 8 * t, i & 1, abort, A.status)) {
+                    if (!wait_warp(p_full + 16 * t + 8 * (i & 1), j & 1, abort, A.status)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
 #pragma unroll
-                    for (int kk = 0; kk < KEYS / 16; ++kk)
-                        tc_mma_ta(tmem + 256 + 128 * t, tmem + 128 * t + 8 * kk, vd + kk * (2048 >> 4), id_pv, i > 0 || kk > 0);
-                    if (t == tiles - 1) tc_commit(conv_empty + 8 * uv);
-                    if (i + 1 < n) {
-                        if (t == 0 && !wait_warp(conv_full + 8 * uk, ((2 * i + 2) >> 2) & 1, abort, A.status)) {
+                    for (int kk = 0; kk < STEP / 16; ++kk)
+                        tc_mma_ta(tmem + 256 + 128 * t, tmem + 128 * t + STEP * (i & 1) + 8 * kk, vd + kk * (2048 >> 4), id_pv, i > 0 || kk > 0);
+                    tc_commit(pv_done + 8 * t);
+                    if (i == n2 - 1) tc_commit(o_full + 8 * t);  // (of its own: the last two phases of pv_done may both be over)
+                    if (t == tiles - 1 && ((i & 1) || i == n2 - 1)) tc_commit(conv_empty + 8 * uv);
+                    if ((i & 1) && j + 1 < n) {
+                        if (t == 0 && !have(2 * j + 2)) {
                             ok = false;
                             break;
                         }
                         tc_fence_after();
-                        scores(t, i + 1);
-                        tc_commit(s_full + 8 * t);
-                        if (t == tiles - 1) tc_commit(conv_empty + 8 * uk);
-                    } else
-                        tc_commit(o_full + 8 * t);
+                        scores(t, j + 1);
+                    }
                 }
             }
         }
@@ -403,8 +430,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             int boxes = 0;
             for (int g = 0; g < 8; g += box / 16) boxes += (have >> g) & 1;
             for (int v = 0; v < 2; ++v, ++u) {
-                const uint32_t bar = raw_full + 8 * (u & 1), dst = base + S::raw0 + (u & 1) * S::RAW;
-                if (!wait_warp(raw_empty + 8 * (u & 1), ((u >> 1) & 1) ^ 1, abort, A.status)) {
+                const int rs = u % RAWS;
+                const uint32_t bar = raw_full + 8 * rs, dst = base + S::raw0 + rs * S::RAW;
+                if (!wait_warp(raw_empty + 8 * rs, ((u / RAWS) & 1) ^ 1, abort, A.status)) {
                     ok = false;
                     break;
                 }
@@ -419,9 +447,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 nxt = fetch(i + 5);
             }
         }
-        for (int k = max(0, u - 2); k < u; ++k) {  // every copy has landed
-            drain_warp(raw_full + 8 * (k & 1), (k >> 1) & 1);
-        }
+        for (int k = max(0, u - RAWS); k < u; ++k) drain_warp(raw_full + 8 * (k % RAWS), (k / RAWS) & 1);  // every copy has landed
     }
     tc_fence_before();
     __syncthreads();
