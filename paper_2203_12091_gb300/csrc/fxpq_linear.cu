@@ -10,12 +10,13 @@ namespace fxpq {
 namespace llm {
 namespace {
 
-// One block per row: the row stays in registers between the maximum and the codes (KEEP steps of 8 values per
-// thread; longer rows are read again, from L2).
-constexpr int QT_THREADS = 256, QT_KEEP = 4;
+// One block per row: the row stays in registers between the maximum and the codes (QT_KEEP steps of 8 values per
+// thread; longer rows are read again, from L2).  Rows of more than 8192 values take 1024 threads: 64 rows of 25088 5.2 us
+// with 256.
+constexpr int QT_KEEP = 4;
 
 // C: int8 codes, or fp16 ones for the tensor-core kernel that takes them so.
-template <typename T, typename C>
+template <typename T, typename C, int QT_THREADS>
 __global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __restrict__ x, int K, long long x_stride, int vec,
                                                                      C* __restrict__ codes, long long c_stride, int c_vec,
                                                                      float* __restrict__ scale, int* status) {
@@ -105,12 +106,15 @@ __device__ __forceinline__ void store_y(void* y, int type, long long at, float v
 }
 
 struct LinArgs {
-    CUtensorMap tw, tx;  // codes as [N][K], [M][K] bytes, boxes of 128 codes x 128 (tw) or `cols` (tx) rows
+    // weights' codes as [N][K] bytes in boxes of 128 codes x 128 rows (tw), or x the rows that the last tile has (tw2: a box is
+    // slow where it lies outside the tensor); tokens' as [M][K] bytes in boxes of 128 x `rows`, or as fp16 in 64 x `rows`
+    CUtensorMap tw, tw2, tx;
     const float *sx, *sw, *bias;
     void* y;
     long long ys, M;
     int N, y_type, n_kb;
-    int cols;  // tokens of a tile: a multiple of 16, at most 128
+    int rows, cols;  // tokens of a tile, and rounded up to 16, at most 128 (the columns past `rows` hold whatever the stage does)
+    int w_rows;      // channels of the last tile
     int stages;
     int* status;
 };
@@ -119,17 +123,19 @@ struct LinArgs {
 // y^T = w x^T on tcgen05 (kind::f16: the 8-bit kind does not exist on sm_103a; products of codes are exact in fp16): 128
 // output channels on the accumulator's lanes, up to 128 tokens on its columns.  The weights are the traffic.  They
 // arrive as codes (TMA, 128 x 128 bytes a block) and go through registers into tensor memory as the fp16 A operand,
-// so that their shared-memory traffic stays at two bytes a code; the tokens' few rows are expanded in shared memory.
+// so that their shared-memory traffic stays at two bytes a code.  The tokens' rows come as fp16 codes (HALF: written so by the
+// quantizer) or as bytes that are expanded in shared memory.
 //   warp 0   copies;   warp 1   tensor memory, products;   warps 4-7, 8-11   converters (blocks in turn), then the epilogue.
 // The reduction is shared by the CTAs of a cluster, whose fp32 sums meet through distributed shared memory: one launch, a
 // fixed order.  Up to 64 tokens two CTAs fit an SM.
 constexpr int LS_THREADS = 384, LS_KB = 128, LS_A = 128 * LS_KB;
 
-__host__ __device__ inline int ls_smem(int cols, int stages) {  // raw stages, two expanded token stages
-    const int ring = stages * (LS_A + cols * LS_KB) + 2 * cols * LS_KB * 2, sums = cols * 128 * 4;
+__host__ __device__ inline int ls_smem(int cols, int stages, bool half) {  // stages, with bytes two expanded token stages
+    const int ring = half ? stages * (LS_A + cols * LS_KB * 2) : stages * (LS_A + cols * LS_KB) + 2 * cols * LS_KB * 2, sums = cols * 128 * 4;
     return 1024 + (ring > sums ? ring : sums);
 }
 
+template <bool HALF>
 __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_constant__ LinArgs P) {
     using namespace tc;
     extern __shared__ unsigned char smem_raw[];
@@ -141,12 +147,12 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, ST = P.stages, cols = P.cols;
     const uint32_t raw_full = smem_u32(bars), raw_empty = raw_full + 8 * 8, conv_full = raw_empty + 8 * 8, conv_empty = conv_full + 16,
                    done = conv_empty + 16;
-    const int raw_bytes = LS_A + cols * LS_KB;
+    const int raw_bytes = LS_A + cols * LS_KB * (HALF ? 2 : 1);
     const uint32_t raw0 = smem_u32(smem), conv0 = raw0 + ST * raw_bytes;
     if (threadIdx.x == 0) {
         for (int i = 0; i < ST; ++i) {
             mbar_init(raw_full + 8 * i, 1);
-            mbar_init(raw_empty + 8 * i, 4);
+            mbar_init(raw_empty + 8 * i, HALF ? 1 : 4);  // the products' completion, or the converting group's warps
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(conv_full + 8 * i, 4);
@@ -156,7 +162,7 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (P.n_kb) {
-            prefetch_tmap(&P.tw);
+            prefetch_tmap(blockIdx.y == gridDim.y - 1 ? &P.tw2 : &P.tw);
             prefetch_tmap(&P.tx);
         }
     }
@@ -170,34 +176,40 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
     tc_fence_after();
     const uint32_t tmem = tmem_slot, tmem_a = tmem + 128;
     const int rank = blockIdx.x, shares = gridDim.x, n0 = blockIdx.y * 128;
-    const long long m0 = (long long)blockIdx.z * cols;
+    const long long m0 = (long long)blockIdx.z * P.rows;
     const int kb0 = (int)((long long)P.n_kb * rank / shares), n_kb = (int)((long long)P.n_kb * (rank + 1) / shares) - kb0;
 
     if (warp == 0) {
         int i = 0;
+        const bool last = blockIdx.y == gridDim.y - 1;
+        const CUtensorMap* tw = last ? &P.tw2 : &P.tw;
+        const uint32_t bytes = (uint32_t)((last ? P.w_rows : 128) * LS_KB + P.rows * LS_KB * (HALF ? 2 : 1));
         for (; i < n_kb; ++i) {
             const int s = i % ST;
             if (!wait_warp(raw_empty + 8 * s, ((i / ST) & 1) ^ 1, abort, P.status)) break;
             const uint32_t bar = raw_full + 8 * s, dst = raw0 + s * raw_bytes;
-            mbar_arrive_expect_tx(bar, (uint32_t)raw_bytes);
-            tma_load_2d(dst, &P.tw, (kb0 + i) * LS_KB, n0, bar);
+            mbar_arrive_expect_tx(bar, bytes);
+            tma_load_2d(dst, tw, (kb0 + i) * LS_KB, n0, bar);
             tma_load_2d(dst + LS_A, &P.tx, (kb0 + i) * LS_KB, (int)m0, bar);
+            if (HALF) tma_load_2d(dst + LS_A + cols * 128, &P.tx, (kb0 + i) * LS_KB + 64, (int)m0, bar);
         }
         for (int j = max(0, i - ST); j < i; ++j) {  // every copy has landed before this CTA's memory is used again
             drain_warp(raw_full + 8 * (j % ST), (j / ST) & 1);
         }
     } else if (warp == 1) {
         const uint32_t idesc = make_idesc(128, cols);
-        const uint64_t bdesc = make_sdesc(conv0);
+        const uint64_t bdesc = make_sdesc(HALF ? raw0 : conv0);
         for (int i = 0; i < n_kb; ++i) {
-            const int c = i & 1;
+            const int c = i & 1, s = i % ST;
             if (!wait_warp(conv_full + 8 * c, (i >> 1) & 1, abort, P.status)) break;
+            if (HALF && !wait_warp(raw_full + 8 * s, (i / ST) & 1, abort, P.status)) break;
             tc_fence_after();
+            const uint64_t bd = bdesc + (uint64_t)((HALF ? s * raw_bytes + LS_A : c * cols * 256) >> 4);
 #pragma unroll
             for (int kk = 0; kk < LS_KB / 16; ++kk)
-                tc_mma_ta(tmem, tmem_a + 64 * c + 8 * kk, bdesc + (uint64_t)((c * cols * 256 + (kk >> 2) * cols * 128) >> 4) + 2 * (kk & 3), idesc,
-                          i > 0 || kk > 0);
+                tc_mma_ta(tmem, tmem_a + 64 * c + 8 * kk, bd + (uint64_t)(((kk >> 2) * cols * 128) >> 4) + 2 * (kk & 3), idesc, i > 0 || kk > 0);
             tc_commit(conv_empty + 8 * c);
+            if (HALF) tc_commit(raw_empty + 8 * s);
         }
         tc_commit(done);
         drain_warp(done, 0);
@@ -227,6 +239,7 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
                 }
                 tmem_st32_nw(tmem_a + ((uint32_t)(quad * 32) << 16) + 64 * grp + 32 * hf, r);
             }
+            if constexpr (!HALF) {
             const unsigned char* rb = ra + LS_A;
             unsigned char* cb = smem + ST * raw_bytes + grp * cols * 256;
             for (int rr = t >> 3; rr < cols; rr += 16) {  // 16 codes of one token
@@ -243,12 +256,13 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
                 *reinterpret_cast<uint4*>(dst + (((j + hf) ^ (rr & 7)) << 4)) = hf ? o[1] : o[0];
                 *reinterpret_cast<uint4*>(dst + (((j + 1 - hf) ^ (rr & 7)) << 4)) = hf ? o[0] : o[1];
             }
-            tmem_wait_st();
             fence_proxy_async();
+            }
+            tmem_wait_st();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(raw_empty + 8 * s);
+                if (!HALF) mbar_arrive(raw_empty + 8 * s);
                 mbar_arrive(conv_full + 8 * grp);
             }
         }
@@ -273,15 +287,18 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
     }
     // ---- four channels of one token per thread and step, summed over the cluster
     if (shares > 1) cluster_sync();
-    const int c_lo = cols * rank / shares, c_hi = (int)min((long long)(cols * (rank + 1) / shares), P.M - m0);
+    const int mine = (int)min((long long)P.rows, P.M - m0), c_lo = mine * rank / shares, c_hi = mine * (rank + 1) / shares;
     for (int i = c_lo * 32 + threadIdx.x; i < c_hi * 32; i += LS_THREADS) {
         const int c = i >> 5, ch = n0 + 4 * (i & 31);
         const uint32_t at = raw0 + (uint32_t)i * 16;
-        float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int r = 0; r < shares; ++r) {
-            const float4 b = ld_cluster_f4(cluster_addr(at, r));
-            a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w;
-        }
+        float4 b[8], a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        // (all loads in flight: one after the other they took half of a small product's time)
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < shares) b[r] = ld_cluster_f4(cluster_addr(at, r));
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < shares) a.x += b[r].x, a.y += b[r].y, a.z += b[r].z, a.w += b[r].w;
         const float v[4] = {a.x, a.y, a.z, a.w}, sx = __ldg(P.sx + m0 + c);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -597,11 +614,11 @@ bool encode_rows(CUtensorMap* map, const int8_t* codes, long long rows, int K, l
                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Tokens' fp16 codes in boxes of 64 codes x 128 rows.
-bool encode_half_rows(CUtensorMap* map, const __half* codes, long long rows, int K, long long pitch) {
+// Tokens' fp16 codes in boxes of 64 codes x `box` rows.
+bool encode_half_rows(CUtensorMap* map, const __half* codes, long long rows, int K, long long pitch, int box) {
     EncodeTiledFn enc = encode_tiled();
     const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch * 2};
-    const cuuint32_t b[2] = {64, 128}, es[2] = {1, 1};
+    const cuuint32_t b[2] = {64, (cuuint32_t)box}, es[2] = {1, 1};
     return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(codes), dims, strides, b, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -626,18 +643,20 @@ fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
     return after_launch("linear_many");
 }
 
+template <bool HALF>
 fxpq_status launch_few(LinArgs& P, cudaStream_t st) {
     static bool set = false;
     if (!set) {
-        if (cudaFuncSetAttribute(linear_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ls_smem(128, 4)) != cudaSuccess) return FXPQ_ERR_CUDA;
+        if (cudaFuncSetAttribute(linear_few_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, ls_smem(128, 4, HALF)) != cudaSuccess)
+            return FXPQ_ERR_CUDA;
         set = true;
     }
-    const long long tn = (P.N + 127) / 128, tm = (P.M + P.cols - 1) / P.cols;
+    const long long tn = (P.N + 127) / 128, tm = (P.M + P.rows - 1) / P.rows;
     if (tn > 65535 || tm > 65535) return FXPQ_ERR_UNSUPPORTED;
     const int room = (P.cols <= 64 ? 2 : 1) * num_sms();
     int shares = 1;
     while (shares < 8 && tn * tm * shares * 2 <= room && P.n_kb >= 4 * shares) shares *= 2;
-    P.stages = P.cols <= 32 ? 4 : 3;
+    P.stages = P.cols <= 32 || P.cols > 64 ? 4 : 3;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -646,11 +665,11 @@ fxpq_status launch_few(LinArgs& P, cudaStream_t st) {
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3((unsigned)shares, (unsigned)tn, (unsigned)tm);
     c.blockDim = dim3(LS_THREADS);
-    c.dynamicSmemBytes = ls_smem(P.cols, P.stages);
+    c.dynamicSmemBytes = ls_smem(P.cols, P.stages, HALF);
     c.stream = st;
     c.attrs = at;
     c.numAttrs = shares > 1 ? 2 : 1;
-    (void)cudaLaunchKernelEx(&c, linear_few_kernel, P);
+    (void)cudaLaunchKernelEx(&c, linear_few_kernel<HALF>, P);
     return after_launch("linear_few");
 }
 
@@ -667,11 +686,14 @@ fxpq_status quantize_rows(const void* d_x, int32_t x_type, int64_t M, int32_t K,
                           float* d_scale, cudaStream_t st) {
     const int e = ftype_bytes(x_type), vec = aligned(d_x, 16) && x_stride * e % 16 == 0;
     const int c_vec = aligned(d_codes, 8) && codes_stride % 8 == 0;
-    const dim3 grid((unsigned)M), block(QT_THREADS);
+    const dim3 grid((unsigned)M);
     int* status = status_ptr();
     auto launch = [&](auto* x) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(x)>>;
-        launch_pdl(quantize_tokens_kernel<T, C>, grid, block, 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
+        if (K > 8192)
+            launch_pdl(quantize_tokens_kernel<T, C, 1024>, grid, dim3(1024), 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
+        else
+            launch_pdl(quantize_tokens_kernel<T, C, 256>, grid, dim3(256), 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
     };
     if (x_type == FXPQ_FT_F32)
         launch(static_cast<const float*>(d_x));
@@ -712,21 +734,31 @@ fxpq_status check_linear(const int8_t* d_x, int64_t x_stride, const float* d_sx,
     return FXPQ_OK;
 }
 
-fxpq_status product_few(const int8_t* d_x, int64_t x_stride, const float* d_sx, const int8_t* d_w, int64_t w_stride, const float* d_sw,
-                        const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st) {
+// Codes of the tokens: bytes at d_x, or fp16 at half (one of them is null).
+fxpq_status product_few(const int8_t* d_x, const __half* half, int64_t x_stride, const float* d_sx, const int8_t* d_w, int64_t w_stride,
+                        const float* d_sw, const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride,
+                        cudaStream_t st) {
     LinArgs P;
-    P.cols = M >= 128 ? 128 : (int)(M + 15) / 16 * 16;
+    const int64_t tiles = (M + 127) / 128;  // M's equal parts
+    P.rows = (int)((M + tiles - 1) / tiles);
+    P.cols = (P.rows + 15) / 16 * 16;
     P.n_kb = (K + LS_KB - 1) / LS_KB;
-    if (K > 0 && (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_rows(&P.tx, d_x, M, K, x_stride, P.cols))) return FXPQ_ERR_CUDA;
+    P.w_rows = N % 128 ? N % 128 : 128;
+    if (K > 0) {
+        if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !(half ? encode_half_rows(&P.tx, half, M, K, x_stride, P.rows) : encode_rows(&P.tx, d_x, M, K, x_stride, P.rows)))
+            return FXPQ_ERR_CUDA;
+        P.tw2 = P.tw;
+        if (P.w_rows < 128 && !encode_rows(&P.tw2, d_w, N, K, w_stride, P.w_rows)) return FXPQ_ERR_CUDA;
+    }
     P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.y_type = y_type;
     P.status = status_ptr();
-    return launch_few(P, st);
+    return half ? launch_few<true>(P, st) : launch_few<false>(P, st);
 }
 
 fxpq_status product_many(const __half* half, size_t pitch, const float* d_sx, const int8_t* d_w, int64_t w_stride, const float* d_sw,
                          const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st) {
     ManyArgs P;
-    if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_half_rows(&P.tx, half, M, K, (long long)pitch)) return FXPQ_ERR_CUDA;
+    if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_half_rows(&P.tx, half, M, K, (long long)pitch, 128)) return FXPQ_ERR_CUDA;
     P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.K = K, P.y_type = y_type;
     P.status = status_ptr();
     return launch_many(P, st);
@@ -754,20 +786,18 @@ extern "C" fxpq_status fxpq_linear_i8(const int8_t* d_x, int64_t x_stride, const
         }
         return product_many(half, pitch, d_sx, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, as_stream(stream));
     }
-    return product_few(d_x, x_stride, d_sx, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, as_stream(stream));
+    return product_few(d_x, nullptr, x_stride, d_sx, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, as_stream(stream));
 }
 
 namespace {
-// The workspace of fxpq_linear_tokens: codes (fp16 ones for many tokens), then scales.
+// The workspace of fxpq_linear_tokens: the tokens' fp16 codes, then their scales.
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-size_t tokens_codes(int64_t M, int32_t N, int32_t K) {
-    return up256((size_t)M * codes_pitch(K) * (many_tokens(M, N, K) ? sizeof(__half) : 1));
-}
+size_t tokens_codes(int64_t M, int32_t K) { return up256((size_t)M * codes_pitch(K) * sizeof(__half)); }
 }  // namespace
 
 extern "C" size_t fxpq_linear_tokens_workspace(int64_t M, int32_t N, int32_t K) {
     if (M <= 0 || N < 0 || K < 0) return 0;
-    return tokens_codes(M, N, K) + up256((size_t)M * sizeof(float));
+    return tokens_codes(M, K) + up256((size_t)M * sizeof(float));
 }
 
 extern "C" fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64_t x_stride, const int8_t* d_w, int64_t w_stride,
@@ -777,18 +807,13 @@ extern "C" fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64
     if (M == 0 || N == 0) return FXPQ_OK;
     if (!d_ws || ws_bytes < fxpq_linear_tokens_workspace(M, N, K) || !aligned(d_ws, 256)) return FXPQ_ERR_WORKSPACE;
     const size_t pitch = codes_pitch(K);
-    float* scale = reinterpret_cast<float*>(static_cast<char*>(d_ws) + tokens_codes(M, N, K));
+    __half* half = static_cast<__half*>(d_ws);
+    float* scale = reinterpret_cast<float*>(static_cast<char*>(d_ws) + tokens_codes(M, K));
     cudaStream_t st = as_stream(stream);
-    int8_t* codes = static_cast<int8_t*>(d_ws);
-    const fxpq_status bad = check_linear(codes, (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride);
+    const fxpq_status bad = check_linear(static_cast<int8_t*>(d_ws), (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride);
     if (bad != FXPQ_OK) return bad;  // (before anything is launched)
-    if (many_tokens(M, N, K)) {
-        __half* half = static_cast<__half*>(d_ws);
-        const fxpq_status rc = quantize_rows(d_x, x_type, M, K, x_stride, half, (int64_t)pitch, scale, st);
-        if (rc != FXPQ_OK) return rc;
-        return product_many(half, pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, st);
-    }
-    const fxpq_status rc = quantize_rows(d_x, x_type, M, K, x_stride, codes, (int64_t)pitch, scale, st);
+    const fxpq_status rc = quantize_rows(d_x, x_type, M, K, x_stride, half, (int64_t)pitch, scale, st);
     if (rc != FXPQ_OK) return rc;
-    return product_few(codes, (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, st);
+    if (many_tokens(M, N, K)) return product_many(half, pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, st);
+    return product_few(nullptr, half, (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, st);
 }

@@ -89,5 +89,5 @@ def test_the_other_order_of_waits_reads_too_early_with_an_odd_ring():
 def test_the_kernel_waits_in_that_order():
     import os
     src = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2203_12091_gb300", "csrc", "fxpq_linear.cu")).read()
-    kernel = src[src.index("linear_few_kernel(const"):src.index("encode_rows(CUtensorMap")]
-    assert kernel.index("wait_warp(conv_empty + 8 * grp") < kernel.index("wait_warp(raw_full + 8 * s, (i / ST)")
+    converters = src[src.index("const int grp = "):]
+    assert converters.index("wait_warp(conv_empty + 8 * grp") < converters.index("wait_warp(raw_full + 8 * s, (i / ST)")
