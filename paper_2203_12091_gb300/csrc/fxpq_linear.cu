@@ -10,89 +10,104 @@ namespace fxpq {
 namespace llm {
 namespace {
 
-// One block per row: the row stays in registers between the maximum and the codes (QT_KEEP steps of 8 values per
-// thread; longer rows are read again, from L2).  Rows of more than 8192 values take 1024 threads: 64 rows of 25088 5.2 us
-// with 256.
+// One block per row: the row stays in registers as it came (QT_KEEP steps of 8 values per thread; longer rows are read
+// again, from L2) between the maximum and the codes.  Bytes bound it, so what counts is rows in flight: magnitudes are
+// compared as bits, with infinities and NaN sorted out only where one is found, and codes are rounded by adding 1.5 * 2^23.
+// Rows of more than 8192 values take 1024 threads: 64 rows of 25088 5.2 us with 256, 3.9 with 1024.
 constexpr int QT_KEEP = 4;
 
-// C: int8 codes, or fp16 ones for the tensor-core kernel that takes them so.
+template <typename T>
+struct Raw8 {
+    alignas(16) T v[8];
+    __device__ __forceinline__ void load(const T* __restrict__ p, bool vec) {
+        if (vec) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(v)[i] = reinterpret_cast<const uint4*>(p)[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = p[i];
+        }
+    }
+};
+
+// C: int8 codes, or fp16 ones for the tensor-core kernels that take them so.
 template <typename T, typename C, int QT_THREADS>
-__global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __restrict__ x, int K, long long x_stride, int vec,
-                                                                     C* __restrict__ codes, long long c_stride, int c_vec,
-                                                                     float* __restrict__ scale, int* status) {
+__global__ void __launch_bounds__(QT_THREADS)
+    quantize_tokens_kernel(const T* __restrict__ x, int K, long long x_stride, int vec, C* __restrict__ codes, long long c_stride, int c_vec,
+                           float* __restrict__ scale, int* status) {
     constexpr bool HALF = sizeof(C) == 2;
     pdl_wait();
     const T* row = x + (long long)blockIdx.x * x_stride;
     C* out = codes + (long long)blockIdx.x * c_stride;
-    const int t = threadIdx.x, groups = K / 8;  // whole groups of eight; the rest of the row one value at a time
-    float keep[QT_KEEP][8], tail = 0.0f, top = 0.0f;
-    bool bad = false;
-    auto see = [&](float& v) {
-        const float u = fabsf(v);
-        if (!(u <= FLT_MAX)) {
-            bad = true;
-            v = 0.0f;
-        } else
-            top = fmaxf(top, u);
-    };
+    const int t = threadIdx.x, groups = K / 8, tail = 8 * groups + t;  // whole groups of eight; the rest of the row one value at a time
+    Raw8<T> keep[QT_KEEP];
+    auto each = [&](auto&& f) {  // f(group, its values) for this thread's groups
 #pragma unroll
-    for (int s = 0; s < QT_KEEP; ++s) {
-        const int g = t + s * QT_THREADS;
-        if (g < groups) {
-            load_f32<8>(row + 8 * g, vec, keep[s]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) see(keep[s][e]);
+        for (int s = 0; s < QT_KEEP; ++s)
+            if (t + s * QT_THREADS < groups) f(t + s * QT_THREADS, keep[s]);
+        for (int g = t + QT_KEEP * QT_THREADS; g < groups; g += QT_THREADS) {
+            Raw8<T> v;
+            v.load(row + 8 * g, vec);
+            f(g, v);
         }
-    }
-    for (int g = t + QT_KEEP * QT_THREADS; g < groups; g += QT_THREADS) {
-        float v[8];
-        load_f32<8>(row + 8 * g, vec, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) see(v[e]);
-    }
-    if (t < K - 8 * groups) {
-        tail = to_f32(row[8 * groups + t]);
-        see(tail);
-    }
-    __shared__ float part[QT_THREADS / 32];
-#pragma unroll
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    if ((t & 31) == 0) part[t >> 5] = top;
-    __syncthreads();
-    top = part[0];
-#pragma unroll
-    for (int w = 1; w < QT_THREADS / 32; ++w) top = fmaxf(top, part[w]);
-    if (bad) latch_status(status, FXPQ_ERR_NONFINITE);
-    const bool live = top >= 7.888609052210118e-31f;  // 2^-100
-    const float inv = live ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f;
-    if (t == 0) scale[blockIdx.x] = live ? __fmul_rn(top, 1.0f / 127.0f) : 0.0f;
-    auto code = [&](float v) { return max(-127, min(127, __float2int_rn(__fmul_rn(v, inv)))); };
-    auto put = [&](int g, const float (&v)[8]) {
-        int c[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) c[e] = code(v[e]);
-        if constexpr (HALF) {  // (always aligned)
-            uint32_t h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = h2_bits(__halves2half2(__int2half_rn(c[2 * e]), __int2half_rn(c[2 * e + 1])));
-            *reinterpret_cast<uint4*>(out + 8 * g) = make_uint4(h[0], h[1], h[2], h[3]);
-        } else if (c_vec)
-            *reinterpret_cast<uint2*>(out + 8 * g) = make_uint2(pack_i8(c[0], c[1], c[2], c[3]), pack_i8(c[4], c[5], c[6], c[7]));
-        else
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out[8 * g + e] = (C)c[e];
     };
 #pragma unroll
     for (int s = 0; s < QT_KEEP; ++s)
-        if (t + s * QT_THREADS < groups) put(t + s * QT_THREADS, keep[s]);
-    for (int g = t + QT_KEEP * QT_THREADS; g < groups; g += QT_THREADS) {
-        float v[8];
-        load_f32<8>(row + 8 * g, vec, v);
+        if (t + s * QT_THREADS < groups) keep[s].load(row + 8 * (t + s * QT_THREADS), vec);
+    __shared__ uint32_t part[QT_THREADS / 32];
+    auto largest = [&](bool finite) {  // magnitudes as bits
+        uint32_t top = 0;
+        auto see = [&](float v) {
+            const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+            top = max(top, finite && b >= 0x7f800000u ? 0u : b);
+        };
+        each([&](int, const Raw8<T>& v) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fabsf(v[e]) <= FLT_MAX ? v[e] : 0.0f;
-        put(g, v);
+            for (int e = 0; e < 8; ++e) see(to_f32(v.v[e]));
+        });
+        if (tail < K) see(to_f32(row[tail]));
+        top = __reduce_max_sync(0xffffffffu, top);
+        __syncthreads();
+        if ((t & 31) == 0) part[t >> 5] = top;
+        __syncthreads();
+        top = 0;
+#pragma unroll
+        for (int w = 0; w < QT_THREADS / 32; ++w) top = max(top, part[w]);
+        return top;
+    };
+    uint32_t bits = largest(false);
+    const bool bad = bits >= 0x7f800000u;
+    if (bad) {
+        if (t == 0) latch_status(status, FXPQ_ERR_NONFINITE);
+        bits = largest(true);
     }
-    if (t < K - 8 * groups) out[8 * groups + t] = (C)code(tail);
+    const float top = __uint_as_float(bits);
+    const bool live = top >= 7.888609052210118e-31f;  // 2^-100
+    const float inv = live ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f;
+    if (t == 0) scale[blockIdx.x] = live ? __fmul_rn(top, 1.0f / 127.0f) : 0.0f;
+    // (a product is at most 127 (1 + 2^-22) and rounds to 127)
+    auto scaled = [&](T v) {
+        const float f = to_f32(v);
+        return __fmul_rn(bad && !(fabsf(f) <= FLT_MAX) ? 0.0f : f, inv);
+    };
+    auto code = [&](T v) { return (int)(int8_t)__float_as_uint(scaled(v) + 12582912.0f); };
+    each([&](int g, const Raw8<T>& v) {
+        if constexpr (HALF) {  // (always aligned)
+            *reinterpret_cast<uint4*>(out + 8 * g) =
+                make_uint4(f32_codes_f16x2(scaled(v.v[0]), scaled(v.v[1])), f32_codes_f16x2(scaled(v.v[2]), scaled(v.v[3])),
+                           f32_codes_f16x2(scaled(v.v[4]), scaled(v.v[5])), f32_codes_f16x2(scaled(v.v[6]), scaled(v.v[7])));
+        } else {
+            int c[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = code(v.v[e]);
+            if (c_vec)
+                *reinterpret_cast<uint2*>(out + 8 * g) = make_uint2(pack_i8(c[0], c[1], c[2], c[3]), pack_i8(c[4], c[5], c[6], c[7]));
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[8 * g + e] = (C)c[e];
+        }
+    });
+    if (tail < K) out[tail] = (C)code(row[tail]);
     for (long long i = K + t; i < c_stride; i += QT_THREADS) out[i] = (C)0;
 }
 
@@ -690,7 +705,9 @@ fxpq_status quantize_rows(const void* d_x, int32_t x_type, int64_t M, int32_t K,
     int* status = status_ptr();
     auto launch = [&](auto* x) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(x)>>;
-        if (K > 8192)
+        if (K <= 4096)
+            launch_pdl(quantize_tokens_kernel<T, C, 128>, grid, dim3(128), 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
+        else if (K > 8192)
             launch_pdl(quantize_tokens_kernel<T, C, 1024>, grid, dim3(1024), 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
         else
             launch_pdl(quantize_tokens_kernel<T, C, 256>, grid, dim3(256), 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
