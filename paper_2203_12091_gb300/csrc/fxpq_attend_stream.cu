@@ -20,11 +20,14 @@ namespace {
 using namespace tc;
 
 constexpr int TILE = 32;          // tokens of a stage
-constexpr int RING = 96 * 1024;   // bytes of stages per CTA: two CTAs per SM, one streams while the other merges
 constexpr int WARPS = 4;
+// CTAs of an SM (one streams while another merges) and the bytes of stages of each.  With 8 rows a unit three of them fit
+// the registers: a warp's chain of loads, products and exponentials leaves the SM's issue slots half empty with two.
+__host__ __device__ constexpr int ctas_of(int NT) { return NT == 1 ? 3 : 2; }
+__host__ __device__ constexpr int ring_of(int NT) { return (NT == 1 ? 64 : 96) * 1024; }
 
-template <int D>
-__host__ __device__ constexpr int stages() { return RING / WARPS / (TILE * D * 2); }
+template <int D, int NT>
+__host__ __device__ constexpr int stages() { return ring_of(NT) / WARPS / (TILE * D * 2); }
 
 // Row of a 16-token half tile that product row g (and g + 8: eight rows on) stands for.
 template <int D>
@@ -119,8 +122,8 @@ __device__ __forceinline__ float* slot_at(const AttendArgs& A, int cta, int slot
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(32 * WARPS, 2) attend_stream_kernel(const __grid_constant__ AttendArgs A) {
-    constexpr int ST = stages<D>(), STAGE = TILE * D * 2, KS = D / 16, MT = D / 16;
+__global__ void __launch_bounds__(32 * WARPS, ctas_of(NT)) attend_stream_kernel(const __grid_constant__ AttendArgs A) {
+    constexpr int ST = stages<D, NT>(), STAGE = TILE * D * 2, KS = D / 16, MT = D / 16;
     constexpr bool QREG = NT <= 2;  // query fragments in registers; the widest instance keeps them in shared memory
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -442,7 +445,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_stream_kernel(const __gr
         if (abort_flag) ok = false;
         float* sums = reinterpret_cast<float*>(smem);  // [WARPS][8 NT][D + 4]
         constexpr int PITCH = D + 4;
-        static_assert(WARPS * 8 * NT * PITCH * 4 <= RING, "merge buffer within the ring");
+        static_assert(WARPS * 8 * NT * PITCH * 4 <= ring_of(NT), "merge buffer within the ring");
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -550,19 +553,19 @@ template <int D, int NT>
 fxpq_status launch(AttendArgs& A, bool whole, cudaStream_t st) {
     static bool set = false;  // (setting it twice does no harm)
     if (!set) {
-        if (cudaFuncSetAttribute(attend_stream_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 1024) != cudaSuccess)
+        if (cudaFuncSetAttribute(attend_stream_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_of(NT) + 1024) != cudaSuccess)
             return FXPQ_ERR_CUDA;
         set = true;
     }
     A.whole = whole;
     A.share_min = 16;
-    const int ctas = 2 * num_sms();
+    const int ctas = ctas_of(NT) * num_sms();
     long long grid = ctas;
     if (whole)
         grid = A.heads * (A.s.starts ? unit_base(A.s.n_tokens, A.s.n_seqs, A.group, 8 * NT, 1)
                                      : (long long)A.s.n_seqs * ((A.s.each * A.group + 8 * NT - 1) / (8 * NT)));
     if (grid > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
-    launch_pdl(attend_stream_kernel<D, NT>, dim3((unsigned)grid), dim3(32 * WARPS), RING + 1024, st, A);
+    launch_pdl(attend_stream_kernel<D, NT>, dim3((unsigned)grid), dim3(32 * WARPS), ring_of(NT) + 1024, st, A);
     fxpq_status rc = after_launch("attend_stream");
     if (rc != FXPQ_OK || whole) return rc;
     const long long rows = (long long)A.s.n_tokens * A.q_heads;
@@ -575,7 +578,7 @@ fxpq_status launch(AttendArgs& A, bool whole, cudaStream_t st) {
 int stream_nt(long long rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
 
 size_t attend_stream_workspace(int dim, int nt) {
-    return (size_t)2 * 2 * num_sms() * 8 * nt * (dim + 2) * sizeof(float);
+    return (size_t)2 * ctas_of(nt) * num_sms() * 8 * nt * (dim + 2) * sizeof(float);
 }
 
 fxpq_status launch_attend_stream(AttendArgs& A, int dim, int nt, bool whole, cudaStream_t st) {
