@@ -1,5 +1,6 @@
 // fxpq_linear.cu -- rows quantized to 8 bits with a scale each, and the product of 8-bit rows with scales for
 // each token and each output channel.
+#include <atomic>
 #include <cfloat>
 #include <type_traits>
 
@@ -130,6 +131,7 @@ struct LinArgs {
     int N, y_type, n_kb;
     int rows, cols;  // tokens of a tile, and rounded up to 16, at most 128 (the columns past `rows` hold whatever the stage does)
     int w_rows;      // channels of the last tile
+    int y_four;      // four outputs of a row in one aligned access
     int stages;
     int* status;
 };
@@ -300,26 +302,42 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u));
     }
-    // ---- four channels of one token per thread and step, summed over the cluster
-    if (shares > 1) cluster_sync();
+    // ---- four channels of one token per lane, a token per warp and step, summed over the cluster
     const int mine = (int)min((long long)P.rows, P.M - m0), c_lo = mine * rank / shares, c_hi = mine * (rank + 1) / shares;
-    for (int i = c_lo * 32 + threadIdx.x; i < c_hi * 32; i += LS_THREADS) {
-        const int c = i >> 5, ch = n0 + 4 * (i & 31);
-        const uint32_t at = raw0 + (uint32_t)i * 16;
+    const int ch = n0 + 4 * lane;
+    constexpr int TOKENS = LS_THREADS / 32;
+    float sw[4], bias[4], sx = c_lo + warp < c_hi ? __ldg(P.sx + m0 + c_lo + warp) : 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // (on their way while the CTAs meet)
+        sw[e] = ch + e < P.N ? __ldg(P.sw + ch + e) : 0.0f;
+        bias[e] = P.bias && ch + e < P.N ? __ldg(P.bias + ch + e) : 0.0f;
+    }
+    if (shares > 1) cluster_sync();
+    for (int c = c_lo + warp; c < c_hi; c += TOKENS) {
+        const uint32_t at = raw0 + (uint32_t)(c * 32 + lane) * 16;
         float4 b[8], a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        // (all loads in flight: one after the other they took half of a small product's time)
 #pragma unroll
         for (int r = 0; r < 8; ++r)
             if (r < shares) b[r] = ld_cluster_f4(cluster_addr(at, r));
+        const float s = sx;
+        if (c + TOKENS < c_hi) sx = __ldg(P.sx + m0 + c + TOKENS);
 #pragma unroll
         for (int r = 0; r < 8; ++r)
             if (r < shares) a.x += b[r].x, a.y += b[r].y, a.z += b[r].z, a.w += b[r].w;
-        const float v[4] = {a.x, a.y, a.z, a.w}, sx = __ldg(P.sx + m0 + c);
+        const float v[4] = {fmaf(a.x * s, sw[0], bias[0]), fmaf(a.y * s, sw[1], bias[1]), fmaf(a.z * s, sw[2], bias[2]), fmaf(a.w * s, sw[3], bias[3])};
+        const long long to = (m0 + c) * P.ys + ch;
+        if (P.y_four && ch + 4 <= P.N) {
+            if (P.y_type == FXPQ_FT_F32)
+                store_f32<4>(static_cast<float*>(P.y) + to, v);
+            else if (P.y_type == FXPQ_FT_F16)
+                store_f32<4>(static_cast<__half*>(P.y) + to, v);
+            else
+                store_f32<4>(static_cast<__nv_bfloat16*>(P.y) + to, v);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (ch + e < P.N)
-                store_y(P.y, P.y_type, (m0 + c) * P.ys + ch + e,
-                        fmaf(v[e] * sx, __ldg(P.sw + ch + e), P.bias ? __ldg(P.bias + ch + e) : 0.0f));
+            for (int e = 0; e < 4; ++e)
+                if (ch + e < P.N) store_y(P.y, P.y_type, to + e, v[e]);
+        }
     }
     if (shares > 1) cluster_sync();  // (the others have read this CTA's sums)
 }
@@ -668,21 +686,40 @@ fxpq_status launch_few(LinArgs& P, cudaStream_t st) {
     }
     const long long tn = (P.N + 127) / 128, tm = (P.M + P.rows - 1) / P.rows;
     if (tn > 65535 || tm > 65535) return FXPQ_ERR_UNSUPPORTED;
-    const int room = (P.cols <= 64 ? 2 : 1) * num_sms();
-    int shares = 1;
-    while (shares < 8 && tn * tm * shares * 2 <= room && P.n_kb >= 4 * shares) shares *= 2;
     P.stages = P.cols <= 32 || P.cols > 64 ? 4 : 3;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = shares, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3((unsigned)shares, (unsigned)tn, (unsigned)tm);
     c.blockDim = dim3(LS_THREADS);
     c.dynamicSmemBytes = ls_smem(P.cols, P.stages, HALF);
     c.stream = st;
     c.attrs = at;
+    // As many CTAs to a reduction as run at once, with at least 1024 codes each (4096 x 4096, 64 tokens: 10.9 us with four of
+    // 1024 codes, 11.9 with eight of 512), or 512 where they leave half of the SMs free (1000 x 4096, one token: 5.5 and 6.8).  Clusters are placed within a group of SMs: 16 clusters of 8 CTAs that fill an SM
+    // each left one for a second round (251 x 1001 of 4090: 19.4 us, 13.3 with clusters of 4).
+    int shares = 1;
+    for (; shares < 8 && P.n_kb >= (tn * tm * shares * 4 <= num_sms() ? 8 : 16) * shares; shares *= 2) {
+        static std::atomic<int> room[2][9][4];  // clusters that run at once, by tile width and size, asked for once
+        const int w = P.cols / 16, l = shares == 1 ? 1 : shares == 2 ? 2 : 3;
+        int n = room[HALF][w][l].load(std::memory_order_relaxed);
+        if (n == 0) {
+            at[1].val.clusterDim.x = 2 * shares;
+            c.gridDim = dim3(2 * shares, 1024, 1);
+            c.numAttrs = 2;
+            if (cudaOccupancyMaxActiveClusters(&n, linear_few_kernel<HALF>, &c) != cudaSuccess || n <= 0) {
+                (void)cudaGetLastError();
+                n = -1;
+            }
+            room[HALF][w][l].store(n, std::memory_order_relaxed);
+        }
+        // (the query counts one CTA to an SM: it says 15 clusters of 8 where 32 of two CTAs to an SM ran at once)
+        if (tn * tm > (P.cols <= 64 ? 2 * n + 2 : n)) break;
+    }
+    at[1].val.clusterDim.x = shares;
+    c.gridDim = dim3((unsigned)shares, (unsigned)tn, (unsigned)tm);
     c.numAttrs = shares > 1 ? 2 : 1;
     (void)cudaLaunchKernelEx(&c, linear_few_kernel<HALF>, P);
     return after_launch("linear_few");
@@ -761,6 +798,7 @@ fxpq_status product_few(const int8_t* d_x, const __half* half, int64_t x_stride,
     P.cols = (P.rows + 15) / 16 * 16;
     P.n_kb = (K + LS_KB - 1) / LS_KB;
     P.w_rows = N % 128 ? N % 128 : 128;
+    P.y_four = aligned(d_y, 4 * ftype_bytes(y_type)) && y_stride % 4 == 0;
     if (K > 0) {
         if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !(half ? encode_half_rows(&P.tx, half, M, K, x_stride, P.rows) : encode_rows(&P.tx, d_x, M, K, x_stride, P.rows)))
             return FXPQ_ERR_CUDA;
