@@ -2,15 +2,16 @@
 //
 // A CTA takes 256 query rows (tokens x grouped heads) of one sequence and key head as two tiles of 128 rows and walks
 // the keys 128 at a time.  Two products of 128 x 128 x dim per tile and 128 keys bound it: S = Q K^T into tensor memory, then
-// O += W V with the weights W as the operand in tensor memory, in place of S.  The weights go in two steps of 64 keys, so
-// that the first's product runs while the second's are formed, and the two tiles alternate: one's products run
+// O += W V with the weights W as the operand in tensor memory, in place of S.  The two tiles alternate: one's products run
 // during the other's exponentials.
-//   warps 0-3, 4-7  a tile's softmax each, a thread per row: weights to fp16, sums; at the end O / l
-//   warps 8-11      converters: codes to fp16 operand tiles of 128 keys, once for both row tiles
-//   warp 12         tensor memory, products;   warp 13   pages, scales, copies
-// A step's weights are formed with the maximum as it was; only where some t has passed it by 2^8 (a few times per row) are
-// they formed again, after the sums have been rescaled.  The maximum then moves by whole powers of two, so that
-// rescaling is exact.
+//   warps 0-3, 4-7, 8-11, 12-15  softmax: X and Y of tile 0, X and Y of tile 1, a thread per row; X forms the weights of a step's
+//                   first 64 keys and Y those of the others, at the same time; at the end each writes half of O / l
+//   warps 16-19     converters: codes to fp16 operand tiles of 128 keys, once for both row tiles
+//   warp 20         tensor memory, products;   warp 21   pages, scales, copies;   22, 23   none
+// A step's weights are formed with the maximum m as it was; only where 16 of them sum past 2^8 (a few times per row) are
+// they formed again, after the sums have been rescaled.  m then moves by whole powers of two, so that rescaling is
+// exact.  X and Y share m: X's goes to Y before Y hands over its weights, Y's to X before the next step.
+// With one thread a row forming the weights of 64 keys after the other a tile's chain was 2300 cycles of softmax for 128 keys.
 // Codes arrive as they are stored ([keys][dim] bytes, one TMA box per page): K is a K-major operand and V, with the
 // same bytes, an operand whose columns are contiguous, so that neither is transposed.
 // Tried: two buffers of S of 64 keys, so that no softmax waits for a product.  The scores' products of 64 columns read Q twice
@@ -24,9 +25,10 @@ namespace {
 
 using namespace tc;
 
-constexpr int KEYS = 128, STEP = 64, ROWS = 256, THREADS = 14 * 32;  // keys of an operand tile, of a step
+constexpr int KEYS = 128, STEP = 64, ROWS = 256, THREADS = 24 * 32;  // keys of an operand tile, of X or Y
 // Operand tiles K 0, V 0, K 1, .. pass through RAWS stages of codes (copies in flight) and CONVS expanded ones (the products hold V of one step and K of the next, a third is being written).
-constexpr int RAWS = 4, CONVS = 3;
+constexpr int RAWS = 3, CONVS = 3;
+constexpr float MANY = 256.0f;  // 16 weights may sum to this much, so that each is within fp16's range
 constexpr int TABS = 8;  // scale tables in flight: the copies run at most five tiles ahead of the softmax
 
 template <int D>
@@ -34,7 +36,7 @@ struct Smem {  // offsets from the 1024-byte aligned base
     static constexpr int Q = 128 * D * 2, CONV = KEYS * D * 2, RAW = KEYS * D;
     static constexpr int conv0 = 2 * Q, raw0 = conv0 + CONVS * CONV, bytes = raw0 + RAWS * RAW + 1024;
 };
-static_assert(Smem<128>::bytes + 2048 <= 232448, "shared memory of a CTA");
+static_assert(Smem<128>::bytes + 8192 <= 232448, "shared memory of a CTA");
 
 // Operand whose columns (the rows of O^T) are contiguous: 64 of them in a 128-byte swizzled row, 8 reduction steps to a
 // 1024-byte group, the next 64 columns 16 KB on.
@@ -54,19 +56,21 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     using S = Smem<D>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    __shared__ __align__(8) uint64_t bars[2 * RAWS + 2 * CONVS + TABS + 2 + 4 + 2 + 2 + 1 + 1];
+    __shared__ __align__(8) uint64_t bars[2 * RAWS + 2 * CONVS + TABS + 2 + 4 + 2 + 2 + 1 + 1 + 16];
     __shared__ float tab[TABS][3][8];  // per 16 keys: key scale, log2 of the value scale, its inverse
+    __shared__ float row_m[ROWS], end_m[2][ROWS], end_l[2][ROWS];  // m as X and Y share it; theirs at the end
     __shared__ int abort_flag;
     __shared__ uint32_t tmem_slot;
     volatile int* abort = &abort_flag;
     const uint32_t raw_full = smem_u32(bars), raw_empty = raw_full + 8 * RAWS, conv_full = raw_empty + 8 * RAWS,
-                   conv_empty = conv_full + 8 * CONVS, tab_full = conv_empty + 8 * CONVS, s_full = tab_full + 8 * TABS, p_full = s_full + 16, pv_done = p_full + 32,
-                   o_full = pv_done + 16, q_full = o_full + 16, drained = q_full + 8;  // p_full: [tile][step of two]
+                   conv_empty = conv_full + 8 * CONVS, tab_full = conv_empty + 8 * CONVS, s_full = tab_full + 8 * TABS, p_full = s_full + 16, pva_done = p_full + 32,
+                   o_full = pva_done + 16, q_full = o_full + 16, drained = q_full + 8,
+                   told = drained + 8;  // p_full: [tile][X, Y]; told: [tile][X to Y, Y to X][32 rows]
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_full + 8 * i, 1);
-            mbar_init(pv_done + 8 * i, 1);
+            mbar_init(pva_done + 8 * i, 1);
             mbar_init(o_full + 8 * i, 1);
         }
         for (int i = 0; i < 4; ++i) mbar_init(p_full + 8 * i, 4);
@@ -79,7 +83,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             mbar_init(conv_empty + 8 * i, 1);
         }
         for (int i = 0; i < TABS; ++i) mbar_init(tab_full + 8 * i, 1);
-        mbar_init(q_full, 8);
+        mbar_init(q_full, 16);
+        for (int i = 0; i < 16; ++i) mbar_init(told + 8 * i, 1);
         mbar_init(drained, 1);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -107,7 +112,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     const int j0 = (int)((long long)n_all * blockIdx.y / gridDim.y), n = (int)((long long)n_all * (blockIdx.y + 1) / gridDim.y) - j0;
     const int n2 = n == 0 ? 0 : min(2 * n, (seen - j0 * KEYS + STEP - 1) / STEP);  // steps
 
-    if (warp == 12) {
+    if (warp == 20) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -117,9 +122,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     const uint32_t tmem = tmem_slot;
     const uint32_t base = smem_u32(smem);
 
-    if (warp < 8) {
+    // (the launch holds 768 x 80 registers: 512 x 96 + 256 x 48 of them)
+    if (warp < 16)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+    else
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+
+    if (warp < 16) {
         // ================================================================ softmax: one row per thread
-        const int t = warp >> 2, quad = warp & 3, r = quad * 32 + lane, rr = rb * ROWS + t * 128 + r, tok = rr / A.group;
+        const int t = warp >> 3, y = (warp >> 2) & 1, quad = warp & 3, r = quad * 32 + lane, rr = rb * ROWS + t * 128 + r, tok = rr / A.group;
         const bool live = t * 128 + r < rows;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16, ts = tmem + 128 * t + lanes, to = tmem + 256 + 128 * t + lanes;
         const long long qrow = (long long)(first + tok) * A.q_token + (long long)(h * A.group + rr - tok * A.group) * A.q_head;
@@ -156,11 +167,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             const float up = pow2i(e);
             cf = A.scale * LOG2E * pow2i(-e);
 #pragma unroll
-            for (int d = 0; d < D; d += 8) {
+            for (int k = 0; k < D / 2; k += 8) {  // X writes the row's first half, Y the second
+                const int d = (D / 2) * y + k;
                 uint32_t h[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float2 v = pair(x[d / 2 + i]);
+                    const float2 v = pair(y ? x[D / 4 + k / 2 + i] : x[k / 2 + i]);
                     h[i] = h2_bits(__floats2half2_rn(v.x * up, v.y * up));
                 }
                 *reinterpret_cast<uint4*>(smem + t * S::Q + (d >> 6) * 16384 + r * 128 + ((((d >> 3) & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
@@ -174,87 +186,111 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             const int limit = !live || pos < 0 ? 0 : A.causal ? min(pos + 1, end) : end;
             float m = NO_MAX, l = 0.0f;
             bool ok = true;
-            for (int i = 0; i < n2; ++i) {
-                const int slot = (i >> 1) % TABS;
-                if ((i & 1) == 0) {
-                    if (!wait_warp(tab_full + 8 * slot, ((i >> 1) / TABS) & 1, abort, A.status) ||
-                        !wait_warp(s_full + 8 * t, (i >> 1) & 1, abort, A.status)) {
+            const uint32_t tell = told + 64 * t + 32 * y + 8 * quad, hear = told + 64 * t + 32 * (1 - y) + 8 * quad, sb = ts + STEP * y;
+            float* shared_m = row_m + 128 * t + r;
+            // m as the other one has left it; whether it moved
+            auto follow = [&]() {
+                const float now = *shared_m;
+                if (now == m) return false;
+                l *= ex2(m - now);
+                m = now;
+                return true;
+            };
+            if (!y) *shared_m = NO_MAX;
+            const int steps = (n2 + 1 - y) >> 1;
+            for (int i = 0; i < steps; ++i) {
+                const int slot = i % TABS;
+                if (!wait_warp(tab_full + 8 * slot, (i / TABS) & 1, abort, A.status) || !wait_warp(s_full + 8 * t, i & 1, abort, A.status)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const int room = limit - (j0 + i) * KEYS - STEP * y;  // of these 64 keys, those that the row sees
+                const float *kf = tab[slot][0] + 4 * y, *lg = tab[slot][1] + 4 * y, *iv = tab[slot][2] + 4 * y;
+                const bool masked = __any_sync(0xffffffffu, live && room < STEP);  // the last steps of a row
+                if (!y && i > 0) {  // Y's m of the step before
+                    if (!wait_warp(hear, (i - 1) & 1, abort, A.status)) {
                         ok = false;
                         break;
                     }
-                    tc_fence_after();
+                    follow();
                 }
-                const int room = limit - j0 * KEYS - i * STEP;  // keys of this step that the row sees
-                const uint32_t sb = ts + STEP * (i & 1);
-                const float *kf = tab[slot][0] + 4 * (i & 1), *lg = tab[slot][1] + 4 * (i & 1), *iv = tab[slot][2] + 4 * (i & 1);
-                const bool masked = __any_sync(0xffffffffu, live && room < STEP);  // the last steps of a row
-                uint32_t s[64], w[32];
-                float part, over;  // the step's normaliser, the largest t - m
-                auto load = [&]() {
-                    tmem_ld32_nw(sb, *reinterpret_cast<uint32_t(*)[32]>(s));
-                    tmem_ld32_nw(sb + 32, *reinterpret_cast<uint32_t(*)[32]>(s + 32));
+                uint32_t w[32];
+                float part, over;  // the normaliser, the largest sum of 16 weights
+                auto load = [&](int c, uint32_t (&s)[32]) {  // 32 scores
+                    tmem_ld32_nw(sb + 32 * c, s);
                     tmem_wait_ld();
                     reg_fence(s);
                     if (masked) {
 #pragma unroll
-                        for (int e = 0; e < 64; ++e) s[e] = e < room ? s[e] : 0xff800000u;
+                        for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < room ? s[e] : 0xff800000u;
                     }
                 };
-                auto weights = [&]() {  // 16 keys of one scale at a time, four independent chains
-                    float top[4], sums[4];
-                    float2 x[32];
+                auto weights = [&]() {
+                    float sums[4];
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        // (FLT_MIN: a page outside the cache has scale 0, which must not meet the -inf of a masked score)
-                        const float f = fmaxf(kf[g] * cf, FLT_MIN), lv = lg[g] - m;
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t s[32];
+                        float2 x[16];
+                        load(c, s);
 #pragma unroll
-                        for (int e = 8 * g; e < 8 * g + 8; ++e)
-                            x[e] = __ffma2_rn(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), make_float2(f, f), make_float2(lv, lv));
+                        for (int g = 0; g < 2; ++g) {  // 16 keys of one scale
+                            // (FLT_MIN: a page outside the cache has scale 0, which must not meet the -inf of a masked score)
+                            const float f = fmaxf(kf[2 * c + g] * cf, FLT_MIN), lv = lg[2 * c + g] - m;
+#pragma unroll
+                            for (int e = 8 * g; e < 8 * g + 8; ++e)
+                                x[e] = __ffma2_rn(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), make_float2(f, f), make_float2(lv, lv));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = make_float2(ex2(x[e].x), ex2(x[e].y));
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
+                            float2 a = __fadd2_rn(x[8 * g], x[8 * g + 1]), b2 = __fadd2_rn(x[8 * g + 2], x[8 * g + 3]);
+                            a = __fadd2_rn(a, __fadd2_rn(x[8 * g + 4], x[8 * g + 5]));
+                            b2 = __fadd2_rn(b2, __fadd2_rn(x[8 * g + 6], x[8 * g + 7]));
+                            a = __fadd2_rn(a, b2);
+                            sums[2 * c + g] = a.x + a.y;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[16 * c + e] = h2_bits(__floats2half2_rn(x[e].x, x[e].y));
                     }
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        top[g] = fmaxf(x[8 * g].x, x[8 * g].y);
-#pragma unroll
-                        for (int e = 8 * g + 1; e < 8 * g + 8; ++e) top[g] = max3(top[g], x[e].x, x[e].y);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] = make_float2(ex2(x[e].x), ex2(x[e].y));
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        float2 a = __fadd2_rn(x[8 * g], x[8 * g + 1]), b2 = __fadd2_rn(x[8 * g + 2], x[8 * g + 3]);
-                        a = __fadd2_rn(a, __fadd2_rn(x[8 * g + 4], x[8 * g + 5]));
-                        b2 = __fadd2_rn(b2, __fadd2_rn(x[8 * g + 6], x[8 * g + 7]));
-                        a = __fadd2_rn(a, b2);
-                        sums[g] = a.x + a.y;
-#pragma unroll
-                        for (int e = 8 * g; e < 8 * g + 8; ++e) w[e] = h2_bits(__floats2half2_rn(x[e].x, x[e].y));
-                    }
-                    over = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+                    over = fmaxf(max3(sums[0], sums[1], sums[2]), sums[3]);
                     part = fmaf(sums[0], iv[0], sums[1] * iv[1]) + fmaf(sums[2], iv[2], sums[3] * iv[3]);
                 };
-                load();
                 weights();
-                if (__any_sync(0xffffffffu, over > LAZY)) {
-                    load();
+                if (y) {  // X's m of this step
+                    if (!wait_warp(hear, i & 1, abort, A.status)) {
+                        ok = false;
+                        break;
+                    }
+                    if (__any_sync(0xffffffffu, follow())) weights();
+                }
+                if (__any_sync(0xffffffffu, over > MANY)) {
                     float top = -INFINITY;
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        float mx = -INFINITY;
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t s[32];
+                        load(c, s);
 #pragma unroll
-                        for (int e = 16 * g; e < 16 * g + 16; e += 2) mx = max3(mx, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-                        top = fmaxf(top, mx == -INFINITY ? mx : fmaf(mx, kf[g] * cf, lg[g]));
+                        for (int g = 0; g < 2; ++g) {
+                            float mx = -INFINITY;
+#pragma unroll
+                            for (int e = 16 * g; e < 16 * g + 16; e += 2) mx = max3(mx, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+                            top = fmaxf(top, mx == -INFINITY ? mx : fmaf(mx, kf[2 * c + g] * cf, lg[2 * c + g]));
+                        }
                     }
-                    const bool grow = over > LAZY;
+                    const bool grow = over > MANY;
                     const float now = grow ? ceilf(top) : m, f = grow ? ex2(m - now) : 1.0f;
                     m = now;
                     l *= f;
-                    if (i > 0) {
-                        // O holds all steps before this one once the last one's product is complete (the one before that
-                        // is: this step's scores, or the scores this step shares, were issued after it)
-                        if (!wait_warp(pv_done + 8 * t, (i - 1) & 1, abort, A.status)) {
-                            ok = false;
-                            break;
-                        }
+                    *shared_m = m;
+                    // O holds all that came before: for X because this step's scores were issued after the last value product,
+                    // for Y once the product of X's weights is complete
+                    if (y && !wait_warp(pva_done + 8 * t, i & 1, abort, A.status)) {
+                        ok = false;
+                        break;
+                    }
+                    if (i > 0 || y) {
                         tc_fence_after();
 #pragma unroll
                         for (int c = 0; c < D / 16; ++c) {
@@ -269,22 +305,30 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                     }
                     weights();
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(tell);
                 l += part;
                 tmem_st32_nw(sb, w);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * (i & 1));
+                if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * y);
             }
             if (ok && n > 0) ok = wait_warp(o_full + 8 * t, 0, abort, A.status);
             tc_fence_after();
+            end_m[y][128 * t + r] = m;
+            end_l[y][128 * t + r] = l;
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * t + quad) : "memory");  // this X and Y, whatever became of them
             if (ok) {
                 const long long orow = (long long)(first + tok) * A.q_heads + h * A.group + rr - tok * A.group;
                 const bool split = gridDim.y > 1;
                 float* part = A.part + ((long long)blockIdx.y * A.s.n_tokens * A.q_heads + orow) * (D + 4);
+                const float om = end_m[1 - y][128 * t + r], all = fmaxf(m, om);
+                l = (l == 0.0f ? 0.0f : l * ex2(m - all)) + (end_l[1 - y][128 * t + r] == 0.0f ? 0.0f : end_l[1 - y][128 * t + r] * ex2(om - all));
                 const float inv = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
+                for (int k = 0; k < D / 32; ++k) {
+                    const int c = (D / 32) * y + k;
                     uint32_t o[16];
                     if (n > 0) {
                         tmem_ld16_nw(to + 16 * c, o);
@@ -304,13 +348,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                             store_f32<16>(static_cast<__nv_bfloat16*>(A.out) + orow * D + 16 * c, v);
                     }
                 }
-                if (live && split) *reinterpret_cast<float2*>(part) = make_float2(m, l);
-                if (live && !split && A.lse) A.lse[orow] = l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
+                if (live && split && !y) *reinterpret_cast<float2*>(part) = make_float2(all, l);
+                if (live && !split && A.lse && !y) A.lse[orow] = l == 0.0f ? -INFINITY : (all + log2f(l)) * LN2;
             }
         }
-    } else if (warp < 12) {
+    } else if (warp < 20) {
         // ================================================================ converters
-        const int t = threadIdx.x - 256;
+        const int t = threadIdx.x - 512;
         for (int u = 0; u < 2 * n; ++u) {  // K 0, V 0, K 1, V 1 ..
             const int rs = u % RAWS, cs = u % CONVS;
             if (!wait_warp(raw_full + 8 * rs, (u / RAWS) & 1, abort, A.status) ||
@@ -344,7 +388,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 mbar_arrive(conv_full + 8 * cs);
             }
         }
-    } else if (warp == 12) {
+    } else if (warp == 20) {
         // ================================================================ products
         const uint32_t id_qk = make_idesc(128, KEYS), id_pv = make_idesc(128, D) | (1u << 16);
         // operand tile u of the ring (K 0, V 0, K 1, ..)
@@ -361,23 +405,26 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
         if (ok && n > 0 && have(0)) {
             tc_fence_after();
             for (int t = 0; t < tiles; ++t) scores(t, 0);
-            for (int i = 0; i < n2 && ok; ++i) {
-                const int j = i >> 1, uv = (2 * j + 1) % CONVS;
-                if ((i & 1) == 0 && !have(2 * j + 1)) break;
-                const uint64_t vd = make_sdesc_mn(base + S::conv0 + uv * S::CONV + (i & 1) * (STEP * 128));
-                for (int t = 0; t < tiles; ++t) {
-                    if (!wait_warp(p_full + 16 * t + 8 * (i & 1), j & 1, abort, A.status)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
+            for (int j = 0; j < n && ok; ++j) {
+                const int uv = (2 * j + 1) % CONVS;
+                if (!have(2 * j + 1)) break;
+                for (int t = 0; t < tiles && ok; ++t) {
+                    for (int y = 0; y < (2 * j + 1 < n2 ? 2 : 1); ++y) {
+                        if (!wait_warp(p_full + 16 * t + 8 * y, j & 1, abort, A.status)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint64_t vd = make_sdesc_mn(base + S::conv0 + uv * S::CONV + y * (STEP * 128));
 #pragma unroll
-                    for (int kk = 0; kk < STEP / 16; ++kk)
-                        tc_mma_ta(tmem + 256 + 128 * t, tmem + 128 * t + STEP * (i & 1) + 8 * kk, vd + kk * (2048 >> 4), id_pv, i > 0 || kk > 0);
-                    tc_commit(pv_done + 8 * t);
-                    if (i == n2 - 1) tc_commit(o_full + 8 * t);  // (of its own: the last two phases of pv_done may both be over)
-                    if (t == tiles - 1 && ((i & 1) || i == n2 - 1)) tc_commit(conv_empty + 8 * uv);
-                    if ((i & 1) && j + 1 < n) {
+                        for (int kk = 0; kk < STEP / 16; ++kk)
+                            tc_mma_ta(tmem + 256 + 128 * t, tmem + 128 * t + STEP * y + 8 * kk, vd + kk * (2048 >> 4), id_pv, j > 0 || y > 0 || kk > 0);
+                        if (y == 0) tc_commit(pva_done + 8 * t);
+                    }
+                    if (!ok) break;
+                    if (j == n - 1) tc_commit(o_full + 8 * t);
+                    if (t == tiles - 1) tc_commit(conv_empty + 8 * uv);
+                    if (j + 1 < n) {
                         if (t == 0 && !have(2 * j + 2)) {
                             ok = false;
                             break;
@@ -390,7 +437,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
         }
         tc_commit(drained);  // every product issued here has completed once it fires
         drain_warp(drained, 0);
-    } else if (warp == 13) {
+    } else if (warp == 21) {
         // ================================================================ pages, scales, copies
         const int* table = A.s.pages + (long long)b * A.s.pages_stride;
         struct Info {
@@ -451,7 +498,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 20) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
     }
