@@ -200,7 +200,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             const int steps = (n2 + 1 - y) >> 1;
             for (int i = 0; i < steps; ++i) {
                 const int slot = i % TABS;
-                if (!wait_warp(tab_full + 8 * slot, (i / TABS) & 1, abort, A.status) || !wait_warp(s_full + 8 * t, i & 1, abort, A.status)) {
+                // (a wait that is already over takes some 200 cycles, so the scores' comes last; Y's m of the step before was told
+                // before these scores were begun)
+                if (!wait_warp(tab_full + 8 * slot, (i / TABS) & 1, abort, A.status) ||
+                    (!y && i > 0 && !wait_warp(hear, (i - 1) & 1, abort, A.status))) {
+                    ok = false;
+                    break;
+                }
+                if (!y && i > 0) follow();
+                if (!wait_warp(s_full + 8 * t, i & 1, abort, A.status)) {
                     ok = false;
                     break;
                 }
@@ -208,13 +216,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 const int room = limit - (j0 + i) * KEYS - STEP * y;  // of these 64 keys, those that the row sees
                 const float *kf = tab[slot][0] + 4 * y, *lg = tab[slot][1] + 4 * y, *iv = tab[slot][2] + 4 * y;
                 const bool masked = __any_sync(0xffffffffu, live && room < STEP);  // the last steps of a row
-                if (!y && i > 0) {  // Y's m of the step before
-                    if (!wait_warp(hear, (i - 1) & 1, abort, A.status)) {
-                        ok = false;
-                        break;
-                    }
-                    follow();
-                }
                 uint32_t w[32];
                 float part, over;  // the normaliser, the largest sum of 16 weights
                 auto load = [&](int c, uint32_t (&s)[32]) {  // 32 scores
@@ -363,23 +364,26 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             const unsigned char* src = smem + S::raw0 + rs * S::RAW;
             unsigned char* dst = smem + S::conv0 + cs * S::CONV;
             constexpr int CH = D / 16, IT = KEYS * CH / 128;  // 16-code chunks of a row, of a thread
-            uint4 v[IT];  // all loads in flight together
 #pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const int i = it * 128 + t, row = i / CH, c = i % CH;
-                v[it] = *reinterpret_cast<const uint4*>(src + (D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4)));
-            }
+            for (int half = 0; half < IT / 4; ++half) {  // four loads in flight together
+                uint4 v[4];
 #pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const int i = it * 128 + t, row = i / CH, c = i % CH, hf = c >> 2;
-                uint32_t x = v[it].x ^ 0x80808080u, y = v[it].y ^ 0x80808080u;
-                const uint4 o0 = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
-                x = v[it].z ^ 0x80808080u, y = v[it].w ^ 0x80808080u;
-                const uint4 o1 = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
-                unsigned char* d = dst + hf * 16384 + row * 128;
-                const int j = 2 * (c & 3), odd = D == 128 ? hf : 0;  // (lanes that would meet in a bank begin with the other chunk)
-                *reinterpret_cast<uint4*>(d + (((j + odd) ^ (row & 7)) << 4)) = odd ? o1 : o0;
-                *reinterpret_cast<uint4*>(d + (((j + 1 - odd) ^ (row & 7)) << 4)) = odd ? o0 : o1;
+                for (int it = 0; it < 4; ++it) {
+                    const int i = (4 * half + it) * 128 + t, row = i / CH, c = i % CH;
+                    v[it] = *reinterpret_cast<const uint4*>(src + (D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4)));
+                }
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    const int i = (4 * half + it) * 128 + t, row = i / CH, c = i % CH, hf = c >> 2;
+                    uint32_t x = v[it].x ^ 0x80808080u, y = v[it].y ^ 0x80808080u;
+                    const uint4 o0 = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
+                    x = v[it].z ^ 0x80808080u, y = v[it].w ^ 0x80808080u;
+                    const uint4 o1 = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
+                    unsigned char* d = dst + hf * 16384 + row * 128;
+                    const int j = 2 * (c & 3), odd = D == 128 ? hf : 0;  // (lanes that would meet in a bank begin with the other chunk)
+                    *reinterpret_cast<uint4*>(d + (((j + odd) ^ (row & 7)) << 4)) = odd ? o1 : o0;
+                    *reinterpret_cast<uint4*>(d + (((j + 1 - odd) ^ (row & 7)) << 4)) = odd ? o0 : o1;
+                }
             }
             fence_proxy_async();
             __syncwarp();
