@@ -21,13 +21,16 @@ bool encode_codes(CUtensorMap* map, const fxpq_kv_cache& c, const int8_t* codes,
 // kernel's, the others the tile kernel's; where the counts are only on the device (ragged batches) both are launched
 // unless there is but one kind, and each leaves the other's sequences alone.
 constexpr int FEW = 32;
+constexpr long long EXPAND_ROWS = 1024;
+constexpr size_t EXPAND_ROOM = (size_t)1 << 30;
 
 struct Plan {
     bool stream, tile;
     int nt;      // 8 nt query rows share a read of the cache
     bool whole;  // one CTA per unit
     int shares;  // CTAs that share the keys of a block of rows
-    size_t ws_stream, ws;
+    bool expand; // the codes are expanded to fp16 once, before the tile kernel
+    size_t ws_stream, ws_join, ws;
 };
 Plan plan(const fxpq_kv_cache& c, const fxpq_kv_batch& b, int q_heads) {
     Plan p;
@@ -46,7 +49,11 @@ Plan plan(const fxpq_kv_cache& c, const fxpq_kv_batch& b, int q_heads) {
         const long long units = tile_blocks(b.n_tokens, b.n_seqs, (int)group, false) * c.heads + (b.d_starts ? c.heads : 0);
         while (p.shares < 16 && units * (p.shares + 1) <= num_sms() && tokens >= 512LL * (p.shares + 1)) ++p.shares;
     }
-    p.ws = p.ws_stream + (p.tile ? (attend_tile_workspace(b.n_tokens, q_heads, c.dim, p.shares) + 255) / 256 * 256 : 0);
+    p.ws_join = p.tile ? (attend_tile_workspace(b.n_tokens, q_heads, c.dim, p.shares) + 255) / 256 * 256 : 0;
+    // Expanding costs five bytes of traffic a code and saves every block of 256 rows its own; the room is for max_pages.
+    const size_t room = p.tile ? attend_expand_workspace(b.n_seqs, c.heads, c.dim, tokens) : 0;
+    p.expand = p.tile && mean >= EXPAND_ROWS && room <= EXPAND_ROOM && b.n_seqs <= 65535 && c.heads <= 65535 && tokens <= INT32_MAX - 128;
+    p.ws = p.ws_stream + p.ws_join + (p.expand ? room : 0);
     return p;
 }
 
@@ -84,9 +91,15 @@ extern "C" fxpq_status fxpq_kv_attention(const fxpq_kv_cache* cache, const fxpq_
     A.status = status_ptr();
     cudaStream_t st = as_stream(stream);
     if (p.tile) {  // (first: its CTAs run longest)
-        if (!encode_codes(&A.tk, *cache, cache->d_k, 128) || !encode_codes(&A.tv, *cache, cache->d_v, 128)) return FXPQ_ERR_CUDA;
-        A.part = reinterpret_cast<float*>(static_cast<char*>(d_ws) + p.ws_stream);
-        const fxpq_status rc = launch_attend_tile(A, cache->dim, p.shares, st);
+        char* ws = static_cast<char*>(d_ws);
+        A.part = reinterpret_cast<float*>(ws + p.ws_stream);
+        fxpq_status rc;
+        if (p.expand) {
+            rc = launch_attend_tile_expanded(A, cache->d_k, cache->d_v, cache->dim, ws + p.ws_stream + p.ws_join, p.shares, st);
+        } else {
+            if (!encode_codes(&A.tk, *cache, cache->d_k, 128) || !encode_codes(&A.tv, *cache, cache->d_v, 128)) return FXPQ_ERR_CUDA;
+            rc = launch_attend_tile(A, cache->dim, p.shares, st);
+        }
         if (rc != FXPQ_OK || !p.stream) return rc;
     }
     if (!encode_codes(&A.tk, *cache, cache->d_k, 32) || !encode_codes(&A.tv, *cache, cache->d_v, 32)) return FXPQ_ERR_CUDA;

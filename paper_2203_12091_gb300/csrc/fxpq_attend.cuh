@@ -68,6 +68,9 @@ int stream_nt(long long rows);
 long long tile_blocks(int n_tokens, int n_seqs, int group, bool ragged);  // blocks of 256 rows for each key head
 fxpq_status launch_attend_tile(AttendArgs& A, int dim, int shares, cudaStream_t st);
 size_t attend_tile_workspace(int n_tokens, int q_heads, int dim, int shares);
+// The same with the batch's codes expanded to fp16 before, into ws (attend_expand_workspace bytes).
+fxpq_status launch_attend_tile_expanded(AttendArgs& A, const int8_t* k, const int8_t* v, int dim, void* ws, int shares, cudaStream_t st);
+size_t attend_expand_workspace(int n_seqs, int heads, int dim, long long max_tokens);
 
 }  // namespace llm
 }  // namespace fxpq

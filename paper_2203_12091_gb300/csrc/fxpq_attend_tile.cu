@@ -27,16 +27,17 @@ using namespace tc;
 
 constexpr int KEYS = 128, STEP = 64, ROWS = 256, THREADS = 24 * 32;  // keys of an operand tile, of X or Y
 // Operand tiles K 0, V 0, K 1, .. pass through RAWS stages of codes (copies in flight) and CONVS expanded ones (the products hold V of one step and K of the next, a third is being written).
-constexpr int RAWS = 3, CONVS = 3;
+constexpr int RAWS = 3;
+__host__ __device__ constexpr int convs(bool pre) { return pre ? 4 : 3; }
 constexpr float MANY = 256.0f;  // 16 weights may sum to this much, so that each is within fp16's range
 constexpr int TABS = 8;  // scale tables in flight: the copies run at most five tiles ahead of the softmax
 
-template <int D>
+template <int D, bool PRE>
 struct Smem {  // offsets from the 1024-byte aligned base
     static constexpr int Q = 128 * D * 2, CONV = KEYS * D * 2, RAW = KEYS * D;
-    static constexpr int conv0 = 2 * Q, raw0 = conv0 + CONVS * CONV, bytes = raw0 + RAWS * RAW + 1024;
+    static constexpr int conv0 = 2 * Q, raw0 = conv0 + convs(PRE) * CONV, bytes = raw0 + (PRE ? 0 : RAWS * RAW) + 1024;
 };
-static_assert(Smem<128>::bytes + 8192 <= 232448, "shared memory of a CTA");
+static_assert(Smem<128, false>::bytes + 8192 <= 232448 && Smem<128, true>::bytes + 8192 <= 232448, "shared memory of a CTA");
 
 // Operand whose columns (the rows of O^T) are contiguous: 64 of them in a 128-byte swizzled row, 8 reduction steps to a
 // 1024-byte group, the next 64 columns 16 KB on.
@@ -51,9 +52,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
-template <int D>
+template <int D, bool PRE>
 __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_constant__ AttendArgs A) {
-    using S = Smem<D>;
+    using S = Smem<D, PRE>;
+    constexpr int CONVS = convs(PRE);
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     __shared__ __align__(8) uint64_t bars[2 * RAWS + 2 * CONVS + TABS + 2 + 4 + 2 + 2 + 1 + 1 + 16];
@@ -79,7 +81,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             mbar_init(raw_empty + 8 * i, 4);
         }
         for (int i = 0; i < CONVS; ++i) {
-            mbar_init(conv_full + 8 * i, 4);
+            mbar_init(conv_full + 8 * i, PRE ? 1 : 4);
             mbar_init(conv_empty + 8 * i, 1);
         }
         for (int i = 0; i < TABS; ++i) mbar_init(tab_full + 8 * i, 1);
@@ -356,7 +358,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     } else if (warp < 20) {
         // ================================================================ converters
         const int t = threadIdx.x - 512;
-        for (int u = 0; u < 2 * n; ++u) {  // K 0, V 0, K 1, V 1 ..
+        for (int u = 0; u < (PRE ? 0 : 2 * n); ++u) {  // K 0, V 0, K 1, V 1 ..
             const int rs = u % RAWS, cs = u % CONVS;
             if (!wait_warp(raw_full + 8 * rs, (u / RAWS) & 1, abort, A.status) ||
                 !wait_warp(conv_empty + 8 * cs, ((u / CONVS) & 1) ^ 1, abort, A.status))
@@ -477,20 +479,35 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(tab_full + 8 * slot);
-            const unsigned have = __ballot_sync(0xffffffffu, cur.pid >= 0) >> from;
-            int boxes = 0;
-            for (int g = 0; g < 8; g += box / 16) boxes += (have >> g) & 1;
-            for (int v = 0; v < 2; ++v, ++u) {
-                const int rs = u % RAWS;
-                const uint32_t bar = raw_full + 8 * rs, dst = base + S::raw0 + rs * S::RAW;
-                if (!wait_warp(raw_empty + 8 * rs, ((u / RAWS) & 1) ^ 1, abort, A.status)) {
-                    ok = false;
-                    break;
+            if constexpr (PRE) {
+                for (int v = 0; v < 2; ++v, ++u) {
+                    const int cs = u % CONVS;
+                    const uint32_t bar = conv_full + 8 * cs, dst = base + S::conv0 + cs * S::CONV;
+                    if (!wait_warp(conv_empty + 8 * cs, ((u / CONVS) & 1) ^ 1, abort, A.status)) {
+                        ok = false;
+                        break;
+                    }
+                    mbar_arrive_expect_tx(bar, (uint32_t)S::CONV);
+#pragma unroll
+                    for (int d = 0; d < D; d += 64)
+                        tma_load_3d(dst + (d >> 6) * 16384, v ? &A.tv : &A.tk, d, (j0 + i) * KEYS, b * A.heads + h, bar);
                 }
-                mbar_arrive_expect_tx(bar, (uint32_t)(boxes * box * D));
-                for (int g = 0; g < 8; g += box / 16) {
-                    const int pid = __shfl_sync(0xffffffffu, cur.pid, from + g);
-                    if (pid >= 0) tma_load_3d(dst + 16 * g * D, v ? &A.tv : &A.tk, 0, 0, pid * A.heads + h, bar);
+            } else {
+                const unsigned have = __ballot_sync(0xffffffffu, cur.pid >= 0) >> from;
+                int boxes = 0;
+                for (int g = 0; g < 8; g += box / 16) boxes += (have >> g) & 1;
+                for (int v = 0; v < 2; ++v, ++u) {
+                    const int rs = u % RAWS;
+                    const uint32_t bar = raw_full + 8 * rs, dst = base + S::raw0 + rs * S::RAW;
+                    if (!wait_warp(raw_empty + 8 * rs, ((u / RAWS) & 1) ^ 1, abort, A.status)) {
+                        ok = false;
+                        break;
+                    }
+                    mbar_arrive_expect_tx(bar, (uint32_t)(boxes * box * D));
+                    for (int g = 0; g < 8; g += box / 16) {
+                        const int pid = __shfl_sync(0xffffffffu, cur.pid, from + g);
+                        if (pid >= 0) tma_load_3d(dst + 16 * g * D, v ? &A.tv : &A.tk, 0, 0, pid * A.heads + h, bar);
+                    }
                 }
             }
             if ((i & 3) == 3) {
@@ -498,7 +515,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 nxt = fetch(i + 5);
             }
         }
-        for (int k = max(0, u - RAWS); k < u; ++k) drain_warp(raw_full + 8 * (k % RAWS), (k / RAWS) & 1);  // every copy has landed
+        constexpr int RING = PRE ? CONVS : RAWS;  // every copy has landed
+        for (int k = max(0, u - RING); k < u; ++k) drain_warp((PRE ? conv_full : raw_full) + 8 * (k % RING), (k / RING) & 1);
     }
     tc_fence_before();
     __syncthreads();
@@ -543,22 +561,71 @@ __global__ void __launch_bounds__(128) attend_tile_join_kernel(const __grid_cons
     if (A.lse && lane == 0) A.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
 }
 
+// The codes of a batch as fp16, [sequence][head][token][dim], tokens up to a whole operand tile (zeros past the pages).
 template <int D>
+__global__ void __launch_bounds__(256) expand_kernel(const __grid_constant__ AttendArgs A, const int8_t* k, const int8_t* v, __half* kx, __half* vx,
+                                                     int tokens) {
+    pdl_wait();
+    const int b = blockIdx.z, h = blockIdx.y, p0 = blockIdx.x * KEYS;
+    const int len = max(0, __ldg(A.s.lens + b)), end = (int)min((long long)len, (long long)A.s.max_pages * A.page);
+    if (p0 >= end) return;
+    const int* table = A.s.pages + (long long)b * A.s.pages_stride;
+    constexpr int CH = D / 16, ALL = KEYS * CH;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < 2 * ALL; i += 256) {
+        const int is_v = i / ALL, row = i % ALL / CH, c = i % CH, p = p0 + row;
+        const int pid = p < end ? __ldg(table + p / A.page) : -1;
+        uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+        if ((unsigned)pid < (unsigned)A.n_pages) {
+            const uint4 w = *reinterpret_cast<const uint4*>((is_v ? v : k) + (((long long)pid * A.heads + h) * A.page + p % A.page) * D + 16 * c);
+            uint32_t x = w.x ^ 0x80808080u, y = w.y ^ 0x80808080u;
+            lo = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
+            x = w.z ^ 0x80808080u, y = w.w ^ 0x80808080u;
+            hi = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
+        }
+        uint4* dst = reinterpret_cast<uint4*>((is_v ? vx : kx) + (((long long)b * A.heads + h) * tokens + p) * D + 16 * c);
+        dst[0] = lo;
+        dst[1] = hi;
+    }
+}
+
+bool encode_expanded(CUtensorMap* map, __half* x, int D, long long tokens, long long units) {
+    EncodeTiledFn enc = encode_tiled();
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)tokens, (cuuint64_t)units}, strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)(D * tokens * 2)};
+    const cuuint32_t box[3] = {64, KEYS, 1}, es[3] = {1, 1, 1};
+    return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, x, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+long long expanded_tokens(const AttendArgs& A) { return ((long long)A.s.max_pages * A.page + KEYS - 1) / KEYS * KEYS; }
+
+template <int D, bool PRE>
 fxpq_status launch(AttendArgs& A, int shares, cudaStream_t st) {
     static bool set = false;
     if (!set) {
-        if (cudaFuncSetAttribute(attend_tile_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::bytes) != cudaSuccess)
+        if (cudaFuncSetAttribute(attend_tile_kernel<D, PRE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D, PRE>::bytes) != cudaSuccess)
             return FXPQ_ERR_CUDA;
         set = true;
     }
     const long long blocks = tile_blocks(A.s.n_tokens, A.s.n_seqs, A.group, A.s.starts != nullptr);
     if (blocks * A.heads > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
-    launch_pdl(attend_tile_kernel<D>, dim3((unsigned)(blocks * A.heads), (unsigned)shares), dim3(THREADS), Smem<D>::bytes, st, A);
+    launch_pdl(attend_tile_kernel<D, PRE>, dim3((unsigned)(blocks * A.heads), (unsigned)shares), dim3(THREADS), Smem<D, PRE>::bytes, st, A);
     fxpq_status rc = after_launch("attend_tile");
     if (rc != FXPQ_OK || shares == 1) return rc;
     const long long rows = (long long)A.s.n_tokens * A.q_heads;
     launch_pdl(attend_tile_join_kernel<D>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, A, shares);
     return after_launch("attend_tile_join");
+}
+
+template <int D>
+fxpq_status launch_expanded(AttendArgs& A, const int8_t* k, const int8_t* v, __half* x, int shares, cudaStream_t st) {
+    const long long tokens = expanded_tokens(A), each = (long long)A.s.n_seqs * A.heads * tokens * D;
+    launch_pdl(expand_kernel<D>, dim3((unsigned)(tokens / KEYS), (unsigned)A.heads, (unsigned)A.s.n_seqs), dim3(256), 0, st, A, k, v, x, x + each, (int)tokens);
+    const fxpq_status rc = after_launch("attend_expand");
+    if (rc != FXPQ_OK) return rc;
+    if (!encode_expanded(&A.tk, x, D, tokens, (long long)A.s.n_seqs * A.heads) || !encode_expanded(&A.tv, x + each, D, tokens, (long long)A.s.n_seqs * A.heads))
+        return FXPQ_ERR_CUDA;
+    return launch<D, true>(A, shares, st);
 }
 
 }  // namespace
@@ -570,8 +637,15 @@ long long tile_blocks(int n_tokens, int n_seqs, int group, bool ragged) {
 size_t attend_tile_workspace(int n_tokens, int q_heads, int dim, int shares) {
     return shares > 1 ? (size_t)shares * n_tokens * q_heads * (dim + 4) * sizeof(float) : 0;
 }
+size_t attend_expand_workspace(int n_seqs, int heads, int dim, long long max_tokens) {
+    return (size_t)n_seqs * heads * ((max_tokens + KEYS - 1) / KEYS * KEYS) * dim * 2 * sizeof(__half);
+}
 fxpq_status launch_attend_tile(AttendArgs& A, int dim, int shares, cudaStream_t st) {
-    return dim == 64 ? launch<64>(A, shares, st) : launch<128>(A, shares, st);
+    return dim == 64 ? launch<64, false>(A, shares, st) : launch<128, false>(A, shares, st);
+}
+fxpq_status launch_attend_tile_expanded(AttendArgs& A, const int8_t* k, const int8_t* v, int dim, void* ws, int shares, cudaStream_t st) {
+    return dim == 64 ? launch_expanded<64>(A, k, v, static_cast<__half*>(ws), shares, st)
+                     : launch_expanded<128>(A, k, v, static_cast<__half*>(ws), shares, st);
 }
 
 }  // namespace llm

@@ -357,6 +357,27 @@ def test_attention_long_caches_are_split(ops, n, dim, page):
     check_attention(ops, [n, n], [9000 - n, 4097], page, 4, 2, dim, "bf16", True, False, seed=n)
 
 
+@pytest.mark.parametrize("page,dim,hq,hkv,dtype,causal", [(16, 64, 8, 1, "bf16", True), (64, 128, 8, 2, "f16", True), (128, 128, 5, 1, "bf16", False),
+                                                          (32, 64, 16, 2, "f16", False)])
+def test_attention_of_many_rows_expands_the_codes_first(ops, page, dim, hq, hkv, dtype, causal):
+    check_attention(ops, [301, 260, 0, 513], [0, 77, 9, 130], page, hq, hkv, dim, dtype, causal, True, seed=page)
+    check_attention(ops, [600, 600], [0, 1], page, hq, hkv, dim, dtype, causal, False, seed=page + 1)
+    check_attention(ops, [400] * 3, None, page, hq, hkv, dim, dtype, causal, False, lens=[390, 0, 400])
+
+
+def test_attention_of_many_rows_masks_bad_pages(ops):
+    rng = np.random.default_rng(17)
+    c, table = make(rng, [400], 32, 1, 64)
+    q, tl = cuda(rng.normal(size=(150, 8, 64)), torch.bfloat16), torch.tensor([400], dtype=torch.int32, device="cuda")
+    bad = table.copy()
+    bad[0, 2], bad[0, 5] = -7, len(c.k)
+    out, lse = ops.kv_attention(on_gpu(ops, c), cuda(bad), tl, q, return_lse=True)
+    assert F.fxpq_get_device_status() == L.ERR_RANGE
+    keep = [i for i in range(table.shape[1]) if i not in (2, 5)]
+    want, wl, spread, slack = O.attention(c, table[:, keep], [400 - 64], [0, 150], q.double().cpu().numpy(), O.default_scale(64), True)
+    compare_attention(out, lse, want, wl, spread, slack, "bf16", 400, np.abs(c.v).max() * c.v_scale.max())
+
+
 def test_attention_rows_that_see_nothing(ops):
     # length 0, fewer tokens than new rows, and a sequence without pages, in both sizes of batch
     check_attention(ops, [1] * 4, None, 16, 4, 2, 64, "bf16", True, False, lens=[0, 1, 5, 0])
