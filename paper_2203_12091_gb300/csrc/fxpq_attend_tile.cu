@@ -220,10 +220,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 const bool masked = __any_sync(0xffffffffu, live && room < STEP);  // the last steps of a row
                 uint32_t w[32];
                 float part, over;  // the normaliser, the largest sum of 16 weights
-                auto load = [&](int c, uint32_t (&s)[32]) {  // 32 scores
-                    tmem_ld32_nw(sb + 32 * c, s);
-                    tmem_wait_ld();
-                    reg_fence(s);
+                auto mask = [&](int c, uint32_t (&s)[32]) {
                     if (masked) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < room ? s[e] : 0xff800000u;
@@ -231,11 +228,17 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 };
                 auto weights = [&]() {
                     float sums[4];
+                    uint32_t both[2][32];  // (one round trip for all 64 scores)
+                    tmem_ld32_nw(sb, both[0]);
+                    tmem_ld32_nw(sb + 32, both[1]);
+                    tmem_wait_ld();
+                    reg_fence(both[0]);
+                    reg_fence(both[1]);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        uint32_t s[32];
+                        uint32_t(&s)[32] = both[c];
                         float2 x[16];
-                        load(c, s);
+                        mask(c, s);
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {  // 16 keys of one scale
                             // (FLT_MIN: a page outside the cache has scale 0, which must not meet the -inf of a masked score)
@@ -273,7 +276,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         uint32_t s[32];
-                        load(c, s);
+                        tmem_ld32_nw(sb + 32 * c, s);
+                        tmem_wait_ld();
+                        reg_fence(s);
+                        mask(c, s);
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
                             float mx = -INFINITY;

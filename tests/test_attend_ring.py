@@ -8,11 +8,12 @@ import pytest
 
 from tests.test_linear_ring import Barrier
 
-RAWS, CONVS = 3, 3  # as in the kernel
+RAWS = 3  # as in the kernel
 
 
-def simulate(rng, n2, tiles, one_p=False, deaf=False):
-    """"" or what went wrong.  one_p: one barrier for X's and Y's weights; deaf: X does not wait for Y's maximum."""
+def simulate(rng, n2, tiles, one_p=False, deaf=False, CONVS=3):
+    """"" or what went wrong.  one_p: one barrier for X's and Y's weights; deaf: X does not wait for Y's maximum; CONVS: 3, or 4
+    as where the codes come expanded."""
     n = (n2 + 1) // 2
     raw_full, raw_empty = [Barrier(1) for _ in range(RAWS)], [Barrier(1) for _ in range(RAWS)]
     conv_full, conv_empty = [Barrier(1) for _ in range(CONVS)], [Barrier(1) for _ in range(CONVS)]
@@ -156,11 +157,12 @@ def simulate(rng, n2, tiles, one_p=False, deaf=False):
 
 
 @pytest.mark.parametrize("tiles", [1, 2])
+@pytest.mark.parametrize("convs", [3, 4])
 @pytest.mark.parametrize("n2", [1, 2, 3, 4, 5, 8, 21, 40])
-def test_every_step_uses_its_own_data(n2, tiles):
+def test_every_step_uses_its_own_data(n2, convs, tiles):
     rng = random.Random(n2 * 10 + tiles)
-    for _ in range(60):
-        assert simulate(rng, n2, tiles) == ""
+    for _ in range(40):
+        assert simulate(rng, n2, tiles, CONVS=convs) == ""
 
 
 def test_one_barrier_for_both_groups_weights_is_not_enough():
