@@ -372,12 +372,15 @@ __device__ __forceinline__ void tile_of(const ManyArgs& P, int t, int& tn, int& 
     tm = 8 * g + in - tn * wide;
 }
 
+// NT: tokens of a tile, 256 or, where those tiles would leave pairs idle, 128.
+template <int NT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linear_many_kernel(const __grid_constant__ ManyArgs P) {
     using namespace tc;
+    constexpr int ROWS = NT / 2, STAGE = ROWS * 128;  // tokens of a CTA's half of the operand and of an epilogue warp; its stage
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     __shared__ __align__(8) uint64_t bars[2 * LM_RAW + 2 * LM_B + 2 * LM_A + 3];
-    __shared__ __align__(16) float s_sx[8][128];
+    __shared__ __align__(16) float s_sx[8][ROWS];
     __shared__ int abort_flag;
     __shared__ uint32_t tmem_slot;
     volatile int* abort = &abort_flag;
@@ -454,8 +457,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                     ok = false;
                     break;
                 }
-                if (rank == 0) mbar_arrive_expect_tx(b_full + 8 * s, 2 * 128 * 128);
-                tma_load_2d_pair(b0 + s * 128 * 128, &P.tx, hb * 64, tm * 256 + rank * 128, lead + 8 * s);
+                if (rank == 0) mbar_arrive_expect_tx(b_full + 8 * s, 2 * STAGE);
+                tma_load_2d_pair(b0 + s * STAGE, &P.tx, hb * 64, tm * NT + rank * ROWS, lead + 8 * s);
             }
         }
         if (rank == 0)
@@ -464,7 +467,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
             }
     } else if (warp == 2) {
         if (rank == 0) {
-            const uint32_t idesc = make_idesc(256, 256);
+            const uint32_t idesc = make_idesc(256, NT);
             const uint64_t bd0 = make_sdesc(b0);
             uint32_t ia = 0, ib = 0, it = 0;
             bool ok = true;
@@ -487,7 +490,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                         }
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) {
-                            tc_mma_ta_pair(tmem, tmem_a + 64 * c + 32 * hf + 8 * kk, bd0 + s * (128 * 128 >> 4) + 2 * kk, idesc, acc);
+                            tc_mma_ta_pair(tmem, tmem_a + 64 * c + 32 * hf + 8 * kk, bd0 + s * (STAGE >> 4) + 2 * kk, idesc, acc);
                             acc = 1;
                         }
                         tc_commit_pair(b_empty + 8 * s);
@@ -537,23 +540,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                 if (lane == 0) mbar_arrive_cluster(lead + 8 * c);
             }
     } else if (warp >= 8) {
-        const int quad = warp & 3, half = (warp - 8) >> 2;  // channels 32 quad + lane, tokens 128 half ..
-        const uint32_t lead = cluster_addr(acc_empty, 0), at = tmem + ((uint32_t)(quad * 32) << 16) + 128 * half;
+        const int quad = warp & 3, half = (warp - 8) >> 2;  // channels 32 quad + lane, tokens ROWS half ..
+        const uint32_t lead = cluster_addr(acc_empty, 0), at = tmem + ((uint32_t)(quad * 32) << 16) + ROWS * half;
         float* sxs = s_sx[warp - 8];
         uint32_t it = 0;
         for (int t = pair; t < P.n_tiles; t += pairs, ++it) {
             int tn, tm;
             tile_of(P, t, tn, tm);
             const int ch = tn * 256 + rank * 128 + quad * 32 + lane;
-            const long long m0 = (long long)tm * 256 + 128 * half;
+            const long long m0 = (long long)tm * NT + ROWS * half;
             const float sw = ch < P.N ? __ldg(P.sw + ch) : 0.0f, bias = P.bias && ch < P.N ? __ldg(P.bias + ch) : 0.0f;
-            for (int i = lane; i < 128; i += 32) sxs[i] = m0 + i < P.M ? __ldg(P.sx + m0 + i) : 0.0f;
+            for (int i = lane; i < ROWS; i += 32) sxs[i] = m0 + i < P.M ? __ldg(P.sx + m0 + i) : 0.0f;
             __syncwarp();
             if (!wait_warp_cluster(acc_full, it & 1, abort, P.status)) break;
             tc_fence_after();
-            const int cols = (int)min(128LL, P.M - m0);
+            const int cols = (int)min((long long)ROWS, P.M - m0);
             if (P.y_type == FXPQ_FT_F32) {
-                for (int c = 0; c < 128; c += 16) {
+                for (int c = 0; c < ROWS; c += 16) {
                     uint32_t v[16];
                     tmem_ld16_nw(at + c, v);
                     tmem_wait_ld();
@@ -568,9 +571,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                 if (lane == 0) mbar_arrive_cluster(lead);
                 continue;
             }
-            uint32_t y[64];  // tokens 2 i, 2 i + 1 of this thread's channel
+            uint32_t y[ROWS / 2];  // tokens 2 i, 2 i + 1 of this thread's channel
 #pragma unroll
-            for (int c = 0; c < 128; c += 16) {
+            for (int c = 0; c < ROWS; c += 16) {
                 uint32_t v[16];
                 tmem_ld16_nw(at + c, v);
                 tmem_wait_ld();
@@ -594,7 +597,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
             if (P.y_pair) {  // even lanes store the even token's two channels, odd lanes the odd token's
                 const int odd = lane & 1, c0 = ch - odd;
 #pragma unroll
-                for (int i = 0; i < 64; ++i) {
+                for (int i = 0; i < ROWS / 2; ++i) {
                     const uint32_t o = __shfl_xor_sync(0xffffffffu, y[i], 1);
                     const uint32_t w = odd ? __byte_perm(o, y[i], 0x7632) : __byte_perm(y[i], o, 0x5410);
                     const long long m = m0 + 2 * i + odd;
@@ -607,7 +610,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 64; ++i)
+                for (int i = 0; i < ROWS / 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
                         if (2 * i + e < cols && ch < P.N) out[(m0 + 2 * i + e) * P.ys + ch] = (unsigned short)(y[i] >> (16 * e));
@@ -661,18 +664,19 @@ size_t codes_pitch(int32_t K) { return ((size_t)K + 15) / 16 * 16; }
 // Many tokens go to the pairs of CTAs.
 bool many_tokens(int64_t M, int32_t N, int32_t K) { return M > 256 && N >= 128 && K >= 128; }
 
+template <int NT>
 fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
     static bool set = false;
     if (!set) {
-        if (cudaFuncSetAttribute(linear_many_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LM_SMEM) != cudaSuccess) return FXPQ_ERR_CUDA;
+        if (cudaFuncSetAttribute(linear_many_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, LM_SMEM) != cudaSuccess) return FXPQ_ERR_CUDA;
         set = true;
     }
-    const long long tn = ((long long)P.N + 255) / 256, tm = (P.M + 255) / 256;
+    const long long tn = ((long long)P.N + 255) / 256, tm = (P.M + NT - 1) / NT;
     if (tn * tm > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
     P.tiles_n = (int)tn, P.tiles_m = (int)tm, P.n_tiles = (int)(tn * tm);
     P.y_pair = aligned(P.y, 4) && P.ys % 2 == 0;
     const int pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
-    launch_pdl(linear_many_kernel, dim3(2 * (unsigned)(P.n_tiles < pairs ? P.n_tiles : pairs)), dim3(LM_THREADS), LM_SMEM, st, P);
+    launch_pdl(linear_many_kernel<NT>, dim3(2 * (unsigned)(P.n_tiles < pairs ? P.n_tiles : pairs)), dim3(LM_THREADS), LM_SMEM, st, P);
     return after_launch("linear_many");
 }
 
@@ -813,10 +817,14 @@ fxpq_status product_few(const int8_t* d_x, const __half* half, int64_t x_stride,
 fxpq_status product_many(const __half* half, size_t pitch, const float* d_sx, const int8_t* d_w, int64_t w_stride, const float* d_sw,
                          const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st) {
     ManyArgs P;
-    if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_half_rows(&P.tx, half, M, K, (long long)pitch, 128)) return FXPQ_ERR_CUDA;
+    // tiles of 256 tokens, or of 128 where fewer rounds of those over the pairs take less time
+    const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1, tn = ((int64_t)N + 255) / 256;
+    const auto rounds = [&](int64_t nt) { return (tn * ((M + nt - 1) / nt) + pairs - 1) / pairs * nt; };
+    const int nt = rounds(128) < rounds(256) ? 128 : 256;
+    if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_half_rows(&P.tx, half, M, K, (long long)pitch, nt / 2)) return FXPQ_ERR_CUDA;
     P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.K = K, P.y_type = y_type;
     P.status = status_ptr();
-    return launch_many(P, st);
+    return nt == 128 ? launch_many<128>(P, st) : launch_many<256>(P, st);
 }
 }  // namespace
 
