@@ -164,6 +164,30 @@ def test_linear_layer_from_floats(ops):
     assert bool(((y - (x.float() @ w.t() + b)).abs() <= bound).all())
 
 
+def test_linear_layers_on_two_streams_and_in_a_graph(ops):
+    """Calls of growing and shrinking size on two streams at once, and a captured one replayed after others."""
+    torch.manual_seed(1)
+    layers = [ops.Linear8.from_float(torch.randn(200, 256, device="cuda")) for _ in range(2)]
+    xs = [torch.randn(m, 256, device="cuda").half() for m in (3, 700, 40, 1500, 1)]
+    want = [[lay(x) for x in xs] for lay in layers]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(20):
+        for s, lay, g in zip(streams, layers, got):
+            with torch.cuda.stream(s):
+                g[:] = [lay(x) for x in xs]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for w, g in zip(want, got) for a, b in zip(w, g))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = layers[0](xs[2])
+    big = [layers[1](torch.randn(4000, 256, device="cuda").half()) for _ in range(3)]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want[0][2]) and len(big) == 3
+
+
 # ------------------------------------------------------------------------------ appending
 def make(rng, lens, page, heads, dim, **kw):
     c, table = O.paged(rng, lens, page, heads, dim, **kw)
