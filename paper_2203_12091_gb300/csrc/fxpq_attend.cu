@@ -21,7 +21,7 @@ bool encode_codes(CUtensorMap* map, const fxpq_kv_cache& c, const int8_t* codes,
 // kernel's, the others the tile kernel's; where the counts are only on the device (ragged batches) both are launched
 // unless there is but one kind, and each leaves the other's sequences alone.
 constexpr int FEW = 32;
-constexpr long long EXPAND_ROWS = 1024;
+constexpr long long EXPAND_ROWS = 2048;
 constexpr size_t EXPAND_ROOM = (size_t)1 << 30;
 
 struct Plan {
@@ -51,8 +51,11 @@ Plan plan(const fxpq_kv_cache& c, const fxpq_kv_batch& b, int q_heads) {
     }
     p.ws_join = p.tile ? (attend_tile_workspace(b.n_tokens, q_heads, c.dim, p.shares) + 255) / 256 * 256 : 0;
     // Expanding costs five bytes of traffic a code and saves every block of 256 rows its own; the room is for max_pages.
+    // Both ways measured (us, expanded and not, 65536 rows of dim 128 over 4096 tokens and their own): blocks of 1024 rows
+    // 1092 and 910, 2048 rows 1013 and 999, 4096 rows 980 and 1040, 8192 rows 1027 and 1128; dim 64 845 and 817, 805 and 840,
+    // 806 and 868, 868 and 949.
     const size_t room = p.tile ? attend_expand_workspace(b.n_seqs, c.heads, c.dim, tokens) : 0;
-    p.expand = p.tile && mean >= EXPAND_ROWS && room <= EXPAND_ROOM && b.n_seqs <= 65535 && c.heads <= 65535 && tokens <= INT32_MAX - 128;
+    p.expand = p.tile && mean > EXPAND_ROWS && room <= EXPAND_ROOM && b.n_seqs <= 65535 && c.heads <= 65535 && tokens <= INT32_MAX - 128;
     p.ws = p.ws_stream + p.ws_join + (p.expand ? room : 0);
     return p;
 }

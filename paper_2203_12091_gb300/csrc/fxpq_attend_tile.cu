@@ -6,11 +6,15 @@
 // during the other's exponentials.
 //   warps 0-3, 4-7, 8-11, 12-15  softmax: X and Y of tile 0, X and Y of tile 1, a thread per row; X forms the weights of a step's
 //                   first 64 keys and Y those of the others, at the same time; at the end each writes half of O / l
-//   warps 16-19     converters: codes to fp16 operand tiles of 128 keys, once for both row tiles
+//   warps 16-19     converters: codes to fp16 operand tiles of 128 keys, once for both row tiles (none where the codes came
+//                   expanded; the warps that follow are then 16 to 19)
 //   warp 20         tensor memory, products;   warp 21   pages, scales, copies;   22, 23   none
 // A step's weights are formed with the maximum m as it was; only where 16 of them sum past 2^8 (a few times per row) are
 // they formed again, after the sums have been rescaled.  m then moves by whole powers of two, so that rescaling is
-// exact.  X and Y share m: X's goes to Y before Y hands over its weights, Y's to X before the next step.
+// exact.  X and Y share m: one barrier of their two warps tells both whether either's weights have to be formed again.
+// (Told by one mbarrier each way instead, X and Y waited for one another in turn: 913 us for 2 prompts of 8192, 835 now.)
+// A register that spills in the loop costs more than anything else here: converters of 48 registers with eight loads in flight
+// took 2067 ns a step of 128 keys, with 64 registers 1626; the expanded form needs none, so that softmax has 112.
 // With one thread a row forming the weights of 64 keys after the other a tile's chain was 2300 cycles of softmax for 128 keys.
 // Codes arrive as they are stored ([keys][dim] bytes, one TMA box per page): K is a K-major operand and V, with the
 // same bytes, an operand whose columns are contiguous, so that neither is transposed.
@@ -25,10 +29,11 @@ namespace {
 
 using namespace tc;
 
-constexpr int KEYS = 128, STEP = 64, ROWS = 256, THREADS = 24 * 32;  // keys of an operand tile, of X or Y
+constexpr int KEYS = 128, STEP = 64, ROWS = 256;  // keys of an operand tile, of X or Y
 // Operand tiles K 0, V 0, K 1, .. pass through RAWS stages of codes (copies in flight) and CONVS expanded ones (the products hold V of one step and K of the next, a third is being written).
 constexpr int RAWS = 3;
 __host__ __device__ constexpr int convs(bool pre) { return pre ? 4 : 3; }
+__host__ __device__ constexpr int threads(bool pre) { return pre ? 640 : 768; }  // (without converters)
 constexpr float MANY = 256.0f;  // 16 weights may sum to this much, so that each is within fp16's range
 constexpr int TABS = 8;  // scale tables in flight: the copies run at most five tiles ahead of the softmax
 
@@ -52,30 +57,44 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
+// Whether the predicate holds in any thread of two warps.
+__device__ __forceinline__ bool bar_any(int id, bool pred) {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %2, 0;\n\t"
+        "bar.red.or.pred q, %1, 64, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(any)
+        : "r"(id), "r"((uint32_t)pred)
+        : "memory");
+    return any != 0;
+}
+
 template <int D, bool PRE>
-__global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_constant__ AttendArgs A) {
+__global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __grid_constant__ AttendArgs A) {
     using S = Smem<D, PRE>;
-    constexpr int CONVS = convs(PRE);
+    constexpr int CONVS = convs(PRE), ISSUER = PRE ? 16 : 20;  // the warp of the products
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    __shared__ __align__(8) uint64_t bars[2 * RAWS + 2 * CONVS + TABS + 2 + 4 + 2 + 2 + 1 + 1 + 16];
+    __shared__ __align__(8) uint64_t bars[2 * RAWS + 2 * CONVS + TABS + 2 + 2 + 2 + 1 + 1];
     __shared__ float tab[TABS][3][8];  // per 16 keys: key scale, log2 of the value scale, its inverse
-    __shared__ float row_m[ROWS], end_m[2][ROWS], end_l[2][ROWS];  // m as X and Y share it; theirs at the end
+    __shared__ float top_of[2][ROWS], end_l[2][ROWS];  // of X and Y: what m has to grow to, the normaliser at the end
+    __shared__ volatile int quits[8];                  // X or Y of [tile][32 rows] waited too long
     __shared__ int abort_flag;
     __shared__ uint32_t tmem_slot;
     volatile int* abort = &abort_flag;
     const uint32_t raw_full = smem_u32(bars), raw_empty = raw_full + 8 * RAWS, conv_full = raw_empty + 8 * RAWS,
-                   conv_empty = conv_full + 8 * CONVS, tab_full = conv_empty + 8 * CONVS, s_full = tab_full + 8 * TABS, p_full = s_full + 16, pva_done = p_full + 32,
-                   o_full = pva_done + 16, q_full = o_full + 16, drained = q_full + 8,
-                   told = drained + 8;  // p_full: [tile][X, Y]; told: [tile][X to Y, Y to X][32 rows]
+                   conv_empty = conv_full + 8 * CONVS, tab_full = conv_empty + 8 * CONVS, s_full = tab_full + 8 * TABS, p_full = s_full + 16, o_full = p_full + 16,
+                   q_full = o_full + 16, drained = q_full + 8;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_full + 8 * i, 1);
-            mbar_init(pva_done + 8 * i, 1);
+            mbar_init(p_full + 8 * i, 8);
             mbar_init(o_full + 8 * i, 1);
         }
-        for (int i = 0; i < 4; ++i) mbar_init(p_full + 8 * i, 4);
+        for (int i = 0; i < 8; ++i) quits[i] = 0;
         for (int i = 0; i < RAWS; ++i) {
             mbar_init(raw_full + 8 * i, 1);
             mbar_init(raw_empty + 8 * i, 4);
@@ -86,7 +105,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
         }
         for (int i = 0; i < TABS; ++i) mbar_init(tab_full + 8 * i, 1);
         mbar_init(q_full, 16);
-        for (int i = 0; i < 16; ++i) mbar_init(told + 8 * i, 1);
         mbar_init(drained, 1);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -112,9 +130,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     const int seen = last_pos < 0 ? 0 : A.causal ? min(last_pos + 1, end) : end;  // keys that any row sees
     const int n_all = (seen + KEYS - 1) / KEYS;
     const int j0 = (int)((long long)n_all * blockIdx.y / gridDim.y), n = (int)((long long)n_all * (blockIdx.y + 1) / gridDim.y) - j0;
-    const int n2 = n == 0 ? 0 : min(2 * n, (seen - j0 * KEYS + STEP - 1) / STEP);  // steps
 
-    if (warp == 20) {
+    if (warp == ISSUER) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -124,11 +141,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     const uint32_t tmem = tmem_slot;
     const uint32_t base = smem_u32(smem);
 
-    // (the launch holds 768 x 80 registers: 512 x 96 + 256 x 48 of them)
+    // (the launch holds 768 x 80 registers, 512 x 88 + 256 x 64, or 640 x 96, 512 x 112 + 128 x 32)
     if (warp < 16)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PRE ? 112 : 88));
     else
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRE ? 32 : 64));
 
     if (warp < 16) {
         // ================================================================ softmax: one row per thread
@@ -188,29 +205,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
             const int limit = !live || pos < 0 ? 0 : A.causal ? min(pos + 1, end) : end;
             float m = NO_MAX, l = 0.0f;
             bool ok = true;
-            const uint32_t tell = told + 64 * t + 32 * y + 8 * quad, hear = told + 64 * t + 32 * (1 - y) + 8 * quad, sb = ts + STEP * y;
-            float* shared_m = row_m + 128 * t + r;
-            // m as the other one has left it; whether it moved
-            auto follow = [&]() {
-                const float now = *shared_m;
-                if (now == m) return false;
-                l *= ex2(m - now);
-                m = now;
-                return true;
-            };
-            if (!y) *shared_m = NO_MAX;
-            const int steps = (n2 + 1 - y) >> 1;
-            for (int i = 0; i < steps; ++i) {
+            const int id = 1 + 4 * t + quad;  // the barrier of this X and Y, who both come to it in every step whatever happened
+            const uint32_t sb = ts + STEP * y;
+            for (int i = 0; i < n; ++i) {
                 const int slot = i % TABS;
-                // (a wait that is already over takes some 200 cycles, so the scores' comes last; Y's m of the step before was told
-                // before these scores were begun)
-                if (!wait_warp(tab_full + 8 * slot, (i / TABS) & 1, abort, A.status) ||
-                    (!y && i > 0 && !wait_warp(hear, (i - 1) & 1, abort, A.status))) {
-                    ok = false;
-                    break;
-                }
-                if (!y && i > 0) follow();
-                if (!wait_warp(s_full + 8 * t, i & 1, abort, A.status)) {
+                // (a wait that is already over takes some 200 cycles, so the scores' comes last)
+                if (!wait_warp(tab_full + 8 * slot, (i / TABS) & 1, abort, A.status) || !wait_warp(s_full + 8 * t, i & 1, abort, A.status)) {
+                    quits[id - 1] = 1;
+                    bar_any(id, true);
                     ok = false;
                     break;
                 }
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 const int room = limit - (j0 + i) * KEYS - STEP * y;  // of these 64 keys, those that the row sees
                 const float *kf = tab[slot][0] + 4 * y, *lg = tab[slot][1] + 4 * y, *iv = tab[slot][2] + 4 * y;
                 const bool masked = __any_sync(0xffffffffu, live && room < STEP);  // the last steps of a row
-                uint32_t w[32];
+                uint32_t w[2][16];
                 float part, over;  // the normaliser, the largest sum of 16 weights
                 auto mask = [&](int c, uint32_t (&s)[32]) {
                     if (masked) {
@@ -226,7 +228,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                         for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < room ? s[e] : 0xff800000u;
                     }
                 };
-                auto weights = [&]() {
+                bool quit = false;
+                for (int raised = 0;; raised = 1) {
                     float sums[4];
                     uint32_t both[2][32];  // (one round trip for all 64 scores)
                     tmem_ld32_nw(sb, both[0]);
@@ -258,20 +261,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                             sums[2 * c + g] = a.x + a.y;
                         }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) w[16 * c + e] = h2_bits(__floats2half2_rn(x[e].x, x[e].y));
+                        for (int e = 0; e < 16; ++e) w[c][e] = h2_bits(__floats2half2_rn(x[e].x, x[e].y));
                     }
                     over = fmaxf(max3(sums[0], sums[1], sums[2]), sums[3]);
                     part = fmaf(sums[0], iv[0], sums[1] * iv[1]) + fmaf(sums[2], iv[2], sums[3] * iv[3]);
-                };
-                weights();
-                if (y) {  // X's m of this step
-                    if (!wait_warp(hear, i & 1, abort, A.status)) {
-                        ok = false;
-                        break;
-                    }
-                    if (__any_sync(0xffffffffu, follow())) weights();
-                }
-                if (__any_sync(0xffffffffu, over > MANY)) {
+                    if (!bar_any(id, over > MANY && !raised) || (quit = quits[id - 1])) break;
+                    int row = 128 * t + r;
+                    asm volatile("" : "+r"(row));  // (what follows is rare: nothing of it is to be kept in registers)
                     float top = -INFINITY;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -288,21 +284,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                             top = fmaxf(top, mx == -INFINITY ? mx : fmaf(mx, kf[2 * c + g] * cf, lg[2 * c + g]));
                         }
                     }
-                    const bool grow = over > MANY;
-                    const float now = grow ? ceilf(top) : m, f = grow ? ex2(m - now) : 1.0f;
+                    top_of[y][row] = over > MANY ? ceilf(top) : m;
+                    asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
+                    const float now = fmaxf(top_of[0][row], top_of[1][row]), f = now == m ? 1.0f : ex2(m - now);
                     m = now;
                     l *= f;
-                    *shared_m = m;
-                    // O holds all that came before: for X because this step's scores were issued after the last value product,
-                    // for Y once the product of X's weights is complete
-                    if (y && !wait_warp(pva_done + 8 * t, i & 1, abort, A.status)) {
-                        ok = false;
-                        break;
-                    }
-                    if (i > 0 || y) {
-                        tc_fence_after();
+                    if (i > 0) {  // O holds all steps before (their products were issued before this step's scores); half of it each
 #pragma unroll
-                        for (int c = 0; c < D / 16; ++c) {
+                        for (int k = 0; k < D / 32; ++k) {
+                            const int c = (D / 32) * y + k;
                             uint32_t o[16];
                             tmem_ld16_nw(to + 16 * c, o);
                             tmem_wait_ld();
@@ -312,28 +302,28 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                             tmem_st16_nw(to + 16 * c, o);
                         }
                     }
-                    weights();
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(tell);
+                if (quit) {
+                    ok = false;
+                    break;
+                }
                 l += part;
-                tmem_st32_nw(sb, w);
+                tmem_st16_nw(sb, w[0]);
+                tmem_st16_nw(sb + 16, w[1]);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * y);
+                if (lane == 0) mbar_arrive(p_full + 8 * t);
             }
             if (ok && n > 0) ok = wait_warp(o_full + 8 * t, 0, abort, A.status);
             tc_fence_after();
-            end_m[y][128 * t + r] = m;
             end_l[y][128 * t + r] = l;
-            asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * t + quad) : "memory");  // this X and Y, whatever became of them
+            asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
             if (ok) {
                 const long long orow = (long long)(first + tok) * A.q_heads + h * A.group + rr - tok * A.group;
                 const bool split = gridDim.y > 1;
                 float* part = A.part + ((long long)blockIdx.y * A.s.n_tokens * A.q_heads + orow) * (D + 4);
-                const float om = end_m[1 - y][128 * t + r], all = fmaxf(m, om);
-                l = (l == 0.0f ? 0.0f : l * ex2(m - all)) + (end_l[1 - y][128 * t + r] == 0.0f ? 0.0f : end_l[1 - y][128 * t + r] * ex2(om - all));
+                l += end_l[1 - y][128 * t + r];
                 const float inv = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) {
@@ -357,14 +347,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                             store_f32<16>(static_cast<__nv_bfloat16*>(A.out) + orow * D + 16 * c, v);
                     }
                 }
-                if (live && split && !y) *reinterpret_cast<float2*>(part) = make_float2(all, l);
-                if (live && !split && A.lse && !y) A.lse[orow] = l == 0.0f ? -INFINITY : (all + log2f(l)) * LN2;
+                if (live && split && !y) *reinterpret_cast<float2*>(part) = make_float2(m, l);
+                if (live && !split && A.lse && !y) A.lse[orow] = l == 0.0f ? -INFINITY : (m + log2f(l)) * LN2;
             }
         }
-    } else if (warp < 20) {
+    } else if (!PRE && warp < 20) {
         // ================================================================ converters
         const int t = threadIdx.x - 512;
-        for (int u = 0; u < (PRE ? 0 : 2 * n); ++u) {  // K 0, V 0, K 1, V 1 ..
+        for (int u = 0; u < 2 * n; ++u) {  // K 0, V 0, K 1, V 1 ..
             const int rs = u % RAWS, cs = u % CONVS;
             if (!wait_warp(raw_full + 8 * rs, (u / RAWS) & 1, abort, A.status) ||
                 !wait_warp(conv_empty + 8 * cs, ((u / CONVS) & 1) ^ 1, abort, A.status))
@@ -400,7 +390,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 mbar_arrive(conv_full + 8 * cs);
             }
         }
-    } else if (warp == 20) {
+    } else if (warp == ISSUER) {
         // ================================================================ products
         const uint32_t id_qk = make_idesc(128, KEYS), id_pv = make_idesc(128, D) | (1u << 16);
         // operand tile u of the ring (K 0, V 0, K 1, ..)
@@ -421,19 +411,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
                 const int uv = (2 * j + 1) % CONVS;
                 if (!have(2 * j + 1)) break;
                 for (int t = 0; t < tiles && ok; ++t) {
-                    for (int y = 0; y < (2 * j + 1 < n2 ? 2 : 1); ++y) {
-                        if (!wait_warp(p_full + 16 * t + 8 * y, j & 1, abort, A.status)) {
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-                        const uint64_t vd = make_sdesc_mn(base + S::conv0 + uv * S::CONV + y * (STEP * 128));
-#pragma unroll
-                        for (int kk = 0; kk < STEP / 16; ++kk)
-                            tc_mma_ta(tmem + 256 + 128 * t, tmem + 128 * t + STEP * y + 8 * kk, vd + kk * (2048 >> 4), id_pv, j > 0 || y > 0 || kk > 0);
-                        if (y == 0) tc_commit(pva_done + 8 * t);
+                    if (!wait_warp(p_full + 8 * t, j & 1, abort, A.status)) {
+                        ok = false;
+                        break;
                     }
-                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t vd = make_sdesc_mn(base + S::conv0 + uv * S::CONV);
+#pragma unroll
+                    for (int kk = 0; kk < KEYS / 16; ++kk)
+                        tc_mma_ta(tmem + 256 + 128 * t, tmem + 128 * t + STEP * (kk >> 2) + 8 * (kk & 3), vd + kk * (2048 >> 4), id_pv, j > 0 || kk > 0);
                     if (j == n - 1) tc_commit(o_full + 8 * t);
                     if (t == tiles - 1) tc_commit(conv_empty + 8 * uv);
                     if (j + 1 < n) {
@@ -449,7 +435,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
         }
         tc_commit(drained);  // every product issued here has completed once it fires
         drain_warp(drained, 0);
-    } else if (warp == 21) {
+    } else if (warp == ISSUER + 1) {
         // ================================================================ pages, scales, copies
         const int* table = A.s.pages + (long long)b * A.s.pages_stride;
         struct Info {
@@ -526,7 +512,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tile_kernel(const __grid_co
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 20) {
+    if (warp == ISSUER) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
     }
@@ -615,7 +601,7 @@ fxpq_status launch(AttendArgs& A, int shares, cudaStream_t st) {
     }
     const long long blocks = tile_blocks(A.s.n_tokens, A.s.n_seqs, A.group, A.s.starts != nullptr);
     if (blocks * A.heads > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
-    launch_pdl(attend_tile_kernel<D, PRE>, dim3((unsigned)(blocks * A.heads), (unsigned)shares), dim3(THREADS), Smem<D, PRE>::bytes, st, A);
+    launch_pdl(attend_tile_kernel<D, PRE>, dim3((unsigned)(blocks * A.heads), (unsigned)shares), dim3(threads(PRE)), Smem<D, PRE>::bytes, st, A);
     fxpq_status rc = after_launch("attend_tile");
     if (rc != FXPQ_OK || shares == 1) return rc;
     const long long rows = (long long)A.s.n_tokens * A.q_heads;

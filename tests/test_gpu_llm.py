@@ -402,6 +402,49 @@ def test_attention_of_many_rows_masks_bad_pages(ops):
     compare_attention(out, lse, want, wl, spread, slack, "bf16", 400, np.abs(c.v).max() * c.v_scale.max())
 
 
+@pytest.mark.parametrize("rows", [150, 260, 300])  # the last two are of more than 2048 rows a key head: their codes are expanded
+def test_attention_of_more_rows_masks_bad_pages(ops, rows):
+    rng = np.random.default_rng(rows)
+    c, table = make(rng, [700, 333], 32, 1, 64)
+    q, tl = cuda(rng.normal(size=(2 * rows, 8, 64)), torch.float16), torch.tensor([700, 333], dtype=torch.int32, device="cuda")
+    bad = table.copy()
+    bad[0, 1], bad[0, 4], bad[0, 9], bad[1, 0] = -1, len(c.k), 2**31 - 1, -5
+    out, lse = ops.kv_attention(on_gpu(ops, c), cuda(bad), tl, q, causal=False, return_lse=True)
+    assert F.fxpq_get_device_status() == L.ERR_RANGE
+    for b, (n, gone) in enumerate([(700, (1, 4, 9)), (333, (0,))]):
+        keep = [i for i in range(-(-n // 32)) if i not in gone]
+        mine = slice(b * rows, (b + 1) * rows)
+        want, wl, spread, slack = O.attention(c, table[b:b + 1, keep], [n - 32 * len(gone)], [0, rows], q[mine].double().cpu().numpy(),
+                                              O.default_scale(64), False)
+        compare_attention(out[mine], lse[mine], want, wl, spread, slack, "f16", n, np.abs(c.v).max() * c.v_scale.max())
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, "bf16"), (128, "f16")])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_more_rows_expanded_and_ragged(ops, dim, dtype, causal):
+    check_attention(ops, [700, 513, 1, 1100], [0, 77, 900, 130], 64, 8, 2, dim, dtype, causal, True, seed=dim)
+    check_attention(ops, [2100, 2100], [3, 0], 16, 1, 1, dim, dtype, causal, False, seed=dim + 1)
+    check_attention(ops, [600] * 3, None, 128, 4, 1, dim, dtype, causal, False, lens=[590, 0, 600])
+
+
+@pytest.mark.parametrize("n", [40, 300, 600])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_maxima_that_grow_in_either_half_of_a_step(ops, n, dim):
+    """Keys that grow along the sequence, so that the running maximum moves in most steps, by turns in either 64 of 128."""
+    rng = np.random.default_rng(n + dim)
+    c, table = make(rng, [1500], 64, 1, dim)
+    c.k[:] = np.sign(rng.normal(size=dim) + 0.2)[None, None, None] * 20
+    block = np.argsort(np.argsort(table[0]))
+    for i, p in enumerate(table[0]):
+        c.k[p, 0, :, :] = np.clip(c.k[p, 0] * (1 + block[i] % 5), -127, 127)
+        c.k_scale[p] = 2.0 ** (-9 + i // 4)
+    q = cuda(np.abs(rng.normal(size=(n, 4, dim))) * np.sign(c.k[table[0, 0], 0, 0]), torch.float16)
+    tl = torch.tensor([1500], dtype=torch.int32, device="cuda")
+    out, lse = ops.kv_attention(on_gpu(ops, c), cuda(table), tl, q, causal=False, return_lse=True)
+    want, wl, spread, slack = O.attention(c, table, [1500], [0, n], q.double().cpu().numpy(), O.default_scale(dim), False)
+    compare_attention(out, lse, want, wl, spread, slack, "f16", 1500, np.abs(c.v).max() * c.v_scale.max())
+
+
 def test_attention_rows_that_see_nothing(ops):
     # length 0, fewer tokens than new rows, and a sequence without pages, in both sizes of batch
     check_attention(ops, [1] * 4, None, 16, 4, 2, 64, "bf16", True, False, lens=[0, 1, 5, 0])
