@@ -51,9 +51,9 @@ Plan plan(const fxpq_kv_cache& c, const fxpq_kv_batch& b, int q_heads) {
     }
     p.ws_join = p.tile ? (attend_tile_workspace(b.n_tokens, q_heads, c.dim, p.shares) + 255) / 256 * 256 : 0;
     // Expanding costs five bytes of traffic a code and saves every block of 256 rows its own; the room is for max_pages.
-    // Both ways measured (us, expanded and not, 65536 rows of dim 128 over 4096 tokens and their own): blocks of 1024 rows
-    // 1092 and 910, 2048 rows 1013 and 999, 4096 rows 980 and 1040, 8192 rows 1027 and 1128; dim 64 845 and 817, 805 and 840,
-    // 806 and 868, 868 and 949.
+    // Both ways measured (us, expanded and not; 65536 rows in all, 8 key heads of 128, groups of 4, causal, 4096 tokens and
+    // the new ones): with 1024 rows a key head 1092 and 910, 2048 1013 and 999, 4096 980 and 1040, 8192 1027 and 1128; heads
+    // of 64 845 and 817, 805 and 840, 806 and 868, 868 and 949.
     const size_t room = p.tile ? attend_expand_workspace(b.n_seqs, c.heads, c.dim, tokens) : 0;
     p.expand = p.tile && mean > EXPAND_ROWS && room <= EXPAND_ROOM && b.n_seqs <= 65535 && c.heads <= 65535 && tokens <= INT32_MAX - 128;
     p.ws = p.ws_stream + p.ws_join + (p.expand ? room : 0);
