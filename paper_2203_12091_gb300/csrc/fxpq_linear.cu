@@ -257,23 +257,23 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
                 tmem_st32_nw(tmem_a + ((uint32_t)(quad * 32) << 16) + 64 * grp + 32 * hf, r);
             }
             if constexpr (!HALF) {
-            const unsigned char* rb = ra + LS_A;
-            unsigned char* cb = smem + ST * raw_bytes + grp * cols * 256;
-            for (int rr = t >> 3; rr < cols; rr += 16) {  // 16 codes of one token
-                const int c = t & 7, hf = c >> 2;
-                const uint4 v = *reinterpret_cast<const uint4*>(rb + rr * 128 + ((c ^ (rr & 7)) << 4));
-                uint4 o[2];
-                uint32_t x = v.x ^ 0x80808080u, y = v.y ^ 0x80808080u;
-                o[0] = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
-                x = v.z ^ 0x80808080u, y = v.w ^ 0x80808080u;
-                o[1] = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
-                unsigned char* dst = cb + hf * cols * 128 + rr * 128;
-                const int j = 2 * (c & 3);
-                // (the second half's lanes begin with their odd chunk, else the two halves meet in the banks)
-                *reinterpret_cast<uint4*>(dst + (((j + hf) ^ (rr & 7)) << 4)) = hf ? o[1] : o[0];
-                *reinterpret_cast<uint4*>(dst + (((j + 1 - hf) ^ (rr & 7)) << 4)) = hf ? o[0] : o[1];
-            }
-            fence_proxy_async();
+                const unsigned char* rb = ra + LS_A;
+                unsigned char* cb = smem + ST * raw_bytes + grp * cols * 256;
+                for (int rr = t >> 3; rr < cols; rr += 16) {  // 16 codes of one token
+                    const int c = t & 7, hf = c >> 2;
+                    const uint4 v = *reinterpret_cast<const uint4*>(rb + rr * 128 + ((c ^ (rr & 7)) << 4));
+                    uint4 o[2];
+                    uint32_t x = v.x ^ 0x80808080u, y = v.y ^ 0x80808080u;
+                    o[0] = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
+                    x = v.z ^ 0x80808080u, y = v.w ^ 0x80808080u;
+                    o[1] = make_uint4(code_pair(x, LOW_PAIR), code_pair(x, HIGH_PAIR), code_pair(y, LOW_PAIR), code_pair(y, HIGH_PAIR));
+                    unsigned char* dst = cb + hf * cols * 128 + rr * 128;
+                    const int j = 2 * (c & 3);
+                    // (the second half's lanes begin with their odd chunk, else the two halves meet in the banks)
+                    *reinterpret_cast<uint4*>(dst + (((j + hf) ^ (rr & 7)) << 4)) = hf ? o[1] : o[0];
+                    *reinterpret_cast<uint4*>(dst + (((j + 1 - hf) ^ (rr & 7)) << 4)) = hf ? o[0] : o[1];
+                }
+                fence_proxy_async();
             }
             tmem_wait_st();
             tc_fence_before();
