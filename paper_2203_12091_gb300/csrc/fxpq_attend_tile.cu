@@ -12,9 +12,9 @@
 // A step's weights are formed with the maximum m as it was; only where 16 of them sum past 2^8 (a few times per row) are
 // they formed again, after the sums have been rescaled.  m then moves by whole powers of two, so that rescaling is
 // exact.  X and Y share m: one barrier of their two warps tells both whether either's weights have to be formed again.
-// (Told by one mbarrier each way instead, X and Y waited for one another in turn: 913 us for 2 prompts of 8192, 835 now.)
-// A register that spills in the loop costs more than anything else here: converters of 48 registers with eight loads in flight
-// took 2067 ns a step of 128 keys, with 64 registers 1626; the expanded form needs none, so that softmax has 112.
+// (Told by one mbarrier each way instead, X and Y waited for one another in turn: 913 us for 2 prompts of 8192, with it 835.)
+// A register that spills costs more than anything else here: with the converters' loop over its two halves unrolled, which
+// spills 64 bytes, a step of 128 keys takes 1761 ns, so 1608.  The expanded form has no converters and leaves the softmax 112.
 // With one thread a row forming the weights of 64 keys after the other a tile's chain was 2300 cycles of softmax for 128 keys.
 // Codes arrive as they are stored ([keys][dim] bytes, one TMA box per page): K is a K-major operand and V, with the
 // same bytes, an operand whose columns are contiguous, so that neither is transposed.
@@ -79,6 +79,7 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     __shared__ __align__(8) uint64_t bars[2 * RAWS + 2 * CONVS + TABS + 2 + 2 + 2 + 1 + 1];
     __shared__ float tab[TABS][3][8];  // per 16 keys: key scale, log2 of the value scale, its inverse
+    __shared__ float row_cf[ROWS];  // what a row's scores are multiplied by, but for the key block's scale
     __shared__ float top_of[2][ROWS], end_l[2][ROWS];  // of X and Y: what m has to grow to, the normaliser at the end
     __shared__ volatile int quits[8];                  // X or Y of [tile][32 rows] waited too long
     __shared__ int abort_flag;
@@ -141,71 +142,74 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
     const uint32_t tmem = tmem_slot;
     const uint32_t base = smem_u32(smem);
 
-    // (the launch holds 768 x 80 registers, 512 x 88 + 256 x 64, or 640 x 96, 512 x 112 + 128 x 32)
+    // (the launch holds 768 x 80 registers, 512 x 96 + 256 x 48, or 640 x 96, 512 x 112 + 128 x 32)
     if (warp < 16)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PRE ? 112 : 88));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PRE ? 112 : 96));
     else
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRE ? 32 : 64));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRE ? 32 : 48));
 
     if (warp < 16) {
         // ================================================================ softmax: one row per thread
-        const int t = warp >> 3, y = (warp >> 2) & 1, quad = warp & 3, r = quad * 32 + lane, rr = rb * ROWS + t * 128 + r, tok = rr / A.group;
-        const bool live = t * 128 + r < rows;
+        const int t = warp >> 3, y = (warp >> 2) & 1, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16, ts = tmem + 128 * t + lanes, to = tmem + 256 + 128 * t + lanes;
-        const long long qrow = (long long)(first + tok) * A.q_token + (long long)(h * A.group + rr - tok * A.group) * A.q_head;
-        float cf;
-        {  // the row's values, kept as they come (two to a register) between the maximum and the conversion
-            uint32_t x[D / 2];
+        const int id = 1 + 4 * t + quad;  // the barrier of this X and Y, who both come to it in every step whatever happened
+        {  // 16 rows a warp, 16 bytes a lane: whole rows at once (a row per thread took 15000 cycles; 2 prompts of 8192 835 us, so 775)
+            constexpr int LANES = D / 8, EACH = 32 / LANES, IT = 8 / EACH;  // lanes of a row, rows of a load
             const bool f16 = A.q_f16;
-            const unsigned short* src = static_cast<const unsigned short*>(A.q) + qrow;
-            if (!live) {
+            const int d = 8 * (lane % LANES), row0 = quad * 32 + 16 * y + lane / LANES;
+#pragma unroll 1  // (in one go, 8 loads more in flight, a few registers of the loop below spill)
+            for (int from = 0; from < 16; from += 8) {
+                uint4 x[IT];
 #pragma unroll
-                for (int i = 0; i < D / 2; ++i) x[i] = 0u;
-            } else if (A.q_vec) {
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(src + 8 * i);
-                    x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
+                for (int it = 0; it < IT; ++it) {
+                    const int row = t * 128 + row0 + from + it * EACH, at = rb * ROWS + row, token = at / A.group;
+                    x[it] = make_uint4(0u, 0u, 0u, 0u);
+                    if (row < rows) {
+                        const unsigned short* src = static_cast<const unsigned short*>(A.q) + (long long)(first + token) * A.q_token +
+                                                    (long long)(h * A.group + at - token * A.group) * A.q_head + d;
+                        if (A.q_vec)
+                            x[it] = *reinterpret_cast<const uint4*>(src);
+                        else
+                            x[it] = make_uint4(src[0] | (uint32_t)src[1] << 16, src[2] | (uint32_t)src[3] << 16, src[4] | (uint32_t)src[5] << 16,
+                                               src[6] | (uint32_t)src[7] << 16);
+                    }
                 }
-            } else {
 #pragma unroll
-                for (int i = 0; i < D / 2; ++i) x[i] = src[2 * i] | (uint32_t)src[2 * i + 1] << 16;
-            }
-            auto pair = [&](uint32_t v) {
-                return f16 ? __half22float2(*reinterpret_cast<const __half2*>(&v)) : make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-            };
-            float top = 0.0f;
-            bool odd = false;
+                for (int it = 0; it < IT; ++it) {
+                    const int row = row0 + from + it * EACH;
+                    const uint32_t raw[4] = {x[it].x, x[it].y, x[it].z, x[it].w};
+                    float2 v[4];
+                    float top = 0.0f;
 #pragma unroll
-            for (int i = 0; i < D / 2; ++i) {
-                const float2 v = pair(x[i]);
-                odd |= !(fabsf(v.x) <= FLT_MAX) || !(fabsf(v.y) <= FLT_MAX);
-                top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
-            }
-            const int e = odd ? 0 : q_exponent(top);
-            const float up = pow2i(e);
-            cf = A.scale * LOG2E * pow2i(-e);
+                    for (int i = 0; i < 4; ++i) {
+                        v[i] = f16 ? __half22float2(*reinterpret_cast<const __half2*>(&raw[i]))
+                                   : make_float2(__uint_as_float(raw[i] << 16), __uint_as_float(raw[i] & 0xffff0000u));
+                        const float big = fmaxf(fabsf(v[i].x), fabsf(v[i].y));  // (a row with a NaN is not scaled)
+                        top = fmaxf(top, v[i].x != v[i].x || v[i].y != v[i].y ? INFINITY : big);
+                    }
 #pragma unroll
-            for (int k = 0; k < D / 2; k += 8) {  // X writes the row's first half, Y the second
-                const int d = (D / 2) * y + k;
-                uint32_t h[4];
+                    for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const int e = q_exponent(top);
+                    const float up = pow2i(e);
+                    uint32_t w[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 v = pair(y ? x[D / 4 + k / 2 + i] : x[k / 2 + i]);
-                    h[i] = h2_bits(__floats2half2_rn(v.x * up, v.y * up));
+                    for (int i = 0; i < 4; ++i) w[i] = h2_bits(__floats2half2_rn(v[i].x * up, v[i].y * up));
+                    *reinterpret_cast<uint4*>(smem + t * S::Q + (d >> 6) * 16384 + row * 128 + ((((d >> 3) & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (d == 0) row_cf[t * 128 + row] = A.scale * LOG2E * pow2i(-e);
                 }
-                *reinterpret_cast<uint4*>(smem + t * S::Q + (d >> 6) * 16384 + r * 128 + ((((d >> 3) & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
             }
         }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full);
+        asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
+        const float cf = row_cf[t * 128 + r];
         if (t < tiles) {
-            const int pos = len - count + tok;
-            const int limit = !live || pos < 0 ? 0 : A.causal ? min(pos + 1, end) : end;
+            const int pos = len - count + (rb * ROWS + t * 128 + r) / A.group;
+            // keys that the row sees (rows past the last one hold zeros: what they see does not matter)
+            const int limit = t * 128 + r >= rows ? 1 << 30 : pos < 0 ? 0 : A.causal ? min(pos + 1, end) : end;
             float m = NO_MAX, l = 0.0f;
             bool ok = true;
-            const int id = 1 + 4 * t + quad;  // the barrier of this X and Y, who both come to it in every step whatever happened
             const uint32_t sb = ts + STEP * y;
             for (int i = 0; i < n; ++i) {
                 const int slot = i % TABS;
@@ -219,7 +223,7 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
                 tc_fence_after();
                 const int room = limit - (j0 + i) * KEYS - STEP * y;  // of these 64 keys, those that the row sees
                 const float *kf = tab[slot][0] + 4 * y, *lg = tab[slot][1] + 4 * y, *iv = tab[slot][2] + 4 * y;
-                const bool masked = __any_sync(0xffffffffu, live && room < STEP);  // the last steps of a row
+                const bool masked = __any_sync(0xffffffffu, room < STEP);  // the last steps of a row
                 uint32_t w[2][16];
                 float part, over;  // the normaliser, the largest sum of 16 weights
                 auto mask = [&](int c, uint32_t (&s)[32]) {
@@ -320,6 +324,10 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
             end_l[y][128 * t + r] = l;
             asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
             if (ok) {
+                int own = r;
+                asm volatile("" : "+r"(own));  // (computed here: the loop has no register for it)
+                const bool live = t * 128 + own < rows;
+                const int rr = rb * ROWS + t * 128 + own, tok = rr / A.group;
                 const long long orow = (long long)(first + tok) * A.q_heads + h * A.group + rr - tok * A.group;
                 const bool split = gridDim.y > 1;
                 float* part = A.part + ((long long)blockIdx.y * A.s.n_tokens * A.q_heads + orow) * (D + 4);
@@ -362,7 +370,7 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
             const unsigned char* src = smem + S::raw0 + rs * S::RAW;
             unsigned char* dst = smem + S::conv0 + cs * S::CONV;
             constexpr int CH = D / 16, IT = KEYS * CH / 128;  // 16-code chunks of a row, of a thread
-#pragma unroll
+#pragma unroll 1
             for (int half = 0; half < IT / 4; ++half) {  // four loads in flight together
                 uint4 v[4];
 #pragma unroll
