@@ -5,8 +5,10 @@
 // codes become fp16 integers exactly, and their products sum in fp32.  With t = log2(e) * scale * (q . key) +
 // log2(value scale of the key's block), a key's weight in the value sum is 2^t times its value's integer code, and in
 // the normaliser 2^t / (value scale).  So the block's scales cost one fused multiply-add per score, and
-// w = 2^(t - m) is rounded to fp16 once.  m follows the running maximum only when t passes m + 8: sums are rescaled a
-// few times per row instead of per tile, and w <= 2^8 keeps far from fp16's end while its range reaches down to 2^-24.
+// w = 2^(t - m + 7) is rounded to fp16 once.  m follows the running maximum only when t passes m + 8: sums are rescaled a
+// few times per row instead of per tile.  w <= 2^15 is within fp16, whose last step of 2^-24 is then at most 2^-31 of the row's
+// largest weight: with w = 2^(t - m) it was 2^-24 of it, and over 2^20 keys what small weights add was rounded away.  The
+// normaliser sums the weights as they are before they are rounded, in fp32.
 #include <cfloat>
 
 #include "fxpq_llm.cuh"
@@ -17,6 +19,7 @@ namespace llm {
 
 constexpr float NO_MAX = -3.0e38f;   // m of a row that has seen no key
 constexpr float LAZY = 8.0f;         // t may pass m by this much
+constexpr float LIFT = 7.0f, UNLIFT = 0.0078125f;  // weights are 2^LIFT larger than 2^(t - m); the results' division takes it back
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct AttendArgs {

@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(32 * WARPS, ctas_of(NT)) attend_stream_kernel(
                     }
                 }
             }
-            // ---- t, the lazily followed maximum, weights
+            // ---- t + LIFT, the lazily followed maximum, weights
             const int tile = t_lo + warp + WARPS * j, src = j & 31;
             float ks[2], lv[2], iv[2];
 #pragma unroll
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(32 * WARPS, ctas_of(NT)) attend_stream_kernel(
                 const float k = __shfl_sync(0xffffffffu, i && two ? cur.ks[1] : cur.ks[0], src);
                 const float v = __shfl_sync(0xffffffffu, i && two ? cur.vs[1] : cur.vs[0], src);
                 ks[i] = k;
-                lv[i] = v > 0.0f ? __log2f(v) : -INFINITY;
+                lv[i] = v > 0.0f ? __log2f(v) + LIFT : -INFINITY;
                 iv[i] = v > 0.0f ? ex2(-lv[i]) : 0.0f;
             }
             const bool masked = tile * TILE + TILE > free_of_mask;
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(32 * WARPS, ctas_of(NT)) attend_stream_kernel(
                         float t = fmaf(c[mt][nt][e], ks[mt] * cf[nt][e & 1], lv[mt]);
                         if (masked && tile * TILE + 16 * mt + row_of<D>(g) + 8 * (e >> 1) >= limit[nt][e & 1]) t = -INFINITY;
                         c[mt][nt][e] = t;
-                        over |= t > m[nt][e & 1] + LAZY;
+                        over |= t > m[nt][e & 1] + (LAZY + LIFT);
                     }
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
@@ -372,9 +372,9 @@ __global__ void __launch_bounds__(32 * WARPS, ctas_of(NT)) attend_stream_kernel(
                         float top = fmaxf(fmaxf(c[0][nt][e], c[0][nt][e + 2]), fmaxf(c[1][nt][e], c[1][nt][e + 2]));
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                        if (top > m[nt][e] + LAZY) {
-                            const float f = ex2(m[nt][e] - top);
-                            m[nt][e] = top;
+                        if (top > m[nt][e] + (LAZY + LIFT)) {
+                            const float now = top - LIFT, f = ex2(m[nt][e] - now);
+                            m[nt][e] = now;
                             l[nt][e] *= f;
 #pragma unroll
                             for (int i = 0; i < MT; ++i) {
@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(32 * WARPS, ctas_of(NT)) attend_stream_kernel(
             if (complete) {
                 const int rr = rb * 8 * NT + r, tok = rr / A.group;
                 const long long row = (long long)(q.first + tok) * A.q_heads + h * A.group + rr - tok * A.group;
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                const float inv = sum == 0.0f ? 0.0f : UNLIFT / sum;
                 put_out(A, row * D + d, a * inv, c2 * inv);
                 if (A.lse && d == 0) A.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
             } else {
@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
         }
         top = now;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float inv = sum == 0.0f ? 0.0f : UNLIFT / sum;
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) put_out(A, row * D + 64 * e + 2 * lane, a[2 * e] * inv, a[2 * e + 1] * inv);
     if (A.lse && lane == 0) A.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;

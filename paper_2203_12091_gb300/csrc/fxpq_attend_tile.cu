@@ -9,7 +9,7 @@
 //   warps 16-19     converters: codes to fp16 operand tiles of 128 keys, once for both row tiles (none where the codes came
 //                   expanded; the warps that follow are then 16 to 19)
 //   warp 20         tensor memory, products;   warp 21   pages, scales, copies;   22, 23   none
-// A step's weights are formed with the maximum m as it was; only where 16 of them sum past 2^8 (a few times per row) are
+// A step's weights are formed with the maximum m as it was; only where 16 of them sum past 2^15 (a few times per row) are
 // they formed again, after the sums have been rescaled.  m then moves by whole powers of two, so that rescaling is
 // exact.  X and Y share m: one barrier of their two warps tells both whether either's weights have to be formed again.
 // (Told by one mbarrier each way instead, X and Y waited for one another in turn: 913 us for 2 prompts of 8192, with it 835.)
@@ -34,7 +34,7 @@ constexpr int KEYS = 128, STEP = 64, ROWS = 256;  // keys of an operand tile, of
 constexpr int RAWS = 3;
 __host__ __device__ constexpr int convs(bool pre) { return pre ? 4 : 3; }
 __host__ __device__ constexpr int threads(bool pre) { return pre ? 640 : 768; }  // (without converters)
-constexpr float MANY = 256.0f;  // 16 weights may sum to this much, so that each is within fp16's range
+constexpr float MANY = 32768.0f;  // 16 weights may sum to this much, so that each is within fp16's range
 constexpr int TABS = 8;  // scale tables in flight: the copies run at most five tiles ahead of the softmax
 
 template <int D, bool PRE>
@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     __shared__ __align__(8) uint64_t bars[2 * RAWS + 2 * CONVS + TABS + 2 + 2 + 2 + 1 + 1];
-    __shared__ float tab[TABS][3][8];  // per 16 keys: key scale, log2 of the value scale, its inverse
+    __shared__ float tab[TABS][3][8];  // per 16 keys: key scale, log2 of the value scale lifted, its inverse
     __shared__ float row_cf[ROWS];  // what a row's scores are multiplied by, but for the key block's scale
     __shared__ float top_of[2][ROWS], end_l[2][ROWS];  // of X and Y: what m has to grow to, the normaliser at the end
     __shared__ volatile int quits[8];                  // X or Y of [tile][32 rows] waited too long
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
                             top = fmaxf(top, mx == -INFINITY ? mx : fmaf(mx, kf[2 * c + g] * cf, lg[2 * c + g]));
                         }
                     }
-                    top_of[y][row] = over > MANY ? ceilf(top) : m;
+                    top_of[y][row] = over > MANY ? ceilf(top) - LIFT : m;
                     asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
                     const float now = fmaxf(top_of[0][row], top_of[1][row]), f = now == m ? 1.0f : ex2(m - now);
                     m = now;
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
                 const bool split = gridDim.y > 1;
                 float* part = A.part + ((long long)blockIdx.y * A.s.n_tokens * A.q_heads + orow) * (D + 4);
                 l += end_l[1 - y][128 * t + r];
-                const float inv = split ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+                const float inv = split ? 1.0f : l == 0.0f ? 0.0f : UNLIFT / l;
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) {
                     const int c = (D / 32) * y + k;
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(threads(PRE), 1) attend_tile_kernel(const __gr
         for (int i = 0; i < n && ok; ++i) {
             const int from = 8 * (i & 3), slot = i % TABS;
             if (lane >= from && lane < from + 8) {
-                const float lv = cur.vs > 0.0f ? __log2f(cur.vs) : -INFINITY;
+                const float lv = cur.vs > 0.0f ? __log2f(cur.vs) + LIFT : -INFINITY;
                 tab[slot][0][lane - from] = cur.ks;
                 tab[slot][1][lane - from] = lv;
                 tab[slot][2][lane - from] = cur.vs > 0.0f ? ex2(-lv) : 0.0f;
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(128) attend_tile_join_kernel(const __grid_cons
         }
         top = now;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float inv = sum == 0.0f ? 0.0f : UNLIFT / sum;
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) put_out(A, row * D + 64 * e + 2 * lane, a[2 * e] * inv, a[2 * e + 1] * inv);
     if (A.lse && lane == 0) A.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
