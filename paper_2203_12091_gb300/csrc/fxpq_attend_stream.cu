@@ -48,6 +48,13 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// Two weights as fp16, the first in the low half.  They are at most 2^15, but past 2^15 where scores are so large that
+// m + LAZY + LIFT rounds up (from 2^27 on fp32's steps are 16), and must not become infinite there.
+__device__ __forceinline__ uint32_t weight_pair(float a, float b) {
+    uint32_t w;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    return w;
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t y;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -394,8 +401,8 @@ __global__ void __launch_bounds__(32 * WARPS, ctas_of(NT)) attend_stream_kernel(
                     for (int e = 0; e < 4; ++e) p[e] = ex2(c[mt][nt][e] - m[nt][e & 1]);
                     l[nt][0] = fmaf(p[0] + p[2], iv[mt], l[nt][0]);
                     l[nt][1] = fmaf(p[1] + p[3], iv[mt], l[nt][1]);
-                    wt[mt][nt][0] = transpose8x8(h2_bits(__floats2half2_rn(p[0], p[1])));
-                    wt[mt][nt][1] = transpose8x8(h2_bits(__floats2half2_rn(p[2], p[3])));
+                    wt[mt][nt][0] = transpose8x8(weight_pair(p[0], p[1]));
+                    wt[mt][nt][1] = transpose8x8(weight_pair(p[2], p[3]));
                 }
             // ---- values: four rows of this thread, their bytes interleaved by pairs of rows
 #pragma unroll

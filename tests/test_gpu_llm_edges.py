@@ -55,3 +55,20 @@ def test_attention_keeps_the_small_weights_of_a_long_cache(ops, seqs, n):
     # normaliser, where fp32 may lose what the small ones add to it, and the output's own rounding
     assert (out.double() - want).abs().max().item() <= want * (2.0 ** -4.5 + 2.0 ** -8)
     assert (lse.double() - math.log(total)).abs().max().item() <= 2.0 ** -8
+
+
+@pytest.mark.parametrize("n", [1, 150])
+def test_attention_of_scores_that_are_steps_of_fp32_apart(ops, n):
+    """Scores near 2^27, where fp32 has steps of 16 between their exponents of two, growing by one or two from a warp's tile to its next:
+    the result is a mean of values between 0.5 and 1 all the same."""
+    pages, page = 160, 16
+    c = ops.KVCache.empty(pages, 1, page, 64)
+    c.k[..., 0] = 100
+    c.k_scale[:, 0] = torch.from_numpy((2.0 ** -4 * (1 + np.arange(pages) // 8 * 2.0 ** -23)).astype(np.float32)).cuda()
+    c.v.copy_(torch.randint(64, 129, c.v.shape, device="cuda").clamp(max=127))
+    c.v_scale.fill_(2.0 ** -7)
+    q = torch.zeros(n, 1, 64, dtype=torch.float16, device="cuda")
+    q[..., 0] = 1
+    out, lse = ops.kv_attention(c, torch.arange(pages, dtype=torch.int32, device="cuda")[None], ints(pages * page), q,
+                                scale=1.5 * 2 ** 27 * math.log(2) / 6.25, causal=False, return_lse=True)
+    assert bool(lse.isfinite().all()) and 0.5 * (1 - 2.0 ** -10) <= out.min().item() <= out.max().item() <= 1 + 2.0 ** -10
