@@ -603,8 +603,8 @@ FXPQ_API fxpq_status fxpq_kv_values(const fxpq_kv_cache* cache, const int32_t* d
  * q_heads heads (a multiple of cache->heads) of type F16 or BF16; d_out: contiguous [n_tokens][q_heads][dim]
  * of the same type, 16-byte aligned; d_lse (may be NULL): fp32 [n_tokens][q_heads], the natural logarithm of the sum
  * of exponentials.  A row that sees no key gives zeros and lse -inf.  softmax_scale > 0.
- * Queries are held in fp16 with a power of two per row (nothing is lost of bf16 or fp16 values within 2^-31
- * of their row's largest), codes are exact, products sum in fp32.  A key's part of the value sum, its probability times
+ * Queries are held in fp16 with a power of two per row (nothing is lost of fp16 values; of bf16 ones nothing within 2^-32 of
+ * their row's largest, if that is 2^-111 or more), codes are exact, products sum in fp32.  A key's part of the value sum, its probability times
  * its block's value scale, is rounded to fp16, to 2^-11 of itself or 2^-31 of the row's largest part, whichever is more; the
  * normaliser sums probabilities before that rounding, in fp32.
  * Workspace: fxpq_kv_attention_workspace bytes, 256-byte aligned, scratch; for batches of more than 2048 rows (new tokens x

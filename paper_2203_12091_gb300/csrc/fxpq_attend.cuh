@@ -1,7 +1,7 @@
 #pragma once
 // fxpq_attend.cuh -- what the attention kernels over the paged 8-bit cache share.
 //
-// Scores and weights.  A query row is held in fp16 with a power of two of its own (its largest value in [2^14, 2^15)),
+// Scores and weights.  A query row is held in fp16 with a power of two of its own (its largest value in [2^15, 2^16)),
 // codes become fp16 integers exactly, and their products sum in fp32.  With t = log2(e) * scale * (q . key) +
 // log2(value scale of the key's block), a key's weight in the value sum is 2^t times its value's integer code, and in
 // the normaliser 2^t / (value scale).  So the block's scales cost one fused multiply-add per score, and
@@ -43,10 +43,12 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// The power of two that brings a row's largest value into [2^14, 2^15) (rows of zeros or not finite: 1).
+// The power of two that brings a row's largest value into [2^15, 2^16) (rows of zeros or not finite: 1): no value of type fp16
+// is scaled down, which would cost its last bit.  2^126 is the largest whose inverse is a normal number: below 2^-111 a
+// row's largest value comes to lie lower, and at the other end bf16's 2^127 asks for 2^-112.
 __device__ __forceinline__ int q_exponent(float amax) {
     const int e = (__float_as_int(amax) >> 23) - 127;
-    return amax > 0.0f && amax <= FLT_MAX ? max(-100, min(100, 14 - e)) : 0;
+    return amax > 0.0f && amax <= FLT_MAX ? min(126, 15 - e) : 0;
 }
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }
 

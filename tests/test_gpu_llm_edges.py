@@ -57,6 +57,40 @@ def test_attention_keeps_the_small_weights_of_a_long_cache(ops, seqs, n):
     assert (lse.double() - math.log(total)).abs().max().item() <= 2.0 ** -8
 
 
+# ------------------------------------------------------------------------------ attention: queries near the ends of their type
+@pytest.mark.parametrize("n", [1, 150])
+@pytest.mark.parametrize("power", [100, 115, 120, -90, -105, -112])
+def test_attention_of_huge_and_tiny_queries(ops, n, power):
+    """Queries times 2^p under a scale of 2^-p: the same numbers, scaled exactly, so the same results."""
+    rng = np.random.default_rng(n)
+    c, table = O.paged(rng, [300, 200], 32, 2, 64)
+    gpu = ops.KVCache(*[torch.from_numpy(t).cuda() for t in (c.k, c.v, c.k_scale, c.v_scale)])
+    q = rng.normal(size=(2 * n, 8, 64))
+    q = torch.from_numpy(np.copysign(np.maximum(np.abs(q), 2.0 ** -8), q)).bfloat16().cuda()  # (none becomes subnormal)
+    args = gpu, torch.from_numpy(table).cuda(), ints(300, 200)
+    want = ops.kv_attention(*args, q, scale=0.125, return_lse=True)
+    got = ops.kv_attention(*args, (q.double() * 2.0 ** power).bfloat16(), scale=0.125 * 2.0 ** -power, return_lse=True)
+    assert bool(want[0].isfinite().all()) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("n", [1, 150])
+@pytest.mark.parametrize("large", [32768.0, 65504.0])
+def test_attention_keeps_every_bit_of_float16_queries(ops, n, large):
+    """A row's largest value past 2^15, the others with their last bit at 2^-24, float16's smallest step: scores of 63 of the small
+    ones alone, whose last bits are 2^-10 of them."""
+    dim, small = 64, (1 + 2.0 ** -10) * 2.0 ** -14
+    c = ops.KVCache.empty((n + 15) // 16, 1, 16, dim)
+    c.k.fill_(100)
+    c.k[..., 0] = 0
+    q = torch.full((n, 1, dim), small, dtype=torch.float16, device="cuda")
+    q[..., 0] = large
+    score = 50.0
+    lse = ops.kv_attention(c, torch.arange((n + 15) // 16, dtype=torch.int32, device="cuda")[None], ints(n), q,
+                           scale=score / (63 * 100 * small), causal=False, return_lse=True)[1]
+    # 63 products summed in fp32, log2(e) * scale and its product with the sum rounded, log2 and its way back: 2^-18 is ample
+    assert (lse.double() - score - math.log(n)).abs().max().item() <= 50 * 2.0 ** -18
+
+
 @pytest.mark.parametrize("n", [1, 150])
 def test_attention_of_scores_that_are_steps_of_fp32_apart(ops, n):
     """Scores near 2^27, where fp32 has steps of 16 between their exponents of two, growing by one or two from a warp's tile to its next:
