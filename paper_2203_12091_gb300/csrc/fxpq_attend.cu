@@ -55,7 +55,7 @@ Plan plan(const fxpq_kv_cache& c, const fxpq_kv_batch& b, int q_heads) {
     // the new ones): with 1024 rows a key head 1092 and 910, 2048 1013 and 999, 4096 980 and 1040, 8192 1027 and 1128; heads
     // of 64 845 and 817, 805 and 840, 806 and 868, 868 and 949.
     const size_t room = p.tile ? attend_expand_workspace(b.n_seqs, c.heads, c.dim, tokens) : 0;
-    p.expand = p.tile && mean > EXPAND_ROWS && room <= EXPAND_ROOM && b.n_seqs <= 65535 && c.heads <= 65535 && tokens <= INT32_MAX - 128;
+    p.expand = p.tile && mean > EXPAND_ROWS && tokens > 0 && room <= EXPAND_ROOM && b.n_seqs <= 65535 && c.heads <= 65535 && tokens <= INT32_MAX - 128;
     p.ws = p.ws_stream + p.ws_join + (p.expand ? room : 0);
     return p;
 }

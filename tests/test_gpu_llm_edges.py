@@ -91,6 +91,16 @@ def test_attention_keeps_every_bit_of_float16_queries(ops, n, large):
     assert (lse.double() - score - math.log(n)).abs().max().item() <= 50 * 2.0 ** -18
 
 
+# ------------------------------------------------------------------------------ attention: tables
+@pytest.mark.parametrize("n", [1, 40, 2100])  # few rows, a block of rows, codes expanded before
+def test_attention_over_a_table_without_pages(ops, n):
+    c = ops.KVCache.empty(3, 1, 16, 64)
+    q = torch.randn(2 * n, 1, 64, device="cuda").half()
+    pages, lens = torch.empty((2, 0), dtype=torch.int32, device="cuda"), ints(0, 0)
+    out, lse = ops.kv_attention(c, pages, lens, q, return_lse=True)
+    assert not bool(out.any()) and bool((lse == -math.inf).all())
+
+
 @pytest.mark.parametrize("n", [1, 150])
 def test_attention_of_scores_that_are_steps_of_fp32_apart(ops, n):
     """Scores near 2^27, where fp32 has steps of 16 between their exponents of two, growing by one or two from a warp's tile to its next:
