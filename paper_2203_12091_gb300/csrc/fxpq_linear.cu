@@ -770,7 +770,7 @@ bool rows_ok(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_st
 
 extern "C" fxpq_status fxpq_quantize_tokens(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, int8_t* d_codes,
                                             int64_t codes_stride, float* d_scale, void* stream) {
-    if (!rows_ok(d_x, x_type, M, K, x_stride) || codes_stride < K || (M > 0 && !d_scale) || (M > 0 && K > 0 && !d_codes) || !aligned(d_scale, 4))
+    if (!rows_ok(d_x, x_type, M, K, x_stride) || codes_stride < K || (M > 0 && !d_scale) || (M > 0 && codes_stride > 0 && !d_codes) || !aligned(d_scale, 4))
         return FXPQ_ERR_INVALID_ARG;
     if (M == 0) return FXPQ_OK;
     return quantize_rows(d_x, x_type, M, K, x_stride, d_codes, codes_stride, d_scale, as_stream(stream));
