@@ -10,11 +10,13 @@ namespace llm {
 bool batch_ok(const fxpq_kv_batch* b) {
     return b && b->n_seqs >= 0 && b->n_tokens >= 0 && b->max_pages >= 0 && b->pages_stride >= b->max_pages &&
            (b->n_seqs == 0 ? b->n_tokens == 0 : (b->d_pages || b->max_pages == 0) && b->d_lens != nullptr) &&
-           (b->d_starts || b->n_seqs == 0 || b->n_tokens % b->n_seqs == 0);
+           (b->d_starts || b->n_seqs == 0 || b->n_tokens % b->n_seqs == 0) && aligned(b->d_pages, 4) && aligned(b->d_lens, 4) &&
+           aligned(b->d_starts, 4);
 }
 bool cache_ok(const fxpq_kv_cache* c) {
     return c && c->n_pages > 0 && c->heads > 0 && c->d_k && c->d_v && c->d_k_scale && c->d_v_scale && aligned(c->d_k, 16) &&
-           aligned(c->d_v, 16) && (c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128) &&
+           aligned(c->d_v, 16) && aligned(c->d_k_scale, 4) && aligned(c->d_v_scale, 4) &&
+           (c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128) &&
            (c->dim == 64 || c->dim == 128);
 }
 
@@ -437,7 +439,7 @@ extern "C" fxpq_status fxpq_kv_append(const fxpq_kv_cache* cache, const fxpq_kv_
 
 extern "C" fxpq_status fxpq_kv_values(const fxpq_kv_cache* cache, const int32_t* d_list, int32_t n, int32_t type, void* d_k_out,
                                       void* d_v_out, void* stream) {
-    if (!cache_ok(cache) || n < 0 || !ftype_ok(type) || (n > 0 && !d_list) || !aligned(d_k_out, 16) || !aligned(d_v_out, 16))
+    if (!cache_ok(cache) || n < 0 || !ftype_ok(type) || (n > 0 && !d_list) || !aligned(d_list, 4) || !aligned(d_k_out, 16) || !aligned(d_v_out, 16))
         return FXPQ_ERR_INVALID_ARG;
     if (n == 0 || (!d_k_out && !d_v_out)) return FXPQ_OK;
     const int all = cache->page * cache->dim / 16 * cache->heads;
