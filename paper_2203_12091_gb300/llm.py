@@ -6,6 +6,9 @@ is also the stream that the results belong to.  Shapes and types are checked her
 alignment in the library (``_lib.FxpqError``).  What a kernel finds wrong with the data (non-finite values,
 page ids outside the cache, positions past the rotation tables) is latched and read by
 ``fxpq.fxpq_get_device_status``.
+
+The operators are for inference and have no gradient: tensors that require one are refused while gradients are
+recorded (RuntimeError).
 """
 from __future__ import annotations
 
@@ -33,6 +36,12 @@ def _ftype(name, dtype, types=_FT):
     return ft
 
 
+def _no_grad(name, *tensors):
+    """Refuses what would silently come back without its gradient."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise RuntimeError(f"{name} has no gradient: call it under torch.no_grad() or with detached tensors")
+
+
 def _want(name, t, dtype, dims):
     if t.dtype != dtype or t.dim() != dims or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dims}-dimensional CUDA tensor of {dtype} is needed, "
@@ -51,6 +60,8 @@ def quantize_tokens(x):
     """Rows x [..., K] (float32, float16 or bfloat16) -> (codes int8 [..., K], scales float32 [...]), value =
     code * scale.  The codes' rows lie a multiple of 16 bytes apart, as `linear_i8` needs them."""
     ft = _ftype("quantize_tokens", x.dtype)
+    if x.requires_grad:
+        _no_grad("quantize_tokens", x)
     rows = _float_rows("quantize_tokens", x)
     M, K = rows.shape
     pitch = (K + 15) // 16 * 16
@@ -69,6 +80,7 @@ def linear_i8(codes, scale, w, w_scale, bias=None, out_dtype=torch.bfloat16):
     """y [M, N] = (codes [M, K] . w [N, K]^T) * scale[:, None] * w_scale + bias.  Both code tensors: rows a multiple of
     16 bytes apart (`quantize_tokens` makes such rows)."""
     ft = _ftype("linear_i8", out_dtype)
+    _no_grad("linear_i8", scale, w_scale, bias)
     M, K = codes.shape
     N = w.shape[0]
     if codes.dtype != _i8 or not codes.is_cuda or (K > 1 and codes.stride(1) != 1):
@@ -101,7 +113,7 @@ def _pitch(t, K):  # (a single row, or rows of nothing, may have any stride)
 
 class Linear8:
     """A layer with 8-bit weights w int8 [N, K], one scale for each output channel: rows that are not whole 16 bytes
-    are padded once."""
+    are padded once.  Its tensors are constants: what they require of a gradient is dropped."""
 
     def __init__(self, w, w_scale, bias=None):
         _want("Linear8: w", w, _i8, 2)
@@ -115,18 +127,20 @@ class Linear8:
     def _set(self, w, w_scale, bias):
         self.N, self.K = w.shape
         _check_layer("Linear8", w, w_scale, bias, self.K)
-        self.w, self.w_scale, self.bias = w, w_scale, bias
+        self.w, self.w_scale, self.bias = w, w_scale.detach(), None if bias is None else bias.detach()
 
     @classmethod
     def from_float(cls, w, bias=None):
         """Quantizes float weights [N, K]."""
         layer = cls.__new__(cls)
-        layer._set(*quantize_tokens(w), None if bias is None else bias.float().contiguous())
+        layer._set(*quantize_tokens(w.detach()), None if bias is None else bias.detach().float().contiguous())
         return layer
 
     def __call__(self, x, out_dtype=None):
         """x [..., K] in a float type -> [..., N] in out_dtype (x's own by default): `quantize_tokens` and `linear_i8`
         as one call."""
+        if x.requires_grad:
+            _no_grad("Linear8", x)
         rows = _float_rows("Linear8", x)
         M, K = rows.shape
         if K != self.K:
@@ -209,6 +223,8 @@ def kv_append(cache, pages, lens, k, v, q=None, starts=None, cos=None, sin=None,
     ft = _ftype("kv_append", dtype)
     if v.dtype != dtype or (q is not None and q.dtype != dtype):
         raise TypeError("kv_append: k, v and q must have one type")
+    if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
+        _no_grad("kv_append", k, v, q)
     T = k.shape[0]
     batch = _batch("kv_append", pages, lens, starts, T)
     rk, rv = _rows("kv_append: k", k, T, cache.heads, cache.dim), _rows("kv_append: v", v, T, cache.heads, cache.dim)
@@ -256,6 +272,8 @@ def kv_attention(cache, pages, lens, q, starts=None, scale=None, causal=True, re
     float32 [T, q_heads] of the sums of exponentials; rows that see no key are zeros and -inf."""
     dtype, dim = q.dtype, cache.dim
     ft = _ftype("kv_attention", dtype, _Q_TYPES)
+    if q.requires_grad:
+        _no_grad("kv_attention", q)
     if q.dim() != 3:
         raise ValueError(f"kv_attention: q must be [tokens, heads, dim], got {tuple(q.shape)}")
     T, heads, _ = q.shape

@@ -101,6 +101,32 @@ def test_attention_over_a_table_without_pages(ops, n):
     assert not bool(out.any()) and bool((lse == -math.inf).all())
 
 
+# ------------------------------------------------------------------------------ gradients
+def test_tensors_that_want_a_gradient_are_refused(ops):
+    """The operators have no gradient: a result without one, and no word of it, would leave a model untrained."""
+    c = ops.KVCache.empty(4, 2, 16, 64)
+    pages, lens = ints(0, 1, 2, 3)[:, None], ints(1, 1, 1, 1)
+    x = torch.randn(4, 2, 64, device="cuda").half()
+    g = x.clone().requires_grad_()
+    w, b = torch.nn.Parameter(torch.randn(40, 128, device="cuda")), torch.nn.Parameter(torch.randn(40, device="cuda"))
+    layer = ops.Linear8.from_float(w, b)  # (a layer's own weights are constants)
+    flat = g.view(4, 128)
+    codes, scale = ops.quantize_tokens(x.view(4, 128))
+    calls = [lambda: ops.quantize_tokens(flat), lambda: layer(flat),
+             lambda: ops.linear_i8(codes, scale, layer.w, layer.w_scale, b),
+             lambda: ops.linear_i8(codes, scale.clone().requires_grad_(), layer.w, layer.w_scale),
+             lambda: ops.kv_append(c, pages, lens, g, x), lambda: ops.kv_append(c, pages, lens, x, g),
+             lambda: ops.kv_append(c, pages, lens, x, x, q=g), lambda: ops.kv_attention(c, pages, lens, g)]
+    for call in calls:
+        with pytest.raises(RuntimeError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    y = layer(x.view(4, 128))
+    assert not y.requires_grad and not layer.bias.requires_grad and not layer.w_scale.requires_grad
+    assert not ops.Linear8(layer.w.contiguous(), layer.w_scale, b)(x.view(4, 128)).requires_grad
+
+
 @pytest.mark.parametrize("n", [1, 150])
 def test_attention_of_scores_that_are_steps_of_fp32_apart(ops, n):
     """Scores near 2^27, where fp32 has steps of 16 between their exponents of two, growing by one or two from a warp's tile to its next:
