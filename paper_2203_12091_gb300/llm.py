@@ -49,11 +49,14 @@ def _want(name, t, dtype, dims):
 
 
 def _float_rows(name, x):
-    """x [..., K] as [M, K] with contiguous rows."""
+    """x [..., K] as [M, K] with contiguous rows that do not overlap (expanded ones and windows are copied)."""
     if not x.is_cuda or x.dim() < 1:
         raise ValueError(f"{name}: rows on a CUDA device are needed, got {tuple(x.shape)} on {x.device}")
     rows = x if x.dim() == 2 else x.reshape(math.prod(x.shape[:-1]), x.shape[-1])
-    return rows if rows.stride(1) == 1 or rows.shape[1] <= 1 else rows.contiguous()
+    if rows.is_contiguous():
+        return rows
+    K = rows.shape[1]
+    return rows if (rows.stride(1) == 1 or K <= 1) and rows.stride(0) >= K else rows.contiguous()
 
 
 def quantize_tokens(x):

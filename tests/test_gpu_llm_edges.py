@@ -101,6 +101,17 @@ def test_attention_over_a_table_without_pages(ops, n):
     assert not bool(out.any()) and bool((lse == -math.inf).all())
 
 
+# ------------------------------------------------------------------------------ rows that share memory
+@pytest.mark.parametrize("rows", ["expanded", "windows"])
+def test_rows_that_share_memory(ops, rows):
+    x = torch.randn(1, 96, device="cuda").expand(5, -1) if rows == "expanded" else torch.randn(150, device="cuda").unfold(0, 96, 3)
+    codes, scale = ops.quantize_tokens(x)
+    want = ops.quantize_tokens(x.clone(memory_format=torch.contiguous_format))
+    assert torch.equal(codes, want[0]) and torch.equal(scale, want[1])
+    layer = ops.Linear8.from_float(torch.randn(40, 96, device="cuda"))
+    assert torch.equal(layer(x), layer(x.clone(memory_format=torch.contiguous_format)))
+
+
 # ------------------------------------------------------------------------------ gradients
 def test_tensors_that_want_a_gradient_are_refused(ops):
     """The operators have no gradient: a result without one, and no word of it, would leave a model untrained."""
