@@ -282,6 +282,8 @@ def kv_attention(cache, pages, lens, q, starts=None, scale=None, causal=True, re
     T, heads, _ = q.shape
     if heads == 0 or heads % cache.heads:
         raise ValueError(f"kv_attention: {heads} query heads are no multiple of {cache.heads}")
+    if pages.dim() == 2 and pages.stride(0) < pages.shape[1]:  # (sequences may share a row here; it stays referenced until the launch)
+        pages = pages.contiguous()
     batch, rq = _batch("kv_attention", pages, lens, starts, T), _rows("kv_attention: q", q, T, heads, dim)
     out = _empty((T, heads, dim), dtype=dtype, device=q.device)
     lse = _empty((T, heads), dtype=_f32, device=q.device) if return_lse else None

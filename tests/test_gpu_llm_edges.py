@@ -101,6 +101,15 @@ def test_attention_over_a_table_without_pages(ops, n):
     assert not bool(out.any()) and bool((lse == -math.inf).all())
 
 
+def test_attention_of_sequences_that_share_their_row_of_pages(ops):
+    rng = np.random.default_rng(21)
+    c, table = O.paged(rng, [100], 16, 1, 64)
+    gpu = ops.KVCache(*[torch.from_numpy(t).cuda() for t in (c.k, c.v, c.k_scale, c.v_scale)])
+    pages, lens, q = torch.from_numpy(table).cuda(), ints(100, 100, 100), torch.from_numpy(rng.normal(size=(3, 2, 64))).half().cuda()
+    want = ops.kv_attention(gpu, pages.repeat(3, 1), lens, q)
+    assert torch.equal(ops.kv_attention(gpu, pages.expand(3, -1), lens, q), want)
+
+
 # ------------------------------------------------------------------------------ rows that share memory
 @pytest.mark.parametrize("rows", ["expanded", "windows"])
 def test_rows_that_share_memory(ops, rows):
