@@ -52,8 +52,9 @@ Plan plan(const fxpq_kv_cache& c, const fxpq_kv_batch& b, int q_heads) {
     p.ws_join = p.tile ? (attend_tile_workspace(b.n_tokens, q_heads, c.dim, p.shares) + 255) / 256 * 256 : 0;
     // Expanding costs five bytes of traffic a code and saves every block of 256 rows its own; the room is for max_pages.
     // Both ways measured (us, expanded and not; 65536 rows in all, 8 key heads of 128, groups of 4, causal, 4096 tokens and
-    // the new ones): with 1024 rows a key head 1092 and 910, 2048 1013 and 999, 4096 980 and 1040, 8192 1027 and 1128; heads
-    // of 64 845 and 817, 805 and 840, 806 and 868, 868 and 949.
+    // the new ones): with 1024 rows a key head 1057 and 908, 2048 941 and 925, 4096 903 and 963, 8192 945 and 1051; heads
+    // of 64 881 and 804, 839 and 822, 844 and 857, 905 and 940.  Without tokens before, 2048 rows 235 and 231, 4096 267 and 271;
+    // behind 12288 2378 and 2332, 2216 and 2365.
     const size_t room = p.tile ? attend_expand_workspace(b.n_seqs, c.heads, c.dim, tokens) : 0;
     p.expand = p.tile && mean > EXPAND_ROWS && tokens > 0 && room <= EXPAND_ROOM && b.n_seqs <= 65535 && c.heads <= 65535 && tokens <= INT32_MAX - 128;
     p.ws = p.ws_stream + p.ws_join + (p.expand ? room : 0);

@@ -6,8 +6,8 @@
 // log2(value scale of the key's block), a key's weight in the value sum is 2^t times its value's integer code, and in
 // the normaliser 2^t / (value scale).  So the block's scales cost one fused multiply-add per score, and
 // w = 2^(t - m + 7) is rounded to fp16 once.  m follows the running maximum only when t passes m + 8: sums are rescaled a
-// few times per row instead of per tile.  w <= 2^15 is within fp16, whose last step of 2^-24 is then at most 2^-31 of the row's
-// largest weight: with w = 2^(t - m) it was 2^-24 of it, and over 2^20 keys what small weights add was rounded away.  The
+// few times per row instead of per tile.  w <= 2^15 is within fp16, and rounding to fp16's last step of 2^-24 costs at most
+// 2^-31 of the row's largest weight: with w = 2^(t - m) it was 2^-24, and over 2^20 keys what small weights add was lost.  The
 // normaliser sums the weights as they are before they are rounded, in fp32.
 #include <cfloat>
 

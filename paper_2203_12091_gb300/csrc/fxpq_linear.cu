@@ -14,7 +14,7 @@ namespace {
 // One block per row: the row stays in registers as it came (QT_KEEP steps of 8 values per thread; longer rows are read
 // again, from L2) between the maximum and the codes.  Bytes bound it, so what counts is rows in flight: magnitudes are
 // compared as bits, with infinities and NaN sorted out only where one is found, and codes are rounded by adding 1.5 * 2^23.
-// Rows of more than 8192 values take 1024 threads: 64 rows of 25088 5.2 us with 256, 3.9 with 1024.
+// Rows of more than 8192 values take 1024 threads: 64 rows of 25088 4.2 us with 256, 3.1 with 1024.
 constexpr int QT_KEEP = 4;
 
 template <typename T>
@@ -137,7 +137,7 @@ struct LinArgs {
 };
 
 // ------------------------------------------------------------------ few tokens
-// y^T = w x^T on tcgen05 (kind::f16: the 8-bit kind does not exist on sm_103a; products of codes are exact in fp16): 128
+// y^T = w x^T on tcgen05 (kind::f16: the 8-bit kind does not exist on sm_103a; codes are exact in fp16, their products in fp32): 128
 // output channels on the accumulator's lanes, up to 128 tokens on its columns.  The weights are the traffic.  They
 // arrive as codes (TMA, 128 x 128 bytes a block) and go through registers into tensor memory as the fp16 A operand,
 // so that their shared-memory traffic stays at two bytes a code.  The tokens' rows come as fp16 codes (HALF: written so by the
