@@ -68,10 +68,12 @@ class Decoder:
 
     def generate(self, prompts, count):
         """The `count` likeliest next tokens, one after the other, of each prompt (lists of tokens): int64 [B, count]."""
-        dev = self.embed.device
+        dev, vocab = self.embed.device, self.embed.shape[0]
+        if not 1 <= len(prompts) <= self.pages.shape[0] or count < 1 or any(not 1 <= len(p) <= self.max_tokens - count for p in prompts):
+            raise ValueError("generate: no sequence or too many, an empty prompt, no token wanted, or more tokens than max_tokens")
+        if any(not 0 <= t < vocab for p in prompts for t in p):
+            raise ValueError(f"generate: tokens are 0 to {vocab - 1}")
         sizes = torch.tensor([len(p) for p in prompts], dtype=torch.int32)
-        if int(sizes.min()) < 1 or int(sizes.max()) + count > self.max_tokens or len(prompts) > self.pages.shape[0]:
-            raise ValueError("generate: too many sequences, an empty prompt, or more tokens than max_tokens")
         starts = torch.cat([torch.zeros(1, dtype=torch.int32), sizes.cumsum(0).int()]).to(dev)
         lens = sizes.to(dev)
         logits = self.forward(torch.tensor([t for p in prompts for t in p], device=dev), lens, starts)
