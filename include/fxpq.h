@@ -607,6 +607,8 @@ FXPQ_API fxpq_status fxpq_kv_values(const fxpq_kv_cache* cache, const int32_t* d
  * their row's largest, if that is 2^-111 or more), codes are exact, products sum in fp32.  A key's part of the value sum, its probability times
  * its block's value scale, is rounded to fp16, to 2^-11 of itself or 2^-31 of the row's largest part, whichever is more; the
  * normaliser sums probabilities before that rounding, in fp32.
+ * Value scales: from 2^-96 to 2^96, those of one sequence within 2^96 of one another (fxpq_kv_append's are 2^-40 to 2^32), so
+ * that every part of the normaliser is within fp32.
  * Workspace: fxpq_kv_attention_workspace bytes, 256-byte aligned, scratch; for batches of more than 2048 rows (new tokens x
  * grouped heads) per key head it holds their codes as fp16 too, where that takes at most 1 GiB. */
 FXPQ_API size_t fxpq_kv_attention_workspace(const fxpq_kv_cache* cache, const fxpq_kv_batch* batch, int32_t q_heads);
