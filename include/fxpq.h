@@ -538,6 +538,69 @@ FXPQ_API fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64_t
                                         const float* d_sw, const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type,
                                         void* d_y, int64_t y_stride, void* d_ws, size_t ws_bytes, void* stream);
 
+/* A layer with 8-bit weights and what stands around its product:
+ *   n(x) = x, or with d_norm  x * weight * (1 / sqrt(mean(x^2) + eps))     (mean over the K values of a row)
+ *   z[m, n] = (sum_k codes(n(x))[m, k] w[n, k]) * sx[m] * d_sw[n] + d_bias[n]
+ *   y[m, n] = act(z[m, n]) + residual[m, n]                                 (N values a row)
+ *   y[m, j] = act(z[m, 2 j]) * z[m, 2 j + 1]        with `gated`            (N / 2 values a row)
+ * Codes and scales are fxpq_quantize_tokens' of the rows; with d_norm those of the products x * weight in fp32 (a product past fp32
+ * counts as non-finite), the scale then times 1 / sqrt(mean + eps), so that no normalised row is rounded on the way; non-finite x count
+ * as 0 in the mean.  Activations are computed in fp32: GELU is z Phi(z), GELU_TANH z / (1 + exp(-2 u)), u = sqrt(2 / pi) (z + 0.044715 z^3).
+ * Everything after the sum is in fp32, with one rounding to y_type.
+ * Rows of x, w, y: as for fxpq_linear_tokens.  residual: rows of N values of y_type, residual_stride elements apart; it may be y itself.
+ * Not with `gated`, which needs an activation and an even N: weight rows 2 j and 2 j + 1 are gate and value of y's column j.
+ * For a gradient (fxpq_layer_gradient): d_pre, contiguous [M][N] of pre_type, gets the sums before any scale (F32: as they are; F16: times
+ * 2^-p, p by K alone such that the largest possible sum fits: they are integers, so every one keeps 11 bits), d_sx the rows' scales.
+ * Either may be NULL.  eps: 0 to 1.  Workspace: fxpq_layer_workspace bytes, 256-byte aligned, scratch. */
+typedef enum { FXPQ_ACT_NONE = 0, FXPQ_ACT_RELU = 1, FXPQ_ACT_SILU = 2, FXPQ_ACT_GELU = 3, FXPQ_ACT_GELU_TANH = 4 } fxpq_activation;
+typedef struct {
+    const void* d_x;
+    int64_t x_stride;
+    const float* d_norm;    /* K weights, or NULL: no norm */
+    const int8_t* d_w;
+    int64_t w_stride;
+    const float* d_sw;
+    const float* d_bias;    /* or NULL */
+    const void* d_residual; /* or NULL */
+    int64_t residual_stride;
+    void* d_y;
+    int64_t y_stride;
+    void* d_pre;            /* or NULL */
+    float* d_sx;            /* or NULL */
+    int64_t M;
+    int32_t N, K, x_type, y_type, activation, gated, pre_type;
+    float eps;
+} fxpq_layer;
+FXPQ_API size_t fxpq_layer_workspace(const fxpq_layer* layer);
+FXPQ_API fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, size_t ws_bytes, void* stream);
+
+/* The gradient of such a layer (without norm) to its rows; its weights are constants and the rounding of rows to codes counts as the
+ * identity:
+ *   dz[m, n] = dy[m, n] act'(z[m, n]);   gated: dz[m, 2 j] = dy[m, j] z[m, 2 j + 1] act'(z[m, 2 j]), dz[m, 2 j + 1] = dy[m, j] act(z[m, 2 j])
+ *   dx[m, k] = sum_n dz[m, n] d_sw[n] w[n, k]
+ * d_dy: rows of N (gated: N / 2) values of y_type; d_pre, pre_type, d_sx: what fxpq_layer_forward left (not read without activation);
+ * d_wt: the weights' codes transposed, [K][N], 16-byte aligned rows a multiple of 16 bytes apart; d_dx: rows of K values of dx_type.
+ * A row's dz * sw is rounded to fp16 with a power of two of its own (to 2^-11 of each value, or 2^-39 of the row's largest), for dx of F32 to
+ * 21 bits below the row's largest in two parts; products are exact, sums fp32.  ReLU's derivative at 0 is 0.  A row with a
+ * non-finite dz * sw gives NaN and latches FXPQ_ERR_NONFINITE.
+ * Workspace: fxpq_layer_gradient_workspace bytes, 256-byte aligned, scratch. */
+typedef struct {
+    const void* d_dy;
+    int64_t dy_stride;
+    const void* d_pre;
+    const float* d_sx;
+    const float* d_sw;
+    const float* d_bias;
+    const int8_t* d_wt;
+    int64_t wt_stride;
+    void* d_dx;
+    int64_t dx_stride;
+    int64_t M;
+    int32_t N, K, y_type, dx_type, activation, gated, pre_type, reserved;
+} fxpq_layer_grad;
+FXPQ_API size_t fxpq_layer_gradient_workspace(const fxpq_layer_grad* grad);
+FXPQ_API fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_ws, size_t ws_bytes, void* stream);
+
 /* A paged cache of keys and values: int8 codes [n_pages][heads][page][dim] each (16-byte aligned), value =
  * code * scale with one fp32 scale > 0 for each block, a page of one head: [n_pages][heads].  page is 16,
  * 32, 64 or 128 tokens; dim is 64 or 128. */

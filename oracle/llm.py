@@ -152,3 +152,62 @@ def rope_tables(n, rot):
 
 def default_scale(dim):
     return 1.0 / math.sqrt(dim)
+
+
+# ------------------------------------------------------------------------------ layers: norm, activation, gate, residual, gradient
+def norm_codes(x, weight, eps):
+    """Rows under a norm -> (codes int8, scales in 64 bits): the codes are those of x * weight in fp32."""
+    x = np.asarray(x, dtype=f32)
+    with np.errstate(over="ignore", invalid="ignore"):
+        v = (x * weight.astype(f32)).astype(f32)
+    codes, scale = quantize_tokens(np.where(np.isfinite(x), v, f32(np.inf)))
+    square = np.where(np.isfinite(x), x, 0).astype(np.float64) ** 2
+    mean = square.sum(1) / max(x.shape[1], 1) + eps
+    return codes, np.where(mean > 0, scale / np.sqrt(np.where(mean > 0, mean, 1)), 0.0)
+
+
+_erf = np.vectorize(math.erf, otypes=[np.float64])
+_erfc = np.vectorize(math.erfc, otypes=[np.float64])
+
+
+def activation(z, name):
+    """(act(z), act'(z)) in 64 bits."""
+    z = np.asarray(z, dtype=np.float64)
+    if name is None:
+        return z, np.ones_like(z)
+    if name == "relu":
+        return np.maximum(z, 0), (z > 0).astype(np.float64)
+    if name == "gelu":
+        p = 0.5 * _erfc(-z / math.sqrt(2))
+        return z * p, p + z * np.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    v, dv = (z, np.ones_like(z)) if name == "silu" else (2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3),
+                                                        2 * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * z * z))
+    with np.errstate(over="ignore"):
+        p, q = 1 / (1 + np.exp(-v)), 1 / (1 + np.exp(v))
+    return z * p, p + z * p * q * dv
+
+
+def layer_sums(codes, w):
+    """(codes . w^T, sum of |products|), exact integers in 64 bits."""
+    c, ww = codes.astype(np.float64), w.astype(np.float64)
+    return c @ ww.T, np.abs(c) @ np.abs(ww).T
+
+
+def layer(z, act, residual=None):
+    """y of z [M, N]."""
+    return activation(z, act)[0] + (0 if residual is None else np.asarray(residual, dtype=np.float64))
+
+
+def gated(z, act):
+    """y of z [M, 2 N], gates and values in turn."""
+    return activation(z[:, ::2], act)[0] * z[:, 1::2]
+
+
+def layer_slopes(z, dy, act, is_gated):
+    """dz of dy."""
+    if not is_gated:
+        return dy * activation(z, act)[1]
+    f, slope = activation(z[:, ::2], act)
+    dz = np.empty_like(z)
+    dz[:, ::2], dz[:, 1::2] = dy * z[:, 1::2] * slope, dy * f
+    return dz

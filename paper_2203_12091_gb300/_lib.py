@@ -70,6 +70,20 @@ class Net(ctypes.Structure):
                 ("fmt_in", Fmt), ("ops", ctypes.POINTER(OpDesc))]
 
 
+class LayerDesc(ctypes.Structure):
+    _fields_ = [("d_x", VP), ("x_stride", I64), ("d_norm", VP), ("d_w", VP), ("w_stride", I64), ("d_sw", VP), ("d_bias", VP),
+                ("d_residual", VP), ("residual_stride", I64), ("d_y", VP), ("y_stride", I64), ("d_pre", VP), ("d_sx", VP), ("M", I64),
+                ("N", I32), ("K", I32), ("x_type", I32), ("y_type", I32), ("activation", I32), ("gated", I32), ("pre_type", I32),
+                ("eps", ctypes.c_float)]
+
+
+class LayerGradDesc(ctypes.Structure):
+    _fields_ = [("d_dy", VP), ("dy_stride", I64), ("d_pre", VP), ("d_sx", VP), ("d_sw", VP), ("d_bias", VP), ("d_wt", VP),
+                ("wt_stride", I64), ("d_dx", VP), ("dx_stride", I64), ("M", I64),
+                ("N", I32), ("K", I32), ("y_type", I32), ("dx_type", I32), ("activation", I32), ("gated", I32), ("pre_type", I32),
+                ("reserved", I32)]
+
+
 class KVCacheDesc(ctypes.Structure):
     _fields_ = [("d_k", VP), ("d_v", VP), ("d_k_scale", VP), ("d_v_scale", VP),
                 ("n_pages", I32), ("page", I32), ("heads", I32), ("dim", I32)]
@@ -91,6 +105,7 @@ SCORE_L2, SCORE_L1 = 0, 1
 OUT_CODES, OUT_ACC64, OUT_F32 = range(3)
 QB_ROWS_F16, QB_FLAT_I32 = range(2)
 FT_F32, FT_F16, FT_BF16 = range(3)
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
 OP_CONV, OP_MAXPOOL, OP_ELTWISE, OP_AVGPOOL = range(4)
 
 _SIGS = {
@@ -139,6 +154,10 @@ _SIGS = {
     "fxpq_linear_i8": (I32, [VP, I64, VP, VP, I64, VP, VP, I64, I32, I32, I32, VP, I64, VP, SZ, VP]),
     "fxpq_linear_tokens_workspace": (SZ, [I64, I32, I32]),
     "fxpq_linear_tokens": (I32, [VP, I32, I64, VP, I64, VP, VP, I64, I32, I32, I32, VP, I64, VP, SZ, VP]),
+    "fxpq_layer_workspace": (SZ, [VP]),
+    "fxpq_layer_forward": (I32, [VP, VP, SZ, VP]),
+    "fxpq_layer_gradient_workspace": (SZ, [VP]),
+    "fxpq_layer_gradient": (I32, [VP, VP, SZ, VP]),
     "fxpq_kv_append": (I32, [VP, VP, I32, VP, VP, VP, I32, VP, VP, VP, I32, I32, I32, VP]),
     "fxpq_kv_values": (I32, [VP, VP, I32, I32, VP, VP, VP]),
     "fxpq_kv_attention_workspace": (SZ, [VP, VP, I32]),

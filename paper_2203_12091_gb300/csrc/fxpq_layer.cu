@@ -1,0 +1,359 @@
+// fxpq_layer.cu -- layers with 8-bit weights and what stands around their products: a norm before, activation, gate and residual
+// after, and the gradient to their rows.
+#include <cfloat>
+#include <type_traits>
+
+#include "fxpq_layer.cuh"
+
+namespace fxpq {
+namespace llm {
+namespace {
+
+// ------------------------------------------------------------------ rows under a norm, to codes
+// f = x * weight; the codes of f are those of f / rms, only the scale sees the root mean square.
+template <typename T>
+__global__ void __launch_bounds__(256) norm_codes_kernel(const T* __restrict__ x, const float* __restrict__ norm, float eps, int K, long long x_stride,
+                                                         __half* __restrict__ codes, long long pitch, float* __restrict__ scale, int* status) {
+    pdl_wait();
+    const T* row = x + (long long)blockIdx.x * x_stride;
+    __half* out = codes + (long long)blockIdx.x * pitch;
+    __shared__ float part[3][8];
+    __shared__ int any_bad;
+    const int t = threadIdx.x;
+    if (t == 0) any_bad = 0;
+    float top = 0.0f, far = 0.0f, sum = 0.0f;
+    bool bad = false;
+    auto value = [&](int k, float& v) {  // f, and x as v; 0 where either is not finite
+        v = to_f32(row[k]);
+        const float f = __fmul_rn(v, __ldg(norm + k));
+        const bool fine = fabsf(f) <= FLT_MAX && fabsf(v) <= FLT_MAX;
+        bad |= !fine;
+        if (!(fabsf(v) <= FLT_MAX)) v = 0.0f;
+        return fine ? f : 0.0f;
+    };
+    for (int k = t; k < K; k += 256) {
+        float v;
+        top = fmaxf(top, fabsf(value(k, v)));
+        far = fmaxf(far, fabsf(v));
+        sum = fmaf(v, v, sum);
+    }
+    auto join = [&](float v, int slot, bool add) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            const float w = __shfl_xor_sync(0xffffffffu, v, o);
+            v = add ? v + w : fmaxf(v, w);
+        }
+        if ((t & 31) == 0) part[slot][t >> 5] = v;
+        __syncthreads();
+        v = part[slot][0];
+        for (int w = 1; w < 8; ++w) v = add ? v + part[slot][w] : fmaxf(v, part[slot][w]);
+        __syncthreads();
+        return v;
+    };
+    if (bad) any_bad = 1;
+    top = join(top, 0, false), far = join(far, 1, false), sum = join(sum, 2, true);
+    if (t == 0 && any_bad) latch_status(status, FXPQ_ERR_NONFINITE);
+    float unit = 1.0f;  // squares of very large or small rows leave fp32: they are taken in units of a power of two
+    if (far > 1.0e15f || (far < 1.0e-15f && far > 0.0f)) {
+        unit = exp2f((float)max(ilogbf(far), -60));
+        sum = 0.0f;
+        for (int k = t; k < K; k += 256) {
+            float v;
+            value(k, v);
+            v *= 1.0f / unit;
+            sum = fmaf(v, v, sum);
+        }
+        sum = join(sum, 2, true);
+    }
+    const float iu = 1.0f / unit, mean = fmaf(eps * iu, iu, sum / (float)K);
+    const bool live = top >= 7.888609052210118e-31f && mean > 0.0f;  // 2^-100
+    const float inv = live ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f;
+    if (t == 0) scale[blockIdx.x] = live ? __fmul_rn(top, 1.0f / 127.0f) * iu * __frsqrt_rn(mean) : 0.0f;
+    for (int k = t; k < (int)pitch; k += 256) {
+        float v;
+        out[k] = k < K ? __float2half_rn(rintf(__fmul_rn(value(k, v), inv))) : __float2half_rn(0.0f);
+    }
+}
+
+// ------------------------------------------------------------------ after the product
+struct Rest {
+    const float *sx, *sw, *bias;
+    const void* res;
+    long long res_stride;
+    void* y;
+    long long ys;
+    void* pre;
+    float pre_scale;
+    int pre_f32, act, gated;
+};
+
+template <typename Y>
+__global__ void __launch_bounds__(256) rest_kernel(const float* __restrict__ sums, long long M, int N, Rest R) {
+    pdl_wait();
+    const int wide = R.gated ? N / 2 : N;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < M * wide; i += (long long)gridDim.x * 256) {
+        const long long m = i / wide;
+        const int j = (int)(i - m * wide);
+        const float sx = __ldg(R.sx + m);
+        auto z = [&](int n) {
+            const float a = sums[m * N + n];
+            if (R.pre) {
+                if (R.pre_f32)
+                    static_cast<float*>(R.pre)[m * N + n] = a;
+                else
+                    static_cast<__half*>(R.pre)[m * N + n] = __float2half_rn(a * R.pre_scale);
+            }
+            return fmaf(a * sx, __ldg(R.sw + n), R.bias ? __ldg(R.bias + n) : 0.0f);
+        };
+        float v;
+        if (R.gated) {
+            const float g = z(2 * j), u = z(2 * j + 1);
+            v = activate(g, R.act) * u;
+        } else {
+            v = activate(z(j), R.act);
+            if (R.res) v += to_f32(static_cast<const Y*>(R.res)[m * R.res_stride + j]);
+        }
+        static_cast<Y*>(R.y)[m * R.ys + j] = from_f32<Y>(v);
+    }
+}
+
+// ------------------------------------------------------------------ rows of the gradient
+struct GradRows {
+    const void* dy;
+    long long dy_stride;
+    const void* pre;
+    const float *sx, *sw, *bias;
+    float pre_unit;
+    int pre_f32, act, gated, N;
+    __half* rows;
+    long long pitch, M;
+    float* scale;
+    int* status;
+};
+
+// dz * sw of one row, as fp16 with a power of two of the row's own; SPLIT: in two parts of 11 bits each, integers, the lower ones M rows
+// further on.
+template <typename Y, bool SPLIT>
+__global__ void __launch_bounds__(256) grad_rows_kernel(GradRows G) {
+    pdl_wait();
+    const long long m = blockIdx.x;
+    const int t = threadIdx.x, N = G.N;
+    const Y* dy = static_cast<const Y*>(G.dy) + m * G.dy_stride;
+    const bool needs = G.gated || G.act != FXPQ_ACT_NONE;
+    const float sx = needs ? __ldg(G.sx + m) : 0.0f;
+    auto z = [&](int n) {
+        const float a = G.pre_f32 ? static_cast<const float*>(G.pre)[m * N + n] : __half2float(static_cast<const __half*>(G.pre)[m * N + n]) * G.pre_unit;
+        return fmaf(a * sx, __ldg(G.sw + n), G.bias ? __ldg(G.bias + n) : 0.0f);
+    };
+    auto pair = [&](int i, float& a, float& b) {  // channels 2 i, 2 i + 1
+        const int n = 2 * i;
+        float slope;
+        if (G.gated) {
+            const float f = activate_slope(z(n), G.act, slope), d = to_f32(dy[i]);
+            a = d * z(n + 1) * slope, b = d * f;
+        } else {
+            a = to_f32(dy[n]), b = n + 1 < N ? to_f32(dy[n + 1]) : 0.0f;
+            if (needs) {
+                activate_slope(z(n), G.act, slope);
+                a *= slope;
+                if (n + 1 < N) {
+                    activate_slope(z(n + 1), G.act, slope);
+                    b *= slope;
+                }
+            }
+        }
+        a *= __ldg(G.sw + n);
+        b = n + 1 < N ? b * __ldg(G.sw + n + 1) : 0.0f;
+    };
+    __shared__ uint32_t part[8];
+    const int pairs = (N + 1) / 2;
+    uint32_t top = 0;
+    for (int i = t; i < pairs; i += 256) {
+        float a, b;
+        pair(i, a, b);
+        top = max(top, max(__float_as_uint(a) & 0x7fffffffu, __float_as_uint(b) & 0x7fffffffu));
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if ((t & 31) == 0) part[t >> 5] = top;
+    __syncthreads();
+    for (int w = 0; w < 8; ++w) top = max(top, part[w]);
+    const bool bad = top >= 0x7f800000u;
+    if (bad && t == 0) latch_status(G.status, FXPQ_ERR_NONFINITE);
+    // top < 2^e; the rows' largest value lies in [2^14, 2^15), or as an integer in [2^20, 2^21)
+    const int e = max(top ? ilogbf(__uint_as_float(top)) + 1 : 0, -100);
+    constexpr int UP = SPLIT ? 21 : 15;
+    const float lift = bad || top == 0 ? 0.0f : ldexpf(1.0f, UP - e);
+    if (t == 0) G.scale[m] = bad ? __int_as_float(0x7fffffff) : ldexpf(1.0f, e - UP);
+    __half2* hi = reinterpret_cast<__half2*>(G.rows + m * G.pitch);
+    __half2* lo = reinterpret_cast<__half2*>(G.rows + (G.M + m) * G.pitch);
+    for (int i = t; i < G.pitch / 2; i += 256) {
+        float a = 0.0f, b = 0.0f;
+        if (i < pairs && lift != 0.0f) pair(i, a, b);
+        a *= lift, b *= lift;
+        if (SPLIT) {
+            const float ha = rintf(a * (1.0f / 2048.0f)), hb = rintf(b * (1.0f / 2048.0f));
+            hi[i] = __floats2half2_rn(ha, hb);
+            lo[i] = __floats2half2_rn(rintf(fmaf(ha, -2048.0f, a)), rintf(fmaf(hb, -2048.0f, b)));
+        } else {
+            hi[i] = __floats2half2_rn(a, b);
+        }
+    }
+}
+
+// dx = (2048 high sums + low sums) * scale
+__global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ sums, const float* __restrict__ scale, long long M, int K,
+                                                         float* __restrict__ dx, long long dx_stride) {
+    pdl_wait();
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < M * K; i += (long long)gridDim.x * 256) {
+        const long long m = i / K;
+        dx[m * dx_stride + (i - m * K)] = fmaf(sums[i], 2048.0f, sums[M * K + i]) * __ldg(scale + m);
+    }
+}
+
+unsigned blocks_of(long long n) {
+    const long long b = (n + 255) / 256, most = 64LL * num_sms();
+    return (unsigned)(b < most ? b : most);
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Strides and alignment of rows of n values of `type`.
+bool rows_fit(const void* p, int type, int64_t M, int64_t n, int64_t stride) {
+    return p && aligned(p, ftype_bytes(type)) && (M <= 1 || stride >= n);
+}
+
+struct LayerSpace {
+    size_t codes, scale, sums, end;
+    explicit LayerSpace(const fxpq_layer& d) {
+        codes = up256((size_t)d.M * half_pitch(d.K) * 2);
+        scale = codes + up256((size_t)d.M * 4);
+        sums = scale;
+        end = sums + up256((size_t)d.M * d.N * 4);
+    }
+};
+bool sizes_ok(int64_t M, int32_t N, int32_t K) { return M >= 0 && N >= 0 && K >= 0 && M <= INT32_MAX; }
+
+struct GradSpace {
+    size_t rows, scale, sums, end;
+    explicit GradSpace(const fxpq_layer_grad& d) {
+        const int parts = d.dx_type == FXPQ_FT_F32 ? 2 : 1;
+        rows = up256((size_t)parts * d.M * half_pitch(d.N) * 2);
+        scale = rows + up256((size_t)d.M * 4);
+        sums = scale;
+        end = sums + (parts == 2 ? up256((size_t)parts * d.M * d.K * 4) : 0);
+    }
+};
+
+template <typename T>
+void launch_norm(const fxpq_layer& d, __half* codes, float* scale, cudaStream_t st) {
+    launch_pdl(norm_codes_kernel<T>, dim3((unsigned)d.M), dim3(256), 0, st, static_cast<const T*>(d.d_x), d.d_norm, d.eps, d.K, (long long)d.x_stride, codes,
+               (long long)half_pitch(d.K), scale, status_ptr());
+}
+
+template <typename F>
+void by_type(int type, F&& f) {
+    if (type == FXPQ_FT_F32)
+        f(float());
+    else if (type == FXPQ_FT_F16)
+        f(__half());
+    else
+        f(__nv_bfloat16());
+}
+
+}  // namespace
+}  // namespace llm
+}  // namespace fxpq
+
+using namespace fxpq;
+using namespace fxpq::llm;
+
+extern "C" size_t fxpq_layer_workspace(const fxpq_layer* d) {
+    if (!d || !sizes_ok(d->M, d->N, d->K) || d->M == 0 || d->N == 0) return 0;
+    return LayerSpace(*d).end;
+}
+
+extern "C" fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, size_t ws_bytes, void* stream) {
+    if (!layer) return FXPQ_ERR_INVALID_ARG;
+    const fxpq_layer& d = *layer;
+    if (!sizes_ok(d.M, d.N, d.K) || !ftype_ok(d.x_type) || !ftype_ok(d.y_type) || !act_ok(d.activation) || d.gated < 0 || d.gated > 1 ||
+        !(d.eps >= 0.0f && d.eps <= 1.0f) || (d.pre_type != FXPQ_FT_F16 && d.pre_type != FXPQ_FT_F32))
+        return FXPQ_ERR_INVALID_ARG;
+    if (d.gated && (d.N % 2 || d.activation == FXPQ_ACT_NONE || d.d_residual)) return FXPQ_ERR_INVALID_ARG;
+    if (d.M == 0 || d.N == 0) return FXPQ_OK;
+    const int wide = d.gated ? d.N / 2 : d.N;
+    if ((d.K > 0 && (!rows_fit(d.d_x, d.x_type, d.M, d.K, d.x_stride) || !d.d_w || !aligned(d.d_w, 16) || d.w_stride % 16 || d.w_stride < d.K)) ||
+        !d.d_sw || !aligned(d.d_sw, 4) || !aligned(d.d_bias, 4) || !aligned(d.d_norm, 4) || !aligned(d.d_sx, 4) ||
+        !rows_fit(d.d_y, d.y_type, d.M, wide, d.y_stride) || (d.d_residual && !rows_fit(d.d_residual, d.y_type, d.M, d.N, d.residual_stride)) ||
+        !aligned(d.d_pre, ftype_bytes(d.pre_type)))
+        return FXPQ_ERR_INVALID_ARG;
+    const LayerSpace at(d);
+    if (!d_ws || ws_bytes < at.end || !aligned(d_ws, 256)) return FXPQ_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(d_ws);
+    cudaStream_t st = as_stream(stream);
+    __half* codes = reinterpret_cast<__half*>(ws);
+    float* scale = d.d_sx ? d.d_sx : reinterpret_cast<float*>(ws + at.codes);
+    float* sums = reinterpret_cast<float*>(ws + at.sums);
+    fxpq_status rc;
+    if (d.d_norm) {
+        by_type(d.x_type, [&](auto t) { launch_norm<decltype(t)>(d, codes, scale, st); });
+        rc = after_launch("norm_codes");
+    } else {
+        rc = half_codes(d.d_x, d.x_type, d.M, d.K, d.x_stride, codes, scale, st);
+    }
+    if (rc != FXPQ_OK) return rc;
+    rc = half_product(codes, nullptr, d.d_w, d.w_stride, nullptr, nullptr, d.M, d.N, d.K, FXPQ_FT_F32, sums, d.N, st);
+    if (rc != FXPQ_OK) return rc;
+    Rest R = {scale, d.d_sw, d.d_bias, d.d_residual, d.residual_stride, d.d_y, d.y_stride, d.d_pre, 1.0f / (float)(1LL << sum_shift(d.K)),
+              d.pre_type == FXPQ_FT_F32, d.activation, d.gated};
+    by_type(d.y_type, [&](auto t) {
+        launch_pdl(rest_kernel<decltype(t)>, dim3(blocks_of(d.M * wide)), dim3(256), 0, st, static_cast<const float*>(sums), (long long)d.M, (int)d.N, R);
+    });
+    return after_launch("layer_rest");
+}
+
+extern "C" size_t fxpq_layer_gradient_workspace(const fxpq_layer_grad* d) {
+    if (!d || !sizes_ok(d->M, d->N, d->K) || d->M == 0 || d->K == 0 || d->M > INT32_MAX / 2) return 0;
+    return GradSpace(*d).end;
+}
+
+extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_ws, size_t ws_bytes, void* stream) {
+    if (!grad) return FXPQ_ERR_INVALID_ARG;
+    const fxpq_layer_grad& d = *grad;
+    if (!sizes_ok(d.M, d.N, d.K) || d.M > INT32_MAX / 2 || !ftype_ok(d.y_type) || !ftype_ok(d.dx_type) || !act_ok(d.activation) || d.gated < 0 ||
+        d.gated > 1 || (d.pre_type != FXPQ_FT_F16 && d.pre_type != FXPQ_FT_F32))
+        return FXPQ_ERR_INVALID_ARG;
+    if (d.gated && (d.N % 2 || d.activation == FXPQ_ACT_NONE)) return FXPQ_ERR_INVALID_ARG;
+    if (d.M == 0 || d.K == 0) return FXPQ_OK;
+    const int wide = d.gated ? d.N / 2 : d.N;
+    if (!rows_fit(d.d_dx, d.dx_type, d.M, d.K, d.dx_stride) ||
+        (d.N > 0 && (!rows_fit(d.d_dy, d.y_type, d.M, wide, d.dy_stride) || !d.d_sw || !aligned(d.d_sw, 4) || !aligned(d.d_bias, 4) || !d.d_wt ||
+                     !aligned(d.d_wt, 16) || d.wt_stride % 16 || d.wt_stride < d.N)))
+        return FXPQ_ERR_INVALID_ARG;
+    if (d.N > 0 && d.activation != FXPQ_ACT_NONE && (!d.d_pre || !d.d_sx || !aligned(d.d_pre, ftype_bytes(d.pre_type)) || !aligned(d.d_sx, 4)))
+        return FXPQ_ERR_INVALID_ARG;
+    const GradSpace at(d);
+    if (!d_ws || ws_bytes < at.end || !aligned(d_ws, 256)) return FXPQ_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(d_ws);
+    cudaStream_t st = as_stream(stream);
+    __half* rows = reinterpret_cast<__half*>(ws);
+    float* scale = reinterpret_cast<float*>(ws + at.rows);
+    float* sums = reinterpret_cast<float*>(ws + at.sums);
+    const bool split = d.dx_type == FXPQ_FT_F32;
+    GradRows G = {d.d_dy, d.dy_stride, d.d_pre, d.d_sx, d.d_sw, d.d_bias, (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32,
+                  d.activation, d.gated, d.N, rows, (long long)half_pitch(d.N), (long long)d.M, scale, status_ptr()};
+    by_type(d.y_type, [&](auto t) {
+        using Y = decltype(t);
+        if (split)
+            launch_pdl(grad_rows_kernel<Y, true>, dim3((unsigned)d.M), dim3(256), 0, st, G);
+        else
+            launch_pdl(grad_rows_kernel<Y, false>, dim3((unsigned)d.M), dim3(256), 0, st, G);
+    });
+    fxpq_status rc = after_launch("layer_grad_rows");
+    if (rc != FXPQ_OK) return rc;
+    if (!split) return half_product(rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride, st);
+    rc = half_product(rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K, st);
+    if (rc != FXPQ_OK) return rc;
+    launch_pdl(join_parts_kernel, dim3(blocks_of(d.M * d.K)), dim3(256), 0, st, static_cast<const float*>(sums), static_cast<const float*>(scale), (long long)d.M,
+               (int)d.K, static_cast<float*>(d.d_dx), (long long)d.dx_stride);
+    return after_launch("layer_join_parts");
+}

@@ -125,7 +125,7 @@ struct LinArgs {
     // weights' codes as [N][K] bytes in boxes of 128 codes x 128 rows (tw), or x the rows that the last tile has (tw2: a box is
     // slow where it lies outside the tensor); tokens' as [M][K] bytes in boxes of 128 x `rows`, or as fp16 in 64 x `rows`
     CUtensorMap tw, tw2, tx;
-    const float *sx, *sw, *bias;
+    const float *sx, *sw, *bias;  // null: ones, ones, zeros
     void* y;
     long long ys, M;
     int N, y_type, n_kb;
@@ -306,10 +306,10 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
     const int mine = (int)min((long long)P.rows, P.M - m0), c_lo = mine * rank / shares, c_hi = mine * (rank + 1) / shares;
     const int ch = n0 + 4 * lane;
     constexpr int TOKENS = LS_THREADS / 32;
-    float sw[4], bias[4], sx = c_lo + warp < c_hi ? __ldg(P.sx + m0 + c_lo + warp) : 0.0f;
+    float sw[4], bias[4], sx = !P.sx ? 1.0f : c_lo + warp < c_hi ? __ldg(P.sx + m0 + c_lo + warp) : 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {  // (on their way while the CTAs meet)
-        sw[e] = ch + e < P.N ? __ldg(P.sw + ch + e) : 0.0f;
+        sw[e] = !P.sw ? 1.0f : ch + e < P.N ? __ldg(P.sw + ch + e) : 0.0f;
         bias[e] = P.bias && ch + e < P.N ? __ldg(P.bias + ch + e) : 0.0f;
     }
     if (shares > 1) cluster_sync();
@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
         for (int r = 0; r < 8; ++r)
             if (r < shares) b[r] = ld_cluster_f4(cluster_addr(at, r));
         const float s = sx;
-        if (c + TOKENS < c_hi) sx = __ldg(P.sx + m0 + c + TOKENS);
+        if (P.sx && c + TOKENS < c_hi) sx = __ldg(P.sx + m0 + c + TOKENS);
 #pragma unroll
         for (int r = 0; r < 8; ++r)
             if (r < shares) a.x += b[r].x, a.y += b[r].y, a.z += b[r].z, a.w += b[r].w;
@@ -549,8 +549,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
             tile_of(P, t, tn, tm);
             const int ch = tn * 256 + rank * 128 + quad * 32 + lane;
             const long long m0 = (long long)tm * NT + ROWS * half;
-            const float sw = ch < P.N ? __ldg(P.sw + ch) : 0.0f, bias = P.bias && ch < P.N ? __ldg(P.bias + ch) : 0.0f;
-            for (int i = lane; i < ROWS; i += 32) sxs[i] = m0 + i < P.M ? __ldg(P.sx + m0 + i) : 0.0f;
+            const float sw = !P.sw ? 1.0f : ch < P.N ? __ldg(P.sw + ch) : 0.0f, bias = P.bias && ch < P.N ? __ldg(P.bias + ch) : 0.0f;
+            for (int i = lane; i < ROWS; i += 32) sxs[i] = !P.sx ? 1.0f : m0 + i < P.M ? __ldg(P.sx + m0 + i) : 0.0f;
             __syncwarp();
             if (!wait_warp_cluster(acc_full, it & 1, abort, P.status)) break;
             tc_fence_after();
@@ -881,3 +881,18 @@ extern "C" fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64
     if (many_tokens(M, N, K)) return product_many(half, pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, st);
     return product_few(nullptr, half, (int64_t)pitch, scale, d_w, w_stride, d_sw, d_bias, M, N, K, y_type, d_y, y_stride, st);
 }
+
+namespace fxpq {
+namespace llm {
+size_t half_pitch(int32_t K) { return codes_pitch(K); }
+fxpq_status half_codes(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, __half* codes, float* scale, cudaStream_t st) {
+    return quantize_rows(d_x, x_type, M, K, x_stride, codes, (int64_t)codes_pitch(K), scale, st);
+}
+fxpq_status half_product(const __half* rows, const float* sx, const int8_t* d_w, int64_t w_stride, const float* sw, const float* bias, int64_t M,
+                         int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st) {
+    const size_t pitch = codes_pitch(K);
+    if (many_tokens(M, N, K)) return product_many(rows, pitch, sx, d_w, w_stride, sw, bias, M, N, K, y_type, d_y, y_stride, st);
+    return product_few(nullptr, rows, (int64_t)pitch, sx, d_w, w_stride, sw, bias, M, N, K, y_type, d_y, y_stride, st);
+}
+}  // namespace llm
+}  // namespace fxpq

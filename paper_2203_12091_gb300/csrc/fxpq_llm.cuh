@@ -120,5 +120,12 @@ __device__ __forceinline__ int find_seq(const Seqs& s, long long x, int mul, int
 bool batch_ok(const fxpq_kv_batch* b);
 bool cache_ok(const fxpq_kv_cache* c);
 
+// Rows as fp16 in memory, half_pitch(K) apart, 256-byte aligned, zeros behind K: 8-bit codes of float rows (half_codes), and the product
+// of such rows with 8-bit weights, y = (rows . w^T) * sx * sw + bias (null: ones, ones, zeros; fxpq_linear.cu).
+size_t half_pitch(int32_t K);
+fxpq_status half_codes(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, __half* codes, float* scale, cudaStream_t st);
+fxpq_status half_product(const __half* rows, const float* sx, const int8_t* d_w, int64_t w_stride, const float* sw, const float* bias, int64_t M,
+                         int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st);
+
 }  // namespace llm
 }  // namespace fxpq

@@ -354,6 +354,22 @@ def fxpq_linear_tokens(x, x_type: int, x_stride: int, w, w_stride: int, sw, bias
                                                              y_type, _p(y), y_stride, _p(ws), ws.nbytes, _s(stream)))
 
 
+def fxpq_layer_workspace(layer: L.LayerDesc) -> int:
+    return L.lib().fxpq_layer_workspace(ctypes.byref(layer))
+
+
+def fxpq_layer_forward(layer: L.LayerDesc, ws, stream=None):
+    L.check("fxpq_layer_forward", L.lib().fxpq_layer_forward(ctypes.byref(layer), _p(ws), ws.nbytes, _s(stream)))
+
+
+def fxpq_layer_gradient_workspace(grad: L.LayerGradDesc) -> int:
+    return L.lib().fxpq_layer_gradient_workspace(ctypes.byref(grad))
+
+
+def fxpq_layer_gradient(grad: L.LayerGradDesc, ws, stream=None):
+    L.check("fxpq_layer_gradient", L.lib().fxpq_layer_gradient(ctypes.byref(grad), _p(ws), ws.nbytes, _s(stream)))
+
+
 def fxpq_kv_append(cache: L.KVCacheDesc, batch: L.KVBatchDesc, ftype: int, k: L.KVRows, v: L.KVRows, q, q_heads: int,
                    q_out, cos, sin, n_positions: int, rot: int, interleaved: int, stream=None):
     L.check("fxpq_kv_append", L.lib().fxpq_kv_append(

@@ -8,7 +8,8 @@ page ids outside the cache, positions past the rotation tables) is latched and r
 ``fxpq.fxpq_get_device_status``.
 
 The operators are for inference and have no gradient: tensors that require one are refused while gradients are
-recorded (RuntimeError).
+recorded (RuntimeError).  Layers are the exception once `with_gradient` was called: then gradients reach their rows through
+the frozen weights.
 """
 from __future__ import annotations
 
@@ -26,6 +27,9 @@ from . import fxpq as F
 _FT = {torch.float32: L.FT_F32, torch.float16: L.FT_F16, torch.bfloat16: L.FT_BF16}
 _BATCH = struct.Struct("PPPiiiiq").pack  # fxpq_kv_batch
 _ROWS = struct.Struct("Pqq").pack        # fxpq_kv_rows
+_LAYER = struct.Struct("PqPPqPPPqPqPPqiiiiiiif").pack      # fxpq_layer
+_LAYER_GRAD = struct.Struct("PqPPPPPqPqqiiiiiiii").pack    # fxpq_layer_grad
+_ACTS = {None: L.ACT_NONE, "relu": L.ACT_RELU, "silu": L.ACT_SILU, "gelu": L.ACT_GELU, "gelu_tanh": L.ACT_GELU_TANH}
 _empty, _i8, _i32, _u8, _f32 = torch.empty, torch.int8, torch.int32, torch.uint8, torch.float32
 
 
@@ -114,18 +118,137 @@ def _pitch(t, K):  # (a single row, or rows of nothing, may have any stride)
     return t.stride(0) if t.shape[0] > 1 and K else (K + 15) // 16 * 16
 
 
-class Linear8:
+def _whole_rows(w):
+    """w int8 [N, K] with rows that begin at 16-byte boundaries."""
+    N, K = w.shape
+    if K % 16 == 0 and w.is_contiguous() and w.data_ptr() % 16 == 0:
+        return w
+    padded = torch.zeros((N, (K + 15) // 16 * 16), dtype=_i8, device=w.device)
+    padded[:, :K] = w
+    return padded[:, :K]
+
+
+def _activation(name, activation):
+    act = _ACTS.get(activation) if activation is None or isinstance(activation, str) else None
+    if act is None:
+        raise ValueError(f"{name}: activation {activation!r} is none of {', '.join(str(a) for a in _ACTS)}")
+    return act
+
+
+class _Layer8:
+    """What layers with 8-bit weights share: w [N, K] codes, w_scale [N], bias [N] or None, and after `with_gradient` wt, the codes
+    transposed."""
+
+    wt = None
+    gated = 0
+
+    def with_gradient(self):
+        """Lays out the transposed weights (one more byte for each) that a gradient is formed with, and returns the layer: from
+        now on, rows (and residuals) that require a gradient get one.  The weights stay constants, and the rounding of rows to
+        codes counts as the identity."""
+        if self.wt is None:
+            self.wt = _whole_rows(self.w.t())
+        return self
+
+    def _forward(self, name, x, dtype, norm, eps, act, residual, keep):
+        """y, and with keep the sums and scales that `_gradient` reads."""
+        rows = _float_rows(name, x)
+        M, K = rows.shape
+        N = self.w.shape[0]
+        if K != self.w.shape[1]:
+            raise ValueError(f"{name}: rows of {self.w.shape[1]} values are needed, got {tuple(x.shape)}")
+        wide = N // 2 if self.gated else N
+        xt, yt, dev = _ftype(name, x.dtype), _ftype(name, dtype), x.device
+        nrm = res = res_stride = pre_at = sx_at = 0
+        if norm is not None:
+            _want(name + ": norm", norm, _f32, 1)
+            if norm.shape[0] != K:
+                raise ValueError(f"{name}: one norm weight for each of {K} inputs is needed")
+            nrm = norm.data_ptr()
+            if not 0.0 <= eps <= 1.0:
+                raise ValueError(f"{name}: eps is 0 to 1, got {eps}")
+        if residual is not None:
+            if residual.dtype != dtype or residual.shape != x.shape[:-1] + (N,):
+                raise ValueError(f"{name}: a residual {(*x.shape[:-1], N)} of {dtype} is needed, got {tuple(residual.shape)} of {residual.dtype}")
+            r = _float_rows(name + ": residual", residual)
+            res, res_stride = r.data_ptr(), r.stride(0)
+        y = _empty((M, wide), dtype=dtype, device=dev)
+        pre = sx = None
+        pre_t = L.FT_F32 if xt == L.FT_F32 or yt == L.FT_F32 else L.FT_F16
+        if keep and act:
+            pre = _empty((M, N), dtype=_f32 if pre_t == L.FT_F32 else torch.float16, device=dev)
+            sx = _empty(M, dtype=_f32, device=dev)
+            pre_at, sx_at = pre.data_ptr(), sx.data_ptr()
+        w = self.w
+        desc = _LAYER(rows.data_ptr(), rows.stride(0), nrm, w.data_ptr(), _pitch(w, K), self.w_scale.data_ptr(),
+                      0 if self.bias is None else self.bias.data_ptr(), res, res_stride, y.data_ptr(), wide, pre_at, sx_at,
+                      M, N, K, xt, yt, act, self.gated, pre_t, eps)
+        lib = L.lib()
+        ws = _empty(lib.fxpq_layer_workspace(desc), dtype=_u8, device=dev)
+        rc = lib.fxpq_layer_forward(desc, ws.data_ptr(), ws.nbytes, F._s(None))
+        if rc:
+            L.check(name, rc)
+        if x.dim() != 2:
+            y = y.view(*x.shape[:-1], wide)
+        return (y, pre, sx) if keep else y
+
+    def _gradient(self, name, dy, dtype, act, pre, sx):
+        """dx [..., K] of `dtype` for dy [..., N or N / 2] and what `_forward` kept."""
+        rows = _float_rows(name, dy)
+        M, (N, K), wt = rows.shape[0], self.w.shape, self.wt
+        dx = _empty((M, K), dtype=dtype, device=dy.device)
+        xt, yt = _ftype(name, dtype), _ftype(name, dy.dtype)
+        desc = _LAYER_GRAD(rows.data_ptr(), rows.stride(0), 0 if pre is None else pre.data_ptr(), 0 if sx is None else sx.data_ptr(),
+                           self.w_scale.data_ptr(), 0 if self.bias is None else self.bias.data_ptr(), wt.data_ptr(), _pitch(wt, N),
+                           dx.data_ptr(), K, M, N, K, yt, xt, act, self.gated,
+                           L.FT_F32 if xt == L.FT_F32 or yt == L.FT_F32 else L.FT_F16, 0)
+        lib = L.lib()
+        ws = _empty(lib.fxpq_layer_gradient_workspace(desc), dtype=_u8, device=dy.device)
+        rc = lib.fxpq_layer_gradient(desc, ws.data_ptr(), ws.nbytes, F._s(None))
+        if rc:
+            L.check(name, rc)
+        return dx if dy.dim() == 2 else dx.view(*dy.shape[:-1], K)
+
+    def _call(self, name, x, dtype, norm, eps, act, residual):
+        """The forward pass, recorded where rows or residual require a gradient."""
+        if torch.is_grad_enabled() and (x.requires_grad or (residual is not None and residual.requires_grad)):
+            if self.wt is None:
+                _no_grad(name + " without with_gradient()", x, residual)
+            if norm is not None:
+                raise RuntimeError(f"{name}: norm has no gradient: apply it before the layer, or call it under torch.no_grad()")
+            return _LayerStep.apply(x, residual, self, name, dtype, act)
+        if norm is not None and norm.requires_grad:
+            _no_grad(name + ": norm", norm)
+        return self._forward(name, x, dtype, norm, eps, act, residual, False)
+
+
+class _LayerStep(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, layer, name, dtype, act):
+        keep = ctx.needs_input_grad[0]
+        y = layer._forward(name, x, dtype, None, 0.0, act, residual, keep)
+        ctx.layer, ctx.name, ctx.act, ctx.dtype = layer, name, act, x.dtype
+        if keep:
+            y, pre, sx = y
+            ctx.save_for_backward(pre, sx)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dx = None
+        if ctx.needs_input_grad[0]:
+            dx = ctx.layer._gradient(ctx.name, dy, ctx.dtype, ctx.act, *ctx.saved_tensors)
+        return dx, dy if ctx.needs_input_grad[1] else None, None, None, None, None
+
+
+class Linear8(_Layer8):
     """A layer with 8-bit weights w int8 [N, K], one scale for each output channel: rows that are not whole 16 bytes
     are padded once.  Its tensors are constants: what they require of a gradient is dropped."""
 
     def __init__(self, w, w_scale, bias=None):
         _want("Linear8: w", w, _i8, 2)
-        N, K = w.shape
-        if K % 16 or w.data_ptr() % 16:
-            padded = torch.zeros((N, (K + 15) // 16 * 16), dtype=_i8, device=w.device)
-            padded[:, :K] = w
-            w = padded[:, :K]
-        self._set(w, w_scale, bias)
+        self._set(_whole_rows(w), w_scale, bias)
 
     def _set(self, w, w_scale, bias):
         self.N, self.K = w.shape
@@ -139,9 +262,13 @@ class Linear8:
         layer._set(*quantize_tokens(w.detach()), None if bias is None else bias.detach().float().contiguous())
         return layer
 
-    def __call__(self, x, out_dtype=None):
+    def __call__(self, x, out_dtype=None, norm=None, eps=1e-5, activation=None, residual=None):
         """x [..., K] in a float type -> [..., N] in out_dtype (x's own by default): `quantize_tokens` and `linear_i8`
-        as one call."""
+        as one call, with what stands around them: norm, float32 [K], turns x into x / sqrt(mean(x^2) + eps) * norm before, and
+        y = activation(z) + residual after, all in fp32 with one rounding.  activation: "relu", "silu", "gelu" (z times the normal
+        distribution's integral), "gelu_tanh" (its tanh form); residual: [..., N] of out_dtype."""
+        if norm is not None or activation is not None or residual is not None or (self.wt is not None and x.requires_grad):
+            return self._call("Linear8", x, out_dtype or x.dtype, norm, eps, _activation("Linear8", activation), residual)
         if x.requires_grad:
             _no_grad("Linear8", x)
         rows = _float_rows("Linear8", x)
@@ -159,6 +286,39 @@ class Linear8:
         if rc:
             L.check("fxpq_linear_tokens", rc)
         return y if x.dim() == 2 else y.view(*x.shape[:-1], N)
+
+
+class GatedLinear8(_Layer8):
+    """Two layers of the same rows whose results are multiplied, as one product: activation(gate(x)) * up(x).  gate and up are int8
+    [N, K] with one scale for each output channel, and may have biases; their rows are laid out alternately, once.  activation:
+    as in `Linear8`, one is needed.  Its tensors are constants: what they require of a gradient is dropped."""
+
+    gated = 1
+
+    def __init__(self, gate, gate_scale, up, up_scale, gate_bias=None, up_bias=None, activation="silu"):
+        self.act = _activation("GatedLinear8", activation)
+        if not self.act:
+            raise ValueError("GatedLinear8: an activation is needed")
+        for side, w, scale, bias in (("gate", gate, gate_scale, gate_bias), ("up", up, up_scale, up_bias)):
+            if w.dim() != 2 or w.shape != gate.shape or w.device != gate.device:
+                raise ValueError("GatedLinear8: gate and up must have one shape [N, K]")
+            _check_layer(f"GatedLinear8: {side}", w, scale, bias, gate.shape[1])
+        if (gate_bias is None) != (up_bias is None):
+            raise ValueError("GatedLinear8: gate_bias and up_bias go together")
+        self.N, self.K = gate.shape
+        self.w = _whole_rows(torch.stack((gate, up), 1).flatten(0, 1))
+        self.w_scale = torch.stack((gate_scale.detach(), up_scale.detach()), 1).flatten()
+        self.bias = None if gate_bias is None else torch.stack((gate_bias.detach(), up_bias.detach()), 1).flatten()
+
+    @classmethod
+    def from_float(cls, gate, up, gate_bias=None, up_bias=None, activation="silu"):
+        """Quantizes float weights [N, K]."""
+        biases = [None if b is None else b.detach().float().contiguous() for b in (gate_bias, up_bias)]
+        return cls(*quantize_tokens(gate.detach()), *quantize_tokens(up.detach()), *biases, activation)
+
+    def __call__(self, x, out_dtype=None, norm=None, eps=1e-5):
+        """x [..., K] in a float type -> [..., N] in out_dtype (x's own by default); norm and eps: as in `Linear8`."""
+        return self._call("GatedLinear8", x, out_dtype or x.dtype, norm, eps, self.act, None)
 
 
 class KVCache:
