@@ -3,7 +3,7 @@
 #include <cfloat>
 #include <type_traits>
 
-#include "fxpq_layer.cuh"
+#include "fxpq_linear.cuh"
 
 namespace fxpq {
 namespace llm {
@@ -75,48 +75,6 @@ __global__ void __launch_bounds__(256) norm_codes_kernel(const T* __restrict__ x
     }
 }
 
-// ------------------------------------------------------------------ after the product
-struct Rest {
-    const float *sx, *sw, *bias;
-    const void* res;
-    long long res_stride;
-    void* y;
-    long long ys;
-    void* pre;
-    float pre_scale;
-    int pre_f32, act, gated;
-};
-
-template <typename Y>
-__global__ void __launch_bounds__(256) rest_kernel(const float* __restrict__ sums, long long M, int N, Rest R) {
-    pdl_wait();
-    const int wide = R.gated ? N / 2 : N;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < M * wide; i += (long long)gridDim.x * 256) {
-        const long long m = i / wide;
-        const int j = (int)(i - m * wide);
-        const float sx = __ldg(R.sx + m);
-        auto z = [&](int n) {
-            const float a = sums[m * N + n];
-            if (R.pre) {
-                if (R.pre_f32)
-                    static_cast<float*>(R.pre)[m * N + n] = a;
-                else
-                    static_cast<__half*>(R.pre)[m * N + n] = __float2half_rn(a * R.pre_scale);
-            }
-            return fmaf(a * sx, __ldg(R.sw + n), R.bias ? __ldg(R.bias + n) : 0.0f);
-        };
-        float v;
-        if (R.gated) {
-            const float g = z(2 * j), u = z(2 * j + 1);
-            v = activate(g, R.act) * u;
-        } else {
-            v = activate(z(j), R.act);
-            if (R.res) v += to_f32(static_cast<const Y*>(R.res)[m * R.res_stride + j]);
-        }
-        static_cast<Y*>(R.y)[m * R.ys + j] = from_f32<Y>(v);
-    }
-}
-
 // ------------------------------------------------------------------ rows of the gradient
 struct GradRows {
     const void* dy;
@@ -131,8 +89,8 @@ struct GradRows {
     int* status;
 };
 
-// dz * sw of one row, as fp16 with a power of two of the row's own; SPLIT: in two parts of 11 bits each, integers, the lower ones M rows
-// further on.
+// dz * sw of one row, as fp16 with a power of two of the row's own; SPLIT: in two parts, integers up to 2^11 (exact in
+// fp16, as are their products' sums below 2^24), the lower ones M rows further on.
 template <typename Y, bool SPLIT>
 __global__ void __launch_bounds__(256) grad_rows_kernel(GradRows G) {
     pdl_wait();
@@ -179,9 +137,9 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(GradRows G) {
     for (int w = 0; w < 8; ++w) top = max(top, part[w]);
     const bool bad = top >= 0x7f800000u;
     if (bad && t == 0) latch_status(G.status, FXPQ_ERR_NONFINITE);
-    // top < 2^e; the rows' largest value lies in [2^14, 2^15), or as an integer in [2^20, 2^21)
+    // top < 2^e; the row's largest value lies in [2^14, 2^15), or as an integer in [2^22, 2^23)
     const int e = max(top ? ilogbf(__uint_as_float(top)) + 1 : 0, -100);
-    constexpr int UP = SPLIT ? 21 : 15;
+    constexpr int UP = SPLIT ? 23 : 15;
     const float lift = bad || top == 0 ? 0.0f : ldexpf(1.0f, UP - e);
     if (t == 0) G.scale[m] = bad ? __int_as_float(0x7fffffff) : ldexpf(1.0f, e - UP);
     __half2* hi = reinterpret_cast<__half2*>(G.rows + m * G.pitch);
@@ -191,22 +149,22 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(GradRows G) {
         if (i < pairs && lift != 0.0f) pair(i, a, b);
         a *= lift, b *= lift;
         if (SPLIT) {
-            const float ha = rintf(a * (1.0f / 2048.0f)), hb = rintf(b * (1.0f / 2048.0f));
+            const float ha = rintf(a * (1.0f / 4096.0f)), hb = rintf(b * (1.0f / 4096.0f));
             hi[i] = __floats2half2_rn(ha, hb);
-            lo[i] = __floats2half2_rn(rintf(fmaf(ha, -2048.0f, a)), rintf(fmaf(hb, -2048.0f, b)));
+            lo[i] = __floats2half2_rn(rintf(fmaf(ha, -4096.0f, a)), rintf(fmaf(hb, -4096.0f, b)));
         } else {
             hi[i] = __floats2half2_rn(a, b);
         }
     }
 }
 
-// dx = (2048 high sums + low sums) * scale
+// dx = (4096 high sums + low sums) * scale
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ sums, const float* __restrict__ scale, long long M, int K,
                                                          float* __restrict__ dx, long long dx_stride) {
     pdl_wait();
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < M * K; i += (long long)gridDim.x * 256) {
         const long long m = i / K;
-        dx[m * dx_stride + (i - m * K)] = fmaf(sums[i], 2048.0f, sums[M * K + i]) * __ldg(scale + m);
+        dx[m * dx_stride + (i - m * K)] = fmaf(sums[i], 4096.0f, sums[M * K + i]) * __ldg(scale + m);
     }
 }
 
@@ -223,12 +181,10 @@ bool rows_fit(const void* p, int type, int64_t M, int64_t n, int64_t stride) {
 }
 
 struct LayerSpace {
-    size_t codes, scale, sums, end;
+    size_t codes, end;
     explicit LayerSpace(const fxpq_layer& d) {
         codes = up256((size_t)d.M * half_pitch(d.K) * 2);
-        scale = codes + up256((size_t)d.M * 4);
-        sums = scale;
-        end = sums + up256((size_t)d.M * d.N * 4);
+        end = codes + up256((size_t)d.M * 4);
     }
 };
 bool sizes_ok(int64_t M, int32_t N, int32_t K) { return M >= 0 && N >= 0 && K >= 0 && M <= INT32_MAX; }
@@ -248,6 +204,14 @@ template <typename T>
 void launch_norm(const fxpq_layer& d, __half* codes, float* scale, cudaStream_t st) {
     launch_pdl(norm_codes_kernel<T>, dim3((unsigned)d.M), dim3(256), 0, st, static_cast<const T*>(d.d_x), d.d_norm, d.eps, d.K, (long long)d.x_stride, codes,
                (long long)half_pitch(d.K), scale, status_ptr());
+}
+
+template <int EPI>
+fxpq_status layer_product(const fxpq_layer& d, const __half* codes, const float* scale, const Epi& e, cudaStream_t st) {
+    const int64_t pitch = (int64_t)half_pitch(d.K);
+    if (many_tokens(d.M, d.N, d.K))
+        return product_many<EPI>(codes, (size_t)pitch, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e);
+    return product_few<EPI>(nullptr, codes, pitch, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e);
 }
 
 template <typename F>
@@ -292,7 +256,6 @@ extern "C" fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, s
     cudaStream_t st = as_stream(stream);
     __half* codes = reinterpret_cast<__half*>(ws);
     float* scale = d.d_sx ? d.d_sx : reinterpret_cast<float*>(ws + at.codes);
-    float* sums = reinterpret_cast<float*>(ws + at.sums);
     fxpq_status rc;
     if (d.d_norm) {
         by_type(d.x_type, [&](auto t) { launch_norm<decltype(t)>(d, codes, scale, st); });
@@ -301,14 +264,8 @@ extern "C" fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, s
         rc = half_codes(d.d_x, d.x_type, d.M, d.K, d.x_stride, codes, scale, st);
     }
     if (rc != FXPQ_OK) return rc;
-    rc = half_product(codes, nullptr, d.d_w, d.w_stride, nullptr, nullptr, d.M, d.N, d.K, FXPQ_FT_F32, sums, d.N, st);
-    if (rc != FXPQ_OK) return rc;
-    Rest R = {scale, d.d_sw, d.d_bias, d.d_residual, d.residual_stride, d.d_y, d.y_stride, d.d_pre, 1.0f / (float)(1LL << sum_shift(d.K)),
-              d.pre_type == FXPQ_FT_F32, d.activation, d.gated};
-    by_type(d.y_type, [&](auto t) {
-        launch_pdl(rest_kernel<decltype(t)>, dim3(blocks_of(d.M * wide)), dim3(256), 0, st, static_cast<const float*>(sums), (long long)d.M, (int)d.N, R);
-    });
-    return after_launch("layer_rest");
+    Epi e = {d.d_residual, d.residual_stride, d.d_pre, 1.0f / (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32, d.activation};
+    return d.gated ? layer_product<GATED>(d, codes, scale, e, st) : layer_product<LAYER>(d, codes, scale, e, st);
 }
 
 extern "C" size_t fxpq_layer_gradient_workspace(const fxpq_layer_grad* d) {
