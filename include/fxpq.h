@@ -546,12 +546,12 @@ FXPQ_API fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64_t
  * Codes and scales are fxpq_quantize_tokens' of the rows; with d_norm those of the products x * weight in fp32 (a product past fp32
  * counts as non-finite), the scale then times 1 / sqrt(mean + eps), so that no normalised row is rounded on the way; non-finite x count
  * as 0 in the mean.  Activations are computed in fp32: GELU is z Phi(z), GELU_TANH z / (1 + exp(-2 u)), u = sqrt(2 / pi) (z + 0.044715 z^3).
- * Everything after the sum is in fp32, with one rounding to y_type.
+ * Everything after the sum is in fp32, in the order written (a sum * sx past fp32 is infinite), with one rounding to y_type.
  * Rows of x, w, y: as for fxpq_linear_tokens.  residual: rows of N values of y_type, residual_stride elements apart; it may be y itself.
  * Not with `gated`, which needs an activation and an even N: weight rows 2 j and 2 j + 1 are gate and value of y's column j.
  * For a gradient (fxpq_layer_gradient): d_pre, contiguous [M][N] of pre_type, gets the sums before any scale (F32: as they are; F16: times
  * 2^-p, p by K alone such that the largest possible sum fits: they are integers, so every one keeps 11 bits), d_sx the rows' scales.
- * Either may be NULL.  eps: 0 to 1.  Workspace: fxpq_layer_workspace bytes, 256-byte aligned, scratch. */
+ * Either may be NULL.  eps: 0 to 1.  Workspace: fxpq_layer_workspace bytes, 256-byte aligned, scratch (it may be 0: then d_ws may be NULL). */
 typedef enum { FXPQ_ACT_NONE = 0, FXPQ_ACT_RELU = 1, FXPQ_ACT_SILU = 2, FXPQ_ACT_GELU = 3, FXPQ_ACT_GELU_TANH = 4 } fxpq_activation;
 typedef struct {
     const void* d_x;

@@ -25,6 +25,10 @@ fxpq_status after_launch(const char* what);
 // 1041 against 966, its waiting blocks taking places and shared-memory splits that the running kernel uses.)
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// Lets the next kernel of the chain be set up from now on (small kernels only, whose blocks leave room for it).  Called after pdl_wait(),
+// so what ran before this kernel is complete for the next one even before its own pdl_wait().
+__device__ __forceinline__ void pdl_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 template <typename... P, typename... A>
 inline void launch_pdl(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
     cudaLaunchAttribute at;

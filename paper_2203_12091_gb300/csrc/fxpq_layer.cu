@@ -9,72 +9,6 @@ namespace fxpq {
 namespace llm {
 namespace {
 
-// ------------------------------------------------------------------ rows under a norm, to codes
-// f = x * weight; the codes of f are those of f / rms, only the scale sees the root mean square.
-template <typename T>
-__global__ void __launch_bounds__(256) norm_codes_kernel(const T* __restrict__ x, const float* __restrict__ norm, float eps, int K, long long x_stride,
-                                                         __half* __restrict__ codes, long long pitch, float* __restrict__ scale, int* status) {
-    pdl_wait();
-    const T* row = x + (long long)blockIdx.x * x_stride;
-    __half* out = codes + (long long)blockIdx.x * pitch;
-    __shared__ float part[3][8];
-    __shared__ int any_bad;
-    const int t = threadIdx.x;
-    if (t == 0) any_bad = 0;
-    float top = 0.0f, far = 0.0f, sum = 0.0f;
-    bool bad = false;
-    auto value = [&](int k, float& v) {  // f, and x as v; 0 where either is not finite
-        v = to_f32(row[k]);
-        const float f = __fmul_rn(v, __ldg(norm + k));
-        const bool fine = fabsf(f) <= FLT_MAX && fabsf(v) <= FLT_MAX;
-        bad |= !fine;
-        if (!(fabsf(v) <= FLT_MAX)) v = 0.0f;
-        return fine ? f : 0.0f;
-    };
-    for (int k = t; k < K; k += 256) {
-        float v;
-        top = fmaxf(top, fabsf(value(k, v)));
-        far = fmaxf(far, fabsf(v));
-        sum = fmaf(v, v, sum);
-    }
-    auto join = [&](float v, int slot, bool add) {
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            const float w = __shfl_xor_sync(0xffffffffu, v, o);
-            v = add ? v + w : fmaxf(v, w);
-        }
-        if ((t & 31) == 0) part[slot][t >> 5] = v;
-        __syncthreads();
-        v = part[slot][0];
-        for (int w = 1; w < 8; ++w) v = add ? v + part[slot][w] : fmaxf(v, part[slot][w]);
-        __syncthreads();
-        return v;
-    };
-    if (bad) any_bad = 1;
-    top = join(top, 0, false), far = join(far, 1, false), sum = join(sum, 2, true);
-    if (t == 0 && any_bad) latch_status(status, FXPQ_ERR_NONFINITE);
-    float unit = 1.0f;  // squares of very large or small rows leave fp32: they are taken in units of a power of two
-    if (far > 1.0e15f || (far < 1.0e-15f && far > 0.0f)) {
-        unit = exp2f((float)max(ilogbf(far), -60));
-        sum = 0.0f;
-        for (int k = t; k < K; k += 256) {
-            float v;
-            value(k, v);
-            v *= 1.0f / unit;
-            sum = fmaf(v, v, sum);
-        }
-        sum = join(sum, 2, true);
-    }
-    const float iu = 1.0f / unit, mean = fmaf(eps * iu, iu, sum / (float)K);
-    const bool live = top >= 7.888609052210118e-31f && mean > 0.0f;  // 2^-100
-    const float inv = live ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f;
-    if (t == 0) scale[blockIdx.x] = live ? __fmul_rn(top, 1.0f / 127.0f) * iu * __frsqrt_rn(mean) : 0.0f;
-    for (int k = t; k < (int)pitch; k += 256) {
-        float v;
-        out[k] = k < K ? __float2half_rn(rintf(__fmul_rn(value(k, v), inv))) : __float2half_rn(0.0f);
-    }
-}
-
 // ------------------------------------------------------------------ rows of the gradient
 struct GradRows {
     const void* dy;
@@ -183,6 +117,8 @@ bool rows_fit(const void* p, int type, int64_t M, int64_t n, int64_t stride) {
 struct LayerSpace {
     size_t codes, end;
     explicit LayerSpace(const fxpq_layer& d) {
+        codes = end = 0;
+        if (float_rows_fit(d.M, d.K)) return;
         codes = up256((size_t)d.M * half_pitch(d.K) * 2);
         end = codes + up256((size_t)d.M * 4);
     }
@@ -200,18 +136,12 @@ struct GradSpace {
     }
 };
 
-template <typename T>
-void launch_norm(const fxpq_layer& d, __half* codes, float* scale, cudaStream_t st) {
-    launch_pdl(norm_codes_kernel<T>, dim3((unsigned)d.M), dim3(256), 0, st, static_cast<const T*>(d.d_x), d.d_norm, d.eps, d.K, (long long)d.x_stride, codes,
-               (long long)half_pitch(d.K), scale, status_ptr());
-}
-
 template <int EPI>
 fxpq_status layer_product(const fxpq_layer& d, const __half* codes, const float* scale, const Epi& e, cudaStream_t st) {
     const int64_t pitch = (int64_t)half_pitch(d.K);
     if (many_tokens(d.M, d.N, d.K))
         return product_many<EPI>(codes, (size_t)pitch, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e);
-    return product_few<EPI>(nullptr, codes, pitch, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e);
+    return product_few<EPI>(nullptr, codes, pitch, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e, nullptr, true);
 }
 
 template <typename F>
@@ -251,20 +181,21 @@ extern "C" fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, s
         !aligned(d.d_pre, ftype_bytes(d.pre_type)))
         return FXPQ_ERR_INVALID_ARG;
     const LayerSpace at(d);
-    if (!d_ws || ws_bytes < at.end || !aligned(d_ws, 256)) return FXPQ_ERR_WORKSPACE;
-    char* ws = static_cast<char*>(d_ws);
+    if (at.end && (!d_ws || ws_bytes < at.end || !aligned(d_ws, 256))) return FXPQ_ERR_WORKSPACE;
     cudaStream_t st = as_stream(stream);
+    const RowNorm norm = {d.d_norm, d.eps, aligned(d.d_norm, 16), !many_tokens(d.M, d.N, d.K)};
+    const Epi e = {d.d_residual, d.residual_stride, d.d_pre, 1.0f / (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32, d.activation};
+    if (at.end == 0) {
+        const int vec = aligned(d.d_x, 16) && d.x_stride * ftype_bytes(d.x_type) % 16 == 0;
+        const FloatRows rows = {d.d_x, d.x_stride, d.x_type, vec, d.K, d.d_sx, norm};
+        const auto product = d.gated ? product_few<GATED> : product_few<LAYER>;
+        return product(nullptr, nullptr, 0, nullptr, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e, &rows, false);
+    }
+    char* ws = static_cast<char*>(d_ws);
     __half* codes = reinterpret_cast<__half*>(ws);
     float* scale = d.d_sx ? d.d_sx : reinterpret_cast<float*>(ws + at.codes);
-    fxpq_status rc;
-    if (d.d_norm) {
-        by_type(d.x_type, [&](auto t) { launch_norm<decltype(t)>(d, codes, scale, st); });
-        rc = after_launch("norm_codes");
-    } else {
-        rc = half_codes(d.d_x, d.x_type, d.M, d.K, d.x_stride, codes, scale, st);
-    }
+    const fxpq_status rc = half_codes(d.d_x, d.x_type, d.M, d.K, d.x_stride, codes, scale, norm, st);
     if (rc != FXPQ_OK) return rc;
-    Epi e = {d.d_residual, d.residual_stride, d.d_pre, 1.0f / (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32, d.activation};
     return d.gated ? layer_product<GATED>(d, codes, scale, e, st) : layer_product<LAYER>(d, codes, scale, e, st);
 }
 

@@ -31,12 +31,14 @@ struct Raw8 {
 };
 
 // C: int8 codes, or fp16 ones for the tensor-core kernels that take them so.
-template <typename T, typename C, int QT_THREADS>
+// NORM: codes of f = x * weight, which are those of f / rms; the root mean square goes into the scale.
+template <typename T, typename C, int QT_THREADS, bool NORM>
 __global__ void __launch_bounds__(QT_THREADS)
     quantize_tokens_kernel(const T* __restrict__ x, int K, long long x_stride, int vec, C* __restrict__ codes, long long c_stride, int c_vec,
-                           float* __restrict__ scale, int* status) {
+                           float* __restrict__ scale, int* status, const __grid_constant__ RowNorm norm) {
     constexpr bool HALF = sizeof(C) == 2;
     pdl_wait();
+    if (norm.early) pdl_next();
     const T* row = x + (long long)blockIdx.x * x_stride;
     C* out = codes + (long long)blockIdx.x * c_stride;
     const int t = threadIdx.x, groups = K / 8, tail = 8 * groups + t;  // whole groups of eight; the rest of the row one value at a time
@@ -55,6 +57,64 @@ __global__ void __launch_bounds__(QT_THREADS)
     for (int s = 0; s < QT_KEEP; ++s)
         if (t + s * QT_THREADS < groups) keep[s].load(row + 8 * (t + s * QT_THREADS), vec);
     __shared__ uint32_t part[QT_THREADS / 32];
+    if constexpr (NORM) {
+        __shared__ float parts[3][QT_THREADS / 32];
+        __shared__ float row_inv;
+        float wt[8];
+        auto weights = [&](int g) { load_f32<8>(norm.weight + 8 * g, norm.vec, wt); };
+        RowStats st;
+        each([&](int g, const Raw8<T>& v) {
+            weights(g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) st.see(to_f32(v.v[e]), wt[e], 1.0f);
+        });
+        if (tail < K) st.see(to_f32(row[tail]), __ldg(norm.weight + tail), 1.0f);
+        const bool bad = __syncthreads_or(st.bad);
+        auto meet = [&]() {  // the block's statistics, in thread 0's warp
+            st.meet();
+            if ((t & 31) == 0) parts[0][t >> 5] = st.top, parts[1][t >> 5] = st.far, parts[2][t >> 5] = st.sum;
+            __syncthreads();
+            if (t < 32) {
+                const bool in = t < QT_THREADS / 32;
+                st.top = in ? parts[0][t] : 0.0f, st.far = in ? parts[1][t] : 0.0f, st.sum = in ? parts[2][t] : 0.0f;
+                st.meet();
+            }
+        };
+        meet();
+        if (t == 0) parts[0][0] = st.unit();
+        __syncthreads();
+        const float unit = parts[0][0];
+        if (unit != 1.0f) {  // (the block agrees)
+            __syncthreads();
+            st = RowStats();
+            each([&](int g, const Raw8<T>& v) {
+                weights(g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) st.see(to_f32(v.v[e]), wt[e], 1.0f / unit);
+            });
+            if (tail < K) st.see(to_f32(row[tail]), __ldg(norm.weight + tail), 1.0f / unit);
+            meet();
+        }
+        if (t == 0) {
+            float inv;
+            scale[blockIdx.x] = st.scale(K, norm.eps, unit, inv);
+            row_inv = inv;
+            if (bad) latch_status(status, FXPQ_ERR_NONFINITE);
+        }
+        __syncthreads();
+        const float inv = row_inv;
+        each([&](int g, const Raw8<T>& v) {
+            weights(g);
+            float c[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = __fmul_rn(RowStats::value(to_f32(v.v[e]), wt[e]), inv);
+            *reinterpret_cast<uint4*>(out + 8 * g) =
+                make_uint4(f32_codes_f16x2(c[0], c[1]), f32_codes_f16x2(c[2], c[3]), f32_codes_f16x2(c[4], c[5]), f32_codes_f16x2(c[6], c[7]));
+        });
+        if (tail < K) out[tail] = (C)(int)rintf(__fmul_rn(RowStats::value(to_f32(row[tail]), __ldg(norm.weight + tail)), inv));
+        for (long long i = K + t; i < c_stride; i += QT_THREADS) out[i] = (C)0;
+        return;
+    }
     auto largest = [&](bool finite) {  // magnitudes as bits
         uint32_t top = 0;
         auto see = [&](float v) {
@@ -135,19 +195,29 @@ using namespace fxpq::llm;
 namespace {
 template <typename C>
 fxpq_status quantize_rows(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, C* d_codes, int64_t codes_stride,
-                          float* d_scale, cudaStream_t st) {
+                          float* d_scale, cudaStream_t st, const RowNorm& norm = {}) {
     const int e = ftype_bytes(x_type), vec = aligned(d_x, 16) && x_stride * e % 16 == 0;
     const int c_vec = aligned(d_codes, 8) && codes_stride % 8 == 0;
     const dim3 grid((unsigned)M);
     int* status = status_ptr();
     auto launch = [&](auto* x) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(x)>>;
-        if (K <= 4096)
-            launch_pdl(quantize_tokens_kernel<T, C, 128>, grid, dim3(128), 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
-        else if (K > 8192)
-            launch_pdl(quantize_tokens_kernel<T, C, 1024>, grid, dim3(1024), 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
-        else
-            launch_pdl(quantize_tokens_kernel<T, C, 256>, grid, dim3(256), 0, st, x, K, x_stride, vec, d_codes, codes_stride, c_vec, d_scale, status);
+        auto go = [&](auto threads, auto normed) {
+            constexpr int THREADS = decltype(threads)::value;
+            launch_pdl(quantize_tokens_kernel<T, C, THREADS, decltype(normed)::value>, grid, dim3(THREADS), 0, st, x, K, x_stride, vec, d_codes,
+                       codes_stride, c_vec, d_scale, status, norm);
+        };
+        auto sized = [&](auto normed) {
+            if (K <= 4096)
+                go(std::integral_constant<int, 128>(), normed);
+            else if (K > 8192)
+                go(std::integral_constant<int, 1024>(), normed);
+            else
+                go(std::integral_constant<int, 256>(), normed);
+        };
+        if constexpr (sizeof(C) == 2)
+            if (norm.weight) return sized(std::true_type());
+        sized(std::false_type());
     };
     if (x_type == FXPQ_FT_F32)
         launch(static_cast<const float*>(d_x));
@@ -246,8 +316,9 @@ extern "C" fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64
 namespace fxpq {
 namespace llm {
 size_t half_pitch(int32_t K) { return codes_pitch(K); }
-fxpq_status half_codes(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, __half* codes, float* scale, cudaStream_t st) {
-    return quantize_rows(d_x, x_type, M, K, x_stride, codes, (int64_t)codes_pitch(K), scale, st);
+fxpq_status half_codes(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, __half* codes, float* scale, const RowNorm& norm,
+                       cudaStream_t st) {
+    return quantize_rows(d_x, x_type, M, K, x_stride, codes, (int64_t)codes_pitch(K), scale, st, norm);
 }
 fxpq_status half_product(const __half* rows, const float* sx, const int8_t* d_w, int64_t w_stride, const float* sw, const float* bias, int64_t M,
                          int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st) {

@@ -184,8 +184,9 @@ class _Layer8:
                       0 if self.bias is None else self.bias.data_ptr(), res, res_stride, y.data_ptr(), wide, pre_at, sx_at,
                       M, N, K, xt, yt, act, self.gated, pre_t, eps)
         lib = L.lib()
-        ws = _empty(lib.fxpq_layer_workspace(desc), dtype=_u8, device=dev)
-        rc = lib.fxpq_layer_forward(desc, ws.data_ptr(), ws.nbytes, F._s(None))
+        need = lib.fxpq_layer_workspace(desc)
+        ws = _empty(need, dtype=_u8, device=dev) if need else None
+        rc = lib.fxpq_layer_forward(desc, ws.data_ptr() if need else None, need, F._s(None))
         if rc:
             L.check(name, rc)
         if x.dim() != 2:

@@ -494,3 +494,30 @@ def test_the_binding(ops):
     assert torch.equal(dx[:, :90], want_dx) and bool((dx[:, 90:] == 3).all())
     with pytest.raises(L.FxpqError):
         F.fxpq_layer_gradient(g, ws[:256])
+
+
+@pytest.mark.parametrize("M", [1, 3, 9, 16, 17, 300])
+@pytest.mark.parametrize("power", [-98, -60, 0, 60, 118])
+def test_rows_far_from_one(ops, M, power):
+    """Rows times a power of two (without a norm, whose eps would show): results times that power, exactly but for float32's end, which
+    the definition's first product, the sum times the row's scale, passes at 2^118: (some 2^17) * (3.5 to 3.9 / 127) * 2^118 > 2^128."""
+    rng = np.random.default_rng(M)
+    x = rows(rng, M, 500, "bf16").float().clamp(-3.9, 3.9)
+    x[:, 0] = 3.5  # (no row's largest value falls below 2^-100)
+    W = Weights(rng, 140, 500, False)
+    layer = W.layer(ops)
+    want = layer(x, activation="relu")
+    got = layer(x * 2.0 ** power, activation="relu")
+    codes, sx = O.quantize_tokens((x * 2.0 ** power).cpu().numpy())
+    past = torch.from_numpy(O.layer_sums(codes, W.w)[0] * sx.astype(np.float64)[:, None] >= 2.0 ** 128 - 2.0 ** 103).cuda()
+    assert power == 118 or not past.any()
+    assert torch.equal(got, torch.where(past, float("inf"), want * 2.0 ** power))
+
+
+@pytest.mark.parametrize("M,K", [(1, 25088), (2, 32768), (3, 20000), (16, 4096), (16, 4095), (9, 7281), (1, 8), (5, 7), (16, 129)])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_rows_whose_codes_the_product_forms(ops, M, K, x):
+    rng = np.random.default_rng(M + K)
+    for N in (130, 512):
+        check_layer(ops, rng, M, N, K, x, "f32", "silu", True, True, True)
+        check_gated(ops, rng, M, N // 2, K, x, "bf16", "silu", True, False)

@@ -123,7 +123,8 @@ def test_layer_refuses(lib, bad):
 
 
 def test_layer_refuses_workspaces(lib):
-    assert run(lib, layer(), work=None) == run(lib, layer(), short=1) == run(lib, layer(), work=4112) == L.ERR_WORKSPACE
+    many = layer(M=40)
+    assert run(lib, many, work=None) == run(lib, many, short=1) == run(lib, many, work=4112) == L.ERR_WORKSPACE
     assert run(lib, layer(M=0)) == run(lib, layer(N=0)) == L.OK
     assert lib.fxpq_layer_forward(None, None, 0, None) == L.ERR_INVALID_ARG and lib.fxpq_layer_workspace(None) == 0
 
