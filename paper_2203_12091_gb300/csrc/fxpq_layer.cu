@@ -3,7 +3,7 @@
 #include <cfloat>
 #include <type_traits>
 
-#include "fxpq_linear.cuh"
+#include "fxpq_layer_few.cuh"
 
 namespace fxpq {
 namespace llm {
@@ -16,7 +16,7 @@ struct GradRows {
     const void* pre;
     const float *sx, *sw, *bias;
     float pre_unit;
-    int pre_f32, act, gated, N;
+    int pre_f32, act, gated, N, early;
     __half* rows;
     long long pitch, M;
     float* scale;
@@ -28,6 +28,7 @@ struct GradRows {
 template <typename Y, bool SPLIT>
 __global__ void __launch_bounds__(256) grad_rows_kernel(GradRows G) {
     pdl_wait();
+    if (G.early) pdl_next();
     const long long m = blockIdx.x;
     const int t = threadIdx.x, N = G.N;
     const Y* dy = static_cast<const Y*>(G.dy) + m * G.dy_stride;
@@ -136,12 +137,24 @@ struct GradSpace {
     }
 };
 
+// y of rows as fp16: what a layer's forward pass and its gradient have in common.
+struct Product {
+    const __half* rows;
+    const float* scale;
+    const int8_t* w;
+    int64_t w_stride;
+    const float *sw, *bias;
+    int64_t M;
+    int32_t N, K, y_type;
+    void* y;
+    int64_t y_stride;
+};
 template <int EPI>
-fxpq_status layer_product(const fxpq_layer& d, const __half* codes, const float* scale, const Epi& e, cudaStream_t st) {
-    const int64_t pitch = (int64_t)half_pitch(d.K);
-    if (many_tokens(d.M, d.N, d.K))
-        return product_many<EPI>(codes, (size_t)pitch, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e);
-    return product_few<EPI>(nullptr, codes, pitch, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e, nullptr, true);
+fxpq_status product(const Product& p, const Epi& e, cudaStream_t st) {
+    const int64_t pitch = (int64_t)half_pitch(p.K);
+    if (many_tokens(p.M, p.N, p.K))
+        return product_many<EPI>(p.rows, (size_t)pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e);
+    return few_product<EPI>(p.rows, pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e, nullptr, true);
 }
 
 template <typename F>
@@ -188,15 +201,16 @@ extern "C" fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, s
     if (at.end == 0) {
         const int vec = aligned(d.d_x, 16) && d.x_stride * ftype_bytes(d.x_type) % 16 == 0;
         const FloatRows rows = {d.d_x, d.x_stride, d.x_type, vec, d.K, d.d_sx, norm};
-        const auto product = d.gated ? product_few<GATED> : product_few<LAYER>;
-        return product(nullptr, nullptr, 0, nullptr, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e, &rows, false);
+        const auto few = d.gated ? few_product<GATED> : few_product<LAYER>;
+        return few(nullptr, 0, nullptr, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride, st, e, &rows, false);
     }
     char* ws = static_cast<char*>(d_ws);
     __half* codes = reinterpret_cast<__half*>(ws);
     float* scale = d.d_sx ? d.d_sx : reinterpret_cast<float*>(ws + at.codes);
     const fxpq_status rc = half_codes(d.d_x, d.x_type, d.M, d.K, d.x_stride, codes, scale, norm, st);
     if (rc != FXPQ_OK) return rc;
-    return d.gated ? layer_product<GATED>(d, codes, scale, e, st) : layer_product<LAYER>(d, codes, scale, e, st);
+    const Product p = {codes, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride};
+    return d.gated ? product<GATED>(p, e, st) : product<LAYER>(p, e, st);
 }
 
 extern "C" size_t fxpq_layer_gradient_workspace(const fxpq_layer_grad* d) {
@@ -228,7 +242,7 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
     float* sums = reinterpret_cast<float*>(ws + at.sums);
     const bool split = d.dx_type == FXPQ_FT_F32;
     GradRows G = {d.d_dy, d.dy_stride, d.d_pre, d.d_sx, d.d_sw, d.d_bias, (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32,
-                  d.activation, d.gated, d.N, rows, (long long)half_pitch(d.N), (long long)d.M, scale, status_ptr()};
+                  d.activation, d.gated, d.N, !many_tokens(split ? 2 * d.M : d.M, d.K, d.N), rows, (long long)half_pitch(d.N), (long long)d.M, scale, status_ptr()};
     by_type(d.y_type, [&](auto t) {
         using Y = decltype(t);
         if (split)
@@ -238,8 +252,8 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
     });
     fxpq_status rc = after_launch("layer_grad_rows");
     if (rc != FXPQ_OK) return rc;
-    if (!split) return half_product(rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride, st);
-    rc = half_product(rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K, st);
+    if (!split) return product<LAYER>({rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride}, {}, st);
+    rc = product<LAYER>({rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K}, {}, st);
     if (rc != FXPQ_OK) return rc;
     launch_pdl(join_parts_kernel, dim3(blocks_of(d.M * d.K)), dim3(256), 0, st, static_cast<const float*>(sums), static_cast<const float*>(scale), (long long)d.M,
                (int)d.K, static_cast<float*>(d.d_dx), (long long)d.dx_stride);

@@ -117,53 +117,79 @@ __device__ __forceinline__ int find_seq(const Seqs& s, long long x, int mul, int
     return lo;
 }
 
-// What codes of a row x under a norm need to know, f = x * weight: the largest |f| and |x|, the sum of x^2.  Where x or f is not finite
-// f counts as 0 (x only if it is not finite itself).
-struct RowStats {
-    float top = 0.0f, far = 0.0f, sum = 0.0f;
-    bool bad = false;
-    static __device__ __forceinline__ float value(float x, float w) {
-        const float f = __fmul_rn(x, w);
-        return fabsf(f) <= 3.402823466e38f && fabsf(x) <= 3.402823466e38f ? f : 0.0f;
-    }
-    __device__ __forceinline__ void see(float x, float w, float per_unit) {
-        const float f = __fmul_rn(x, w);
-        const bool x_fine = fabsf(x) <= 3.402823466e38f, fine = x_fine && fabsf(f) <= 3.402823466e38f;
-        bad |= !fine;
-        top = fmaxf(top, fine ? fabsf(f) : 0.0f);
-        if (!x_fine) x = 0.0f;
-        far = fmaxf(far, fabsf(x));
-        x *= per_unit;
-        sum = fmaf(x, x, sum);
+// What the codes of a row of f = x * weight (f = x without a norm) need to know: the largest |f|, as bits, and with a norm the sum of x^2.
+// NORM's values take four instructions.  Where the bits are those of an inf or NaN, or the sum left the middle of fp32's range,
+// the row is looked at again by careful_row.
+template <bool NORM>
+struct RowScan {
+    uint32_t top = 0;
+    float sum = 0.0f;
+    __device__ __forceinline__ void see(float x, float w) {
+        if constexpr (NORM) sum = fmaf(x, x, sum);
+        top = max(top, __float_as_uint(NORM ? __fmul_rn(x, w) : x) & 0x7fffffffu);
     }
     __device__ __forceinline__ void meet() {  // over a warp
+        top = __reduce_max_sync(0xffffffffu, top);
+        if constexpr (NORM) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            far = fmaxf(far, __shfl_xor_sync(0xffffffffu, far, o));
-            sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         }
     }
-    // Squares of very large or small rows leave fp32: their sum is taken again in units of a power of two (of 2^-60 or more, so that
-    // eps, at most 1, over its square stays within fp32).
-    __device__ __forceinline__ float unit() const {
-        return far > 1.0e15f || (far < 1.0e-15f && far > 0.0f) ? exp2f((float)max(ilogbf(far), -60)) : 1.0f;
-    }
-    __device__ __forceinline__ float inverse() const { return top >= 7.888609052210118e-31f ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f; }
-    // The row's scale, and what f is multiplied with for its code.  Rows whose largest |f| is below 2^-100 are zero
-    // (inv is 1e-36 at least otherwise).
-    __device__ __forceinline__ float scale(int K, float eps, float unit, float& inv) const {
-        const float iu = 1.0f / unit, mean = fmaf(eps * iu, iu, sum / (float)K);
-        inv = mean > 0.0f ? inverse() : 0.0f;
-        return inv != 0.0f ? __fmul_rn(top, 1.0f / 127.0f) * iu * __frsqrt_rn(mean) : 0.0f;
+    __device__ __forceinline__ void join(uint32_t t, float s) { top = max(top, t), sum += s; }
+    __device__ __forceinline__ bool odd() const { return top >= 0x7f800000u || (NORM && top && !(sum > 1.0e-25f && sum < 1.0e30f)); }
+    // What f is multiplied with for its code.  Rows whose largest |f| is below 2^-100 are zero (inv is 1e-37 at least otherwise).
+    static __device__ __forceinline__ float inverse(float top) { return top >= 7.888609052210118e-31f ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f; }
+    __device__ __forceinline__ float inverse() const { return inverse(__uint_as_float(top)); }
+    __device__ __forceinline__ float scale(int K, float eps) const {
+        if (inverse() == 0.0f) return 0.0f;
+        const float s = __fmul_rn(__uint_as_float(top), 1.0f / 127.0f);
+        return NORM ? s * __frsqrt_rn(sum / (float)K + eps) : s;
     }
 };
+// f as a code before rounding: what is not finite counts as 0.
+__device__ __forceinline__ float scaled_code(float f, float inv) {
+    const float c = __fmul_rn(f, inv);
+    return fabsf(c) <= 128.0f ? c : 0.0f;
+}
+// The same numbers for any row, by one warp: values that are not finite do not count (x in the sum only if it is not finite itself), and the
+// squares are taken in units of a power of two (2^-60 or more, so that eps, at most 1, over its square stays within fp32).
+template <typename T>
+__device__ __noinline__ void careful_row(const T* row, int K, const float* weight, float eps, float& inv, float& scale, int* status) {
+    constexpr float FINITE = 3.402823466e38f;
+    float top = 0.0f, far = 0.0f, sum = 0.0f;
+    bool bad = false;
+    const int lane = threadIdx.x & 31;
+    for (int k = lane; k < K; k += 32) {
+        const float x = to_f32(row[k]), f = weight ? __fmul_rn(x, __ldg(weight + k)) : x;
+        const bool x_fine = fabsf(x) <= FINITE, fine = x_fine && fabsf(f) <= FINITE;
+        bad |= !fine;
+        if (fine) top = fmaxf(top, fabsf(f));
+        if (x_fine) far = fmaxf(far, fabsf(x));
+    }
+    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+    far = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(far)));
+    inv = RowScan<true>::inverse(top);
+    scale = inv != 0.0f ? __fmul_rn(top, 1.0f / 127.0f) : 0.0f;
+    if (__any_sync(0xffffffffu, bad) && lane == 0) latch_status(status, FXPQ_ERR_NONFINITE);
+    if (!weight || inv == 0.0f) return;
+    const float iu = 1.0f / exp2f((float)max(far > 0.0f ? ilogbf(far) : 0, -60));
+    for (int k = lane; k < K; k += 32) {
+        const float x = to_f32(row[k]) * iu;
+        if (fabsf(x) <= 2.0f) sum = fmaf(x, x, sum);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float mean = fmaf(eps * iu, iu, sum / (float)K);
+    if (mean > 0.0f)
+        scale *= iu * __frsqrt_rn(mean);
+    else
+        inv = scale = 0.0f;
+}
 
 bool batch_ok(const fxpq_kv_batch* b);
 bool cache_ok(const fxpq_kv_cache* c);
 
-// Rows as fp16 in memory, half_pitch(K) apart, 256-byte aligned, zeros behind K: 8-bit codes of float rows (half_codes), and the product
-// of such rows with 8-bit weights, y = (rows . w^T) * sx * sw + bias (null: ones, ones, zeros; fxpq_linear.cu).
+// Float rows to 8-bit codes as fp16, half_pitch(K) apart, zeros behind K (fxpq_linear.cu), under a norm or not.
 // early: the product may be set up while the codes are formed (pdl_next).
 struct RowNorm {
     const float* weight;  // null: no norm
@@ -173,8 +199,6 @@ struct RowNorm {
 size_t half_pitch(int32_t K);
 fxpq_status half_codes(const void* d_x, int32_t x_type, int64_t M, int32_t K, int64_t x_stride, __half* codes, float* scale, const RowNorm& norm,
                        cudaStream_t st);
-fxpq_status half_product(const __half* rows, const float* sx, const int8_t* d_w, int64_t w_stride, const float* sw, const float* bias, int64_t M,
-                         int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st);
 
 }  // namespace llm
 }  // namespace fxpq
