@@ -1,6 +1,8 @@
 // fxpq_layer.cu -- layers with 8-bit weights and what stands around their products: a norm before, activation, gate and residual
 // after, and the gradient to their rows.
+#include <algorithm>
 #include <cfloat>
+#include <cmath>
 #include <type_traits>
 
 #include "fxpq_layer_few.cuh"
@@ -16,80 +18,142 @@ struct GradRows {
     const void* pre;
     const float *sx, *sw, *bias;
     float pre_unit;
-    int pre_f32, act, gated, N, early;
+    int pre_f32, act, N, early, split;
+    int vec;  // dy, kept sums, scales, biases in aligned accesses (bits 1, 2, 4, 8)
     __half* rows;
     long long pitch, M;
     float* scale;
     int* status;
 };
 
-// dz * sw of one row, as fp16 with a power of two of the row's own; SPLIT: in two parts, integers up to 2^11 (exact in
-// fp16, as are their products' sums below 2^24), the lower ones M rows further on.
-template <typename Y, bool SPLIT>
-__global__ void __launch_bounds__(256) grad_rows_kernel(GradRows G) {
+// dz * sw of one row, as fp16 with a power of two of the row's own; split: in two parts, integers up to 2^11 (exact in fp16, as are their
+// products' sums below 2^24), the lower ones M rows further on.
+// Bytes bound it (dy and the sums in, the row out), so the row waits in shared memory between its maximum and the rounding; rows past
+// GR_KEEP channels are formed again.
+constexpr int GR_KEEP = 16384;
+template <typename Y, bool GATE, int THREADS>
+__global__ void __launch_bounds__(THREADS) grad_rows_kernel(const __grid_constant__ GradRows G) {
+    extern __shared__ __align__(16) float kept_row[];
     pdl_wait();
     if (G.early) pdl_next();
     const long long m = blockIdx.x;
-    const int t = threadIdx.x, N = G.N;
+    const int t = threadIdx.x, N = G.N, groups = (N + 7) / 8;
     const Y* dy = static_cast<const Y*>(G.dy) + m * G.dy_stride;
-    const bool needs = G.gated || G.act != FXPQ_ACT_NONE;
-    const float sx = needs ? __ldg(G.sx + m) : 0.0f;
-    auto z = [&](int n) {
-        const float a = G.pre_f32 ? static_cast<const float*>(G.pre)[m * N + n] : __half2float(static_cast<const __half*>(G.pre)[m * N + n]) * G.pre_unit;
-        return fmaf(a * sx, __ldg(G.sw + n), G.bias ? __ldg(G.bias + n) : 0.0f);
-    };
-    auto pair = [&](int i, float& a, float& b) {  // channels 2 i, 2 i + 1
-        const int n = 2 * i;
-        float slope;
-        if (G.gated) {
-            const float f = activate_slope(z(n), G.act, slope), d = to_f32(dy[i]);
-            a = d * z(n + 1) * slope, b = d * f;
-        } else {
-            a = to_f32(dy[n]), b = n + 1 < N ? to_f32(dy[n + 1]) : 0.0f;
+    const bool needs = GATE || G.act != FXPQ_ACT_NONE;
+    const float sx = needs ? __ldg(G.sx + m) * (G.pre_f32 ? 1.0f : G.pre_unit) : 0.0f;  // (a power of two: z as in the forward pass)
+    constexpr int D = GATE ? 4 : 8;  // values of dy to eight channels
+    auto form = [&](int g, float (&v)[8]) {
+        const int n = 8 * g, left = min(N - n, 8);
+        const bool whole = left == 8;
+        float d[D], a[8], w[8], b[8];
+        if (whole) {
+            load_f32<D>(dy + n / 8 * D, G.vec & 1, d);
+            load_f32<8>(G.sw + n, G.vec & 4, w);
             if (needs) {
-                activate_slope(z(n), G.act, slope);
-                a *= slope;
-                if (n + 1 < N) {
-                    activate_slope(z(n + 1), G.act, slope);
-                    b *= slope;
+                if (G.pre_f32)
+                    load_f32<8>(static_cast<const float*>(G.pre) + m * N + n, G.vec & 2, a);
+                else
+                    load_f32<8>(static_cast<const __half*>(G.pre) + m * N + n, G.vec & 2, a);
+                if (G.bias) load_f32<8>(G.bias + n, G.vec & 8, b);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool in = e < left;
+                if (e < D) d[e] = (GATE ? 2 * e : e) < left ? to_f32(dy[n / 8 * D + e]) : 0.0f;
+                w[e] = in ? __ldg(G.sw + n + e) : 0.0f;
+                if (needs) {
+                    a[e] = !in ? 0.0f : G.pre_f32 ? static_cast<const float*>(G.pre)[m * N + n + e] : __half2float(static_cast<const __half*>(G.pre)[m * N + n + e]);
+                    if (G.bias) b[e] = in ? __ldg(G.bias + n + e) : 0.0f;
                 }
             }
         }
-        a *= __ldg(G.sw + n);
-        b = n + 1 < N ? b * __ldg(G.sw + n + 1) : 0.0f;
-    };
-    __shared__ uint32_t part[8];
-    const int pairs = (N + 1) / 2;
-    uint32_t top = 0;
-    for (int i = t; i < pairs; i += 256) {
-        float a, b;
-        pair(i, a, b);
-        top = max(top, max(__float_as_uint(a) & 0x7fffffffu, __float_as_uint(b) & 0x7fffffffu));
-    }
-    top = __reduce_max_sync(0xffffffffu, top);
-    if ((t & 31) == 0) part[t >> 5] = top;
-    __syncthreads();
-    for (int w = 0; w < 8; ++w) top = max(top, part[w]);
-    const bool bad = top >= 0x7f800000u;
-    if (bad && t == 0) latch_status(G.status, FXPQ_ERR_NONFINITE);
-    // top < 2^e; the row's largest value lies in [2^14, 2^15), or as an integer in [2^22, 2^23)
-    const int e = max(top ? ilogbf(__uint_as_float(top)) + 1 : 0, -100);
-    constexpr int UP = SPLIT ? 23 : 15;
-    const float lift = bad || top == 0 ? 0.0f : ldexpf(1.0f, UP - e);
-    if (t == 0) G.scale[m] = bad ? __int_as_float(0x7fffffff) : ldexpf(1.0f, e - UP);
-    __half2* hi = reinterpret_cast<__half2*>(G.rows + m * G.pitch);
-    __half2* lo = reinterpret_cast<__half2*>(G.rows + (G.M + m) * G.pitch);
-    for (int i = t; i < G.pitch / 2; i += 256) {
-        float a = 0.0f, b = 0.0f;
-        if (i < pairs && lift != 0.0f) pair(i, a, b);
-        a *= lift, b *= lift;
-        if (SPLIT) {
-            const float ha = rintf(a * (1.0f / 4096.0f)), hb = rintf(b * (1.0f / 4096.0f));
-            hi[i] = __floats2half2_rn(ha, hb);
-            lo[i] = __floats2half2_rn(rintf(fmaf(ha, -4096.0f, a)), rintf(fmaf(hb, -4096.0f, b)));
-        } else {
-            hi[i] = __floats2half2_rn(a, b);
+        if (needs) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] = fmaf(a[e] * sx, w[e], G.bias ? b[e] : 0.0f);
         }
+        auto all = [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 8; e += GATE ? 2 : 1) {
+                float slope;
+                const float f = activate_slope(a[e], decltype(act)::value, slope);
+                if constexpr (GATE)
+                    v[e] = d[e / 2] * a[e + 1] * slope * w[e], v[e + 1] = d[e / 2] * f * w[e + 1];
+                else
+                    v[e] = d[e] * slope * w[e];
+            }
+        };
+        switch (G.act) {
+            case FXPQ_ACT_RELU: all(std::integral_constant<int, FXPQ_ACT_RELU>()); break;
+            case FXPQ_ACT_SILU: all(std::integral_constant<int, FXPQ_ACT_SILU>()); break;
+            case FXPQ_ACT_GELU: all(std::integral_constant<int, FXPQ_ACT_GELU>()); break;
+            case FXPQ_ACT_GELU_TANH: all(std::integral_constant<int, FXPQ_ACT_GELU_TANH>()); break;
+            default:
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = d[GATE ? e / 2 : e] * w[e];
+        }
+    };
+    const bool keep = N <= GR_KEEP;
+    uint32_t top = 0;
+    float lift = 0.0f;
+    bool bad = false;
+    const auto put = [&](int g, const float (&v)[8]) {
+        uint4* hi = reinterpret_cast<uint4*>(G.rows + m * G.pitch) + g;
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = bad ? 0.0f : v[2 * i] * lift, b = bad ? 0.0f : v[2 * i + 1] * lift;
+            if (G.split) {
+                const float ha = rintf(a * (1.0f / 4096.0f)), hb = rintf(b * (1.0f / 4096.0f));
+                h[i] = h2_bits(__floats2half2_rn(ha, hb));
+                l[i] = h2_bits(__floats2half2_rn(rintf(fmaf(ha, -4096.0f, a)), rintf(fmaf(hb, -4096.0f, b))));
+            } else {
+                h[i] = h2_bits(__floats2half2_rn(a, b));
+            }
+        }
+        *hi = make_uint4(h[0], h[1], h[2], h[3]);
+        if (G.split) *reinterpret_cast<uint4*>(G.rows + (G.M + m) * G.pitch + 8 * g) = make_uint4(l[0], l[1], l[2], l[3]);
+    };
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {  // the row and its largest value, then its roundings
+#pragma unroll 1
+        for (int g = t; g < groups; g += THREADS) {
+            float v[8];
+            float4* at = reinterpret_cast<float4*>(kept_row) + 2 * g;
+            if (pass && keep) {
+                const float4 p = at[0], q = at[1];
+                v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w, v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
+            } else {
+                form(g, v);
+            }
+            if (pass) {
+                put(g, v);
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+            if (keep) at[0] = make_float4(v[0], v[1], v[2], v[3]), at[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+        if (pass) break;
+        __shared__ uint32_t part[THREADS / 32];
+        top = __reduce_max_sync(0xffffffffu, top);
+        if ((t & 31) == 0) part[t >> 5] = top;
+        __syncthreads();
+        top = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 32; ++w) top = max(top, part[w]);
+        bad = top >= 0x7f800000u;
+        // top < 2^e; the row's largest value lies in [2^14, 2^15), or as an integer in [2^22, 2^23)
+        const int e = max(top ? ilogbf(__uint_as_float(top)) + 1 : 0, -100), up = G.split ? 23 : 15;
+        lift = ldexpf(1.0f, up - e);
+        if (t == 0) {
+            G.scale[m] = bad ? __int_as_float(0x7fffffff) : ldexpf(1.0f, e - up);
+            if (bad) latch_status(G.status, FXPQ_ERR_NONFINITE);
+        }
+    }
+    if (t == 0 && (groups & 1)) {  // rows are padded to 16
+        reinterpret_cast<uint4*>(G.rows + m * G.pitch)[groups] = make_uint4(0, 0, 0, 0);
+        if (G.split) reinterpret_cast<uint4*>(G.rows + (G.M + m) * G.pitch)[groups] = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -115,27 +179,48 @@ bool rows_fit(const void* p, int type, int64_t M, int64_t n, int64_t stride) {
     return p && aligned(p, ftype_bytes(type)) && (M <= 1 || stride >= n);
 }
 
-struct LayerSpace {
-    size_t codes, end;
-    explicit LayerSpace(const fxpq_layer& d) {
-        codes = end = 0;
-        if (float_rows_fit(d.M, d.K)) return;
-        codes = up256((size_t)d.M * half_pitch(d.K) * 2);
-        end = codes + up256((size_t)d.M * 4);
-    }
+// How a product of rows as fp16 is done, by its sizes: few rows to a tile, or pairs of CTAs, a tile's reduction in `shares` and its sums
+// through memory where that takes less time.
+struct Plan {
+    bool few;
+    ManyPlan many;
+    size_t bytes;  // of the sums
 };
-bool sizes_ok(int64_t M, int32_t N, int32_t K) { return M >= 0 && N >= 0 && K >= 0 && M <= INT32_MAX; }
-
-struct GradSpace {
-    size_t rows, scale, sums, end;
-    explicit GradSpace(const fxpq_layer_grad& d) {
-        const int parts = d.dx_type == FXPQ_FT_F32 ? 2 : 1;
-        rows = up256((size_t)parts * d.M * half_pitch(d.N) * 2);
-        scale = rows + up256((size_t)d.M * 4);
-        sums = scale;
-        end = sums + (parts == 2 ? up256((size_t)parts * d.M * d.K * 4) : 0);
+// Microseconds, measured on products of 300 to 8192 rows (512 x 512 of 25088 in 8 shares 34 us, in one 92, few rows to a tile 38; 1500 x 1024
+// of 8192 in three 38, in one 51, few rows 41; 2000 x 4097 of 2048, GELU and residual, the sums through memory 60, stored by the pairs 88).
+// epilogue: what the pairs take to finish and store a tile of 256 tokens, under the next tile's products or not.
+Plan plan_of(int64_t M, int32_t N, int32_t K, double epilogue) {
+    Plan best = {true, {0, 0, 1, nullptr}, 0};
+    if (!many_tokens(M, N, K)) return best;
+    const double pairs = many_pairs(), blocks = (K + LS_KB - 1) / LS_KB, tn = (N + 255) / 256;
+    const double few_tiles = (double)((N + 127) / 128) * ((M + 127) / 128);
+    int few_shares = 1;
+    while (few_shares < 8 && few_tiles * few_shares <= pairs && blocks >= 16 * few_shares) few_shares *= 2;
+    double least = std::ceil(few_tiles * few_shares / (2 * pairs)) * (7.0 + std::ceil(blocks / few_shares) * 0.5);
+    if (few_tiles > 65535) least = 1e30;
+    for (int nt = 128; nt <= 256; nt += 128) {
+        const int64_t tiles = (int64_t)tn * ((M + nt - 1) / nt), full = tiles / (int64_t)pairs * (int64_t)pairs;
+        if (tiles > INT32_MAX / 16) continue;
+        const double narrow = nt / 256.0, block = nt == 256 ? 0.54 : 0.36, round = std::max(blocks * block, epilogue * narrow) + 1.5;
+        for (int whole = 0; whole < 3; ++whole)  // no tile, the full rounds' or all
+            for (int shares = 1; shares <= 12 && 4 * shares <= blocks + 3; ++shares) {
+                if (whole == 1 && (full == 0 || full == tiles || shares == 1)) continue;
+                if (whole == 2 && shares > 1) continue;
+                const int64_t own = whole == 2 ? tiles : whole == 1 ? full : 0, split = tiles - own;
+                const double sums = (double)split * nt * 1024.0 * shares;  // (bytes)
+                if (sums > 1073741824.0) continue;
+                double time = 6.0 + std::ceil(own / pairs) * round;
+                if (split) time += std::ceil(split * shares / pairs) * (std::ceil(blocks / shares) * block + 3.0) + 4.0 + sums / 2.6e6;
+                if (!split) time += epilogue * narrow;
+                if (time < least) least = time, best = {false, {nt, (int)own, shares, nullptr}, (size_t)sums};
+            }
     }
-};
+    return best;
+}
+// Outputs of 16 bits in pairs are stored fast; others, and above all their residuals, value by value.
+double epilogue_time(int32_t N, int32_t y_type, int gated, bool residual) {
+    return y_type != FXPQ_FT_F32 && N % (gated ? 4 : 2) == 0 ? 4.0 : residual ? 22.0 : 9.0;
+}
 
 // y of rows as fp16: what a layer's forward pass and its gradient have in common.
 struct Product {
@@ -150,12 +235,44 @@ struct Product {
     int64_t y_stride;
 };
 template <int EPI>
-fxpq_status product(const Product& p, const Epi& e, cudaStream_t st) {
+fxpq_status product(const Product& p, const Epi& e, Plan plan, float* part, cudaStream_t st) {
     const int64_t pitch = (int64_t)half_pitch(p.K);
-    if (many_tokens(p.M, p.N, p.K))
-        return product_many<EPI>(p.rows, (size_t)pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e);
-    return few_product<EPI>(p.rows, pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e, nullptr, true);
+    if (plan.few) return few_product<EPI>(p.rows, pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e, nullptr, true);
+    plan.many.part = plan.bytes ? part : nullptr;
+    ManyArgs args;
+    const fxpq_status rc = product_many<EPI>(p.rows, (size_t)pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e,
+                                             &plan.many, &args);
+    if (rc != FXPQ_OK || !plan.bytes) return rc;
+    args.e.vec = fours<EPI>(e, p.N, p.y_type, p.y, p.y_stride);
+    launch_pdl(finish_kernel<EPI>, dim3(2 * (unsigned)(args.n_tiles - args.whole), plan.many.nt / 32), dim3(256), 0, st, args, plan.many.nt);
+    return after_launch("finish");
 }
+struct LayerSpace {
+    Plan plan;
+    size_t codes, sums, end;
+    explicit LayerSpace(const fxpq_layer& d) {
+        codes = sums = end = 0;
+        if (float_rows_fit(d.M, d.K)) return;
+        plan = plan_of(d.M, d.N, d.K, epilogue_time(d.N, d.y_type, d.gated, d.d_residual));
+        codes = up256((size_t)d.M * half_pitch(d.K) * 2);
+        sums = codes + up256((size_t)d.M * 4);
+        end = sums + up256(plan.bytes);
+    }
+};
+bool sizes_ok(int64_t M, int32_t N, int32_t K) { return M >= 0 && N >= 0 && K >= 0 && M <= INT32_MAX; }
+
+struct GradSpace {
+    Plan plan;
+    size_t rows, parts, sums, end;
+    explicit GradSpace(const fxpq_layer_grad& d) {
+        const int n = d.dx_type == FXPQ_FT_F32 ? 2 : 1;
+        plan = plan_of(n * d.M, d.K, d.N, epilogue_time(d.K, d.dx_type, 0, false));
+        rows = up256((size_t)n * d.M * half_pitch(d.N) * 2);
+        parts = rows + up256((size_t)d.M * 4);
+        sums = parts + (n == 2 ? up256((size_t)n * d.M * d.K * 4) : 0);
+        end = sums + up256(plan.bytes);
+    }
+};
 
 template <typename F>
 void by_type(int type, F&& f) {
@@ -196,7 +313,7 @@ extern "C" fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, s
     const LayerSpace at(d);
     if (at.end && (!d_ws || ws_bytes < at.end || !aligned(d_ws, 256))) return FXPQ_ERR_WORKSPACE;
     cudaStream_t st = as_stream(stream);
-    const RowNorm norm = {d.d_norm, d.eps, aligned(d.d_norm, 16), !many_tokens(d.M, d.N, d.K)};
+    const RowNorm norm = {d.d_norm, d.eps, aligned(d.d_norm, 16), at.end && at.plan.few};
     const Epi e = {d.d_residual, d.residual_stride, d.d_pre, 1.0f / (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32, d.activation};
     if (at.end == 0) {
         const int vec = aligned(d.d_x, 16) && d.x_stride * ftype_bytes(d.x_type) % 16 == 0;
@@ -210,7 +327,8 @@ extern "C" fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, s
     const fxpq_status rc = half_codes(d.d_x, d.x_type, d.M, d.K, d.x_stride, codes, scale, norm, st);
     if (rc != FXPQ_OK) return rc;
     const Product p = {codes, scale, d.d_w, d.w_stride, d.d_sw, d.d_bias, d.M, d.N, d.K, d.y_type, d.d_y, d.y_stride};
-    return d.gated ? product<GATED>(p, e, st) : product<LAYER>(p, e, st);
+    float* part = reinterpret_cast<float*>(ws + at.sums);
+    return d.gated ? product<GATED>(p, e, at.plan, part, st) : product<LAYER>(p, e, at.plan, part, st);
 }
 
 extern "C" size_t fxpq_layer_gradient_workspace(const fxpq_layer_grad* d) {
@@ -239,21 +357,33 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
     cudaStream_t st = as_stream(stream);
     __half* rows = reinterpret_cast<__half*>(ws);
     float* scale = reinterpret_cast<float*>(ws + at.rows);
-    float* sums = reinterpret_cast<float*>(ws + at.sums);
+    float *sums = reinterpret_cast<float*>(ws + at.parts), *part = reinterpret_cast<float*>(ws + at.sums);
     const bool split = d.dx_type == FXPQ_FT_F32;
-    GradRows G = {d.d_dy, d.dy_stride, d.d_pre, d.d_sx, d.d_sw, d.d_bias, (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32,
-                  d.activation, d.gated, d.N, !many_tokens(split ? 2 * d.M : d.M, d.K, d.N), rows, (long long)half_pitch(d.N), (long long)d.M, scale, status_ptr()};
+    const int dyb = ftype_bytes(d.y_type), kept = d.pre_type == FXPQ_FT_F32 ? 4 : 2, some = d.gated ? 4 * dyb : 16;
+    const int vec = (aligned(d.d_dy, some < 16 ? some : 16) && d.dy_stride * dyb % (some < 16 ? some : 16) == 0 ? 1 : 0) |
+                    (aligned(d.d_pre, 16) && (int64_t)d.N * kept % 16 == 0 ? 2 : 0) | (aligned(d.d_sw, 16) ? 4 : 0) | (aligned(d.d_bias, 16) ? 8 : 0);
+    const GradRows G = {d.d_dy, d.dy_stride, d.d_pre, d.d_sx, d.d_sw, d.d_bias, (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32,
+                        d.activation, d.N, at.plan.few, split, vec, rows, (long long)half_pitch(d.N), (long long)d.M, scale,
+                        status_ptr()};
     by_type(d.y_type, [&](auto t) {
         using Y = decltype(t);
-        if (split)
-            launch_pdl(grad_rows_kernel<Y, true>, dim3((unsigned)d.M), dim3(256), 0, st, G);
+        const size_t smem = d.N <= GR_KEEP ? (size_t)(d.N + 7) / 8 * 32 : 0;
+        auto go = [&](auto kernel, int threads) {
+            if (smem > 24 * 1024) {  // (with the split that the driver chooses two rows of 45 KB fit an SM)
+                (void)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GR_KEEP * 4);
+                (void)cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 80);
+            }
+            launch_pdl(kernel, dim3((unsigned)d.M), dim3(threads), smem, st, G);
+        };
+        if (d.N <= 2048)
+            d.gated ? go(grad_rows_kernel<Y, true, 128>, 128) : go(grad_rows_kernel<Y, false, 128>, 128);
         else
-            launch_pdl(grad_rows_kernel<Y, false>, dim3((unsigned)d.M), dim3(256), 0, st, G);
+            d.gated ? go(grad_rows_kernel<Y, true, 512>, 512) : go(grad_rows_kernel<Y, false, 512>, 512);
     });
     fxpq_status rc = after_launch("layer_grad_rows");
     if (rc != FXPQ_OK) return rc;
-    if (!split) return product<LAYER>({rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride}, {}, st);
-    rc = product<LAYER>({rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K}, {}, st);
+    if (!split) return product<LAYER>({rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride}, {}, at.plan, part, st);
+    rc = product<LAYER>({rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K}, {}, at.plan, part, st);
     if (rc != FXPQ_OK) return rc;
     launch_pdl(join_parts_kernel, dim3(blocks_of(d.M * d.K)), dim3(256), 0, st, static_cast<const float*>(sums), static_cast<const float*>(scale), (long long)d.M,
                (int)d.K, static_cast<float*>(d.d_dx), (long long)d.dx_stride);

@@ -10,11 +10,34 @@ inline bool act_ok(int a) { return a >= FXPQ_ACT_NONE && a <= FXPQ_ACT_GELU_TANH
 // 1 / (1 + e^-z).  (__expf and __fdividef: 2^-21 of the result where it is 2^-8 or more; past e^88 the quotient is 0.)
 __device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 constexpr float GELU_A = 1.5957691216057308f, GELU_B = 0.044715f;  // 2 sqrt(2 / pi)
+// The normal distribution's tail Phi(-a) = e^(-a^2 / 2) t P(t), a >= 0, t = 1 / (1 + 0.45 a / sqrt 2): P a polynomial of degree 9 fitted to
+// e^(x^2) erfc(x) / (2 t) at x = a / sqrt 2 by weighted least squares, to 4e-8 of itself; with fp32 steps 4e-7.  (erfcf took four times as
+// long: 2000 x 4096 of 2048 with GELU 75 us, without 44.)  e: the exponential.
+__device__ __forceinline__ float normal_tail(float a, float& e) {
+    const float t = __fdividef(1.0f, fmaf(0.31819805f, a, 1.0f));
+    float p = -2.069910988e-02f;
+    p = fmaf(p, t, 9.535939991e-02f);
+    p = fmaf(p, t, -1.503192931e-01f);
+    p = fmaf(p, t, 7.122809440e-02f);
+    p = fmaf(p, t, -1.119495742e-02f);
+    p = fmaf(p, t, 5.998074636e-02f);
+    p = fmaf(p, t, 8.762495220e-02f);
+    p = fmaf(p, t, 1.141359434e-01f);
+    p = fmaf(p, t, 1.269415766e-01f);
+    p = fmaf(p, t, 1.269426644e-01f);
+    e = __expf(-0.5f * a * a);
+    return p * t * e;
+}
+__device__ __forceinline__ float gelu(float z) {
+    float e;
+    const float q = normal_tail(fabsf(z), e);
+    return fmaxf(z, -40.0f) * (z > 0.0f ? 1.0f - q : q);  // (far below, a tail of 0 meets no inf)
+}
 __device__ __forceinline__ float activate(float z, int act) {
     switch (act) {
         case FXPQ_ACT_RELU: return fmaxf(z, 0.0f);
         case FXPQ_ACT_SILU: return z * sigmoid(z);
-        case FXPQ_ACT_GELU: return 0.5f * z * erfcf(-0.70710678118654752f * z);
+        case FXPQ_ACT_GELU: return gelu(z);
         case FXPQ_ACT_GELU_TANH: return z * sigmoid(GELU_A * z * fmaf(GELU_B, z * z, 1.0f));
         default: return z;
     }
@@ -29,9 +52,11 @@ __device__ __forceinline__ float activate_slope(float z, int act, float& slope) 
             return z * s;
         }
         case FXPQ_ACT_GELU: {
-            const float p = 0.5f * erfcf(-0.70710678118654752f * z), c = fminf(fmaxf(z, -20.0f), 20.0f);
-            slope = fmaf(c * 0.3989422804014327f, __expf(-0.5f * c * c), p);
-            return z * p;
+            const float c = fminf(fmaxf(z, -40.0f), 40.0f);
+            float e;
+            const float q = normal_tail(fabsf(c), e), p = z > 0.0f ? 1.0f - q : q;
+            slope = fmaf(c * 0.3989422804014327f, e, p);
+            return fmaxf(z, -40.0f) * p;
         }
         case FXPQ_ACT_GELU_TANH: {
             const float c = fminf(fmaxf(z, -30.0f), 30.0f), p = sigmoid(GELU_A * c * fmaf(GELU_B, c * c, 1.0f));

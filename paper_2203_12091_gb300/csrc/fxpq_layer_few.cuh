@@ -166,6 +166,85 @@ struct Residual {
     }
 };
 
+// What follows the sums a of token m and channels ch .. ch + 3, of which P.N may leave some out.  s, sw, bias: their scales and biases.
+template <int EPI, typename Args>
+__device__ __forceinline__ void finish_four(const Args& P, const Epi& e, long long m, int ch, float4 a, float s, const float (&sw)[4], const float (&bias)[4],
+                                            const Residual& r, bool whole) {
+    const int left = P.N - ch;
+    float v[4] = {fmaf(a.x * s, sw[0], bias[0]), fmaf(a.y * s, sw[1], bias[1]), fmaf(a.z * s, sw[2], bias[2]), fmaf(a.w * s, sw[3], bias[3])};
+    if (e.pre) {
+        const float k = e.pre_f32 ? 1.0f : e.pre_scale, keep[4] = {a.x * k, a.y * k, a.z * k, a.w * k};
+        store_some<4>(e.pre, e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, m * P.N + ch, keep, left, e.vec & 4);
+    }
+    if constexpr (EPI == GATED) {
+        const float y[2] = {activate(v[0], e.act) * v[1], activate(v[2], e.act) * v[3]};
+        store_some<2>(P.y, P.y_type, m * P.ys + ch / 2, y, left / 2, e.vec & 1);
+    } else {
+        if (e.act != FXPQ_ACT_NONE)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = activate(v[i], e.act);
+        if (e.res) {
+            const float4 f = r.values(P.y_type, whole);
+            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+        }
+        store_some<4>(P.y, P.y_type, m * P.ys + ch, v, left, e.vec & 1);
+    }
+}
+// Which of outputs, residuals and kept sums lie in aligned accesses of four channels (gated outputs: of two).
+template <int EPI>
+inline int fours(const Epi& e, int N, int y_type, const void* y, int64_t y_stride) {
+    const int type = ftype_bytes(y_type), each = EPI == GATED ? 2 : 4, kept = e.pre_f32 ? 4 : 2;
+    return (aligned(y, each * type) && y_stride % each == 0 ? 1 : 0) | (aligned(e.res, 4 * type) && e.res_stride % 4 == 0 ? 2 : 0) |
+           (aligned(e.pre, 4 * kept) && N % 4 == 0 ? 4 : 0);
+}
+
+// The sums that pairs of CTAs left in memory, added over a tile's shares in their order, and what follows them: a warp has four tokens of
+// 128 channels.
+template <int EPI>
+__global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ ManyArgs P, int nt) {
+    pdl_wait();
+    constexpr int EACH = 4;
+    const int tile = blockIdx.x >> 1, rank = blockIdx.x & 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int tn, tm;
+    tile_of(P, P.whole + tile, tn, tm);
+    const int ch = tn * 256 + rank * 128 + 4 * lane, left = P.N - ch, c0 = (blockIdx.y * 8 + warp) * EACH;
+    const long long m0 = (long long)tm * nt + c0;
+    const int count = (int)min((long long)EACH, P.M - m0);
+    if (left <= 0 || count <= 0) return;
+    const bool whole = (P.e.vec & 2) && left >= 4;
+    float4 a[EACH];
+    Residual r[EACH];
+    float sw[4], bias[4], sx[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        a[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (i >= count) continue;
+        if (EPI == LAYER && P.e.res) r[i].load(P.e.res, P.y_type, (m0 + i) * P.e.res_stride + ch, left, whole);
+        sx[i] = P.sx ? __ldg(P.sx + m0 + i) : 1.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        sw[e] = !P.sw ? 1.0f : e < left ? __ldg(P.sw + ch + e) : 0.0f;
+        bias[e] = P.bias && e < left ? __ldg(P.bias + ch + e) : 0.0f;
+    }
+    const float* part = P.part + (((long long)tile * 2 + rank) * nt + c0) * 128 + 4 * lane;
+#pragma unroll 2
+    for (int s = 0; s < P.shares; ++s, part += (long long)(P.n_tiles - P.whole) * 2 * nt * 128) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (i >= count) continue;
+            const float4 f = *reinterpret_cast<const float4*>(part + i * 128);
+            a[i].x += f.x, a[i].y += f.y, a[i].z += f.z, a[i].w += f.w;
+        }
+    }
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+        finish_four<EPI>(P, P.e, m0 + i, ch, a[0], sx[0], sw, bias, r[0], whole);
+#pragma unroll
+        for (int j = 0; j + 1 < EACH; ++j) a[j] = a[j + 1], sx[j] = sx[j + 1], r[j] = r[j + 1];
+    }
+}
+
 // A place in a ring and the parity of its phase, without divisions (four of them took a third of a block's time).
 struct Turn {
     int at = 0;
@@ -386,25 +465,7 @@ __global__ void __launch_bounds__(LF_THREADS) layer_few_kernel(const __grid_cons
             s = s_sx[c];
         else
             s = rows_space.sx[c];
-        float v[4] = {fmaf(a.x * s, sw[0], bias[0]), fmaf(a.y * s, sw[1], bias[1]), fmaf(a.z * s, sw[2], bias[2]), fmaf(a.w * s, sw[3], bias[3])};
-        const long long m = m0 + c;
-        if (P.e.pre) {
-            const float k = P.e.pre_f32 ? 1.0f : P.e.pre_scale, keep[4] = {a.x * k, a.y * k, a.z * k, a.w * k};
-            store_some<4>(P.e.pre, P.e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, m * P.N + ch, keep, left, P.e.vec & 4);
-        }
-        if constexpr (EPI == GATED) {
-            const float y[2] = {activate(v[0], P.e.act) * v[1], activate(v[2], P.e.act) * v[3]};
-            store_some<2>(P.y, P.y_type, m * P.ys + ch / 2, y, left / 2, P.e.vec & 1);
-        } else {
-            if (P.e.act != FXPQ_ACT_NONE)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = activate(v[e], P.e.act);
-            if (P.e.res) {
-                const float4 f = r.values(P.y_type, whole);
-                v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
-            }
-            store_some<4>(P.y, P.y_type, m * P.ys + ch, v, left, P.e.vec & 1);
-        }
+        finish_four<EPI>(P, P.e, m0 + c, ch, a, s, sw, bias, r, whole);
     }
     if (shares > 1) cluster_sync();  // (the others have read this CTA's sums)
 }
@@ -503,11 +564,7 @@ fxpq_status few_product(const __half* half, int64_t x_stride, const float* d_sx,
     }
     P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.y_type = y_type;
     P.status = status_ptr();
-    {
-        const int type = ftype_bytes(y_type), each = EPI == GATED ? 2 : 4, kept = e.pre_f32 ? 4 : 2;
-        P.e.vec = (aligned(d_y, each * type) && y_stride % each == 0 ? 1 : 0) | (aligned(e.res, 4 * type) && e.res_stride % 4 == 0 ? 2 : 0) |
-                  (aligned(e.pre, 4 * kept) && N % 4 == 0 ? 4 : 0);
-    }
+    P.e.vec = fours<EPI>(e, N, y_type, d_y, y_stride);
     if (!rows) return launch_few<HALVES, EPI>(P, st);
     P.f = *rows;
     return launch_few<FLOATS, EPI>(P, st);

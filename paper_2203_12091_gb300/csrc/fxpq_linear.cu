@@ -462,8 +462,10 @@ fxpq_status quantize_rows(const void* d_x, int32_t x_type, int64_t M, int32_t K,
         auto sized = [&](auto normed) {
             if (K <= 4096)
                 go(std::integral_constant<int, 128>(), normed);
-            else if (K > 8192)
+            else if (K > 16384 || (K > 8192 && M < 512))
                 go(std::integral_constant<int, 1024>(), normed);
+            else if (K > 8192)
+                go(std::integral_constant<int, 512>(), normed);
             else
                 go(std::integral_constant<int, 256>(), normed);
         };

@@ -28,8 +28,8 @@ struct Epi {
     void* pre;
     float pre_scale;
     int pre_f32, act;
-    int vec;   // few: outputs, residuals and kept sums of four channels in aligned accesses each (bits 1, 2, 4)
-    int fast;  // many: 16-bit outputs, pairs of everything aligned, no erfc
+    int vec;   // outputs, residuals and kept sums (bits 1, 2, 4) of four channels (few rows; gated outputs two), or of two, in aligned accesses each
+    int fast;  // many: 16-bit outputs, pairs of everything aligned
 };
 
 // N values at p + at, one aligned access if vec and all of them count.
@@ -93,6 +93,10 @@ struct ManyArgs {
     long long ys, M;
     int N, K, y_type, y_pair;  // y_pair: two 16-bit outputs in one aligned access
     int tiles_n, tiles_m, n_tiles;
+    // Tiles from `whole` on are left to finish_kernel: their reductions are split into shares, work of pairs of their own, whose sums go
+    // to `part` as they are, [share][tile - whole][CTA][token][128 channels].
+    int whole, shares;
+    float* part;
     int* status;
     Epi e;
 };
@@ -111,6 +115,8 @@ __device__ __forceinline__ float2 channel_pair(float a, float b, int odd) {
     return odd ? make_float2(o, b) : make_float2(a, o);
 }
 
+// Activations by their form: at most a cut, z times a sigmoid, z times the normal distribution's integral.
+enum { CUT, SIGMOID, NORMAL };
 // SiLU and the tanh form of GELU as z / (1 + 2^t), t = c z (1 + b z^2).
 struct SigAct {
     float c, b;
@@ -126,7 +132,7 @@ struct SigAct {
 // The epilogue of a warp's 32 channels and ROWS tokens for LAYER and GATED.  Everything goes by pairs: two lanes exchange sums so that
 // each holds two channels of one token.  The fast form holds all sums in registers (the epilogue's warps have taken the other
 // warps'), and has given the accumulators back before it computes: for GATED 16384 of 4096, 8192 tokens, see fxpq_layer.cu.
-template <int ROWS, int EPI, bool SIG, typename Sum>
+template <int ROWS, int EPI, int FORM, typename Sum>
 __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, const float* sxs, float2 sw, float2 bias, int c0, int odd, long long m0, int cols) {
     const bool f16 = P.y_type == FXPQ_FT_F16;
     const SigAct sig(P.e.act);
@@ -137,79 +143,167 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
     // (addresses that walk along the tokens: computed from the token each, they took more registers than there are)
     const long long y_step = 2 * P.ys * 2, r_step = 2 * P.e.res_stride * 2, p_step = 2LL * P.N * 2;
     char* pre = P.e.pre ? static_cast<char*>(P.e.pre) + ((m0 + odd) * P.N + c0) * 2 : nullptr;
-    auto act = [&](float z) { return SIG ? sig(z) : fmaxf(z, low); };
+    auto act = [&](float z) { return FORM == SIGMOID ? sig(z) : FORM == NORMAL ? gelu(z) : fmaxf(z, low); };
     auto pack = [&](float a, float b) {
         if (f16) return h2_bits(__floats2half2_rn(a, b));
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
     };
-    auto pair = [&](int i) {  // z of channels c0, c0 + 1 for token 2 i + odd
-        const float2 s = channel_pair(sum(2 * i), sum(2 * i + 1), odd);
-        if (P.e.pre) {
-            if (2 * i < cols) *reinterpret_cast<__half2*>(pre) = __floats2half2_rn(s.x * ps, s.y * ps);
-            pre += p_step;
-        }
-        const float sx = sxs[2 * i];
-        return make_float2(fmaf(s.x * sx, sw.x, bias.x), fmaf(s.y * sx, sw.y, bias.y));
+    // STEP pairs of tokens at a time, each step of the arithmetic for all of them: one pair after the other left the warps waiting for
+    // every exchange and exponential in turn (8192 x 2 x 5632 of 2048: 24 thousand clocks a tile, its products 16).
+    constexpr int STEP = 8;
+    const int second = (threadIdx.x >> 1) & 1, reach = EPI == GATED ? cols - 2 * second : cols;
+    char* y = static_cast<char*>(P.y) + (EPI == GATED ? (m0 + odd + 2 * second) * P.ys + (c0 >> 1) - second : (m0 + odd) * P.ys + c0) * 2;
+    const char* res = static_cast<const char*>(P.e.res) + ((m0 + odd) * P.e.res_stride + c0) * 2;
+    // Residuals of the next step's tokens are on their way while these are stored: y may be the residual, so the compiler keeps every
+    // load behind the stores before it (one at a time, 2000 x 4096 of 2048 took 53 us).
+    uint32_t r[STEP];
+    auto ask = [&](int i) {
+        r[i % STEP] = 0;
+        if (2 * i < cols) r[i % STEP] = *reinterpret_cast<const uint32_t*>(res);
+        res += r_step;
     };
-    if constexpr (EPI == GATED) {
-        const int second = (threadIdx.x >> 1) & 1, reach = cols - 2 * second;
-        char* y = static_cast<char*>(P.y) + ((m0 + odd + 2 * second) * P.ys + (c0 >> 1) - second) * 2;
+    if (EPI == LAYER && P.e.res) {
 #pragma unroll
-        for (int i = 0; i < ROWS / 2; i += 2) {  // two columns of token 2 i + odd, or with `second` 2 i + 2 + odd
-            const float2 p = pair(i), q = pair(i + 1);
-            const float a = act(p.x) * p.y, b = act(q.x) * q.y;
-            const float o = __shfl_xor_sync(0xffffffffu, second ? a : b, 2);
-            if (2 * i < reach) *reinterpret_cast<uint32_t*>(y) = second ? pack(o, b) : pack(a, o);
-            y += 2 * y_step;
+        for (int i = 0; i < STEP; ++i) ask(i);
+    }
+#pragma unroll
+    for (int i0 = 0; i0 < ROWS / 2; i0 += STEP) {
+        float a[STEP], b[STEP];  // channels c0, c0 + 1 of token 2 (i0 + i) + odd
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+            const float2 s = channel_pair(sum(2 * (i0 + i)), sum(2 * (i0 + i) + 1), odd);
+            a[i] = s.x, b[i] = s.y;
         }
-    } else {
-        char* y = static_cast<char*>(P.y) + ((m0 + odd) * P.ys + c0) * 2;
-        const char* res = static_cast<const char*>(P.e.res) + ((m0 + odd) * P.e.res_stride + c0) * 2;
+        if (P.e.pre) {
 #pragma unroll
-        for (int i = 0; i < ROWS / 2; ++i) {
-            const float2 p = pair(i);
-            float a = act(p.x), b = act(p.y);
-            if (2 * i < cols) {
-                if (P.e.res) {
-                    const float2 r = pair_f32(*reinterpret_cast<const uint32_t*>(res), P.y_type);
-                    a += r.x, b += r.y;
-                }
-                *reinterpret_cast<uint32_t*>(y) = pack(a, b);
+            for (int i = 0; i < STEP; ++i) {
+                if (2 * (i0 + i) < cols) *reinterpret_cast<__half2*>(pre) = __floats2half2_rn(a[i] * ps, b[i] * ps);
+                pre += p_step;
             }
-            y += y_step, res += r_step;
+        }
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+            const float sx = sxs[2 * (i0 + i)];
+            a[i] = fmaf(a[i] * sx, sw.x, bias.x), b[i] = fmaf(b[i] * sx, sw.y, bias.y);
+        }
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) a[i] = act(a[i]);
+        if constexpr (EPI == GATED) {
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) a[i] *= b[i];
+#pragma unroll
+            for (int i = 0; i < STEP; i += 2) {  // two columns of token 2 (i0 + i) + odd, or with `second` of the one two further on
+                const float o = __shfl_xor_sync(0xffffffffu, second ? a[i] : a[i + 1], 2);
+                if (2 * (i0 + i) < reach) *reinterpret_cast<uint32_t*>(y) = second ? pack(o, a[i + 1]) : pack(a[i], o);
+                y += 2 * y_step;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) b[i] = act(b[i]);
+            if (P.e.res) {
+#pragma unroll
+                for (int i = 0; i < STEP; ++i) {
+                    const float2 f = pair_f32(r[i], P.y_type);
+                    a[i] += f.x, b[i] += f.y;
+                }
+                if (i0 + STEP < ROWS / 2) {
+#pragma unroll
+                    for (int i = 0; i < STEP; ++i) ask(i0 + STEP + i);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) {
+                if (2 * (i0 + i) < cols) *reinterpret_cast<uint32_t*>(y) = pack(a[i], b[i]);
+                y += y_step;
+            }
         }
     }
 }
-// Any types, alignment and activation; 16 tokens of this lane's channel.
+// 16 tokens of any type, alignment and activation.
 template <int EPI>
 __device__ __forceinline__ void epilogue_any(const ManyArgs& P, const uint32_t (&v)[16], const float* sxs, float2 sw, float2 bias, int c0, int odd,
-                                          long long m0, int cols) {
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-        uint32_t a = 0, b = 0;
+                                             long long m0, int cols) {
+    float a[8], b[8];  // channels c0, c0 + 1 of tokens 2 i + odd
+    const int left = P.N - c0, vec = P.e.vec;
+    if (left <= 0) cols = 0;
+    uint32_t ra[8], rb[8];  // their residuals as they lie in memory (asked for before anything is stored: y may be the residual)
+    const bool wide = P.y_type == FXPQ_FT_F32, both = (vec & 2) && left > 1;
+    if (EPI == LAYER && P.e.res) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k == i) a = v[2 * k], b = v[2 * k + 1];
-        const float2 s = channel_pair(__uint_as_float(a), __uint_as_float(b), odd);
-        const int t = 2 * i + odd, left = P.N - c0;
-        if (t >= cols || left <= 0) continue;
-        const long long m = m0 + t;
-        if (P.e.pre) {
-            const float k = P.e.pre_f32 ? 1.0f : P.e.pre_scale, keep[2] = {s.x * k, s.y * k};
-            store_some<2>(P.e.pre, P.e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, m * P.N + c0, keep, left, false);
-        }
-        const float z0 = fmaf(s.x * sxs[t], sw.x, bias.x), z1 = fmaf(s.y * sxs[t], sw.y, bias.y), f = activate(z0, P.e.act);
-        if constexpr (EPI == GATED) {
-            store_y(P.y, P.y_type, m * P.ys + (c0 >> 1), f * z1);
-        } else {
-            float y[2] = {f, activate(z1, P.e.act)};
-            if (P.e.res) {
-                const long long at = m * P.e.res_stride + c0;
-                y[0] += load_y(P.e.res, P.y_type, at);
-                if (left > 1) y[1] += load_y(P.e.res, P.y_type, at + 1);
+        for (int i = 0; i < 8; ++i) {
+            ra[i] = rb[i] = 0;
+            if (2 * i + odd >= cols) continue;
+            const long long at = (m0 + 2 * i + odd) * P.e.res_stride + c0;
+            const uint32_t* r32 = static_cast<const uint32_t*>(P.e.res) + at;
+            const unsigned short* r16 = static_cast<const unsigned short*>(P.e.res) + at;
+            if (wide && both) {
+                const uint2 w = *reinterpret_cast<const uint2*>(r32);
+                ra[i] = w.x, rb[i] = w.y;
+            } else if (wide) {
+                ra[i] = r32[0];
+                if (left > 1) rb[i] = r32[1];
+            } else if (both) {
+                ra[i] = *reinterpret_cast<const uint32_t*>(r16);
+            } else {
+                ra[i] = r16[0];
+                if (left > 1) rb[i] = r16[1];
             }
-            store_some<2>(P.y, P.y_type, m * P.ys + c0, y, left, false);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 s = channel_pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]), odd);
+        a[i] = s.x, b[i] = s.y;
+    }
+    cols -= odd, sxs += odd, m0 += odd;
+    if (P.e.pre) {
+        const float k = P.e.pre_f32 ? 1.0f : P.e.pre_scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float keep[2] = {a[i] * k, b[i] * k};
+            if (2 * i < cols) store_some<2>(P.e.pre, P.e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, (m0 + 2 * i) * P.N + c0, keep, left, vec & 4);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float sx = sxs[2 * i];
+        a[i] = fmaf(a[i] * sx, sw.x, bias.x), b[i] = fmaf(b[i] * sx, sw.y, bias.y);
+    }
+    auto all = [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            a[i] = activate(a[i], decltype(act)::value);
+            if (EPI != GATED) b[i] = activate(b[i], decltype(act)::value);
+        }
+    };
+    switch (P.e.act) {
+        case FXPQ_ACT_RELU: all(std::integral_constant<int, FXPQ_ACT_RELU>()); break;
+        case FXPQ_ACT_SILU: all(std::integral_constant<int, FXPQ_ACT_SILU>()); break;
+        case FXPQ_ACT_GELU: all(std::integral_constant<int, FXPQ_ACT_GELU>()); break;
+        case FXPQ_ACT_GELU_TANH: all(std::integral_constant<int, FXPQ_ACT_GELU_TANH>()); break;
+        default: break;
+    }
+    if constexpr (EPI == GATED) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (2 * i < cols) store_y(P.y, P.y_type, (m0 + 2 * i) * P.ys + (c0 >> 1), a[i] * b[i]);
+    } else {
+        if (P.e.res) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (wide) {
+                    a[i] += __uint_as_float(ra[i]), b[i] += __uint_as_float(rb[i]);
+                } else {
+                    const float2 r = pair_f32(both ? ra[i] : __byte_perm(ra[i], rb[i], 0x5410), P.y_type);
+                    a[i] += r.x, b[i] += r.y;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y[2] = {a[i], b[i]};
+            if (2 * i < cols) store_some<2>(P.y, P.y_type, (m0 + 2 * i) * P.ys + c0, y, left, vec & 1);
         }
     }
 }
@@ -220,7 +314,7 @@ constexpr int LM_REGS = 128, LM_REGS_EPI = 176, LM_REGS_ISSUE = 56, LM_REGS_CONV
 static_assert(LM_REGS_ISSUE + LM_REGS_CONV + 2 * LM_REGS_EPI <= 4 * LM_REGS, "the launch's registers");
 
 // NT: tokens of a tile, 256 or, where those tiles would leave pairs idle, 128.
-template <int NT, int EPI, bool SIG>
+template <int NT, int EPI, int FORM>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linear_many_kernel(const __grid_constant__ ManyArgs P) {
     using namespace tc;
     constexpr int ROWS = NT / 2, STAGE = ROWS * 128;  // tokens of a CTA's half of the operand and of an epilogue warp; its stage
@@ -271,16 +365,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
     cluster_sync();
     const uint32_t tmem = tmem_slot, tmem_a = tmem + 256;
     const int n_kb = (P.K + LS_KB - 1) / LS_KB, n_half = (P.K + 63) / 64;
+    const int n_work = EPI == PLAIN ? P.n_tiles : P.whole + (P.n_tiles - P.whole) * P.shares;
+    // Work t: a tile, and of its reduction the blocks first .. last - 1.
+    const auto share_of = [&](int& t, int& first, int& last) {
+        first = 0, last = n_kb;
+        if (EPI == PLAIN || t < P.whole) return 0;
+        const int share = (t - P.whole) % P.shares;
+        t = P.whole + (t - P.whole) / P.shares;
+        first = (int)((long long)n_kb * share / P.shares), last = (int)((long long)n_kb * (share + 1) / P.shares);
+        return share;
+    };
 
     if (warp < 4) {
         if constexpr (EPI != PLAIN) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LM_REGS_ISSUE));
         if (warp == 0) {
             uint32_t it = 0;
             bool ok = true;
-            for (int t = pair; t < P.n_tiles && ok; t += pairs) {
-                int tn, tm;
+            for (int u = pair; u < n_work && ok; u += pairs) {
+                int tn, tm, t = u, first, last;
+                share_of(t, first, last);
                 tile_of(P, t, tn, tm);
-                for (int kb = 0; kb < n_kb; ++kb, ++it) {
+                for (int kb = first; kb < last; ++kb, ++it) {
                     const uint32_t s = it % LM_RAW;
                     if (!wait_warp(raw_empty + 8 * s, ((it / LM_RAW) & 1) ^ 1, abort, P.status)) {
                         ok = false;
@@ -297,10 +402,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
             uint32_t it = 0;
             bool ok = true;
             const uint32_t lead = cluster_addr(b_full, 0);
-            for (int t = pair; t < P.n_tiles && ok; t += pairs) {
-                int tn, tm;
+            for (int u = pair; u < n_work && ok; u += pairs) {
+                int tn, tm, t = u, first, last;
+                share_of(t, first, last);
                 tile_of(P, t, tn, tm);
-                for (int hb = 0; hb < n_half; ++hb, ++it) {
+                for (int hb = 2 * first; hb < min(n_half, 2 * last); ++hb, ++it) {
                     const uint32_t s = it % LM_B;
                     if (!wait_warp(b_empty + 8 * s, ((it / LM_B) & 1) ^ 1, abort, P.status)) {
                         ok = false;
@@ -320,11 +426,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                 const uint64_t bd0 = make_sdesc(b0);
                 uint32_t ia = 0, ib = 0, it = 0;
                 bool ok = true;
-                for (int t = pair; t < P.n_tiles && ok; t += pairs, ++it) {
+                for (int u = pair; u < n_work && ok; u += pairs, ++it) {
+                int t = u, first, last;
+                share_of(t, first, last);
                     if (!wait_warp_cluster(acc_empty, (it & 1) ^ 1, abort, P.status)) break;
                     tc_fence_after();
                     uint32_t acc = 0;
-                    for (int kb = 0; kb < n_kb && ok; ++kb, ++ia) {
+                    for (int kb = first; kb < last && ok; ++kb, ++ia) {
                         const uint32_t c = ia % LM_A;
                         if (!wait_warp_cluster(a_full + 8 * c, (ia / LM_A) & 1, abort, P.status)) {
                             ok = false;
@@ -358,8 +466,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
         const uint32_t lead = cluster_addr(a_full, 0);
         uint32_t it = 0;
         bool ok = true;
-        for (int t = pair; t < P.n_tiles && ok; t += pairs)
-            for (int kb = 0; kb < n_kb; ++kb, ++it) {
+        for (int u = pair; u < n_work && ok; u += pairs) {
+            int t = u, first, last;
+            share_of(t, first, last);
+            for (int kb = first; kb < last; ++kb, ++it) {
                 const uint32_t s = it % LM_RAW, c = it % LM_A;
                 if (!wait_warp(raw_full + 8 * s, (it / LM_RAW) & 1, abort, P.status) ||
                     !wait_warp_cluster(a_empty + 8 * c, ((it / LM_A) & 1) ^ 1, abort, P.status)) {
@@ -390,14 +500,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(lead + 8 * c);
             }
+        }
     } else {
         if constexpr (EPI != PLAIN) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(LM_REGS_EPI));
         const int quad = warp & 3, half = (warp - 8) >> 2;  // channels 32 quad + lane, tokens ROWS half ..
         const uint32_t lead = cluster_addr(acc_empty, 0), at = tmem + ((uint32_t)(quad * 32) << 16) + ROWS * half;
         float* sxs = s_sx[warp - 8];
         uint32_t it = 0;
-        for (int t = pair; t < P.n_tiles; t += pairs, ++it) {
-            int tn, tm;
+        for (int u = pair; u < n_work; u += pairs, ++it) {
+            int tn, tm, t = u, first, last;
+            const int share = share_of(t, first, last);
             tile_of(P, t, tn, tm);
             const int ch = tn * 256 + rank * 128 + quad * 32 + lane;
             const long long m0 = (long long)tm * NT + ROWS * half;
@@ -411,28 +523,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                 const int odd = lane & 1, c0 = ch - odd;
                 const float sw_o = __shfl_xor_sync(0xffffffffu, sw, 1), bias_o = __shfl_xor_sync(0xffffffffu, bias, 1);
                 const float2 sw2 = odd ? make_float2(sw_o, sw) : make_float2(sw, sw_o), bias2 = odd ? make_float2(bias_o, bias) : make_float2(bias, bias_o);
-                if (P.e.fast) {
-                    uint32_t v[ROWS / 32][32];
+                uint32_t v[ROWS / 32][32];
 #pragma unroll
-                    for (int c = 0; c < ROWS / 32; ++c) tmem_ld32_nw(at + 32 * c, v[c]);
-                    tmem_wait_ld();
+                for (int c = 0; c < ROWS / 32; ++c) tmem_ld32_nw(at + 32 * c, v[c]);
+                tmem_wait_ld();
 #pragma unroll
-                    for (int c = 0; c < ROWS / 32; ++c) reg_fence(v[c]);
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(lead);
-                    epilogue_fast<ROWS, EPI, SIG>(P, [&](int t) { return __uint_as_float(v[t / 32][t % 32]); }, sxs, sw2, bias2, c0, odd, m0, cols);
-                } else {
+                for (int c = 0; c < ROWS / 32; ++c) reg_fence(v[c]);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(lead);  // the accumulators may be overwritten
+                if (t >= P.whole) {
+                    float* to = P.part + ((((long long)share * (P.n_tiles - P.whole) + t - P.whole) * 2 + rank) * NT + ROWS * half) * 128 + quad * 32 + lane;
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i)
+                        if (i < cols) to[i * 128] = __uint_as_float(v[i / 32][i % 32]);
+                } else if (P.e.fast) {
+                    epilogue_fast<ROWS, EPI, FORM>(P, [&](int t) { return __uint_as_float(v[t / 32][t % 32]); }, sxs, sw2, bias2, c0, odd, m0, cols);
+                } else {  // 16 tokens at a time, in one place of the code: the others move up
+#pragma unroll 1
                     for (int c = 0; c < ROWS; c += 16) {
-                        uint32_t v[16];
-                        tmem_ld16_nw(at + c, v);
-                        tmem_wait_ld();
-                        reg_fence(v);
-                        epilogue_any<EPI>(P, v, sxs + c, sw2, bias2, c0, odd, m0 + c, cols - c);
+                        uint32_t now[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) now[i] = v[0][i];
+                        epilogue_any<EPI>(P, now, sxs + c, sw2, bias2, c0, odd, m0 + c, cols - c);
+#pragma unroll
+                        for (int i = 0; i < ROWS - 16; ++i) v[i / 32][i % 32] = v[(i + 16) / 32][(i + 16) % 32];
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(lead);
                 }
                 __syncwarp();  // (the scales are read)
                 continue;
@@ -530,12 +646,25 @@ bool encode_half_rows(CUtensorMap* map, const __half* codes, long long rows, int
 size_t codes_pitch(int32_t K) { return ((size_t)K + 15) / 16 * 16; }
 
 // Many tokens go to the pairs of CTAs.
-bool many_tokens(int64_t M, int32_t N, int32_t K) { return M > 256 && N >= 128 && K >= 128; }
+inline bool many_tokens(int64_t M, int32_t N, int32_t K) { return M > 256 && N >= 128 && K >= 128; }
 
-template <int NT, int EPI, bool SIG>
+inline int many_pairs() { return num_sms() / 2 > 0 ? num_sms() / 2 : 1; }
+// Tiles of 256 tokens, or of 128 where their rounds over the pairs take less time.  A round of the narrow ones takes two
+// thirds of the wide ones' (8192 x 8192 of 4096: 13.2 and 20.1 us; every tile expands 256 channels' weights).
+inline int many_tile(int64_t M, int32_t N) {
+    const int64_t pairs = many_pairs(), tn = ((int64_t)N + 255) / 256;
+    const auto rounds = [&](int64_t nt) { return (tn * ((M + nt - 1) / nt) + pairs - 1) / pairs; };
+    return 2 * rounds(128) < 3 * rounds(256) ? 128 : 256;
+}
+struct ManyPlan {
+    int nt, whole, shares;
+    float* part;
+};
+
+template <int NT, int EPI, int FORM>
 fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
     static bool set = false;
-    const auto kernel = linear_many_kernel<NT, EPI, SIG>;
+    const auto kernel = linear_many_kernel<NT, EPI, FORM>;
     if (!set) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LM_SMEM) != cudaSuccess) return FXPQ_ERR_CUDA;
         set = true;
@@ -544,32 +673,39 @@ fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
     if (tn * tm > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
     P.tiles_n = (int)tn, P.tiles_m = (int)tm, P.n_tiles = (int)(tn * tm);
     P.y_pair = aligned(P.y, 4) && P.ys % 2 == 0;
-    const int pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1;
-    launch_pdl(kernel, dim3(2 * (unsigned)(P.n_tiles < pairs ? P.n_tiles : pairs)), dim3(LM_THREADS), LM_SMEM, st, P);
+    P.whole = P.whole < P.n_tiles ? P.whole : P.n_tiles;
+    const long long work = P.whole + (tn * tm - P.whole) * P.shares, pairs = many_pairs();
+    if (work > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
+    launch_pdl(kernel, dim3(2 * (unsigned)(work < pairs ? work : pairs)), dim3(LM_THREADS), LM_SMEM, st, P);
     return after_launch("linear_many");
 }
 
 template <int EPI>
 fxpq_status product_many(const __half* half, size_t pitch, const float* d_sx, const int8_t* d_w, int64_t w_stride, const float* d_sw,
                          const float* d_bias, int64_t M, int32_t N, int32_t K, int32_t y_type, void* d_y, int64_t y_stride, cudaStream_t st,
-                         const Epi& e = {}) {
-    ManyArgs P;
-    P.e = e;
-    // Tiles of 256 tokens, or of 128 where their rounds over the pairs take less time.  A round of the narrow ones takes two
-    // thirds of the wide ones' (8192 x 8192 of 4096: 13.2 and 20.1 us; every tile expands 256 channels' weights).
-    const int64_t pairs = num_sms() / 2 > 0 ? num_sms() / 2 : 1, tn = ((int64_t)N + 255) / 256;
-    const auto rounds = [&](int64_t nt) { return (tn * ((M + nt - 1) / nt) + pairs - 1) / pairs; };
-    const int nt = 2 * rounds(128) < 3 * rounds(256) ? 128 : 256;
+                         const Epi& e = {}, const ManyPlan* plan = nullptr, ManyArgs* args = nullptr) {
+    ManyArgs mine;
+    ManyArgs& P = args ? *args : mine;  // (what finish_kernel takes)
+    P.e = e, P.whole = plan ? plan->whole : INT32_MAX, P.shares = plan ? plan->shares : 1, P.part = plan ? plan->part : nullptr;
+    const int nt = plan ? plan->nt : many_tile(M, N);
     if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_half_rows(&P.tx, half, M, K, (long long)pitch, nt / 2)) return FXPQ_ERR_CUDA;
     P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.K = K, P.y_type = y_type;
     P.status = status_ptr();
+    const auto go = [&](auto form) {
+        constexpr int FORM = decltype(form)::value;
+        return nt == 128 ? launch_many<128, EPI, FORM>(P, st) : launch_many<256, EPI, FORM>(P, st);
+    };
     if constexpr (EPI != PLAIN) {
-        const bool sig = e.act == FXPQ_ACT_SILU || e.act == FXPQ_ACT_GELU_TANH, gated = EPI == GATED;
-        P.e.fast = y_type != FXPQ_FT_F32 && aligned(d_y, 4) && y_stride % 2 == 0 && N % (gated ? 4 : 2) == 0 && (gated ? sig : e.act != FXPQ_ACT_GELU) &&
-                   aligned(e.res, 4) && e.res_stride % 2 == 0 && (!e.pre || (!e.pre_f32 && aligned(e.pre, 4)));
-        if (gated || sig) return nt == 128 ? launch_many<128, EPI, true>(P, st) : launch_many<256, EPI, true>(P, st);
+        const int type = ftype_bytes(y_type), kept = e.pre_f32 ? 4 : 2;
+        P.e.vec = (aligned(d_y, 2 * type) && y_stride % 2 == 0 ? 1 : 0) | (aligned(e.res, 2 * type) && e.res_stride % 2 == 0 ? 2 : 0) |
+                  (aligned(e.pre, 2 * kept) && N % 2 == 0 ? 4 : 0);
+        // (a gate that is cut, the rarest form, has no kernel of its own)
+        P.e.fast = y_type != FXPQ_FT_F32 && P.e.vec == 7 && N % (EPI == GATED ? 4 : 2) == 0 && !(e.pre && e.pre_f32) &&
+                   !(EPI == GATED && e.act == FXPQ_ACT_RELU);
+        if (e.act == FXPQ_ACT_GELU) return go(std::integral_constant<int, NORMAL>());
+        if (EPI == GATED || e.act == FXPQ_ACT_SILU || e.act == FXPQ_ACT_GELU_TANH) return go(std::integral_constant<int, SIGMOID>());
     }
-    if constexpr (EPI != GATED) return nt == 128 ? launch_many<128, EPI, false>(P, st) : launch_many<256, EPI, false>(P, st);
+    if constexpr (EPI != GATED) return go(std::integral_constant<int, CUT>());
     return FXPQ_ERR_UNSUPPORTED;
 }
 }  // namespace
