@@ -151,64 +151,69 @@ class _Layer8:
         return self
 
     def _forward(self, name, x, dtype, norm, eps, act, residual, keep):
-        """y, and with keep the sums and scales that `_gradient` reads."""
-        rows = _float_rows(name, x)
+        """y, and with keep the sums and scales that `_gradient` reads (of an activation's layer, in one tensor)."""
+        flat = x.dim() == 2
+        rows = x if flat and x.is_cuda and x.is_contiguous() else _float_rows(name, x)
         M, K = rows.shape
-        N = self.w.shape[0]
-        if K != self.w.shape[1]:
-            raise ValueError(f"{name}: rows of {self.w.shape[1]} values are needed, got {tuple(x.shape)}")
+        w, bias = self.w, self.bias
+        N, inputs = w.shape
+        if K != inputs:
+            raise ValueError(f"{name}: rows of {inputs} values are needed, got {tuple(x.shape)}")
         wide = N // 2 if self.gated else N
-        xt, yt, dev = _ftype(name, x.dtype), _ftype(name, dtype), x.device
+        xt, yt, dev = _FT.get(x.dtype), _FT.get(dtype), x.device
+        if xt is None or yt is None:
+            _ftype(name, x.dtype if xt is None else dtype)
         nrm = res = res_stride = pre_at = sx_at = 0
         if norm is not None:
-            _want(name + ": norm", norm, _f32, 1)
-            if norm.shape[0] != K:
+            if norm.dtype != _f32 or norm.dim() != 1 or norm.shape[0] != K or not norm.is_cuda or not norm.is_contiguous():
+                _want(name + ": norm", norm, _f32, 1)
                 raise ValueError(f"{name}: one norm weight for each of {K} inputs is needed")
             nrm = norm.data_ptr()
             if not 0.0 <= eps <= 1.0:
                 raise ValueError(f"{name}: eps is 0 to 1, got {eps}")
         if residual is not None:
-            if residual.dtype != dtype or residual.shape != x.shape[:-1] + (N,):
+            if residual.dtype != dtype or residual.shape != ((M, N) if flat else x.shape[:-1] + (N,)):
                 raise ValueError(f"{name}: a residual {(*x.shape[:-1], N)} of {dtype} is needed, got {tuple(residual.shape)} of {residual.dtype}")
             r = _float_rows(name + ": residual", residual)
             res, res_stride = r.data_ptr(), r.stride(0)
         y = _empty((M, wide), dtype=dtype, device=dev)
-        pre = sx = None
-        pre_t = L.FT_F32 if xt == L.FT_F32 or yt == L.FT_F32 else L.FT_F16
+        kept, pre_t = None, L.FT_F32 if xt == L.FT_F32 or yt == L.FT_F32 else L.FT_F16
         if keep and act:
-            pre = _empty((M, N), dtype=_f32 if pre_t == L.FT_F32 else torch.float16, device=dev)
-            sx = _empty(M, dtype=_f32, device=dev)
-            pre_at, sx_at = pre.data_ptr(), sx.data_ptr()
-        w = self.w
-        desc = _LAYER(rows.data_ptr(), rows.stride(0), nrm, w.data_ptr(), _pitch(w, K), self.w_scale.data_ptr(),
-                      0 if self.bias is None else self.bias.data_ptr(), res, res_stride, y.data_ptr(), wide, pre_at, sx_at,
-                      M, N, K, xt, yt, act, self.gated, pre_t, eps)
+            room = (M * N * (4 if pre_t == L.FT_F32 else 2) + 15) // 16 * 16
+            kept = _empty(room + 4 * M, dtype=_u8, device=dev)
+            pre_at = kept.data_ptr()
+            sx_at = pre_at + room
+        desc = _LAYER(rows.data_ptr(), rows.stride(0), nrm, w.data_ptr(), _pitch(w, K), self.w_scale.data_ptr(), 0 if bias is None else bias.data_ptr(),
+                      res, res_stride, y.data_ptr(), wide, pre_at, sx_at, M, N, K, xt, yt, act, self.gated, pre_t, eps)
         lib = L.lib()
         need = lib.fxpq_layer_workspace(desc)
         ws = _empty(need, dtype=_u8, device=dev) if need else None
         rc = lib.fxpq_layer_forward(desc, ws.data_ptr() if need else None, need, F._s(None))
         if rc:
             L.check(name, rc)
-        if x.dim() != 2:
+        if not flat:
             y = y.view(*x.shape[:-1], wide)
-        return (y, pre, sx) if keep else y
+        return (y, kept) if keep else y
 
-    def _gradient(self, name, dy, dtype, act, pre, sx):
+    def _gradient(self, name, dy, dtype, act, kept):
         """dx [..., K] of `dtype` for dy [..., N or N / 2] and what `_forward` kept."""
-        rows = _float_rows(name, dy)
-        M, (N, K), wt = rows.shape[0], self.w.shape, self.wt
+        flat = dy.dim() == 2
+        rows = dy if flat and dy.is_contiguous() else _float_rows(name, dy)
+        M, (N, K), wt, bias = rows.shape[0], self.w.shape, self.wt, self.bias
         dx = _empty((M, K), dtype=dtype, device=dy.device)
-        xt, yt = _ftype(name, dtype), _ftype(name, dy.dtype)
-        desc = _LAYER_GRAD(rows.data_ptr(), rows.stride(0), 0 if pre is None else pre.data_ptr(), 0 if sx is None else sx.data_ptr(),
-                           self.w_scale.data_ptr(), 0 if self.bias is None else self.bias.data_ptr(), wt.data_ptr(), _pitch(wt, N),
-                           dx.data_ptr(), K, M, N, K, yt, xt, act, self.gated,
-                           L.FT_F32 if xt == L.FT_F32 or yt == L.FT_F32 else L.FT_F16, 0)
+        xt, yt = _FT[dtype], _FT[dy.dtype]
+        wide32 = xt == L.FT_F32 or yt == L.FT_F32
+        pre = 0 if kept is None else kept.data_ptr()
+        desc = _LAYER_GRAD(rows.data_ptr(), rows.stride(0), pre, pre and pre + (M * N * (4 if wide32 else 2) + 15) // 16 * 16, self.w_scale.data_ptr(),
+                           0 if bias is None else bias.data_ptr(), wt.data_ptr(), _pitch(wt, N), dx.data_ptr(), K, M, N, K, yt, xt, act, self.gated,
+                           L.FT_F32 if wide32 else L.FT_F16, 0)
         lib = L.lib()
-        ws = _empty(lib.fxpq_layer_gradient_workspace(desc), dtype=_u8, device=dy.device)
-        rc = lib.fxpq_layer_gradient(desc, ws.data_ptr(), ws.nbytes, F._s(None))
+        need = lib.fxpq_layer_gradient_workspace(desc)
+        ws = _empty(need, dtype=_u8, device=dy.device)
+        rc = lib.fxpq_layer_gradient(desc, ws.data_ptr(), need, F._s(None))
         if rc:
             L.check(name, rc)
-        return dx if dy.dim() == 2 else dx.view(*dy.shape[:-1], K)
+        return dx if flat else dx.view(*dy.shape[:-1], K)
 
     def _call(self, name, x, dtype, norm, eps, act, residual):
         """The forward pass, recorded where rows or residual require a gradient."""
@@ -223,24 +228,29 @@ class _Layer8:
         return self._forward(name, x, dtype, norm, eps, act, residual, False)
 
 
+def _step_back(ctx, dy):
+    layer, name, act, dtype = ctx.what
+    wants = ctx.needs_input_grad
+    return layer._gradient(name, dy, dtype, act, *ctx.saved_tensors) if wants[0] else None, dy if wants[1] else None, None, None, None, None
+
+
+_step_back_once = torch.autograd.function.once_differentiable(_step_back)
+
+
 class _LayerStep(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, layer, name, dtype, act):
-        keep = ctx.needs_input_grad[0]
-        y = layer._forward(name, x, dtype, None, 0.0, act, residual, keep)
-        ctx.layer, ctx.name, ctx.act, ctx.dtype = layer, name, act, x.dtype
-        if keep:
-            y, pre, sx = y
-            ctx.save_for_backward(pre, sx)
+        ctx.what = layer, name, act, x.dtype
+        if not ctx.needs_input_grad[0]:
+            return layer._forward(name, x, dtype, None, 0.0, act, residual, False)
+        y, kept = layer._forward(name, x, dtype, None, 0.0, act, residual, True)
+        ctx.save_for_backward(kept)
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        dx = None
-        if ctx.needs_input_grad[0]:
-            dx = ctx.layer._gradient(ctx.name, dy, ctx.dtype, ctx.act, *ctx.saved_tensors)
-        return dx, dy if ctx.needs_input_grad[1] else None, None, None, None, None
+        # (the wrapper that refuses second derivatives takes 10 us of a small layer's backward: only where a graph of it is asked for)
+        return _step_back_once(ctx, dy) if torch.is_grad_enabled() else _step_back(ctx, dy)
 
 
 class Linear8(_Layer8):

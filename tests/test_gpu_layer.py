@@ -521,3 +521,28 @@ def test_rows_whose_codes_the_product_forms(ops, M, K, x):
     for N in (130, 512):
         check_layer(ops, rng, M, N, K, x, "f32", "silu", True, True, True)
         check_gated(ops, rng, M, N // 2, K, x, "bf16", "silu", True, False)
+
+
+def test_no_second_derivative(ops):
+    """A graph of the gradient may be asked for, but nothing may silently differentiate through it."""
+    rng = np.random.default_rng(3)
+    layer = Weights(rng, 32, 64, True).layer(ops).with_gradient()
+    x = rows(rng, 4, 64, "f32").requires_grad_()
+    plain = torch.autograd.grad(layer(x, activation="silu").sum(), x)[0]
+    dx = torch.autograd.grad(layer(x, activation="silu").sum(), x, create_graph=True)[0]
+    assert torch.equal(dx.detach(), plain)
+    with pytest.raises(RuntimeError):
+        dx.sum().backward()
+
+
+def test_backward_frees_what_it_kept(ops):
+    rng = np.random.default_rng(3)
+    layer = Weights(rng, 1024, 1024, False).layer(ops).with_gradient()
+    x = rows(rng, 2000, 1024, "bf16").requires_grad_()
+    y = layer(x, activation="silu")
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    torch.autograd.grad(y, x, torch.ones_like(y))
+    assert torch.cuda.memory_allocated() <= before - 2000 * 1024 * 2  # the sums
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(y, x, torch.ones_like(y))
