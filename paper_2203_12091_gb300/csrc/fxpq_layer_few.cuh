@@ -70,14 +70,14 @@ template <typename T, bool NORM>
 __device__ __forceinline__ void own_codes(const FloatRows& F, int M, int kb0, int n_kb, unsigned char* blocks, RowSpace& S, int t, bool first, int* status) {
     const T* x = static_cast<const T*>(F.x);
     const int warp = t >> 5, lane = t & 31, K = F.K, groups = K / 8;
-    const int parts = M <= 1 ? 8 : M <= 2 ? 4 : M <= 4 ? 2 : 1, step = 32 * parts;  // warps of a row
+    const int log_parts = M <= 1 ? 3 : M <= 2 ? 2 : M <= 4 ? 1 : 0, parts = 1 << log_parts, step = 32 * parts;  // warps of a row
     const auto join = []() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
     auto eight = [&](const T* row, int k, float (&v)[8], float (&w)[8]) {
         load_f32<8>(row + k, F.x_vec, v);
         if constexpr (NORM) load_f32<8>(F.norm.weight + k, F.norm.vec, w);
     };
     for (int u = warp; u < M * parts; u += 8) {
-        const int m = u / parts, p = u - m * parts;
+        const int m = u >> log_parts, p = u & (parts - 1);
         const T* row = x + m * F.x_stride;
         RowScan<NORM> scan;
 #pragma unroll 4
@@ -108,10 +108,14 @@ __device__ __forceinline__ void own_codes(const FloatRows& F, int M, int kb0, in
     }
     join();
     const int chunks = n_kb * (LS_KB / 8);
-    for (int i = t; i < M * chunks; i += 256) {
-        const int m = i / chunks, c = i - m * chunks, k = kb0 * LS_KB + 8 * c, b = c >> 4, hf = (c >> 3) & 1;
+    for (int u = warp; u < M * parts; u += 8) {
+        const int m = u >> log_parts;
         const T* row = x + m * F.x_stride;
         const float inv = S.inv[m];
+        unsigned char* to = blocks + m * 128;
+#pragma unroll 2
+        for (int c = (u & (parts - 1)) * 32 + lane; c < chunks; c += step) {
+        const int k = kb0 * LS_KB + 8 * c;
         float v[8], w[8];
         if (k + 8 <= K) {
             eight(row, k, v, w);
@@ -121,8 +125,9 @@ __device__ __forceinline__ void own_codes(const FloatRows& F, int M, int kb0, in
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = scaled_code(NORM ? __fmul_rn(v[e], w[e]) : v[e], inv);
-        *reinterpret_cast<uint4*>(blocks + (2 * b + hf) * LF_HALF + m * 128 + (((c & 7) ^ (m & 7)) << 4)) =
+        *reinterpret_cast<uint4*>(to + (c >> 3) * LF_HALF + (((c & 7) ^ (m & 7)) << 4)) =
             make_uint4(f32_codes_f16x2(v[0], v[1]), f32_codes_f16x2(v[2], v[3]), f32_codes_f16x2(v[4], v[5]), f32_codes_f16x2(v[6], v[7]));
+        }
     }
 }
 template <typename T>

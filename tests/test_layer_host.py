@@ -123,7 +123,7 @@ def test_layer_refuses(lib, bad):
 
 
 def test_layer_refuses_workspaces(lib):
-    many = layer(M=40)
+    many = layer(M=140)
     assert run(lib, many, work=None) == run(lib, many, short=1) == run(lib, many, work=4112) == L.ERR_WORKSPACE
     assert run(lib, layer(M=0)) == run(lib, layer(N=0)) == L.OK
     assert lib.fxpq_layer_forward(None, None, 0, None) == L.ERR_INVALID_ARG and lib.fxpq_layer_workspace(None) == 0
