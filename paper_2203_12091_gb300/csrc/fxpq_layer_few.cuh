@@ -43,28 +43,30 @@ struct FewArgs {
 // fixed order.  Up to 64 tokens two CTAs fit an SM.
 constexpr int LF_THREADS = 384;
 
-// How the rows come: as fp16 (codes, or a gradient's), or as rows of floats (up to 8), whose codes every CTA forms for its share of the
+// How the rows come: as fp16 (codes, or a gradient's), or as rows of floats (up to 16), whose codes every CTA forms for its share of the
 // reduction.
 enum { HALVES, FLOATS };
-// A half block of their codes has 8 rows; the products read 16: what follows (the 1 KB behind the last) stands in for columns that nobody reads.
-constexpr int LF_ROWS = 8, LF_HALF = LF_ROWS * 128, LF_MOST = 32;  // (blocks of a share)
+// A half block of their codes has whole groups of 8 rows; the products read groups of 16: what follows (the 1 KB behind the last) stands in for
+// columns that nobody reads.
+constexpr int LF_ROWS = 16, LF_MOST = 32;  // (blocks of a share)
+__host__ __device__ inline int lf_half(int rows) { return (rows + 7) / 8 * 8 * 128; }
 constexpr int LF_SMEM = 220 * 1024;
 
 // Operands of weights in tensor memory, one more (or two) than there are groups that form them: none waits for the product of its last.
 __host__ __device__ inline int lf_operands(int cols) { return cols > 64 ? 4 : 3; }
 
 // floats: stages of weights alone, and all of the share's codes
-__host__ __device__ inline int lf_smem(int cols, int stages, int tok, int blocks) {
-    const int ring = tok == HALVES ? stages * (LS_A + cols * LS_KB * 2) : stages * LS_A + blocks * 2 * LF_HALF + 1024;
+__host__ __device__ inline int lf_smem(int rows, int cols, int stages, int tok, int blocks) {
+    const int ring = tok == HALVES ? stages * (LS_A + cols * LS_KB * 2) : stages * LS_A + blocks * 2 * lf_half(rows) + 1024;
     const int sums = cols * 128 * 4;
     return 1024 + (ring > sums ? ring : sums);
 }
 
-// Codes of up to 8 rows of floats by 256 threads (8 warps): every row's scale from the whole row, then the fp16 codes of n_kb blocks
+// Codes of up to 16 rows of floats by 256 threads (8 warps): every row's scale from the whole row, then the fp16 codes of n_kb blocks
 // from block kb0 on into shared memory, as the products read them.  The same fp32 steps as the token quantizer's.
 struct RowSpace {
-    uint32_t top[LF_ROWS][8];
-    float sum[LF_ROWS][8], inv[LF_ROWS], sx[LF_ROWS];
+    uint32_t top[LF_ROWS];  // [row][part]
+    float sum[LF_ROWS], inv[LF_ROWS], sx[LF_ROWS];
 };
 template <typename T, bool NORM>
 __device__ __forceinline__ void own_codes(const FloatRows& F, int M, int kb0, int n_kb, unsigned char* blocks, RowSpace& S, int t, bool first, int* status) {
@@ -90,12 +92,12 @@ __device__ __forceinline__ void own_codes(const FloatRows& F, int M, int kb0, in
         const int k = 8 * groups + lane;
         if (p == 0 && k < K) scan.see(to_f32(row[k]), NORM ? __ldg(F.norm.weight + k) : 1.0f);
         scan.meet();
-        if (lane == 0) S.top[m][p] = scan.top, S.sum[m][p] = scan.sum;
+        if (lane == 0) S.top[u] = scan.top, S.sum[u] = scan.sum;
     }
     join();
     for (int m = warp; m < M; m += 8) {
         RowScan<NORM> scan;
-        for (int p = 0; p < parts; ++p) scan.join(S.top[m][p], NORM ? S.sum[m][p] : 0.0f);
+        for (int p = 0; p < parts; ++p) scan.join(S.top[m * parts + p], NORM ? S.sum[m * parts + p] : 0.0f);
         float inv = scan.inverse(), sx;
         if (scan.odd())
             careful_row(x + m * F.x_stride, K, F.norm.weight, F.norm.eps, inv, sx, first ? status : nullptr);
@@ -107,7 +109,7 @@ __device__ __forceinline__ void own_codes(const FloatRows& F, int M, int kb0, in
         }
     }
     join();
-    const int chunks = n_kb * (LS_KB / 8);
+    const int chunks = n_kb * (LS_KB / 8), half = lf_half(M);
     for (int u = warp; u < M * parts; u += 8) {
         const int m = u >> log_parts;
         const T* row = x + m * F.x_stride;
@@ -125,7 +127,7 @@ __device__ __forceinline__ void own_codes(const FloatRows& F, int M, int kb0, in
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = scaled_code(NORM ? __fmul_rn(v[e], w[e]) : v[e], inv);
-        *reinterpret_cast<uint4*>(to + (c >> 3) * LF_HALF + (((c & 7) ^ (m & 7)) << 4)) =
+        *reinterpret_cast<uint4*>(to + (c >> 3) * half + (((c & 7) ^ (m & 7)) << 4)) =
             make_uint4(f32_codes_f16x2(v[0], v[1]), f32_codes_f16x2(v[2], v[3]), f32_codes_f16x2(v[4], v[5]), f32_codes_f16x2(v[6], v[7]));
         }
     }
@@ -341,14 +343,14 @@ __global__ void __launch_bounds__(LF_THREADS) layer_few_kernel(const __grid_cons
     } else if (warp == 1) {
         const uint32_t idesc = make_idesc(128, cols);
         const uint64_t bdesc = make_sdesc(HALF ? raw0 : conv0);
-        const int half_bytes = TOK == FLOATS ? LF_HALF : cols * 128;
+        const int half_bytes = TOK == FLOATS ? lf_half(P.rows) : cols * 128;
         if (TOK == FLOATS && n_kb > 0) wait_warp(tok_full, 0, abort, P.status);
         Turn c, s;
         for (int i = 0; i < n_kb; ++i, c.next(1, NB), s.next(1, ST)) {
             if (!wait_warp(conv_full + 8 * c.at, c.phase, abort, P.status)) break;
             if (HALF && !wait_warp(raw_full + 8 * s.at, s.phase, abort, P.status)) break;
             tc_fence_after();
-            const uint64_t bd = bdesc + (uint64_t)((HALF ? s.at * raw_bytes + LS_A : i * 2 * LF_HALF) >> 4);
+            const uint64_t bd = bdesc + (uint64_t)((HALF ? s.at * raw_bytes + LS_A : i * 2 * half_bytes) >> 4);
 #pragma unroll
             for (int kk = 0; kk < LS_KB / 16; ++kk)
                 tc_mma_ta(tmem, tmem_a + 64 * c.at + 8 * kk, bd + (uint64_t)(((kk >> 2) * half_bytes) >> 4) + 2 * (kk & 3), idesc, i > 0 || kk > 0);
@@ -480,7 +482,7 @@ fxpq_status launch_few(FewArgs& P, cudaStream_t st) {
     static bool set = false;
     const auto kernel = layer_few_kernel<TOK, EPI>;
     if (!set) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TOK == FLOATS ? LF_SMEM : lf_smem(128, 4, TOK, 0)) !=
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TOK == FLOATS ? LF_SMEM : lf_smem(128, 128, 4, TOK, 0)) !=
             cudaSuccess)
             return FXPQ_ERR_CUDA;
         set = true;
@@ -494,8 +496,8 @@ fxpq_status launch_few(FewArgs& P, cudaStream_t st) {
         if (TOK == HALVES) return P.cols <= 64;
         const int blocks = (P.n_kb + shares - 1) / shares;
         for (P.stages = 4; P.stages >= 3; --P.stages)
-            if (lf_smem(P.cols, P.stages, TOK, blocks) <= LF_SMEM / 2) return true;
-        for (P.stages = 8; P.stages > 4 && lf_smem(P.cols, P.stages, TOK, blocks) > LF_SMEM;) --P.stages;
+            if (lf_smem(P.rows, P.cols, P.stages, TOK, blocks) <= LF_SMEM / 2) return true;
+        for (P.stages = 8; P.stages > 4 && lf_smem(P.rows, P.cols, P.stages, TOK, blocks) > LF_SMEM;) --P.stages;
         return false;
     };
     cudaLaunchAttribute at[2];
@@ -505,7 +507,7 @@ fxpq_status launch_few(FewArgs& P, cudaStream_t st) {
     at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c = {};
     c.blockDim = dim3(LF_THREADS);
-    auto smem_for = [&](int shares) { return (size_t)lf_smem(P.cols, P.stages, TOK, (P.n_kb + shares - 1) / shares); };
+    auto smem_for = [&](int shares) { return (size_t)lf_smem(P.rows, P.cols, P.stages, TOK, (P.n_kb + shares - 1) / shares); };
     c.stream = st;
     c.attrs = at;
     // As many CTAs to a reduction as run at once, with at least 1024 codes each (4096 x 4096, 64 tokens: 10.9 us with four of
@@ -543,10 +545,10 @@ fxpq_status launch_few(FewArgs& P, cudaStream_t st) {
 }
 
 // Rows of floats whose codes the product forms itself: few enough that every CTA may read them whole, and 8 shares of at most LF_MOST
-// blocks.  On the GPU it takes as long as quantizer and product (4096 channels, 4096 inputs, 1, 4 and 8 rows: 9.5, 12.0 and 13.7 us, as
-// two launches 10.0, 12.6 and 12.6; 16 rows 17.9 and 12.7; 2 rows of 25088 31 and 25); the host saves a launch and the codes'
-// memory, 5 of 16 us.
-bool float_rows_fit(int64_t M, int32_t K) { return M <= LF_ROWS && M * K <= 32768 && K <= 8 * LF_MOST * LS_KB; }
+// blocks.  On the GPU that takes as long as quantizer and product, or a little longer (4096 channels, 4096 inputs, 1, 4 and 8 rows: 9.7, 11.7
+// and 13.0 us, as two launches 10.0, 12.6 and 12.6; 16 rows of 1024 10.2 and 7.6, of 3640 22 and 12); the host saves a launch and
+// the codes' memory, 9 of 20 us.
+bool float_rows_fit(int64_t M, int32_t K) { return M <= LF_ROWS && M * K <= (M <= 8 ? 32768 : 16384) && K <= 8 * LF_MOST * LS_KB; }
 
 // Rows as fp16 at half, or formed from floats.
 template <int EPI>
