@@ -11,152 +11,6 @@ namespace fxpq {
 namespace llm {
 namespace {
 
-// ------------------------------------------------------------------ rows of the gradient
-struct GradRows {
-    const void* dy;
-    long long dy_stride;
-    const void* pre;
-    const float *sx, *sw, *bias;
-    float pre_unit;
-    int pre_f32, act, N, early, split;
-    int vec;  // dy, kept sums, scales, biases in aligned accesses (bits 1, 2, 4, 8)
-    __half* rows;
-    long long pitch, M;
-    float* scale;
-    int* status;
-};
-
-// dz * sw of one row, as fp16 with a power of two of the row's own; split: in two parts, integers up to 2^11 (exact in fp16, as are their
-// products' sums below 2^24), the lower ones M rows further on.
-// Bytes bound it (dy and the sums in, the row out), so the row waits in shared memory between its maximum and the rounding; rows past
-// GR_KEEP channels are formed again.
-constexpr int GR_KEEP = 16384;
-template <typename Y, bool GATE, int THREADS>
-__global__ void __launch_bounds__(THREADS) grad_rows_kernel(const __grid_constant__ GradRows G) {
-    extern __shared__ __align__(16) float kept_row[];
-    pdl_wait();
-    if (G.early) pdl_next();
-    const long long m = blockIdx.x;
-    const int t = threadIdx.x, N = G.N, groups = (N + 7) / 8;
-    const Y* dy = static_cast<const Y*>(G.dy) + m * G.dy_stride;
-    const bool needs = GATE || G.act != FXPQ_ACT_NONE;
-    const float sx = needs ? __ldg(G.sx + m) * (G.pre_f32 ? 1.0f : G.pre_unit) : 0.0f;  // (a power of two: z as in the forward pass)
-    constexpr int D = GATE ? 4 : 8;  // values of dy to eight channels
-    auto form = [&](int g, float (&v)[8]) {
-        const int n = 8 * g, left = min(N - n, 8);
-        const bool whole = left == 8;
-        float d[D], a[8], w[8], b[8];
-        if (whole) {
-            load_f32<D>(dy + n / 8 * D, G.vec & 1, d);
-            load_f32<8>(G.sw + n, G.vec & 4, w);
-            if (needs) {
-                if (G.pre_f32)
-                    load_f32<8>(static_cast<const float*>(G.pre) + m * N + n, G.vec & 2, a);
-                else
-                    load_f32<8>(static_cast<const __half*>(G.pre) + m * N + n, G.vec & 2, a);
-                if (G.bias) load_f32<8>(G.bias + n, G.vec & 8, b);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool in = e < left;
-                if (e < D) d[e] = (GATE ? 2 * e : e) < left ? to_f32(dy[n / 8 * D + e]) : 0.0f;
-                w[e] = in ? __ldg(G.sw + n + e) : 0.0f;
-                if (needs) {
-                    a[e] = !in ? 0.0f : G.pre_f32 ? static_cast<const float*>(G.pre)[m * N + n + e] : __half2float(static_cast<const __half*>(G.pre)[m * N + n + e]);
-                    if (G.bias) b[e] = in ? __ldg(G.bias + n + e) : 0.0f;
-                }
-            }
-        }
-        if (needs) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] = fmaf(a[e] * sx, w[e], G.bias ? b[e] : 0.0f);
-        }
-        auto all = [&](auto act) {
-#pragma unroll
-            for (int e = 0; e < 8; e += GATE ? 2 : 1) {
-                float slope;
-                const float f = activate_slope(a[e], decltype(act)::value, slope);
-                if constexpr (GATE)
-                    v[e] = d[e / 2] * a[e + 1] * slope * w[e], v[e + 1] = d[e / 2] * f * w[e + 1];
-                else
-                    v[e] = d[e] * slope * w[e];
-            }
-        };
-        switch (G.act) {
-            case FXPQ_ACT_RELU: all(std::integral_constant<int, FXPQ_ACT_RELU>()); break;
-            case FXPQ_ACT_SILU: all(std::integral_constant<int, FXPQ_ACT_SILU>()); break;
-            case FXPQ_ACT_GELU: all(std::integral_constant<int, FXPQ_ACT_GELU>()); break;
-            case FXPQ_ACT_GELU_TANH: all(std::integral_constant<int, FXPQ_ACT_GELU_TANH>()); break;
-            default:
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = d[GATE ? e / 2 : e] * w[e];
-        }
-    };
-    const bool keep = N <= GR_KEEP;
-    uint32_t top = 0;
-    float lift = 0.0f;
-    bool bad = false;
-    const auto put = [&](int g, const float (&v)[8]) {
-        uint4* hi = reinterpret_cast<uint4*>(G.rows + m * G.pitch) + g;
-        uint32_t h[4], l[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float a = bad ? 0.0f : v[2 * i] * lift, b = bad ? 0.0f : v[2 * i + 1] * lift;
-            if (G.split) {
-                const float ha = rintf(a * (1.0f / 4096.0f)), hb = rintf(b * (1.0f / 4096.0f));
-                h[i] = h2_bits(__floats2half2_rn(ha, hb));
-                l[i] = h2_bits(__floats2half2_rn(rintf(fmaf(ha, -4096.0f, a)), rintf(fmaf(hb, -4096.0f, b))));
-            } else {
-                h[i] = h2_bits(__floats2half2_rn(a, b));
-            }
-        }
-        *hi = make_uint4(h[0], h[1], h[2], h[3]);
-        if (G.split) *reinterpret_cast<uint4*>(G.rows + (G.M + m) * G.pitch + 8 * g) = make_uint4(l[0], l[1], l[2], l[3]);
-    };
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {  // the row and its largest value, then its roundings
-#pragma unroll 1
-        for (int g = t; g < groups; g += THREADS) {
-            float v[8];
-            float4* at = reinterpret_cast<float4*>(kept_row) + 2 * g;
-            if (pass && keep) {
-                const float4 p = at[0], q = at[1];
-                v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w, v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
-            } else {
-                form(g, v);
-            }
-            if (pass) {
-                put(g, v);
-                continue;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
-            if (keep) at[0] = make_float4(v[0], v[1], v[2], v[3]), at[1] = make_float4(v[4], v[5], v[6], v[7]);
-        }
-        if (pass) break;
-        __shared__ uint32_t part[THREADS / 32];
-        top = __reduce_max_sync(0xffffffffu, top);
-        if ((t & 31) == 0) part[t >> 5] = top;
-        __syncthreads();
-        top = 0;
-#pragma unroll
-        for (int w = 0; w < THREADS / 32; ++w) top = max(top, part[w]);
-        bad = top >= 0x7f800000u;
-        // top < 2^e; the row's largest value lies in [2^14, 2^15), or as an integer in [2^22, 2^23)
-        const int e = max(top ? ilogbf(__uint_as_float(top)) + 1 : 0, -100), up = G.split ? 23 : 15;
-        lift = ldexpf(1.0f, up - e);
-        if (t == 0) {
-            G.scale[m] = bad ? __int_as_float(0x7fffffff) : ldexpf(1.0f, e - up);
-            if (bad) latch_status(G.status, FXPQ_ERR_NONFINITE);
-        }
-    }
-    if (t == 0 && (groups & 1)) {  // rows are padded to 16
-        reinterpret_cast<uint4*>(G.rows + m * G.pitch)[groups] = make_uint4(0, 0, 0, 0);
-        if (G.split) reinterpret_cast<uint4*>(G.rows + (G.M + m) * G.pitch)[groups] = make_uint4(0, 0, 0, 0);
-    }
-}
-
 // dx = (4096 high sums + low sums) * scale
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ sums, const float* __restrict__ scale, long long M, int K,
                                                          float* __restrict__ dx, long long dx_stride) {
@@ -274,16 +128,6 @@ struct GradSpace {
     }
 };
 
-template <typename F>
-void by_type(int type, F&& f) {
-    if (type == FXPQ_FT_F32)
-        f(float());
-    else if (type == FXPQ_FT_F16)
-        f(__half());
-    else
-        f(__nv_bfloat16());
-}
-
 }  // namespace
 }  // namespace llm
 }  // namespace fxpq
@@ -365,22 +209,7 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
     const GradRows G = {d.d_dy, d.dy_stride, d.d_pre, d.d_sx, d.d_sw, d.d_bias, (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32,
                         d.activation, d.N, at.plan.few, split, vec, rows, (long long)half_pitch(d.N), (long long)d.M, scale,
                         status_ptr()};
-    by_type(d.y_type, [&](auto t) {
-        using Y = decltype(t);
-        const size_t smem = d.N <= GR_KEEP ? (size_t)(d.N + 7) / 8 * 32 : 0;
-        auto go = [&](auto kernel, int threads) {
-            if (smem > 24 * 1024) {  // (with the split that the driver chooses two rows of 45 KB fit an SM)
-                (void)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GR_KEEP * 4);
-                (void)cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 80);
-            }
-            launch_pdl(kernel, dim3((unsigned)d.M), dim3(threads), smem, st, G);
-        };
-        if (d.N <= 2048)
-            d.gated ? go(grad_rows_kernel<Y, true, 128>, 128) : go(grad_rows_kernel<Y, false, 128>, 128);
-        else
-            d.gated ? go(grad_rows_kernel<Y, true, 512>, 512) : go(grad_rows_kernel<Y, false, 512>, 512);
-    });
-    fxpq_status rc = after_launch("layer_grad_rows");
+    fxpq_status rc = grad_rows(G, d.y_type, d.gated, st);
     if (rc != FXPQ_OK) return rc;
     if (!split) return product<LAYER>({rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride}, {}, at.plan, part, st);
     rc = product<LAYER>({rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K}, {}, at.plan, part, st);

@@ -74,5 +74,21 @@ inline int sum_shift(int32_t K) {
     return p;
 }
 
+// The rows of a gradient, dz * sw (fxpq_layer_grad.cu).
+struct GradRows {
+    const void* dy;
+    long long dy_stride;
+    const void* pre;
+    const float *sx, *sw, *bias;
+    float pre_unit;
+    int pre_f32, act, N, early, split;
+    int vec;  // dy, kept sums, scales, biases in aligned accesses (bits 1, 2, 4, 8)
+    __half* rows;
+    long long pitch, M;
+    float* scale;
+    int* status;
+};
+fxpq_status grad_rows(const GradRows& rows, int y_type, int gated, cudaStream_t st);
+
 }  // namespace llm
 }  // namespace fxpq
