@@ -1,7 +1,8 @@
 """A decoder in 8 bits that serves batches: an example of the language-model operators used together.
 
 Every projection is a `Linear8`, keys and values live in paged `KVCache`s, prompts of unequal length go through
-in one ragged batch and then decode a token at a time.  Norms, gates and residual sums are plain torch.
+in one ragged batch and then decode a token at a time.  Norms, gates and residual sums are plain torch, or with `fused` parts of the
+layers' own kernels: a layer is then six calls, and nothing between them is rounded that need not be.
 
     python -m paper_2203_12091_gb300.decoder        # random weights, prints tokens per second
 """
@@ -22,35 +23,45 @@ def rms_norm(x, weight, eps=1e-5):
 class Layer:
     """Grouped-head attention and a gated MLP, each behind a norm and added to its input."""
 
-    def __init__(self, width, heads, kv_heads, dim, hidden, gen, n_pages, page):
+    def __init__(self, width, heads, kv_heads, dim, hidden, gen, n_pages, page, fused=False):
+        def floats(n, k):
+            return torch.randn(n, k, generator=gen, device=gen.device) * k ** -0.5
+
         def weights(n, k):
-            return llm.Linear8.from_float(torch.randn(n, k, generator=gen, device=gen.device) * k ** -0.5)
-        self.heads, self.kv_heads, self.dim = heads, kv_heads, dim
+            return llm.Linear8.from_float(floats(n, k))
+        self.heads, self.kv_heads, self.dim, self.fused = heads, kv_heads, dim, fused
         self.qkv, self.out = weights((heads + 2 * kv_heads) * dim, width), weights(width, heads * dim)
-        self.gate_up, self.down = weights(2 * hidden, width), weights(width, hidden)
+        gate_up = floats(2 * hidden, width)
+        self.gate_up = llm.GatedLinear8.from_float(*gate_up.chunk(2)) if fused else llm.Linear8.from_float(gate_up)
+        self.down = weights(width, hidden)
         self.norm1, self.norm2 = (torch.ones(width, device=gen.device) for _ in range(2))
         self.cache = llm.KVCache.empty(n_pages, kv_heads, page, dim, gen.device)
 
     def __call__(self, x, pages, lens, starts, cos, sin):
         T, h, g = x.shape[0], self.heads, self.kv_heads
-        qkv = self.qkv(rms_norm(x, self.norm1)).view(T, h + 2 * g, self.dim)  # (its views go to the kernels as they are)
+        qkv = self.qkv(x, norm=self.norm1) if self.fused else self.qkv(rms_norm(x, self.norm1))
+        qkv = qkv.view(T, h + 2 * g, self.dim)  # (its views go to the kernels as they are)
         q = llm.kv_append(self.cache, pages, lens, qkv[:, h:h + g], qkv[:, h + g:], q=qkv[:, :h], starts=starts, cos=cos, sin=sin)
         a = llm.kv_attention(self.cache, pages, lens, q, starts=starts)
+        if self.fused:
+            x = self.out(a.view(T, h * self.dim), residual=x)
+            return self.down(self.gate_up(x, norm=self.norm2), residual=x)
         x = x + self.out(a.view(T, h * self.dim))
         gate, up = self.gate_up(rms_norm(x, self.norm2)).chunk(2, -1)
         return x + self.down(torch.nn.functional.silu(gate) * up)
 
 
 class Decoder:
-    """`max_seqs` sequences of up to `max_tokens` tokens each; every sequence has its own pages of each layer's cache."""
+    """`max_seqs` sequences of up to `max_tokens` tokens each; every sequence has its own pages of each layer's cache.  fused: see above
+    (the same weights; results differ from the other form's by roundings to dtype)."""
 
     def __init__(self, vocab=1000, width=512, layers=2, heads=8, kv_heads=2, dim=64, hidden=1024, max_seqs=8, max_tokens=512, page=32,
-                 dtype=torch.bfloat16, seed=0, device="cuda"):
+                 dtype=torch.bfloat16, seed=0, device="cuda", fused=False):
         gen = torch.Generator(device=device).manual_seed(seed)
         per_seq = -(-max_tokens // page)
-        self.dtype, self.max_tokens = dtype, max_tokens
+        self.dtype, self.max_tokens, self.fused = dtype, max_tokens, fused
         self.embed = torch.randn(vocab, width, generator=gen, device=device).to(dtype)
-        self.layers = [Layer(width, heads, kv_heads, dim, hidden, gen, max_seqs * per_seq, page) for _ in range(layers)]
+        self.layers = [Layer(width, heads, kv_heads, dim, hidden, gen, max_seqs * per_seq, page, fused) for _ in range(layers)]
         self.norm = torch.ones(width, device=device)
         self.head = llm.Linear8.from_float(torch.randn(vocab, width, generator=gen, device=device) * width ** -0.5)
         self.pages = torch.randperm(max_seqs * per_seq, generator=gen, device=device).int().view(max_seqs, per_seq)
@@ -64,7 +75,7 @@ class Decoder:
         x, pages = self.embed[tokens], self.pages[:lens.shape[0]]
         for layer in self.layers:
             x = layer(x, pages, lens, starts, self.cos, self.sin)
-        return self.head(rms_norm(x, self.norm), torch.float32)
+        return self.head(x, torch.float32, norm=self.norm) if self.fused else self.head(rms_norm(x, self.norm), torch.float32)
 
     def generate(self, prompts, count):
         """The `count` likeliest next tokens, one after the other, of each prompt (lists of tokens): int64 [B, count]."""
@@ -87,15 +98,16 @@ class Decoder:
 
 
 def main():
-    model = Decoder(vocab=32000, width=2048, layers=8, heads=16, kv_heads=4, dim=128, hidden=5632, max_seqs=32, max_tokens=1024, page=64)
     prompts = [[(7 * i + j) % 32000 for j in range(200 + 17 * i)] for i in range(32)]
-    model.generate(prompts, 4)
-    torch.cuda.synchronize()
-    at = time.perf_counter()
-    model.generate(prompts, 64)
-    torch.cuda.synchronize()
-    took = time.perf_counter() - at
-    print(f"{sum(map(len, prompts))} prompt tokens and 32 x 64 new ones in {took * 1e3:.1f} ms")
+    for fused in (False, True):
+        model = Decoder(vocab=32000, width=2048, layers=8, heads=16, kv_heads=4, dim=128, hidden=5632, max_seqs=32, max_tokens=1024, page=64, fused=fused)
+        model.generate(prompts, 4)
+        torch.cuda.synchronize()
+        at = time.perf_counter()
+        model.generate(prompts, 64)
+        torch.cuda.synchronize()
+        took = time.perf_counter() - at
+        print(f"{sum(map(len, prompts))} prompt tokens and 32 x 64 new ones in {took * 1e3:.1f} ms{', fused' if fused else ''}")
 
 
 if __name__ == "__main__":
