@@ -45,7 +45,7 @@ struct Plan {
 // epilogue: what the pairs take to finish and store a tile of 256 tokens, under the next tile's products or not.
 Plan plan_of(int64_t M, int32_t N, int32_t K, double epilogue) {
     Plan best = {true, {0, 0, 1, nullptr}, 0};
-    if (!many_tokens(M, N, K)) return best;
+    if (M <= 64 || N < 128 || K < 128) return best;
     const double pairs = many_pairs(), blocks = (K + LS_KB - 1) / LS_KB, tn = (N + 255) / 256;
     const double few_tiles = (double)((N + 127) / 128) * ((M + 127) / 128);
     int few_shares = 1;
