@@ -263,7 +263,7 @@ struct Turn {
 };
 
 template <int TOK, int EPI>
-__global__ void __launch_bounds__(LF_THREADS) layer_few_kernel(const __grid_constant__ FewArgs P) {
+__global__ void __launch_bounds__(LF_THREADS, 2) layer_few_kernel(const __grid_constant__ FewArgs P) {
     using namespace tc;
     constexpr bool HALF = TOK == HALVES;
     extern __shared__ unsigned char smem_raw[];

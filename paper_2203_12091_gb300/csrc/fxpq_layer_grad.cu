@@ -51,7 +51,6 @@ constexpr int GR_THREADS = 512, GR_KEEP = 3;
 template <bool GATE, int ACT, int DY, int PRE>
 __global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_constant__ GradRows G, int y_type) {
     pdl_wait();
-    if (G.early) pdl_next();
     constexpr bool NEEDS = GATE || ACT != FXPQ_ACT_NONE;
     constexpr int D = GATE ? 4 : 8;  // values of dy to eight channels
     const long long m = blockIdx.x;
@@ -134,6 +133,7 @@ __global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_c
     top = 0;
 #pragma unroll
     for (int w = 0; w < GR_THREADS / 32; ++w) top = max(top, part[w]);
+    if (G.early) pdl_next();
     const bool bad = top >= 0x7f800000u;
     // top < 2^e; the row's largest value lies in [2^14, 2^15), or as an integer in [2^22, 2^23)
     const int e = max(top ? ilogbf(__uint_as_float(top)) + 1 : 0, -100), up = G.split ? 23 : 15;

@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(QT_THREADS)
                            float* __restrict__ scale, int* status, const __grid_constant__ RowNorm norm) {
     constexpr bool HALF = sizeof(C) == 2;
     pdl_wait();
-    if (norm.early) pdl_next();
+    if (norm.early == 1) pdl_next();
     const T* row = x + (long long)blockIdx.x * x_stride;
     C* out = codes + (long long)blockIdx.x * c_stride;
     const int t = threadIdx.x, groups = K / 8, tail = 8 * groups + t;  // whole groups of eight; the rest of the row one value at a time
@@ -83,6 +83,7 @@ __global__ void __launch_bounds__(QT_THREADS)
             if (t == 0) row_inv = inv, scale[blockIdx.x] = sx;
         }
         __syncthreads();
+        if (norm.early == 2) pdl_next();
         const float inv = row_inv;
         each([&](int g, const Raw8<T>& v) {
             weights(g);
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(QT_THREADS)
     const bool live = top >= 7.888609052210118e-31f;  // 2^-100
     const float inv = live ? __fmul_rn(__frcp_rn(top), 127.0f) : 0.0f;
     if (t == 0) scale[blockIdx.x] = live ? __fmul_rn(top, 1.0f / 127.0f) : 0.0f;
+    if (norm.early == 2) pdl_next();
     // (a product is at most 127 (1 + 2^-22) and rounds to 127)
     auto scaled = [&](T v) {
         const float f = to_f32(v);

@@ -190,7 +190,7 @@ bool batch_ok(const fxpq_kv_batch* b);
 bool cache_ok(const fxpq_kv_cache* c);
 
 // Float rows to 8-bit codes as fp16, half_pitch(K) apart, zeros behind K (fxpq_linear.cu), under a norm or not.
-// early: the product may be set up while the codes are formed (pdl_next).
+// early: the product may be set up from the first block's start on (1), or as the codes are written (2; pdl_next).
 struct RowNorm {
     const float* weight;  // null: no norm
     float eps;
