@@ -50,7 +50,7 @@ Plan find_plan(int64_t M, int32_t N, int32_t K, double epilogue) {
     int few_shares = 1;
     while (few_shares < 8 && few_tiles * few_shares <= pairs && blocks >= 16 * few_shares) few_shares *= 2;
     double least = std::ceil(few_tiles * few_shares / (2 * pairs)) * (7.0 + std::ceil(blocks / few_shares) * 0.5);
-    if (few_tiles > 65535) least = 1e30;
+    if ((N + 127) / 128 > 65535 || (M + 127) / 128 > 65535) least = 1e30;  // (its grid)
     for (int nt = 128; nt <= 256; nt += 128) {
         const int64_t tiles = (int64_t)tn * ((M + nt - 1) / nt), full = tiles / (int64_t)pairs * (int64_t)pairs;
         if (tiles > INT32_MAX / 16) continue;
@@ -221,10 +221,11 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
     const int dyb = ftype_bytes(d.y_type), kept = d.pre_type == FXPQ_FT_F32 ? 4 : 2, some = d.gated ? 4 * dyb : 16;
     const int vec = (aligned(d.d_dy, some < 16 ? some : 16) && d.dy_stride * dyb % (some < 16 ? some : 16) == 0 ? 1 : 0) |
                     (aligned(d.d_pre, 16) && (int64_t)d.N * kept % 16 == 0 ? 2 : 0) | (aligned(d.d_sw, 16) ? 4 : 0) | (aligned(d.d_bias, 16) ? 8 : 0);
+    const int act = d.N > 0 ? d.activation : FXPQ_ACT_NONE;  // (rows of nothing read nothing)
     const GradRows G = {d.d_dy, d.dy_stride, d.d_pre, d.d_sx, d.d_sw, d.d_bias, (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32,
-                        d.activation, d.N, at.plan.few, split, vec, rows, (long long)half_pitch(d.N), (long long)d.M, scale,
+                        act, d.N, at.plan.few, split, vec, rows, (long long)half_pitch(d.N), (long long)d.M, scale,
                         status_ptr()};
-    fxpq_status rc = grad_rows(G, d.y_type, d.gated, st);
+    fxpq_status rc = grad_rows(G, d.y_type, d.N > 0 && d.gated, st);
     if (rc != FXPQ_OK) return rc;
     if (!split) return product<LAYER>({rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride}, {}, at.plan, part, st);
     rc = product<LAYER>({rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K}, {}, at.plan, part, st);

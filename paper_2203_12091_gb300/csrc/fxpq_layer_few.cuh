@@ -479,14 +479,9 @@ __global__ void __launch_bounds__(LF_THREADS, 2) layer_few_kernel(const __grid_c
 
 template <int TOK, int EPI>
 fxpq_status launch_few(FewArgs& P, cudaStream_t st) {
-    static bool set = false;
     const auto kernel = layer_few_kernel<TOK, EPI>;
-    if (!set) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TOK == FLOATS ? LF_SMEM : lf_smem(128, 128, 4, TOK, 0)) !=
-            cudaSuccess)
-            return FXPQ_ERR_CUDA;
-        set = true;
-    }
+    static std::atomic<uint64_t> set{0};
+    if (!allow_smem(kernel, TOK == FLOATS ? LF_SMEM : lf_smem(128, 128, 4, TOK, 0), set)) return FXPQ_ERR_CUDA;
     const long long tn = (P.N + 127) / 128, tm = (P.M + P.rows - 1) / P.rows;
     if (tn > 65535 || tm > 65535) return FXPQ_ERR_UNSUPPORTED;
     P.stages = P.cols <= 32 || P.cols > 64 ? 4 : 3;

@@ -661,14 +661,23 @@ struct ManyPlan {
     float* part;
 };
 
+// Lets a kernel use so much dynamic shared memory, once on each device.
+template <typename Kernel>
+bool allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& set) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (set.load(std::memory_order_relaxed) & bit) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    set.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
 template <int NT, int EPI, int FORM>
 fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
-    static bool set = false;
     const auto kernel = linear_many_kernel<NT, EPI, FORM>;
-    if (!set) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LM_SMEM) != cudaSuccess) return FXPQ_ERR_CUDA;
-        set = true;
-    }
+    static std::atomic<uint64_t> set{0};
+    if (!allow_smem(kernel, LM_SMEM, set)) return FXPQ_ERR_CUDA;
     const long long tn = ((long long)P.N + 255) / 256, tm = (P.M + NT - 1) / NT;
     if (tn * tm > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
     P.tiles_n = (int)tn, P.tiles_m = (int)tm, P.n_tiles = (int)(tn * tm);

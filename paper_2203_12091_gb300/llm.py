@@ -155,12 +155,17 @@ class _Layer8:
         flat = x.dim() == 2
         rows = x if flat and x.is_cuda and x.is_contiguous() else _float_rows(name, x)
         M, K = rows.shape
-        w, bias = self.w, self.bias
+        w, bias, dev = self.w, self.bias, x.device
+        if dev.index != torch.cuda.current_device():
+            with torch.cuda.device(dev):  # (its current stream)
+                return self._forward(name, x, dtype, norm, eps, act, residual, keep)
+        if w.device != dev or (norm is not None and norm.device != dev) or (residual is not None and residual.device != dev):
+            raise ValueError(f"{name}: rows, weights, norm and residual must be on one device, rows are on {dev}, weights on {w.device}")
         N, inputs = w.shape
         if K != inputs:
             raise ValueError(f"{name}: rows of {inputs} values are needed, got {tuple(x.shape)}")
         wide = N // 2 if self.gated else N
-        xt, yt, dev = _FT.get(x.dtype), _FT.get(dtype), x.device
+        xt, yt = _FT.get(x.dtype), _FT.get(dtype)
         if xt is None or yt is None:
             _ftype(name, x.dtype if xt is None else dtype)
         nrm = res = res_stride = pre_at = sx_at = 0
@@ -197,6 +202,9 @@ class _Layer8:
 
     def _gradient(self, name, dy, dtype, act, kept):
         """dx [..., K] of `dtype` for dy [..., N or N / 2] and what `_forward` kept."""
+        if dy.device.index != torch.cuda.current_device():
+            with torch.cuda.device(dy.device):
+                return self._gradient(name, dy, dtype, act, kept)
         flat = dy.dim() == 2
         rows = dy if flat and dy.is_contiguous() else _float_rows(name, dy)
         M, (N, K), wt, bias = rows.shape[0], self.w.shape, self.wt, self.bias

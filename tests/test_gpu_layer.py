@@ -562,3 +562,49 @@ def test_more_rows_whose_codes_the_product_forms(ops, M, K, x):
     for N in (130, 512):
         check_layer(ops, rng, M, N, K, x, "f32", "silu", True, True, True)
         check_gated(ops, rng, M, N // 2, K, x, "bf16", "silu", True, False)
+
+
+def test_layers_without_channels_or_inputs(ops):
+    """No inputs: the biases alone; no channels: no gradient."""
+    one = torch.ones(24, device="cuda")
+    layer = ops.Linear8(torch.zeros((24, 0), dtype=torch.int8, device="cuda"), one, one * 3).with_gradient()
+    y = layer(torch.zeros(70, 0, device="cuda"), activation="silu", norm=torch.zeros(0, device="cuda"))
+    assert torch.allclose(y, torch.nn.functional.silu(one * 3).expand(70, 24))
+    none = ops.Linear8(torch.zeros((0, 48), dtype=torch.int8, device="cuda"), one[:0].contiguous()).with_gradient()
+    x = torch.ones(70, 48, device="cuda", requires_grad=True)
+    y = none(x, activation="silu")
+    assert y.shape == (70, 0) and torch.equal(torch.autograd.grad(y, x, torch.zeros_like(y))[0], torch.zeros_like(x))
+
+
+def test_a_residual_that_is_the_output(ops):
+    """The header lets a residual be y itself, on every path."""
+    rng = np.random.default_rng(0)
+    for M, N, K in ((3, 256, 512), (40, 256, 2048), (300, 256, 512), (300, 255, 512), (700, 512, 8192), (1000, 4096, 256)):
+        layer, x, r = Weights(rng, N, K, True).layer(ops), rows(rng, M, K, "bf16"), rows(rng, M, N, "bf16")
+        want = layer(x, activation="silu", residual=r)
+        pitch = (K + 15) // 16 * 16
+        d = L.LayerDesc(x.data_ptr(), K, None, layer.w.data_ptr(), pitch, layer.w_scale.data_ptr(), layer.bias.data_ptr(), r.data_ptr(), N, r.data_ptr(),
+                        N, None, None, M, N, K, L.FT_BF16, L.FT_BF16, L.ACT_SILU, 0, L.FT_F16, 0.0)
+        ws = torch.empty(max(1, F.fxpq_layer_workspace(d)), dtype=torch.uint8, device="cuda")
+        F.fxpq_layer_forward(d, ws)
+        assert torch.equal(r, want), (M, N, K)
+
+
+@pytest.mark.parametrize("M", [90, 140, 300, 1300])
+def test_unaligned_tensors(ops, M):
+    """Outputs, residuals, gradients and kept sums that begin or step at odd places give what aligned ones give."""
+    rng = np.random.default_rng(M)
+    W = Weights(rng, 256, 512, True)
+    layer, x = W.layer(ops).with_gradient(), rows(rng, M, 512, "bf16").requires_grad_()
+    wide = rows(rng, M, 261, "bf16")
+    r, dy = wide[:, 3:259], rows(rng, M, 259, "bf16")[:, 2:258]
+    y = layer(x, activation="silu", residual=r.contiguous())
+    assert torch.equal(layer(x, activation="silu", residual=r), y)
+    dx = torch.autograd.grad(y, x, dy.contiguous(), retain_graph=True)[0]
+    assert torch.equal(torch.autograd.grad(y, x, dy)[0], dx)
+    big = torch.zeros(M * 257 + 1, dtype=torch.bfloat16, device="cuda")
+    d = L.LayerDesc(x.data_ptr(), 512, None, layer.w.data_ptr(), 512, layer.w_scale.data_ptr(), layer.bias.data_ptr(), r.data_ptr(), 261,
+                    big.data_ptr() + 2, 257, None, None, M, 256, 512, L.FT_BF16, L.FT_BF16, L.ACT_SILU, 0, L.FT_F16, 0.0)
+    F.fxpq_layer_forward(d, torch.empty(max(1, F.fxpq_layer_workspace(d)), dtype=torch.uint8, device="cuda"))
+    got = big[1:].view(M, 257)
+    assert torch.equal(got[:, :256], y.detach()) and not got[:, 256].any()
