@@ -129,11 +129,26 @@ struct SigAct {
     }
 };
 
+// A warp's residuals, two channels of ROWS / 2 tokens a lane: the first asked for before the sums are there, the others three steps ahead.  (Asked for a step ahead, a tile's epilogue took 21 thousand clocks with them and 8 without; y may be the
+// residual, so the compiler keeps every load behind the stores before it.)
+template <int ROWS>
+struct Residuals {
+    const char* at;  // token odd's two channels
+    long long step;  // two tokens, in bytes
+    static constexpr int HELD = ROWS / 8 * 2 > 24 ? 24 : ROWS / 8 * 2;
+    uint32_t r[HELD];
+    __device__ __forceinline__ void ask(int i, int cols) {  // of token 2 i + odd
+        uint32_t w = 0;
+        if (2 * i < cols) w = *reinterpret_cast<const uint32_t*>(at + i * step);
+        r[i % HELD] = w;
+    }
+};
+
 // The epilogue of a warp's 32 channels and ROWS tokens for LAYER and GATED.  Everything goes by pairs: two lanes exchange sums so that
 // each holds two channels of one token.  The fast form holds all sums in registers (the epilogue's warps have taken the other
 // warps'), and has given the accumulators back before it computes: for GATED 16384 of 4096, 8192 tokens, see fxpq_layer.cu.
 template <int ROWS, int EPI, int FORM, typename Sum>
-__device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, const float* sxs, float2 sw, float2 bias, int c0, int odd, long long m0, int cols) {
+__device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, const float* sxs, float2 sw, float2 bias, int c0, int odd, long long m0, int cols, Residuals<ROWS>& held) {
     const bool f16 = P.y_type == FXPQ_FT_F16;
     const SigAct sig(P.e.act);
     const float low = P.e.act == FXPQ_ACT_RELU ? 0.0f : -__int_as_float(0x7f800000);
@@ -141,7 +156,7 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
     sxs += odd;
     const float ps = P.e.pre_scale;
     // (addresses that walk along the tokens: computed from the token each, they took more registers than there are)
-    const long long y_step = 2 * P.ys * 2, r_step = 2 * P.e.res_stride * 2, p_step = 2LL * P.N * 2;
+    const long long y_step = 2 * P.ys * 2, p_step = 2LL * P.N * 2;
     char* pre = P.e.pre ? static_cast<char*>(P.e.pre) + ((m0 + odd) * P.N + c0) * 2 : nullptr;
     auto act = [&](float z) { return FORM == SIGMOID ? sig(z) : FORM == NORMAL ? gelu(z) : fmaxf(z, low); };
     auto pack = [&](float a, float b) {
@@ -154,19 +169,6 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
     constexpr int STEP = 8;
     const int second = (threadIdx.x >> 1) & 1, reach = EPI == GATED ? cols - 2 * second : cols;
     char* y = static_cast<char*>(P.y) + (EPI == GATED ? (m0 + odd + 2 * second) * P.ys + (c0 >> 1) - second : (m0 + odd) * P.ys + c0) * 2;
-    const char* res = static_cast<const char*>(P.e.res) + ((m0 + odd) * P.e.res_stride + c0) * 2;
-    // Residuals of the next step's tokens are on their way while these are stored: y may be the residual, so the compiler keeps every
-    // load behind the stores before it (one at a time, 2000 x 4096 of 2048 took 53 us).
-    uint32_t r[STEP];
-    auto ask = [&](int i) {
-        r[i % STEP] = 0;
-        if (2 * i < cols) r[i % STEP] = *reinterpret_cast<const uint32_t*>(res);
-        res += r_step;
-    };
-    if (EPI == LAYER && P.e.res) {
-#pragma unroll
-        for (int i = 0; i < STEP; ++i) ask(i);
-    }
 #pragma unroll
     for (int i0 = 0; i0 < ROWS / 2; i0 += STEP) {
         float a[STEP], b[STEP];  // channels c0, c0 + 1 of token 2 (i0 + i) + odd
@@ -204,13 +206,12 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
             if (P.e.res) {
 #pragma unroll
                 for (int i = 0; i < STEP; ++i) {
-                    const float2 f = pair_f32(r[i], P.y_type);
+                    const float2 f = pair_f32(held.r[(i0 + i) % held.HELD], P.y_type);
                     a[i] += f.x, b[i] += f.y;
                 }
-                if (i0 + STEP < ROWS / 2) {
 #pragma unroll
-                    for (int i = 0; i < STEP; ++i) ask(i0 + STEP + i);
-                }
+                for (int i = 0; i < STEP; ++i)
+                    if (i0 + i + held.HELD < ROWS / 2) held.ask(i0 + i + held.HELD, cols);
             }
 #pragma unroll
             for (int i = 0; i < STEP; ++i) {
@@ -308,9 +309,9 @@ __device__ __forceinline__ void epilogue_any(const ManyArgs& P, const uint32_t (
     }
 }
 
-// Registers of a thread: the launch holds 512 x 128, of which the epilogue's warps take 256 x 176 and the others 128 x 56 (copies, products)
-// and 128 x 96 (converters).
-constexpr int LM_REGS = 128, LM_REGS_EPI = 176, LM_REGS_ISSUE = 56, LM_REGS_CONV = 96;
+// Registers of a thread: the launch holds 512 x 128, of which the epilogue's warps take 256 x 192 and the others 128 x 40 (copies, products)
+// and 128 x 80 (converters).
+constexpr int LM_REGS = 128, LM_REGS_EPI = 192, LM_REGS_ISSUE = 40, LM_REGS_CONV = 80;
 static_assert(LM_REGS_ISSUE + LM_REGS_CONV + 2 * LM_REGS_EPI <= 4 * LM_REGS, "the launch's registers");
 
 // NT: tokens of a tile, 256 or, where those tiles would leave pairs idle, 128.
@@ -516,9 +517,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
             const float sw = !P.sw ? 1.0f : ch < P.N ? __ldg(P.sw + ch) : 0.0f, bias = P.bias && ch < P.N ? __ldg(P.bias + ch) : 0.0f;
             for (int i = lane; i < ROWS; i += 32) sxs[i] = !P.sx ? 1.0f : m0 + i < P.M ? __ldg(P.sx + m0 + i) : 0.0f;
             __syncwarp();
+            const int cols = (int)min((long long)ROWS, P.M - m0);
+            Residuals<ROWS> held;
+            if constexpr (EPI == LAYER) {
+                const int odd = lane & 1, c0 = ch - odd;
+                held.at = static_cast<const char*>(P.e.res) + ((m0 + odd) * P.e.res_stride + c0) * 2, held.step = 2 * P.e.res_stride * 2;
+                if (P.e.fast && P.e.res && t < P.whole) {
+#pragma unroll
+                    for (int i = 0; i < held.HELD; ++i) held.ask(i, c0 < P.N ? cols - odd : 0);
+                }
+            }
             if (!wait_warp_cluster(acc_full, it & 1, abort, P.status)) break;
             tc_fence_after();
-            const int cols = (int)min((long long)ROWS, P.M - m0);
             if constexpr (EPI != PLAIN) {
                 const int odd = lane & 1, c0 = ch - odd;
                 const float sw_o = __shfl_xor_sync(0xffffffffu, sw, 1), bias_o = __shfl_xor_sync(0xffffffffu, bias, 1);
@@ -538,7 +548,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                     for (int i = 0; i < ROWS; ++i)
                         if (i < cols) to[i * 128] = __uint_as_float(v[i / 32][i % 32]);
                 } else if (P.e.fast) {
-                    epilogue_fast<ROWS, EPI, FORM>(P, [&](int t) { return __uint_as_float(v[t / 32][t % 32]); }, sxs, sw2, bias2, c0, odd, m0, cols);
+                    epilogue_fast<ROWS, EPI, FORM>(P, [&](int t) { return __uint_as_float(v[t / 32][t % 32]); }, sxs, sw2, bias2, c0, odd, m0, cols, held);
                 } else {  // 16 tokens at a time, in one place of the code: the others move up
 #pragma unroll 1
                     for (int c = 0; c < ROWS; c += 16) {
