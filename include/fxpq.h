@@ -549,7 +549,7 @@ FXPQ_API fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64_t
  * Everything after the sum is in fp32, in the order written (a sum * sx past fp32 is infinite), with one rounding to y_type.
  * Rows of x, w, y: as for fxpq_linear_tokens.  residual: rows of N values of y_type, residual_stride elements apart; it may be y itself.
  * Not with `gated`, which needs an activation and an even N: weight rows 2 j and 2 j + 1 are gate and value of y's column j.
- * For a gradient (fxpq_layer_gradient): d_pre, contiguous [M][N] of pre_type, gets the sums before any scale (F32: as they are; F16: times
+ * For a gradient (fxpq_layer_gradient): d_pre, M rows of N values of pre_type, (N + 7) / 8 * 8 of them apart, gets the sums before any scale (F32: as they are; F16: times
  * 2^-p, p by K alone such that the largest possible sum fits: they are integers, so every one keeps 11 bits), d_sx the rows' scales.
  * Either may be NULL.  eps: 0 to 1.  Workspace: fxpq_layer_workspace bytes, 256-byte aligned, scratch (it may be 0: then d_ws may be NULL). */
 typedef enum { FXPQ_ACT_NONE = 0, FXPQ_ACT_RELU = 1, FXPQ_ACT_SILU = 2, FXPQ_ACT_GELU = 3, FXPQ_ACT_GELU_TANH = 4 } fxpq_activation;

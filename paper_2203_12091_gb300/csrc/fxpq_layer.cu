@@ -11,19 +11,18 @@ namespace fxpq {
 namespace llm {
 namespace {
 
-// dx = (4096 high sums + low sums) * scale
+// dx = (4096 high sums + low sums) * scale, a block a row (and 1024 of its values).
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ sums, const float* __restrict__ scale, long long M, int K,
                                                          float* __restrict__ dx, long long dx_stride) {
     pdl_wait();
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < M * K; i += (long long)gridDim.x * 256) {
-        const long long m = i / K;
-        dx[m * dx_stride + (i - m * K)] = fmaf(sums[i], 4096.0f, sums[M * K + i]) * __ldg(scale + m);
+    const long long m = blockIdx.x;
+    const float s = __ldg(scale + m);
+    const float *hi = sums + m * K, *lo = hi + M * K;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = blockIdx.y * 1024 + i * 256 + threadIdx.x;
+        if (k < K) dx[m * dx_stride + k] = fmaf(hi[k], 4096.0f, lo[k]) * s;
     }
-}
-
-unsigned blocks_of(long long n) {
-    const long long b = (n + 255) / 256, most = 64LL * num_sms();
-    return (unsigned)(b < most ? b : most);
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -110,7 +109,7 @@ fxpq_status product(const Product& p, const Epi& e, Plan plan, float* part, cuda
     const fxpq_status rc = product_many<EPI>(p.rows, (size_t)pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e,
                                              &plan.many, &args);
     if (rc != FXPQ_OK || !plan.bytes) return rc;
-    args.e.vec = fours<EPI>(e, p.N, p.y_type, p.y, p.y_stride);
+    args.e.vec = fours<EPI>(e, p.y_type, p.y, p.y_stride);
     launch_pdl(finish_kernel<EPI>, dim3(2 * (unsigned)(args.n_tiles - args.whole), plan.many.nt / 32), dim3(256), 0, st, args, plan.many.nt);
     return after_launch("finish");
 }
@@ -173,7 +172,7 @@ extern "C" fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, s
     // The product of few rows is let in while the quantizer runs, for rows past 8192 as its blocks (of 512 threads and more) end: placed around
     // them earlier, clusters of 8 took a second round (17 x 4096 of 16384 26.8 us, so 18.5; without 19.2).
     const RowNorm norm = {d.d_norm, d.eps, aligned(d.d_norm, 16), !at.end || !at.plan.few ? 0 : d.K > 8192 ? 2 : 1};
-    const Epi e = {d.d_residual, d.residual_stride, d.d_pre, 1.0f / (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32, d.activation};
+    const Epi e = {d.d_residual, d.residual_stride, d.d_pre, 1.0f / (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32, d.activation, pre_pitch(d.N)};
     if (at.end == 0) {
         const int vec = aligned(d.d_x, 16) && d.x_stride * ftype_bytes(d.x_type) % 16 == 0;
         const FloatRows rows = {d.d_x, d.x_stride, d.x_type, vec, d.K, d.d_sx, norm};
@@ -198,7 +197,7 @@ extern "C" size_t fxpq_layer_gradient_workspace(const fxpq_layer_grad* d) {
 extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_ws, size_t ws_bytes, void* stream) {
     if (!grad) return FXPQ_ERR_INVALID_ARG;
     const fxpq_layer_grad& d = *grad;
-    if (!sizes_ok(d.M, d.N, d.K) || d.M > INT32_MAX / 2 || !ftype_ok(d.y_type) || !ftype_ok(d.dx_type) || !act_ok(d.activation) || d.gated < 0 ||
+    if (!sizes_ok(d.M, d.N, d.K) || d.M > INT32_MAX / 2 || d.K > 65535 * 1024 || !ftype_ok(d.y_type) || !ftype_ok(d.dx_type) || !act_ok(d.activation) || d.gated < 0 ||
         d.gated > 1 || (d.pre_type != FXPQ_FT_F16 && d.pre_type != FXPQ_FT_F32))
         return FXPQ_ERR_INVALID_ARG;
     if (d.gated && (d.N % 2 || d.activation == FXPQ_ACT_NONE)) return FXPQ_ERR_INVALID_ARG;
@@ -218,9 +217,9 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
     float* scale = reinterpret_cast<float*>(ws + at.rows);
     float *sums = reinterpret_cast<float*>(ws + at.parts), *part = reinterpret_cast<float*>(ws + at.sums);
     const bool split = d.dx_type == FXPQ_FT_F32;
-    const int dyb = ftype_bytes(d.y_type), kept = d.pre_type == FXPQ_FT_F32 ? 4 : 2, some = d.gated ? 4 * dyb : 16;
+    const int dyb = ftype_bytes(d.y_type), some = d.gated ? 4 * dyb : 16;
     const int vec = (aligned(d.d_dy, some < 16 ? some : 16) && d.dy_stride * dyb % (some < 16 ? some : 16) == 0 ? 1 : 0) |
-                    (aligned(d.d_pre, 16) && (int64_t)d.N * kept % 16 == 0 ? 2 : 0) | (aligned(d.d_sw, 16) ? 4 : 0) | (aligned(d.d_bias, 16) ? 8 : 0);
+                    (aligned(d.d_pre, 16) ? 2 : 0) | (aligned(d.d_sw, 16) ? 4 : 0) | (aligned(d.d_bias, 16) ? 8 : 0);
     const int act = d.N > 0 ? d.activation : FXPQ_ACT_NONE;  // (rows of nothing read nothing)
     const GradRows G = {d.d_dy, d.dy_stride, d.d_pre, d.d_sx, d.d_sw, d.d_bias, (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32,
                         act, d.N, at.plan.few, split, vec, rows, (long long)half_pitch(d.N), (long long)d.M, scale,
@@ -230,7 +229,7 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
     if (!split) return product<LAYER>({rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride}, {}, at.plan, part, st);
     rc = product<LAYER>({rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K}, {}, at.plan, part, st);
     if (rc != FXPQ_OK) return rc;
-    launch_pdl(join_parts_kernel, dim3(blocks_of(d.M * d.K)), dim3(256), 0, st, static_cast<const float*>(sums), static_cast<const float*>(scale), (long long)d.M,
-               (int)d.K, static_cast<float*>(d.d_dx), (long long)d.dx_stride);
+    launch_pdl(join_parts_kernel, dim3((unsigned)d.M, (unsigned)((d.K + 1023) / 1024)), dim3(256), 0, st, static_cast<const float*>(sums),
+               static_cast<const float*>(scale), (long long)d.M, (int)d.K, static_cast<float*>(d.d_dx), (long long)d.dx_stride);
     return after_launch("layer_join_parts");
 }

@@ -74,6 +74,9 @@ inline int sum_shift(int32_t K) {
     return p;
 }
 
+// Elements between rows of kept sums: whole 16 bytes.
+__host__ __device__ inline long long pre_pitch(int32_t N) { return ((long long)N + 7) / 8 * 8; }
+
 // The rows of a gradient, dz * sw (fxpq_layer_grad.cu).
 struct GradRows {
     const void* dy;

@@ -181,7 +181,7 @@ __device__ __forceinline__ void finish_four(const Args& P, const Epi& e, long lo
     float v[4] = {fmaf(a.x * s, sw[0], bias[0]), fmaf(a.y * s, sw[1], bias[1]), fmaf(a.z * s, sw[2], bias[2]), fmaf(a.w * s, sw[3], bias[3])};
     if (e.pre) {
         const float k = e.pre_f32 ? 1.0f : e.pre_scale, keep[4] = {a.x * k, a.y * k, a.z * k, a.w * k};
-        store_some<4>(e.pre, e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, m * P.N + ch, keep, left, e.vec & 4);
+        store_some<4>(e.pre, e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, m * e.pre_stride + ch, keep, left, e.vec & 4);
     }
     if constexpr (EPI == GATED) {
         const float y[2] = {activate(v[0], e.act) * v[1], activate(v[2], e.act) * v[3]};
@@ -199,10 +199,10 @@ __device__ __forceinline__ void finish_four(const Args& P, const Epi& e, long lo
 }
 // Which of outputs, residuals and kept sums lie in aligned accesses of four channels (gated outputs: of two).
 template <int EPI>
-inline int fours(const Epi& e, int N, int y_type, const void* y, int64_t y_stride) {
+inline int fours(const Epi& e, int y_type, const void* y, int64_t y_stride) {
     const int type = ftype_bytes(y_type), each = EPI == GATED ? 2 : 4, kept = e.pre_f32 ? 4 : 2;
     return (aligned(y, each * type) && y_stride % each == 0 ? 1 : 0) | (aligned(e.res, 4 * type) && e.res_stride % 4 == 0 ? 2 : 0) |
-           (aligned(e.pre, 4 * kept) && N % 4 == 0 ? 4 : 0);
+           (aligned(e.pre, 4 * kept) && e.pre_stride % 4 == 0 ? 4 : 0);
 }
 
 // The sums that pairs of CTAs left in memory, added over a tile's shares in their order, and what follows them: a warp has four tokens of
@@ -566,7 +566,7 @@ fxpq_status few_product(const __half* half, int64_t x_stride, const float* d_sx,
     }
     P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.y_type = y_type;
     P.status = status_ptr();
-    P.e.vec = fours<EPI>(e, N, y_type, d_y, y_stride);
+    P.e.vec = fours<EPI>(e, y_type, d_y, y_stride);
     if (!rows) return launch_few<HALVES, EPI>(P, st);
     P.f = *rows;
     return launch_few<FLOATS, EPI>(P, st);

@@ -12,12 +12,22 @@ __device__ __forceinline__ float one_any(const void* p, int type, long long at) 
                                : type == FXPQ_FT_F16 ? to_f32(static_cast<const __half*>(p)[at]) : to_f32(static_cast<const __nv_bfloat16*>(p)[at]);
 }
 
-// N values as they lie in memory, aligned (8 to 32 bytes), and as fp32.
+// N values as they lie in memory (vec: aligned, 8 to 32 bytes), and as fp32.
 template <int N, int BYTES>
 struct Words {
     uint32_t w[N * BYTES / 4];
-    __device__ __forceinline__ void load(const void* p, long long at) {
+    __device__ __forceinline__ void load(const void* p, long long at, bool vec = true) {
         const char* q = static_cast<const char*>(p) + at * BYTES;
+        if (!vec) {
+#pragma unroll
+            for (int i = 0; i < N * BYTES / 4; ++i) {
+                if constexpr (BYTES == 4)
+                    w[i] = reinterpret_cast<const uint32_t*>(q)[i];
+                else
+                    w[i] = __byte_perm(reinterpret_cast<const unsigned short*>(q)[2 * i], reinterpret_cast<const unsigned short*>(q)[2 * i + 1], 0x5410);
+            }
+            return;
+        }
         if constexpr (N * BYTES == 8) {
             const uint2 v = *reinterpret_cast<const uint2*>(q);
             w[0] = v.x, w[1] = v.y;
@@ -44,9 +54,9 @@ struct Words {
 
 // One block a row: as fp16 with a power of two of the row's own; split: in two parts, integers up to 2^11 (exact in fp16, as are their
 // products' sums below 2^24), the lower ones M rows further on.
-// Bytes bound it (dy and the sums in, the row out): 8192 rows of 2 x 5632 460 MB, 68 us.  Aligned rows stay in registers between their maximum
-// and the rounding, GR_KEEP groups of eight channels a thread, which are also on their way together; what does not fit, and rows
-// that are not aligned, are formed again.  (A group at a time, kept in shared memory, the same rows took 185 us.)
+// Bytes bound it (dy and the sums in, the row out): 8192 rows of 2 x 5632 460 MB, 68 us.  Rows stay in registers between their maximum
+// and the rounding, GR_KEEP groups of eight channels a thread, which are also on their way together; what does not fit, the last
+// group of some, and all of constants or sums that are not aligned, is formed again.  (A group at a time, kept in shared memory, the same rows took 185 us.)
 constexpr int GR_THREADS = 512, GR_KEEP = 3;
 template <bool GATE, int ACT, int DY, int PRE>
 __global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_constant__ GradRows G, int y_type) {
@@ -56,6 +66,7 @@ __global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_c
     const long long m = blockIdx.x;
     const int t = threadIdx.x, N = G.N, groups = (N + 7) / 8, pre_type = PRE == 4 ? FXPQ_FT_F32 : FXPQ_FT_F16;
     const float sx = NEEDS ? __ldg(G.sx + m) * (PRE == 4 ? 1.0f : G.pre_unit) : 0.0f;  // (a power of two: z as in the forward pass)
+    const long long pitch = pre_pitch(N);
     auto compute = [&](const float (&d)[D], float (&a)[8], const float (&w)[8], const float (&b)[8], float (&v)[8]) {
         if constexpr (NEEDS) {
 #pragma unroll
@@ -84,7 +95,7 @@ __global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_c
             const bool in = e < left;
             if (e < D) d[e] = (GATE ? 2 * e : e) < left ? one_any(G.dy, y_type, m * G.dy_stride + g * D + e) : 0.0f;
             w[e] = in ? __ldg(G.sw + n + e) : 0.0f;
-            a[e] = NEEDS && in ? one_any(G.pre, pre_type, m * N + n + e) : 0.0f;
+            a[e] = NEEDS && in ? one_any(G.pre, pre_type, m * pitch + n + e) : 0.0f;
             b[e] = NEEDS && G.bias && in ? __ldg(G.bias + n + e) : 0.0f;
         }
         compute(d, a, w, b, v);
@@ -94,7 +105,7 @@ __global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_c
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
     };
-    const int whole = (G.vec | (NEEDS ? 0 : 2) | (G.bias ? 0 : 8)) == 15 ? N / 8 : 0;  // groups in aligned accesses
+    const int whole = (G.vec | 1 | (NEEDS ? 0 : 2) | (G.bias ? 0 : 8)) == 15 ? N / 8 : 0;  // groups whose constants and sums come in aligned accesses
     float keep[GR_KEEP][8];
     {
         Words<D, DY> d[GR_KEEP];
@@ -103,8 +114,8 @@ __global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_c
         for (int s = 0; s < GR_KEEP; ++s) {
             const int g = t + s * GR_THREADS;
             if (g >= whole) continue;
-            d[s].load(G.dy, m * G.dy_stride + g * D);
-            if constexpr (NEEDS) a[s].load(G.pre, m * N + 8 * g);
+            d[s].load(G.dy, m * G.dy_stride + g * D, G.vec & 1);
+            if constexpr (NEEDS) a[s].load(G.pre, m * pitch + 8 * g);
         }
 #pragma unroll
         for (int s = 0; s < GR_KEEP; ++s) {

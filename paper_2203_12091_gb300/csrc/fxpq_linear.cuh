@@ -25,9 +25,10 @@ enum { PLAIN, LAYER, GATED };
 struct Epi {
     const void* res;
     long long res_stride;
-    void* pre;
+    void* pre;  // rows pre_stride apart
     float pre_scale;
     int pre_f32, act;
+    long long pre_stride;
     int vec;   // outputs, residuals and kept sums (bits 1, 2, 4) of four channels (few rows; gated outputs two), or of two, in aligned accesses each
     int fast;  // many: 16-bit outputs, pairs of everything aligned
 };
@@ -156,8 +157,8 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
     sxs += odd;
     const float ps = P.e.pre_scale;
     // (addresses that walk along the tokens: computed from the token each, they took more registers than there are)
-    const long long y_step = 2 * P.ys * 2, p_step = 2LL * P.N * 2;
-    char* pre = P.e.pre ? static_cast<char*>(P.e.pre) + ((m0 + odd) * P.N + c0) * 2 : nullptr;
+    const long long y_step = 2 * P.ys * 2, p_step = 2 * P.e.pre_stride * 2;
+    char* pre = P.e.pre ? static_cast<char*>(P.e.pre) + ((m0 + odd) * P.e.pre_stride + c0) * 2 : nullptr;
     auto act = [&](float z) { return FORM == SIGMOID ? sig(z) : FORM == NORMAL ? gelu(z) : fmaxf(z, low); };
     auto pack = [&](float a, float b) {
         if (f16) return h2_bits(__floats2half2_rn(a, b));
@@ -263,7 +264,7 @@ __device__ __forceinline__ void epilogue_any(const ManyArgs& P, const uint32_t (
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float keep[2] = {a[i] * k, b[i] * k};
-            if (2 * i < cols) store_some<2>(P.e.pre, P.e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, (m0 + 2 * i) * P.N + c0, keep, left, vec & 4);
+            if (2 * i < cols) store_some<2>(P.e.pre, P.e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, (m0 + 2 * i) * P.e.pre_stride + c0, keep, left, vec & 4);
         }
     }
 #pragma unroll
@@ -717,7 +718,7 @@ fxpq_status product_many(const __half* half, size_t pitch, const float* d_sx, co
     if constexpr (EPI != PLAIN) {
         const int type = ftype_bytes(y_type), kept = e.pre_f32 ? 4 : 2;
         P.e.vec = (aligned(d_y, 2 * type) && y_stride % 2 == 0 ? 1 : 0) | (aligned(e.res, 2 * type) && e.res_stride % 2 == 0 ? 2 : 0) |
-                  (aligned(e.pre, 2 * kept) && N % 2 == 0 ? 4 : 0);
+                  (aligned(e.pre, 2 * kept) && e.pre_stride % 2 == 0 ? 4 : 0);
         // (a gate that is cut, the rarest form, has no kernel of its own)
         P.e.fast = y_type != FXPQ_FT_F32 && P.e.vec == 7 && N % (EPI == GATED ? 4 : 2) == 0 && !(e.pre && e.pre_f32) &&
                    !(EPI == GATED && e.act == FXPQ_ACT_RELU);

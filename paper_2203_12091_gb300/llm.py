@@ -135,6 +135,11 @@ def _activation(name, activation):
     return act
 
 
+def _kept_row(N, wide):
+    """Bytes of a row of kept sums."""
+    return (N + 7) // 8 * 8 * (4 if wide else 2)
+
+
 class _Layer8:
     """What layers with 8-bit weights share: w [N, K] codes, w_scale [N], bias [N] or None, and after `with_gradient` wt, the codes
     transposed."""
@@ -184,7 +189,7 @@ class _Layer8:
         y = _empty((M, wide), dtype=dtype, device=dev)
         kept, pre_t = None, L.FT_F32 if xt == L.FT_F32 or yt == L.FT_F32 else L.FT_F16
         if keep and act:
-            room = (M * N * (4 if pre_t == L.FT_F32 else 2) + 15) // 16 * 16
+            room = M * _kept_row(N, pre_t == L.FT_F32)
             kept = _empty(room + 4 * M, dtype=_u8, device=dev)
             pre_at = kept.data_ptr()
             sx_at = pre_at + room
@@ -212,7 +217,7 @@ class _Layer8:
         xt, yt = _FT[dtype], _FT[dy.dtype]
         wide32 = xt == L.FT_F32 or yt == L.FT_F32
         pre = 0 if kept is None else kept.data_ptr()
-        desc = _LAYER_GRAD(rows.data_ptr(), rows.stride(0), pre, pre and pre + (M * N * (4 if wide32 else 2) + 15) // 16 * 16, self.w_scale.data_ptr(),
+        desc = _LAYER_GRAD(rows.data_ptr(), rows.stride(0), pre, pre and pre + M * _kept_row(N, wide32), self.w_scale.data_ptr(),
                            0 if bias is None else bias.data_ptr(), wt.data_ptr(), _pitch(wt, N), dx.data_ptr(), K, M, N, K, yt, xt, act, self.gated,
                            L.FT_F32 if wide32 else L.FT_F16, 0)
         lib = L.lib()

@@ -482,7 +482,7 @@ def test_the_binding(ops):
     dy = rows(rng, 33, 50, "f32")
     want_dx = torch.autograd.grad(want, x, dy)[0]
     y = torch.full((33, 55), -7.0, device="cuda")
-    pre, sx = torch.empty(33, 50, device="cuda"), torch.empty(33, device="cuda")
+    pre, sx = torch.empty(33, 56, device="cuda"), torch.empty(33, device="cuda")
     d = L.LayerDesc(x.data_ptr(), 90, None, layer.w.data_ptr(), 96, layer.w_scale.data_ptr(), layer.bias.data_ptr(), None, 0, y.data_ptr(), 55,
                     pre.data_ptr(), sx.data_ptr(), 33, 50, 90, L.FT_F16, L.FT_F32, L.ACT_SILU, 0, L.FT_F32, 0.0)
     ws = torch.empty(F.fxpq_layer_workspace(d), dtype=torch.uint8, device="cuda")
