@@ -57,9 +57,9 @@ struct Words {
 // Bytes bound it (dy and the sums in, the row out): 8192 rows of 2 x 5632 460 MB, 68 us.  Rows stay in registers between their maximum
 // and the rounding, GR_KEEP groups of eight channels a thread, which are also on their way together; what does not fit, the last
 // group of some, and all of constants or sums that are not aligned, is formed again.  (A group at a time, kept in shared memory, the same rows took 185 us.)
-constexpr int GR_THREADS = 512, GR_KEEP = 3;
-template <bool GATE, int ACT, int DY, int PRE>
-__global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_constant__ GradRows G, int y_type) {
+constexpr int GR_KEEP = 3;
+template <bool GATE, int ACT, int DY, int PRE, int GR_THREADS>
+__global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kernel(const __grid_constant__ GradRows G, int y_type) {
     pdl_wait();
     constexpr bool NEEDS = GATE || ACT != FXPQ_ACT_NONE;
     constexpr int D = GATE ? 4 : 8;  // values of dy to eight channels
@@ -191,15 +191,27 @@ __global__ void __launch_bounds__(GR_THREADS, 2) grad_rows_kernel(const __grid_c
 fxpq_status grad_rows(const GradRows& G, int y_type, int gated, cudaStream_t st) {
     auto go = [&](auto act) {
         constexpr int ACT = decltype(act)::value;
-        const auto run = [&](auto kernel) { launch_pdl(kernel, dim3((unsigned)G.M), dim3(GR_THREADS), 0, st, G, y_type); };
         const auto sized = [&](auto gate) {
             constexpr bool GATE = decltype(gate)::value;
+            const auto run = [&](auto dy, auto pre) {
+                constexpr int DY = decltype(dy)::value, PRE = decltype(pre)::value;
+                const auto go = [&](auto kernel, int threads) { launch_pdl(kernel, dim3((unsigned)G.M), dim3(threads), 0, st, G, y_type); };
+                // As many threads as the row's groups need, so that more rows are under way (3990 rows of 549 channels 54 us with 512).
+                if (G.N <= 8 * GR_KEEP * 128)
+                    go(grad_rows_kernel<GATE, ACT, DY, PRE, 128>, 128);
+                else if (G.N <= 8 * GR_KEEP * 256)
+                    go(grad_rows_kernel<GATE, ACT, DY, PRE, 256>, 256);
+                else
+                    go(grad_rows_kernel<GATE, ACT, DY, PRE, 512>, 512);
+            };
+            using Two = std::integral_constant<int, 2>;
+            using Four = std::integral_constant<int, 4>;
             if (y_type == FXPQ_FT_F32)
-                run(grad_rows_kernel<GATE, ACT, 4, 4>);
+                run(Four(), Four());
             else if (G.pre_f32)
-                run(grad_rows_kernel<GATE, ACT, 2, 4>);
+                run(Two(), Four());
             else
-                run(grad_rows_kernel<GATE, ACT, 2, 2>);
+                run(Two(), Two());
         };
         if (!gated) return sized(std::false_type());
         if constexpr (ACT != FXPQ_ACT_NONE) sized(std::true_type());

@@ -222,91 +222,81 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
         }
     }
 }
-// 16 tokens of any type, alignment and activation.
-template <int EPI>
-__device__ __forceinline__ void epilogue_any(const ManyArgs& P, const uint32_t (&v)[16], const float* sxs, float2 sw, float2 bias, int c0, int odd,
-                                             long long m0, int cols) {
-    float a[8], b[8];  // channels c0, c0 + 1 of tokens 2 i + odd
-    const int left = P.N - c0, vec = P.e.vec;
-    if (left <= 0) cols = 0;
-    uint32_t ra[8], rb[8];  // their residuals as they lie in memory (asked for before anything is stored: y may be the residual)
-    const bool wide = P.y_type == FXPQ_FT_F32, both = (vec & 2) && left > 1;
-    if (EPI == LAYER && P.e.res) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            ra[i] = rb[i] = 0;
-            if (2 * i + odd >= cols) continue;
-            const long long at = (m0 + 2 * i + odd) * P.e.res_stride + c0;
-            const uint32_t* r32 = static_cast<const uint32_t*>(P.e.res) + at;
-            const unsigned short* r16 = static_cast<const unsigned short*>(P.e.res) + at;
-            if (wide && both) {
-                const uint2 w = *reinterpret_cast<const uint2*>(r32);
-                ra[i] = w.x, rb[i] = w.y;
-            } else if (wide) {
-                ra[i] = r32[0];
-                if (left > 1) rb[i] = r32[1];
-            } else if (both) {
-                ra[i] = *reinterpret_cast<const uint32_t*>(r16);
-            } else {
-                ra[i] = r16[0];
-                if (left > 1) rb[i] = r16[1];
-            }
-        }
+// f of the activation as a constant.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+    switch (act) {
+        case FXPQ_ACT_RELU: f(std::integral_constant<int, FXPQ_ACT_RELU>()); break;
+        case FXPQ_ACT_SILU: f(std::integral_constant<int, FXPQ_ACT_SILU>()); break;
+        case FXPQ_ACT_GELU: f(std::integral_constant<int, FXPQ_ACT_GELU>()); break;
+        case FXPQ_ACT_GELU_TANH: f(std::integral_constant<int, FXPQ_ACT_GELU_TANH>()); break;
+        default: f(std::integral_constant<int, FXPQ_ACT_NONE>());
     }
+}
+// n values of a column, rows `step` elements apart, into an array of any type.
+template <int N>
+__device__ __forceinline__ void store_column(void* p, int type, long long at, long long step, const float (&v)[N], int n) {
+    if (type == FXPQ_FT_F32) {
+        float* q = static_cast<float*>(p) + at;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float2 s = channel_pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]), odd);
-        a[i] = s.x, b[i] = s.y;
-    }
-    cols -= odd, sxs += odd, m0 += odd;
-    if (P.e.pre) {
-        const float k = P.e.pre_f32 ? 1.0f : P.e.pre_scale;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float keep[2] = {a[i] * k, b[i] * k};
-            if (2 * i < cols) store_some<2>(P.e.pre, P.e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, (m0 + 2 * i) * P.e.pre_stride + c0, keep, left, vec & 4);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float sx = sxs[2 * i];
-        a[i] = fmaf(a[i] * sx, sw.x, bias.x), b[i] = fmaf(b[i] * sx, sw.y, bias.y);
-    }
-    auto all = [&](auto act) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            a[i] = activate(a[i], decltype(act)::value);
-            if (EPI != GATED) b[i] = activate(b[i], decltype(act)::value);
-        }
-    };
-    switch (P.e.act) {
-        case FXPQ_ACT_RELU: all(std::integral_constant<int, FXPQ_ACT_RELU>()); break;
-        case FXPQ_ACT_SILU: all(std::integral_constant<int, FXPQ_ACT_SILU>()); break;
-        case FXPQ_ACT_GELU: all(std::integral_constant<int, FXPQ_ACT_GELU>()); break;
-        case FXPQ_ACT_GELU_TANH: all(std::integral_constant<int, FXPQ_ACT_GELU_TANH>()); break;
-        default: break;
-    }
-    if constexpr (EPI == GATED) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (2 * i < cols) store_y(P.y, P.y_type, (m0 + 2 * i) * P.ys + (c0 >> 1), a[i] * b[i]);
+        for (int i = 0; i < N; ++i, q += step)
+            if (i < n) *q = v[i];
     } else {
+        unsigned short* q = static_cast<unsigned short*>(p) + at;
+#pragma unroll
+        for (int i = 0; i < N; ++i, q += step) {
+            const unsigned short w = type == FXPQ_FT_F16 ? __half_as_ushort(__float2half_rn(v[i])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[i]));
+            if (i < n) *q = w;
+        }
+    }
+}
+
+// 16 tokens of any type, alignment and activation.  A lane keeps its channel, so that a token's 32 lie side by side whatever their
+// alignment; only gate and value meet first, and then a lane has every other token.
+template <int EPI>
+__device__ __forceinline__ void epilogue_any(const ManyArgs& P, const uint32_t (&v)[16], const float* sxs, float sw, float bias, int ch, long long m0,
+                                             int cols) {
+    if (ch >= P.N) cols = 0;
+    uint32_t r[16];  // residuals as they lie in memory (asked for before anything is stored: y may be the residual)
+    const bool wide = P.y_type == FXPQ_FT_F32;
+    if (EPI == LAYER && P.e.res) {
+        const long long at = m0 * P.e.res_stride + ch;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            r[i] = 0;
+            if (i < cols) r[i] = wide ? (static_cast<const uint32_t*>(P.e.res) + at)[i * P.e.res_stride] : (static_cast<const unsigned short*>(P.e.res) + at)[i * P.e.res_stride];
+        }
+    }
+    float z[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = __uint_as_float(v[i]) * (P.e.pre_f32 ? 1.0f : P.e.pre_scale);
+    if (P.e.pre) store_column(P.e.pre, P.e.pre_f32 ? FXPQ_FT_F32 : FXPQ_FT_F16, m0 * P.e.pre_stride + ch, P.e.pre_stride, z, cols);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = fmaf(__uint_as_float(v[i]) * sxs[i], sw, bias);
+    if constexpr (EPI == GATED) {
+        const int odd = ch & 1;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 p = channel_pair(z[2 * i], z[2 * i + 1], odd);
+            y[i] = p.x, z[i] = p.y;
+        }
+        with_act(P.e.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = activate(y[i], decltype(act)::value) * z[i];
+        });
+        store_column(P.y, P.y_type, (m0 + odd) * P.ys + (ch >> 1), 2 * P.ys, y, (cols - odd + 1) >> 1);
+    } else {
+        with_act(P.e.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = activate(z[i], decltype(act)::value);
+        });
         if (P.e.res) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (wide) {
-                    a[i] += __uint_as_float(ra[i]), b[i] += __uint_as_float(rb[i]);
-                } else {
-                    const float2 r = pair_f32(both ? ra[i] : __byte_perm(ra[i], rb[i], 0x5410), P.y_type);
-                    a[i] += r.x, b[i] += r.y;
-                }
-            }
+            for (int i = 0; i < 16; ++i)
+                z[i] += wide ? __uint_as_float(r[i]) : P.y_type == FXPQ_FT_F16 ? __half2float(__ushort_as_half((unsigned short)r[i])) : __uint_as_float(r[i] << 16);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float y[2] = {a[i], b[i]};
-            if (2 * i < cols) store_some<2>(P.y, P.y_type, (m0 + 2 * i) * P.ys + c0, y, left, vec & 1);
-        }
+        store_column(P.y, P.y_type, m0 * P.ys + ch, P.ys, z, cols);
     }
 }
 
@@ -556,7 +546,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                         uint32_t now[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) now[i] = v[0][i];
-                        epilogue_any<EPI>(P, now, sxs + c, sw2, bias2, c0, odd, m0 + c, cols - c);
+                        epilogue_any<EPI>(P, now, sxs + c, sw, bias, ch, m0 + c, cols - c);
 #pragma unroll
                         for (int i = 0; i < ROWS - 16; ++i) v[i / 32][i % 32] = v[(i + 16) / 32][(i + 16) % 32];
                     }
