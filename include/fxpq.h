@@ -551,7 +551,8 @@ FXPQ_API fxpq_status fxpq_linear_tokens(const void* d_x, int32_t x_type, int64_t
  * Not with `gated`, which needs an activation and an even N: weight rows 2 j and 2 j + 1 are gate and value of y's column j.
  * For a gradient (fxpq_layer_gradient): d_pre, M rows of N values of pre_type, (N + 7) / 8 * 8 of them apart, gets the sums before any scale (F32: as they are; F16: times
  * 2^-p, p by K alone such that the largest possible sum fits: they are integers, so every one keeps 11 bits), d_sx the rows' scales.
- * Either may be NULL.  eps: 0 to 1.  Workspace: fxpq_layer_workspace bytes, 256-byte aligned, scratch (it may be 0: then d_ws may be NULL). */
+ * Either may be NULL.  eps: 0 to 1.  Workspace: fxpq_layer_workspace bytes, 256-byte aligned, scratch (it may be 0: then d_ws may be NULL;
+ * where reductions are split it holds their sums too, in at most 1 GiB). */
 typedef enum { FXPQ_ACT_NONE = 0, FXPQ_ACT_RELU = 1, FXPQ_ACT_SILU = 2, FXPQ_ACT_GELU = 3, FXPQ_ACT_GELU_TANH = 4 } fxpq_activation;
 typedef struct {
     const void* d_x;

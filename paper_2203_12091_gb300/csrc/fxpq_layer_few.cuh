@@ -17,7 +17,7 @@ struct FloatRows {
 
 struct FewArgs {
     // weights' codes as [N][K] bytes in boxes of 128 codes x 128 rows (tw), or x the rows that the last tile has (tw2: a box is
-    // slow where it lies outside the tensor); tokens' as [M][K] bytes in boxes of 128 x `rows`, or as fp16 in 64 x `rows`
+    // slow where it lies outside the tensor); rows as fp16 in 64 x `rows`
     CUtensorMap tw, tw2, tx;
     const float *sx, *sw, *bias;  // null: ones, ones, zeros
     void* y;
@@ -36,8 +36,7 @@ struct FewArgs {
 // y^T = w x^T on tcgen05 (kind::f16: the 8-bit kind does not exist on sm_103a; codes are exact in fp16, their products in fp32): 128
 // output channels on the accumulator's lanes, up to 128 tokens on its columns.  The weights are the traffic.  They
 // arrive as codes (TMA, 128 x 128 bytes a block) and go through registers into tensor memory as the fp16 A operand,
-// so that their shared-memory traffic stays at two bytes a code.  The tokens' rows come as fp16 codes (HALF: written so by the
-// quantizer) or as bytes that are expanded in shared memory.
+// so that their shared-memory traffic stays at two bytes a code.
 //   warp 0   copies;   warp 1   tensor memory, products;   warps 4-7, 8-11   converters (blocks in turn), then the epilogue.
 // The reduction is shared by the CTAs of a cluster, whose fp32 sums meet through distributed shared memory: one launch, a
 // fixed order.  Up to 64 tokens two CTAs fit an SM.
@@ -117,18 +116,18 @@ __device__ __forceinline__ void own_codes(const FloatRows& F, int M, int kb0, in
         unsigned char* to = blocks + m * 128;
 #pragma unroll 2
         for (int c = (u & (parts - 1)) * 32 + lane; c < chunks; c += step) {
-        const int k = kb0 * LS_KB + 8 * c;
-        float v[8], w[8];
-        if (k + 8 <= K) {
-            eight(row, k, v, w);
-        } else {
+            const int k = kb0 * LS_KB + 8 * c;
+            float v[8], w[8];
+            if (k + 8 <= K) {
+                eight(row, k, v, w);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = k + e < K ? to_f32(row[k + e]) : 0.0f, w[e] = NORM && k + e < K ? __ldg(F.norm.weight + k + e) : 1.0f;
-        }
+                for (int e = 0; e < 8; ++e) v[e] = k + e < K ? to_f32(row[k + e]) : 0.0f, w[e] = NORM && k + e < K ? __ldg(F.norm.weight + k + e) : 1.0f;
+            }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = scaled_code(NORM ? __fmul_rn(v[e], w[e]) : v[e], inv);
-        *reinterpret_cast<uint4*>(to + (c >> 3) * half + (((c & 7) ^ (m & 7)) << 4)) =
-            make_uint4(f32_codes_f16x2(v[0], v[1]), f32_codes_f16x2(v[2], v[3]), f32_codes_f16x2(v[4], v[5]), f32_codes_f16x2(v[6], v[7]));
+            for (int e = 0; e < 8; ++e) v[e] = scaled_code(NORM ? __fmul_rn(v[e], w[e]) : v[e], inv);
+            *reinterpret_cast<uint4*>(to + (c >> 3) * half + (((c & 7) ^ (m & 7)) << 4)) =
+                make_uint4(f32_codes_f16x2(v[0], v[1]), f32_codes_f16x2(v[2], v[3]), f32_codes_f16x2(v[4], v[5]), f32_codes_f16x2(v[6], v[7]));
         }
     }
 }
