@@ -81,10 +81,10 @@ constexpr int LS_KB = 128, LS_A = 128 * LS_KB;  // codes of a block of the reduc
 // products) it moves 8 KB of weight codes in and out and 16 KB of tokens in and once through the tensor core: 384 cycles
 // of shared memory, where one CTA alone would need 640, and both operands as fp16 in shared memory 512.  The tokens arrive
 // as fp16 codes (written so by the quantizer, or expanded before), the weights as bytes, expanded into tensor memory.
-//   warp 0  weights' copies;  1  tokens' copies;  2  tensor memory, products (CTA 0);  4-7  converters;  8-15  epilogue.
+//   warp 0  weights' copies;  1  tokens' copies;  2  tensor memory, products (CTA 0);  4-7  converters;  8-15  epilogue (layers': 8-23).
 // The accumulators fill half of tensor memory, the weights' four stages the other half.  The epilogue scales and packs the
 // sums into registers first, so that the next tile's products begin while it still stores.
-constexpr int LM_THREADS = 512, LM_RAW = 3, LM_B = 8, LM_A = 4;
+constexpr int LM_RAW = 3, LM_B = 8, LM_A = 4;
 constexpr int LM_SMEM = 1024 + LM_RAW * LS_A + LM_B * 128 * 128;
 
 struct ManyArgs {
@@ -130,13 +130,14 @@ struct SigAct {
     }
 };
 
-// A warp's residuals, two channels of ROWS / 2 tokens a lane: the first asked for before the sums are there, the others three steps ahead.  (Asked for a step ahead, a tile's epilogue took 21 thousand clocks with them and 8 without; y may be the
-// residual, so the compiler keeps every load behind the stores before it.)
+// A warp's residuals, two channels of ROWS / 2 tokens a lane: the first asked for before the sums are there, the others two steps ahead.  (Asked
+// for a step ahead, a tile's epilogue took 21 thousand clocks with them and 8 without; y may be the residual, so the compiler keeps
+// every load behind the stores before it.)
 template <int ROWS>
 struct Residuals {
     const char* at;  // token odd's two channels
     long long step;  // two tokens, in bytes
-    static constexpr int HELD = ROWS / 8 * 2 > 24 ? 24 : ROWS / 8 * 2;
+    static constexpr int HELD = 8;
     uint32_t r[HELD];
     __device__ __forceinline__ void ask(int i, int cols) {  // of token 2 i + odd
         uint32_t w = 0;
@@ -145,9 +146,10 @@ struct Residuals {
     }
 };
 
-// The epilogue of a warp's 32 channels and ROWS tokens for LAYER and GATED.  Everything goes by pairs: two lanes exchange sums so that
-// each holds two channels of one token.  The fast form holds all sums in registers (the epilogue's warps have taken the other
-// warps'), and has given the accumulators back before it computes: for GATED 16384 of 4096, 8192 tokens, see fxpq_layer.cu.
+// The epilogue of a warp's 32 channels and ROWS tokens for LAYER and GATED: 16-bit outputs in aligned pairs.  Everything goes by pairs: two
+// lanes exchange sums so that each holds two channels of one token.  All sums are in registers, and the accumulators have been given back
+// before anything is computed, so that the next tile's products run meanwhile.  16 warps (of 96 registers) have half the code and
+// twice the loads under way of 8 (of 192): 8071 x 2304 of 1024 with norm and tanh GELU 68 and 52 us, 2000 x 2 x 4096 of 1024 46 and 37.
 template <int ROWS, int EPI, int FORM, typename Sum>
 __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, const float* sxs, float2 sw, float2 bias, int c0, int odd, long long m0, int cols, Residuals<ROWS>& held) {
     const bool f16 = P.y_type == FXPQ_FT_F16;
@@ -167,7 +169,7 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
     };
     // STEP pairs of tokens at a time, each step of the arithmetic for all of them: one pair after the other left the warps waiting for
     // every exchange and exponential in turn (8192 x 2 x 5632 of 2048: 24 thousand clocks a tile, its products 16).
-    constexpr int STEP = 8;
+    constexpr int STEP = EPI == LAYER ? 4 : 8;
     const int second = (threadIdx.x >> 1) & 1, reach = EPI == GATED ? cols - 2 * second : cols;
     char* y = static_cast<char*>(P.y) + (EPI == GATED ? (m0 + odd + 2 * second) * P.ys + (c0 >> 1) - second : (m0 + odd) * P.ys + c0) * 2;
 #pragma unroll
@@ -300,20 +302,23 @@ __device__ __forceinline__ void epilogue_any(const ManyArgs& P, const uint32_t (
     }
 }
 
-// Registers of a thread: the launch holds 512 x 128, of which the epilogue's warps take 256 x 192 and the others 128 x 40 (copies, products)
-// and 128 x 80 (converters).
-constexpr int LM_REGS = 128, LM_REGS_EPI = 192, LM_REGS_ISSUE = 40, LM_REGS_CONV = 80;
-static_assert(LM_REGS_ISSUE + LM_REGS_CONV + 2 * LM_REGS_EPI <= 4 * LM_REGS, "the launch's registers");
+// Registers of a thread where the epilogue has 16 warps: the launch holds 768 x 80, of which the epilogue's take 512 x 96 and the others
+// 128 x 32 (copies, products) and 128 x 64 (converters).
+constexpr int LM_REGS = 80, LM_REGS_EPI = 96, LM_REGS_ISSUE = 32, LM_REGS_CONV = 64;
+static_assert(LM_REGS_ISSUE + LM_REGS_CONV + 4 * LM_REGS_EPI <= 6 * LM_REGS, "the launch's registers");
+
+constexpr int many_threads(int epi) { return epi == PLAIN ? 512 : 768; }
 
 // NT: tokens of a tile, 256 or, where those tiles would leave pairs idle, 128.
 template <int NT, int EPI, int FORM>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linear_many_kernel(const __grid_constant__ ManyArgs P) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(many_threads(EPI), 1) linear_many_kernel(const __grid_constant__ ManyArgs P) {
     using namespace tc;
-    constexpr int ROWS = NT / 2, STAGE = ROWS * 128;  // tokens of a CTA's half of the operand and of an epilogue warp; its stage
+    constexpr int EW = EPI == PLAIN ? 8 : 16, ROWS = NT * 4 / EW;      // warps of the epilogue, and each one's tokens
+    constexpr int HALF_ROWS = NT / 2, STAGE = HALF_ROWS * 128;         // tokens of a CTA's half of the operand, its stage
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     __shared__ __align__(8) uint64_t bars[2 * LM_RAW + 2 * LM_B + 2 * LM_A + 3];
-    __shared__ __align__(16) float s_sx[8][ROWS];
+    __shared__ __align__(16) float s_sx[EW][ROWS];
     __shared__ int abort_flag;
     __shared__ uint32_t tmem_slot;
     volatile int* abort = &abort_flag;
@@ -337,7 +342,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
             mbar_init(a_empty + 8 * i, 1);
         }
         mbar_init(acc_full, 1);
-        mbar_init(acc_empty, 16);  // (CTA 0's: the epilogue warps of both)
+        mbar_init(acc_empty, 2 * EW);  // (CTA 0's: the epilogue warps of both)
         mbar_init(done, 1);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -405,7 +410,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LM_THREADS, 1) linea
                         break;
                     }
                     if (rank == 0) mbar_arrive_expect_tx(b_full + 8 * s, 2 * STAGE);
-                    tma_load_2d_pair(b0 + s * STAGE, &P.tx, hb * 64, tm * NT + rank * ROWS, lead + 8 * s);
+                    tma_load_2d_pair(b0 + s * STAGE, &P.tx, hb * 64, tm * NT + rank * HALF_ROWS, lead + 8 * s);
                 }
             }
             if (rank == 0)
@@ -686,7 +691,7 @@ fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
     P.whole = P.whole < P.n_tiles ? P.whole : P.n_tiles;
     const long long work = P.whole + (tn * tm - P.whole) * P.shares, pairs = many_pairs();
     if (work > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
-    launch_pdl(kernel, dim3(2 * (unsigned)(work < pairs ? work : pairs)), dim3(LM_THREADS), LM_SMEM, st, P);
+    launch_pdl(kernel, dim3(2 * (unsigned)(work < pairs ? work : pairs)), dim3(many_threads(EPI)), LM_SMEM, st, P);
     return after_launch("linear_many");
 }
 
