@@ -667,13 +667,16 @@ struct ManyPlan {
     float* part;
 };
 
-// Lets a kernel use so much dynamic shared memory, once on each device.
+// Lets a kernel use so much dynamic shared memory, once on each device.  regs: what its launch has to hold of them a thread (0: any), for
+// warps that take more later wait for ever if they are not there.
 template <typename Kernel>
-bool allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& set) {
+bool allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& set, int regs = 0) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
     const uint64_t bit = dev < 64 ? 1ull << dev : 0;
     if (set.load(std::memory_order_relaxed) & bit) return true;
+    cudaFuncAttributes has;
+    if (regs && (cudaFuncGetAttributes(&has, kernel) != cudaSuccess || has.numRegs < regs)) return false;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
     set.fetch_or(bit, std::memory_order_relaxed);
     return true;
@@ -683,7 +686,7 @@ template <int NT, int EPI, int FORM>
 fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
     const auto kernel = linear_many_kernel<NT, EPI, FORM>;
     static std::atomic<uint64_t> set{0};
-    if (!allow_smem(kernel, LM_SMEM, set)) return FXPQ_ERR_CUDA;
+    if (!allow_smem(kernel, LM_SMEM, set, EPI == PLAIN ? 0 : LM_REGS)) return FXPQ_ERR_CUDA;
     const long long tn = ((long long)P.N + 255) / 256, tm = (P.M + NT - 1) / NT;
     if (tn * tm > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
     P.tiles_n = (int)tn, P.tiles_m = (int)tm, P.n_tiles = (int)(tn * tm);
