@@ -106,6 +106,22 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
     };
     const int whole = (G.vec | 1 | (NEEDS ? 0 : 2) | (G.bias ? 0 : 8)) == 15 ? N / 8 : 0;  // groups whose constants and sums come in aligned accesses
+    const auto of_words = [&](int g, const Words<D, DY>& d, const Words<8, PRE>& a, float (&v)[8]) {
+        float df[D], af[8], w[8], b[8];
+        load_f32<8>(G.sw + 8 * g, true, w);
+        if (NEEDS && G.bias) load_f32<8>(G.bias + 8 * g, true, b);
+        d.values(y_type == FXPQ_FT_F16, df);
+        a.values(true, af);
+        compute(df, af, w, b, v);
+    };
+    const auto again = [&](int g, float (&v)[8]) {  // a group that is not kept
+        if (g >= whole) return form(g, v);
+        Words<D, DY> d;
+        Words<8, PRE> a;
+        d.load(G.dy, m * G.dy_stride + g * D, G.vec & 1);
+        if constexpr (NEEDS) a.load(G.pre, m * pitch + 8 * g);
+        of_words(g, d, a, v);
+    };
     float keep[GR_KEEP][8];
     {
         Words<D, DY> d[GR_KEEP];
@@ -121,12 +137,7 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
         for (int s = 0; s < GR_KEEP; ++s) {
             const int g = t + s * GR_THREADS;
             if (g >= whole) continue;
-            float df[D], af[8], w[8], b[8];
-            load_f32<8>(G.sw + 8 * g, true, w);
-            if (NEEDS && G.bias) load_f32<8>(G.bias + 8 * g, true, b);
-            d[s].values(y_type == FXPQ_FT_F16, df);
-            a[s].values(true, af);
-            compute(df, af, w, b, keep[s]);
+            of_words(g, d[s], a[s], keep[s]);
             see(keep[s]);
         }
     }
@@ -134,7 +145,7 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
 #pragma unroll 1
     for (int g = first + t; g < groups; g += GR_THREADS) {
         float v[8];
-        form(g, v);
+        again(g, v);
         see(v);
     }
     __shared__ uint32_t part[GR_THREADS / 32];
@@ -177,7 +188,7 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
 #pragma unroll 1
     for (int g = first + t; g < groups; g += GR_THREADS) {
         float v[8];
-        form(g, v);
+        again(g, v);
         put(g, v);
     }
     if (t == 0 && (groups & 1)) {  // rows are padded to 16

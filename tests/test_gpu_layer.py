@@ -608,3 +608,12 @@ def test_unaligned_tensors(ops, M):
     F.fxpq_layer_forward(d, torch.empty(max(1, F.fxpq_layer_workspace(d)), dtype=torch.uint8, device="cuda"))
     got = big[1:].view(M, 257)
     assert torch.equal(got[:, :256], y.detach()) and not got[:, 256].any()
+
+
+@pytest.mark.parametrize("N", [9000, 12285, 12290, 20001])
+def test_gradient_of_very_wide_layers(ops, N):
+    """Rows of more channels than a block keeps: what does not fit is formed again."""
+    rng = np.random.default_rng(N)
+    check_gradient(ops, rng, 5, N, 40, "bf16", "bf16", "silu", True, False)
+    check_gradient(ops, rng, 70, N // 2, 24, "f16", "f16", "gelu", False, True)
+    check_gradient(ops, rng, 3, N, 16, "f32", "f32", None, False, False)
