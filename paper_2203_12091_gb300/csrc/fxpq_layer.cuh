@@ -5,6 +5,12 @@
 namespace fxpq {
 namespace llm {
 
+// The larger of z and low; NaN stays NaN (fmaxf drops it).
+__device__ __forceinline__ float cut(float z, float low) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(z), "f"(low));
+    return y;
+}
 inline bool act_ok(int a) { return a >= FXPQ_ACT_NONE && a <= FXPQ_ACT_GELU_TANH; }
 
 // 1 / (1 + e^-z).  (__expf and __fdividef: 2^-21 of the result where it is 2^-8 or more; past e^88 the quotient is 0.)
@@ -35,7 +41,7 @@ __device__ __forceinline__ float gelu(float z) {
 }
 __device__ __forceinline__ float activate(float z, int act) {
     switch (act) {
-        case FXPQ_ACT_RELU: return fmaxf(z, 0.0f);
+        case FXPQ_ACT_RELU: return cut(z, 0.0f);
         case FXPQ_ACT_SILU: return z * sigmoid(z);
         case FXPQ_ACT_GELU: return gelu(z);
         case FXPQ_ACT_GELU_TANH: return z * sigmoid(GELU_A * z * fmaf(GELU_B, z * z, 1.0f));
@@ -45,7 +51,7 @@ __device__ __forceinline__ float activate(float z, int act) {
 // act(z) and its derivative.  Where the derivative has reached its limits z is cut off, so that no inf meets a zero.
 __device__ __forceinline__ float activate_slope(float z, int act, float& slope) {
     switch (act) {
-        case FXPQ_ACT_RELU: slope = z > 0.0f ? 1.0f : 0.0f; return fmaxf(z, 0.0f);
+        case FXPQ_ACT_RELU: slope = z > 0.0f ? 1.0f : 0.0f; return cut(z, 0.0f);
         case FXPQ_ACT_SILU: {
             const float c = fminf(fmaxf(z, -100.0f), 100.0f), s = sigmoid(c);
             slope = s * fmaf(c, 1.0f - s, 1.0f);

@@ -161,7 +161,7 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
     // (addresses that walk along the tokens: computed from the token each, they took more registers than there are)
     const long long y_step = 2 * P.ys * 2, p_step = 2 * P.e.pre_stride * 2;
     char* pre = P.e.pre ? static_cast<char*>(P.e.pre) + ((m0 + odd) * P.e.pre_stride + c0) * 2 : nullptr;
-    auto act = [&](float z) { return FORM == SIGMOID ? sig(z) : FORM == NORMAL ? gelu(z) : fmaxf(z, low); };
+    auto act = [&](float z) { return FORM == SIGMOID ? sig(z) : FORM == NORMAL ? gelu(z) : cut(z, low); };
     auto pack = [&](float a, float b) {
         if (f16) return h2_bits(__floats2half2_rn(a, b));
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);

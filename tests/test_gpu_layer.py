@@ -617,3 +617,37 @@ def test_gradient_of_very_wide_layers(ops, N):
     check_gradient(ops, rng, 5, N, 40, "bf16", "bf16", "silu", True, False)
     check_gradient(ops, rng, 70, N // 2, 24, "f16", "f16", "gelu", False, True)
     check_gradient(ops, rng, 3, N, 16, "f32", "f32", None, False, False)
+
+
+@pytest.mark.parametrize("M", [7, 100, 300, 1300, 10000])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_nan_stays_in_its_channel(ops, M, out):
+    """A NaN scale or bias gives its own channel NaN, whatever the activation, and leaves every other as it is."""
+    rng = np.random.default_rng(M)
+    W = Weights(rng, 256, 512, True, 2)
+    x, r = rows(rng, M, 512, "bf16"), rows(rng, M, 512, out)
+    calls = lambda act: (W.layer(ops)(x, TYPES[out], activation=act, residual=r), W.gated(ops, act or "silu")(x, TYPES[out]))
+    before = {act: calls(act) for act in ACTS}
+    W.b[6], W.sw[201], W.b[510] = np.nan, np.nan, np.nan
+    for act in ACTS:
+        for y, want, bad in zip(calls(act), before[act], ([6, 201, 510], [3, 100, 255])):
+            good = [c for c in range(y.shape[1]) if c not in bad]
+            assert bool(y[:, bad].isnan().all()), act
+            assert torch.equal(y[:, good], want[:, good]), act
+
+
+@pytest.mark.parametrize("M", [100, 300, 1300, 10000])
+@pytest.mark.parametrize("act", ACTS)
+def test_gradients_of_many_rows_that_are_not_finite(ops, M, act):
+    rng = np.random.default_rng(M)
+    layer = Weights(rng, 256, 512, True).layer(ops).with_gradient()
+    x = rows(rng, M, 512, "bf16").requires_grad_()
+    y = layer(x, activation=act)
+    bad = rows(rng, M, 256, "bf16")
+    want = torch.autograd.grad(y, x, bad, retain_graph=True)[0]
+    at = [4, M // 2, M - 1]
+    bad[at[0], 7], bad[at[1], 0], bad[at[2], 255] = float("nan"), float("nan"), float("nan")
+    dx = torch.autograd.grad(y, x, bad)[0]
+    assert F.fxpq_get_device_status() == L.ERR_NONFINITE
+    good = [m for m in range(M) if m not in at]
+    assert bool(dx[at].isnan().all()) and torch.equal(dx[good], want[good])
