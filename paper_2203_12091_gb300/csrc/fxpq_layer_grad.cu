@@ -218,11 +218,9 @@ fxpq_status grad_rows(const GradRows& G, int y_type, int gated, cudaStream_t st)
             using Two = std::integral_constant<int, 2>;
             using Four = std::integral_constant<int, 4>;
             if (y_type == FXPQ_FT_F32)
-                run(Four(), Four());
-            else if (G.pre_f32)
-                run(Two(), Four());
+                G.pre_f32 ? run(Four(), Four()) : run(Four(), Two());
             else
-                run(Two(), Two());
+                G.pre_f32 ? run(Two(), Four()) : run(Two(), Two());
         };
         if (!gated) return sized(std::false_type());
         if constexpr (ACT != FXPQ_ACT_NONE) sized(std::true_type());

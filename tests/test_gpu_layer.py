@@ -651,3 +651,31 @@ def test_gradients_of_many_rows_that_are_not_finite(ops, M, act):
     assert F.fxpq_get_device_status() == L.ERR_NONFINITE
     good = [m for m in range(M) if m not in at]
     assert bool(dx[at].isnan().all()) and torch.equal(dx[good], want[good])
+
+
+@pytest.mark.parametrize("N", [6, 50, 512, 9000])
+@pytest.mark.parametrize("is_gated", [False, True])
+@pytest.mark.parametrize("dx_type", ["f32", "bf16"])
+def test_kept_sums_of_any_type_with_a_gradient_of_any(ops, N, is_gated, dx_type):
+    """fp32 gradients with sums kept in fp16: what the same gradients in bfloat16 give, bit for bit."""
+    rng = np.random.default_rng(N)
+    M, K = 37, 90
+    W = Weights(rng, N, K, True)
+    layer = W.layer(ops).with_gradient()
+    ft = {"f32": L.FT_F32, "bf16": L.FT_BF16}
+    x, pitch = rows(rng, M, K, "bf16"), (N + 7) // 8 * 8
+    wide = N // 2 if is_gated else N
+    for pre_type, kept in ((L.FT_F16, torch.float16), (L.FT_F32, torch.float32)):
+        y, pre, sx = torch.empty(M, wide, device="cuda"), torch.zeros(M, pitch, dtype=kept, device="cuda"), torch.empty(M, device="cuda")
+        d = L.LayerDesc(x.data_ptr(), K, None, layer.w.data_ptr(), 96, layer.w_scale.data_ptr(), layer.bias.data_ptr(), None, 0, y.data_ptr(), wide,
+                        pre.data_ptr(), sx.data_ptr(), M, N, K, L.FT_BF16, L.FT_F32, L.ACT_GELU, int(is_gated), pre_type, 0.0)
+        F.fxpq_layer_forward(d, torch.empty(F.fxpq_layer_workspace(d), dtype=torch.uint8, device="cuda"))
+        dy, got = rows(rng, M, wide, "bf16"), []
+        for t in ("bf16", "f32"):
+            g_dy, dx = dy.to(TYPES[t]), torch.empty(M, K, dtype=TYPES[dx_type], device="cuda")
+            g = L.LayerGradDesc(g_dy.data_ptr(), wide, pre.data_ptr(), sx.data_ptr(), layer.w_scale.data_ptr(), layer.bias.data_ptr(),
+                                layer.wt.data_ptr(), layer.wt.stride(0), dx.data_ptr(), K, M, N, K, ft[t], ft[dx_type], L.ACT_GELU, int(is_gated),
+                                pre_type, 0)
+            F.fxpq_layer_gradient(g, torch.empty(F.fxpq_layer_gradient_workspace(g), dtype=torch.uint8, device="cuda"))
+            got.append(dx)
+        assert torch.equal(*got) and bool(got[0].isfinite().all()) and bool((got[0] != 0).any())
