@@ -57,8 +57,9 @@ struct Words {
 // Bytes bound it (dy and the sums in, the row out): 8192 rows of 2 x 5632 460 MB, 68 us.  Rows stay in registers between their maximum
 // and the rounding, GR_KEEP groups of eight channels a thread, which are also on their way together; what does not fit, the last
 // group of some, and all of constants or sums that are not aligned, is formed again.  (A group at a time, kept in shared memory, the same rows took 185 us.)
+// ALL: every group is kept; without the code for the others, and what it holds of registers, those rows took 94 us, not 107.
 constexpr int GR_KEEP = 3;
-template <bool GATE, int ACT, int DY, int PRE, int GR_THREADS>
+template <bool GATE, int ACT, int DY, int PRE, int GR_THREADS, bool ALL>
 __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kernel(const __grid_constant__ GradRows G, int y_type) {
     pdl_wait();
     constexpr bool NEEDS = GATE || ACT != FXPQ_ACT_NONE;
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
     };
-    const int whole = (G.vec | 1 | (NEEDS ? 0 : 2) | (G.bias ? 0 : 8)) == 15 ? N / 8 : 0;  // groups whose constants and sums come in aligned accesses
+    const int whole = ALL ? groups : (G.vec | 1 | (NEEDS ? 0 : 2) | (G.bias ? 0 : 8)) == 15 ? N / 8 : 0;  // groups whose constants and sums come in aligned accesses
     const auto of_words = [&](int g, const Words<D, DY>& d, const Words<8, PRE>& a, float (&v)[8]) {
         float df[D], af[8], w[8], b[8];
         load_f32<8>(G.sw + 8 * g, true, w);
@@ -141,12 +142,14 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
             see(keep[s]);
         }
     }
-    const int first = min(whole, GR_KEEP * GR_THREADS);  // of those that are not kept
+    const int first = ALL ? groups : min(whole, GR_KEEP * GR_THREADS);  // of those that are not kept
+    if constexpr (!ALL) {
 #pragma unroll 1
-    for (int g = first + t; g < groups; g += GR_THREADS) {
-        float v[8];
-        again(g, v);
-        see(v);
+        for (int g = first + t; g < groups; g += GR_THREADS) {
+            float v[8];
+            again(g, v);
+            see(v);
+        }
     }
     __shared__ uint32_t part[GR_THREADS / 32];
     top = __reduce_max_sync(0xffffffffu, top);
@@ -185,11 +188,13 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
 #pragma unroll
     for (int s = 0; s < GR_KEEP; ++s)
         if (t + s * GR_THREADS < whole) put(t + s * GR_THREADS, keep[s]);
+    if constexpr (!ALL) {
 #pragma unroll 1
-    for (int g = first + t; g < groups; g += GR_THREADS) {
-        float v[8];
-        again(g, v);
-        put(g, v);
+        for (int g = first + t; g < groups; g += GR_THREADS) {
+            float v[8];
+            again(g, v);
+            put(g, v);
+        }
     }
     if (t == 0 && (groups & 1)) {  // rows are padded to 16
         hi[groups] = make_uint4(0, 0, 0, 0);
@@ -206,14 +211,23 @@ fxpq_status grad_rows(const GradRows& G, int y_type, int gated, cudaStream_t st)
             constexpr bool GATE = decltype(gate)::value;
             const auto run = [&](auto dy, auto pre) {
                 constexpr int DY = decltype(dy)::value, PRE = decltype(pre)::value;
-                const auto go = [&](auto kernel, int threads) { launch_pdl(kernel, dim3((unsigned)G.M), dim3(threads), 0, st, G, y_type); };
+                constexpr bool NEEDS = GATE || ACT != FXPQ_ACT_NONE;
+                const bool fits = DY == 2 && PRE == 2 && G.N % 8 == 0 && G.N <= 8 * GR_KEEP * 512 &&
+                                  (G.vec | 1 | (NEEDS ? 0 : 2) | (G.bias ? 0 : 8)) == 15;
+                const auto go = [&](auto threads) {
+                    constexpr int THREADS = decltype(threads)::value;
+                    const auto with = [&](auto kernel) { launch_pdl(kernel, dim3((unsigned)G.M), dim3(THREADS), 0, st, G, y_type); };
+                    if constexpr (DY == 2 && PRE == 2)
+                        if (fits) return with(grad_rows_kernel<GATE, ACT, DY, PRE, THREADS, true>);
+                    with(grad_rows_kernel<GATE, ACT, DY, PRE, THREADS, false>);
+                };
                 // As many threads as the row's groups need, so that more rows are under way (3990 rows of 549 channels 54 us with 512).
                 if (G.N <= 8 * GR_KEEP * 128)
-                    go(grad_rows_kernel<GATE, ACT, DY, PRE, 128>, 128);
+                    go(std::integral_constant<int, 128>());
                 else if (G.N <= 8 * GR_KEEP * 256)
-                    go(grad_rows_kernel<GATE, ACT, DY, PRE, 256>, 256);
+                    go(std::integral_constant<int, 256>());
                 else
-                    go(grad_rows_kernel<GATE, ACT, DY, PRE, 512>, 512);
+                    go(std::integral_constant<int, 512>());
             };
             using Two = std::integral_constant<int, 2>;
             using Four = std::integral_constant<int, 4>;
