@@ -212,22 +212,25 @@ fxpq_status grad_rows(const GradRows& G, int y_type, int gated, cudaStream_t st)
             const auto run = [&](auto dy, auto pre) {
                 constexpr int DY = decltype(dy)::value, PRE = decltype(pre)::value;
                 constexpr bool NEEDS = GATE || ACT != FXPQ_ACT_NONE;
-                const bool fits = DY == 2 && PRE == 2 && G.N % 8 == 0 && G.N <= 8 * GR_KEEP * 512 &&
+                const bool fits = DY == 2 && PRE == 2 && G.N % 8 == 0 && G.N <= 8 * GR_KEEP * 1024 &&
                                   (G.vec | 1 | (NEEDS ? 0 : 2) | (G.bias ? 0 : 8)) == 15;
                 const auto go = [&](auto threads) {
                     constexpr int THREADS = decltype(threads)::value;
                     const auto with = [&](auto kernel) { launch_pdl(kernel, dim3((unsigned)G.M), dim3(THREADS), 0, st, G, y_type); };
                     if constexpr (DY == 2 && PRE == 2)
                         if (fits) return with(grad_rows_kernel<GATE, ACT, DY, PRE, THREADS, true>);
-                    with(grad_rows_kernel<GATE, ACT, DY, PRE, THREADS, false>);
+                    if constexpr (THREADS <= 512) with(grad_rows_kernel<GATE, ACT, DY, PRE, THREADS, false>);
                 };
-                // As many threads as the row's groups need, so that more rows are under way (3990 rows of 549 channels 54 us with 512).
+                // As many threads as the row's groups need, so that more rows are under way (3990 rows of 549 channels 54 us with 512), or all
+                // there are where that keeps the row (7999 rows of 22400: 231 us, with 512 and the rest formed again 254).
                 if (G.N <= 8 * GR_KEEP * 128)
                     go(std::integral_constant<int, 128>());
                 else if (G.N <= 8 * GR_KEEP * 256)
                     go(std::integral_constant<int, 256>());
-                else
+                else if (G.N <= 8 * GR_KEEP * 512 || !fits)
                     go(std::integral_constant<int, 512>());
+                else
+                    go(std::integral_constant<int, 1024>());
             };
             using Two = std::integral_constant<int, 2>;
             using Four = std::integral_constant<int, 4>;

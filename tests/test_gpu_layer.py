@@ -610,7 +610,7 @@ def test_unaligned_tensors(ops, M):
     assert torch.equal(got[:, :256], y.detach()) and not got[:, 256].any()
 
 
-@pytest.mark.parametrize("N", [9000, 12285, 12290, 20001])
+@pytest.mark.parametrize("N", [9000, 12285, 12288, 12290, 16384, 20001, 24576, 24584])
 def test_gradient_of_very_wide_layers(ops, N):
     """Rows of more channels than a block keeps: what does not fit is formed again."""
     rng = np.random.default_rng(N)
