@@ -581,8 +581,8 @@ FXPQ_API fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, siz
  *   dx[m, k] = sum_n dz[m, n] d_sw[n] w[n, k]
  * d_dy: rows of N (gated: N / 2) values of y_type; d_pre, pre_type, d_sx: what fxpq_layer_forward left (not read without activation);
  * d_wt: the weights' codes transposed, [K][N], 16-byte aligned rows a multiple of 16 bytes apart; d_dx: rows of K values of dx_type.
- * A row's dz * sw is rounded to fp16 with a power of two of its own (to 2^-11 of each value, or 2^-39 of the row's largest), for dx of F32 to
- * 2^-23 of the row's largest in two parts; products are exact, sums fp32.  ReLU's derivative at 0 is 0.  A row with a
+ * A row's dz * sw is taken in two parts of fp16 with a power of two of its own: to 2^-23 of the row's largest value, or to 2^-12 of each value
+ * (2^-47 of the largest) where that is less; products are exact, sums fp32.  ReLU's derivative at 0 is 0.  A row with a
  * non-finite dz * sw gives NaN and latches FXPQ_ERR_NONFINITE.
  * Workspace: fxpq_layer_gradient_workspace bytes, 256-byte aligned, scratch. */
 typedef struct {

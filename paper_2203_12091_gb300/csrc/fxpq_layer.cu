@@ -11,9 +11,9 @@ namespace fxpq {
 namespace llm {
 namespace {
 
-// dx = (4096 high sums + low sums) * scale, a block a row (and 1024 of its values).
-__global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ sums, const float* __restrict__ scale, long long M, int K,
-                                                         float* __restrict__ dx, long long dx_stride) {
+// dx = (PART first sums + second sums) * scale, a block a row (and 1024 of its values).
+__global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ sums, const float* __restrict__ scale, long long M, int K, void* dx,
+                                                         int type, long long dx_stride) {
     pdl_wait();
     const long long m = blockIdx.x;
     const float s = __ldg(scale + m);
@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int k = blockIdx.y * 1024 + i * 256 + threadIdx.x;
-        if (k < K) dx[m * dx_stride + k] = fmaf(hi[k], 4096.0f, lo[k]) * s;
+        if (k < K) store_y(dx, type, m * dx_stride + k, fmaf(hi[k], PART, lo[k]) * s);
     }
 }
 
@@ -103,14 +103,15 @@ struct Product {
 template <int EPI>
 fxpq_status product(const Product& p, const Epi& e, Plan plan, float* part, cudaStream_t st) {
     const int64_t pitch = (int64_t)half_pitch(p.K);
-    if (plan.few) return few_product<EPI>(p.rows, pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e, nullptr, true);
+    if constexpr (EPI != PARTS)
+        if (plan.few) return few_product<EPI>(p.rows, pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e, nullptr, true);
     plan.many.part = plan.bytes ? part : nullptr;
     ManyArgs args;
     const fxpq_status rc = product_many<EPI>(p.rows, (size_t)pitch, p.scale, p.w, p.w_stride, p.sw, p.bias, p.M, p.N, p.K, p.y_type, p.y, p.y_stride, st, e,
                                              &plan.many, &args);
     if (rc != FXPQ_OK || !plan.bytes) return rc;
     args.e.vec = fours<EPI>(e, p.y_type, p.y, p.y_stride);
-    launch_pdl(finish_kernel<EPI>, dim3(2 * (unsigned)(args.n_tiles - args.whole), plan.many.nt / 32), dim3(256), 0, st, args, plan.many.nt);
+    launch_pdl(finish_kernel<EPI>, dim3(2 * (unsigned)(args.n_tiles - args.whole), plan.many.nt / (EPI == PARTS ? 64 : 32)), dim3(256), 0, st, args, plan.many.nt);
     return after_launch("finish");
 }
 struct LayerSpace {
@@ -131,11 +132,11 @@ struct GradSpace {
     Plan plan;
     size_t rows, parts, sums, end;
     explicit GradSpace(const fxpq_layer_grad& d) {
-        const int n = d.dx_type == FXPQ_FT_F32 ? 2 : 1;
-        plan = plan_of(n * d.M, d.K, d.N, epilogue_time(d.K, d.dx_type, 0, false));
-        rows = up256((size_t)n * d.M * half_pitch(d.N) * 2);
+        // Two parts of every row; the product of few rows leaves their sums to join_parts_kernel, pairs of CTAs join them (half as many to store a tile).
+        plan = plan_of(2 * d.M, d.K, d.N, epilogue_time(d.K, d.dx_type, 0, false) / 2);
+        rows = up256((size_t)2 * d.M * half_pitch(d.N) * 2);
         parts = rows + up256((size_t)d.M * 4);
-        sums = parts + (n == 2 ? up256((size_t)n * d.M * d.K * 4) : 0);
+        sums = parts + (plan.few ? up256((size_t)2 * d.M * d.K * 4) : 0);
         end = sums + up256(plan.bytes);
     }
 };
@@ -216,20 +217,23 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
     __half* rows = reinterpret_cast<__half*>(ws);
     float* scale = reinterpret_cast<float*>(ws + at.rows);
     float *sums = reinterpret_cast<float*>(ws + at.parts), *part = reinterpret_cast<float*>(ws + at.sums);
-    const bool split = d.dx_type == FXPQ_FT_F32;
     const int dyb = ftype_bytes(d.y_type), some = d.gated ? 4 * dyb : 16;
     const int vec = (aligned(d.d_dy, some < 16 ? some : 16) && d.dy_stride * dyb % (some < 16 ? some : 16) == 0 ? 1 : 0) |
                     (aligned(d.d_pre, 16) ? 2 : 0) | (aligned(d.d_sw, 16) ? 4 : 0) | (aligned(d.d_bias, 16) ? 8 : 0);
     const int act = d.N > 0 ? d.activation : FXPQ_ACT_NONE;  // (rows of nothing read nothing)
     const GradRows G = {d.d_dy, d.dy_stride, d.d_pre, d.d_sx, d.d_sw, d.d_bias, (float)(1LL << sum_shift(d.K)), d.pre_type == FXPQ_FT_F32,
-                        act, d.N, at.plan.few, split, vec, rows, (long long)half_pitch(d.N), (long long)d.M, scale,
+                        act, d.N, at.plan.few, vec, rows, (long long)half_pitch(d.N), (long long)d.M, scale,
                         status_ptr()};
     fxpq_status rc = grad_rows(G, d.y_type, d.N > 0 && d.gated, st);
     if (rc != FXPQ_OK) return rc;
-    if (!split) return product<LAYER>({rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride}, {}, at.plan, part, st);
-    rc = product<LAYER>({rows, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, 2 * d.M, d.K, d.N, FXPQ_FT_F32, sums, d.K}, {}, at.plan, part, st);
-    if (rc != FXPQ_OK) return rc;
+    if (!at.plan.few) return product<PARTS>({rows, scale, d.d_wt, d.wt_stride, nullptr, nullptr, d.M, d.K, d.N, d.dx_type, d.d_dx, d.dx_stride}, {}, at.plan, part, st);
+    const int64_t pitch = (int64_t)half_pitch(d.N), at_once = 2 * d.M <= 65535 * 128 ? 2 * d.M : d.M;  // (its grid)
+    for (int64_t m = 0; m < 2 * d.M; m += at_once) {
+        rc = few_product<LAYER>(rows + m * pitch, pitch, nullptr, d.d_wt, d.wt_stride, nullptr, nullptr, at_once, d.K, d.N, FXPQ_FT_F32, sums + m * d.K, d.K, st, {},
+                                nullptr, m == 0);
+        if (rc != FXPQ_OK) return rc;
+    }
     launch_pdl(join_parts_kernel, dim3((unsigned)d.M, (unsigned)((d.K + 1023) / 1024)), dim3(256), 0, st, static_cast<const float*>(sums),
-               static_cast<const float*>(scale), (long long)d.M, (int)d.K, static_cast<float*>(d.d_dx), (long long)d.dx_stride);
+               static_cast<const float*>(scale), (long long)d.M, (int)d.K, d.d_dx, (int)d.dx_type, (long long)d.dx_stride);
     return after_launch("layer_join_parts");
 }

@@ -83,14 +83,15 @@ inline int sum_shift(int32_t K) {
 // Elements between rows of kept sums: whole 16 bytes.
 __host__ __device__ inline long long pre_pitch(int32_t N) { return ((long long)N + 7) / 8 * 8; }
 
-// The rows of a gradient, dz * sw (fxpq_layer_grad.cu).
+// The rows of a gradient, dz * sw, in two parts M rows apart (fxpq_layer_grad.cu).  PART: what the first part counts in.
+constexpr float PART = 4096.0f;
 struct GradRows {
     const void* dy;
     long long dy_stride;
     const void* pre;
     const float *sx, *sw, *bias;
     float pre_unit;
-    int pre_f32, act, N, early, split;
+    int pre_f32, act, N, early;
     int vec;  // dy, kept sums, scales, biases in aligned accesses (bits 1, 2, 4, 8)
     __half* rows;
     long long pitch, M;

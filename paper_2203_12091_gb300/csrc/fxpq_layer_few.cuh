@@ -205,25 +205,27 @@ inline int fours(const Epi& e, int y_type, const void* y, int64_t y_stride) {
 }
 
 // The sums that pairs of CTAs left in memory, added over a tile's shares in their order, and what follows them: a warp has four tokens of
-// 128 channels.
+// 128 channels (PARTS: of both their sums, half a tile apart).
 template <int EPI>
 __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ ManyArgs P, int nt) {
     pdl_wait();
-    constexpr int EACH = 4;
+    constexpr int EACH = 4, AFTER = EPI == PARTS ? LAYER : EPI;
+    const int tokens = EPI == PARTS ? nt / 2 : nt;  // of a tile
     const int tile = blockIdx.x >> 1, rank = blockIdx.x & 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int tn, tm;
     tile_of(P, P.whole + tile, tn, tm);
     const int ch = tn * 256 + rank * 128 + 4 * lane, left = P.N - ch, c0 = (blockIdx.y * 8 + warp) * EACH;
-    const long long m0 = (long long)tm * nt + c0;
+    const long long m0 = (long long)tm * tokens + c0;
     const int count = (int)min((long long)EACH, P.M - m0);
     if (left <= 0 || count <= 0) return;
     const bool whole = (P.e.vec & 2) && left >= 4;
-    float4 a[EACH];
+    float4 a[EACH], b[EPI == PARTS ? EACH : 1];  // (PARTS: the second parts' sums)
     Residual r[EACH];
     float sw[4], bias[4], sx[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         a[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if constexpr (EPI == PARTS) b[i] = a[i];
         if (i >= count) continue;
         if (EPI == LAYER && P.e.res) r[i].load(P.e.res, P.y_type, (m0 + i) * P.e.res_stride + ch, left, whole);
         sx[i] = P.sx ? __ldg(P.sx + m0 + i) : 1.0f;
@@ -241,11 +243,20 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Man
             if (i >= count) continue;
             const float4 f = *reinterpret_cast<const float4*>(part + i * 128);
             a[i].x += f.x, a[i].y += f.y, a[i].z += f.z, a[i].w += f.w;
+            if constexpr (EPI == PARTS) {
+                const float4 g = *reinterpret_cast<const float4*>(part + (tokens + i) * 128);
+                b[i].x += g.x, b[i].y += g.y, b[i].z += g.z, b[i].w += g.w;
+            }
         }
+    }
+    if constexpr (EPI == PARTS) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            a[i] = make_float4(fmaf(a[i].x, PART, b[i].x), fmaf(a[i].y, PART, b[i].y), fmaf(a[i].z, PART, b[i].z), fmaf(a[i].w, PART, b[i].w));
     }
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
-        finish_four<EPI>(P, P.e, m0 + i, ch, a[0], sx[0], sw, bias, r[0], whole);
+        finish_four<AFTER>(P, P.e, m0 + i, ch, a[0], sx[0], sw, bias, r[0], whole);
 #pragma unroll
         for (int j = 0; j + 1 < EACH; ++j) a[j] = a[j + 1], sx[j] = sx[j + 1], r[j] = r[j + 1];
     }

@@ -52,8 +52,10 @@ struct Words {
     }
 };
 
-// One block a row: as fp16 with a power of two of the row's own; split: in two parts, integers up to 2^11 (exact in fp16, as are their
-// products' sums below 2^24), the lower ones M rows further on.
+// One block a row, as two rows of fp16 with a power of two of the row's own: v up to 2^23, h = v / 2^12 rounded to an integer (up to 2^11: exact in
+// fp16, as are its products' sums below 2^24), and what h leaves of v (up to 2^11, to 2^-12 of itself), M rows further on.  So a value
+// loses 2^-23 of the row's largest at most, or 2^-12 of its own size where that is less.  (In one part of 11 bits gradients of 16 bits came
+// out 3e-4 to 1e-3 from those of 32-bit products, in their last places.)
 // Bytes bound it (dy and the sums in, the row out): 8192 rows of 2 x 5632 460 MB, 68 us.  Rows stay in registers between their maximum
 // and the rounding, GR_KEEP groups of eight channels a thread, which are also on their way together; what does not fit, the last
 // group of some, and all of constants or sums that are not aligned, is formed again.  (A group at a time, kept in shared memory, the same rows took 185 us.)
@@ -160,8 +162,8 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
     for (int w = 0; w < GR_THREADS / 32; ++w) top = max(top, part[w]);
     if (G.early) pdl_next();
     const bool bad = top >= 0x7f800000u;
-    // top < 2^e; the row's largest value lies in [2^14, 2^15), or as an integer in [2^22, 2^23)
-    const int e = max(top ? ilogbf(__uint_as_float(top)) + 1 : 0, -100), up = G.split ? 23 : 15;
+    // top < 2^e; the row's largest value lies in [2^22, 2^23)
+    const int e = max(top ? ilogbf(__uint_as_float(top)) + 1 : 0, -100), up = 23;
     const float lift = ldexpf(1.0f, up - e);
     if (t == 0) {
         G.scale[m] = bad ? __int_as_float(0x7fffffff) : ldexpf(1.0f, e - up);
@@ -174,16 +176,12 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float a = bad ? 0.0f : v[2 * i] * lift, b = bad ? 0.0f : v[2 * i + 1] * lift;
-            if (G.split) {
-                const float ha = rintf(a * (1.0f / 4096.0f)), hb = rintf(b * (1.0f / 4096.0f));
-                h[i] = h2_bits(__floats2half2_rn(ha, hb));
-                l[i] = h2_bits(__floats2half2_rn(rintf(fmaf(ha, -4096.0f, a)), rintf(fmaf(hb, -4096.0f, b))));
-            } else {
-                h[i] = h2_bits(__floats2half2_rn(a, b));
-            }
+            const float ha = rintf(a * (1.0f / PART)), hb = rintf(b * (1.0f / PART));
+            h[i] = h2_bits(__floats2half2_rn(ha, hb));
+            l[i] = h2_bits(__floats2half2_rn(fmaf(ha, -PART, a), fmaf(hb, -PART, b)));
         }
         hi[g] = make_uint4(h[0], h[1], h[2], h[3]);
-        if (G.split) lo[g] = make_uint4(l[0], l[1], l[2], l[3]);
+        lo[g] = make_uint4(l[0], l[1], l[2], l[3]);
     };
 #pragma unroll
     for (int s = 0; s < GR_KEEP; ++s)
@@ -198,7 +196,7 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
     }
     if (t == 0 && (groups & 1)) {  // rows are padded to 16
         hi[groups] = make_uint4(0, 0, 0, 0);
-        if (G.split) lo[groups] = make_uint4(0, 0, 0, 0);
+        lo[groups] = make_uint4(0, 0, 0, 0);
     }
 }
 

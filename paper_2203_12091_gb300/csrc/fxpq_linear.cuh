@@ -20,8 +20,9 @@ __device__ __forceinline__ void store_y(void* y, int type, long long at, float v
 }
 
 // What follows the sums of a product: PLAIN, y = sum * sx * sw + bias; LAYER, activation and residual after that; GATED, neighbouring
-// channels' activation times value.  Both of the latter may keep the sums (scaled, in fp16, or as they are) for a gradient.
-enum { PLAIN, LAYER, GATED };
+// channels' activation times value.  Both of the latter may keep the sums (scaled, in fp16, or as they are) for a gradient.  PARTS: the rows
+// are a gradient's, in two parts (GradRows): y = (PART sum of the first + sum of the second) * sx.
+enum { PLAIN, LAYER, GATED, PARTS };
 struct Epi {
     const void* res;
     long long res_stride;
@@ -307,13 +308,19 @@ __device__ __forceinline__ void epilogue_any(const ManyArgs& P, const uint32_t (
 constexpr int LM_REGS = 80, LM_REGS_EPI = 96, LM_REGS_ISSUE = 32, LM_REGS_CONV = 64;
 static_assert(LM_REGS_ISSUE + LM_REGS_CONV + 4 * LM_REGS_EPI <= 6 * LM_REGS, "the launch's registers");
 
+__device__ __forceinline__ void load_sums(uint32_t at, uint32_t (&v)[16]) { tc::tmem_ld16_nw(at, v); }
+__device__ __forceinline__ void load_sums(uint32_t at, uint32_t (&v)[32]) { tc::tmem_ld32_nw(at, v); }
+
 constexpr int many_threads(int epi) { return epi == PLAIN ? 512 : 768; }
 
 // NT: tokens of a tile, 256 or, where those tiles would leave pairs idle, 128.
 template <int NT, int EPI, int FORM>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(many_threads(EPI), 1) linear_many_kernel(const __grid_constant__ ManyArgs P) {
     using namespace tc;
-    constexpr int EW = EPI == PLAIN ? 8 : 16, ROWS = NT * 4 / EW;      // warps of the epilogue, and each one's tokens
+    constexpr int EW = EPI == PLAIN ? 8 : 16, ROWS = NT * 4 / EW;      // warps of the epilogue, and each one's columns
+    // Tokens of a tile, and of a warp.  PARTS: the tile's first half of columns are its tokens' first parts, CTA 0's half of the operand, the
+    // second half their second, CTA 1's; a warp has the same tokens of both, and what it stores is joined in registers.
+    constexpr int TILE = EPI == PARTS ? NT / 2 : NT, TOKENS = EPI == PARTS ? ROWS / 2 : ROWS;
     constexpr int HALF_ROWS = NT / 2, STAGE = HALF_ROWS * 128;         // tokens of a CTA's half of the operand, its stage
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -410,7 +417,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(many_threads(EPI), 1
                         break;
                     }
                     if (rank == 0) mbar_arrive_expect_tx(b_full + 8 * s, 2 * STAGE);
-                    tma_load_2d_pair(b0 + s * STAGE, &P.tx, hb * 64, tm * NT + rank * HALF_ROWS, lead + 8 * s);
+                    tma_load_2d_pair(b0 + s * STAGE, &P.tx, hb * 64, tm * TILE + rank * (EPI == PARTS ? (int)P.M : HALF_ROWS), lead + 8 * s);
                 }
             }
             if (rank == 0)
@@ -424,8 +431,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(many_threads(EPI), 1
                 uint32_t ia = 0, ib = 0, it = 0;
                 bool ok = true;
                 for (int u = pair; u < n_work && ok; u += pairs, ++it) {
-                int t = u, first, last;
-                share_of(t, first, last);
+                    int t = u, first, last;
+                    share_of(t, first, last);
                     if (!wait_warp_cluster(acc_empty, (it & 1) ^ 1, abort, P.status)) break;
                     tc_fence_after();
                     uint32_t acc = 0;
@@ -500,8 +507,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(many_threads(EPI), 1
         }
     } else {
         if constexpr (EPI != PLAIN) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(LM_REGS_EPI));
-        const int quad = warp & 3, half = (warp - 8) >> 2;  // channels 32 quad + lane, tokens ROWS half ..
-        const uint32_t lead = cluster_addr(acc_empty, 0), at = tmem + ((uint32_t)(quad * 32) << 16) + ROWS * half;
+        const int quad = warp & 3, half = (warp - 8) >> 2;  // channels 32 quad + lane, tokens TOKENS half ..
+        const uint32_t lead = cluster_addr(acc_empty, 0), at = tmem + ((uint32_t)(quad * 32) << 16) + TOKENS * half;
         float* sxs = s_sx[warp - 8];
         uint32_t it = 0;
         for (int u = pair; u < n_work; u += pairs, ++it) {
@@ -509,12 +516,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(many_threads(EPI), 1
             const int share = share_of(t, first, last);
             tile_of(P, t, tn, tm);
             const int ch = tn * 256 + rank * 128 + quad * 32 + lane;
-            const long long m0 = (long long)tm * NT + ROWS * half;
+            const long long m0 = (long long)tm * TILE + TOKENS * half;
             const float sw = !P.sw ? 1.0f : ch < P.N ? __ldg(P.sw + ch) : 0.0f, bias = P.bias && ch < P.N ? __ldg(P.bias + ch) : 0.0f;
-            for (int i = lane; i < ROWS; i += 32) sxs[i] = !P.sx ? 1.0f : m0 + i < P.M ? __ldg(P.sx + m0 + i) : 0.0f;
+            for (int i = lane; i < TOKENS; i += 32) sxs[i] = !P.sx ? 1.0f : m0 + i < P.M ? __ldg(P.sx + m0 + i) : 0.0f;
             __syncwarp();
-            const int cols = (int)min((long long)ROWS, P.M - m0);
-            Residuals<ROWS> held;
+            const int cols = (int)min((long long)TOKENS, P.M - m0);
+            Residuals<TOKENS> held;
             if constexpr (EPI == LAYER) {
                 const int odd = lane & 1, c0 = ch - odd;
                 held.at = static_cast<const char*>(P.e.res) + ((m0 + odd) * P.e.res_stride + c0) * 2, held.step = 2 * P.e.res_stride * 2;
@@ -529,31 +536,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(many_threads(EPI), 1
                 const int odd = lane & 1, c0 = ch - odd;
                 const float sw_o = __shfl_xor_sync(0xffffffffu, sw, 1), bias_o = __shfl_xor_sync(0xffffffffu, bias, 1);
                 const float2 sw2 = odd ? make_float2(sw_o, sw) : make_float2(sw, sw_o), bias2 = odd ? make_float2(bias_o, bias) : make_float2(bias, bias_o);
-                uint32_t v[ROWS / 32][32];
+                constexpr int W = EPI == PARTS ? TOKENS : 32, APART = EPI == PARTS ? TILE : 32, AFTER = EPI == PARTS ? LAYER : EPI;
+                uint32_t v[ROWS / W][W];  // (both parts)
 #pragma unroll
-                for (int c = 0; c < ROWS / 32; ++c) tmem_ld32_nw(at + 32 * c, v[c]);
+                for (int c = 0; c < ROWS / W; ++c) load_sums(at + APART * c, v[c]);
                 tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < ROWS / 32; ++c) reg_fence(v[c]);
+                for (int c = 0; c < ROWS / W; ++c) reg_fence(v[c]);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(lead);  // the accumulators may be overwritten
                 if (t >= P.whole) {
-                    float* to = P.part + ((((long long)share * (P.n_tiles - P.whole) + t - P.whole) * 2 + rank) * NT + ROWS * half) * 128 + quad * 32 + lane;
+                    float* to = P.part + ((((long long)share * (P.n_tiles - P.whole) + t - P.whole) * 2 + rank) * NT + TOKENS * half) * 128 + quad * 32 + lane;
 #pragma unroll
                     for (int i = 0; i < ROWS; ++i)
-                        if (i < cols) to[i * 128] = __uint_as_float(v[i / 32][i % 32]);
-                } else if (P.e.fast) {
-                    epilogue_fast<ROWS, EPI, FORM>(P, [&](int t) { return __uint_as_float(v[t / 32][t % 32]); }, sxs, sw2, bias2, c0, odd, m0, cols, held);
+                        if ((EPI == PARTS ? i % W : i) < cols) to[(i / W * APART + i % W) * 128] = __uint_as_float(v[i / W][i % W]);
+                    __syncwarp();  // (the scales are read)
+                    continue;
+                }
+                if constexpr (EPI == PARTS) {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) v[0][i] = __float_as_uint(fmaf(__uint_as_float(v[0][i]), PART, __uint_as_float(v[1][i])));
+                }
+                if (P.e.fast) {
+                    epilogue_fast<TOKENS, AFTER, FORM>(P, [&](int t) { return __uint_as_float(v[t / W][t % W]); }, sxs, sw2, bias2, c0, odd, m0, cols, held);
                 } else {  // 16 tokens at a time, in one place of the code: the others move up
 #pragma unroll 1
-                    for (int c = 0; c < ROWS; c += 16) {
+                    for (int c = 0; c < TOKENS; c += 16) {
                         uint32_t now[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) now[i] = v[0][i];
-                        epilogue_any<EPI>(P, now, sxs + c, sw, bias, ch, m0 + c, cols - c);
+                        epilogue_any<AFTER>(P, now, sxs + c, sw, bias, ch, m0 + c, cols - c);
 #pragma unroll
-                        for (int i = 0; i < ROWS - 16; ++i) v[i / 32][i % 32] = v[(i + 16) / 32][(i + 16) % 32];
+                        for (int i = 0; i < TOKENS - 16; ++i) v[i / W][i % W] = v[(i + 16) / W][(i + 16) % W];
                     }
                 }
                 __syncwarp();  // (the scales are read)
@@ -687,7 +702,8 @@ fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
     const auto kernel = linear_many_kernel<NT, EPI, FORM>;
     static std::atomic<uint64_t> set{0};
     if (!allow_smem(kernel, LM_SMEM, set, EPI == PLAIN ? 0 : LM_REGS)) return FXPQ_ERR_CUDA;
-    const long long tn = ((long long)P.N + 255) / 256, tm = (P.M + NT - 1) / NT;
+    constexpr int TILE = EPI == PARTS ? NT / 2 : NT;
+    const long long tn = ((long long)P.N + 255) / 256, tm = (P.M + TILE - 1) / TILE;
     if (tn * tm > INT32_MAX) return FXPQ_ERR_UNSUPPORTED;
     P.tiles_n = (int)tn, P.tiles_m = (int)tm, P.n_tiles = (int)(tn * tm);
     P.y_pair = aligned(P.y, 4) && P.ys % 2 == 0;
@@ -706,7 +722,8 @@ fxpq_status product_many(const __half* half, size_t pitch, const float* d_sx, co
     ManyArgs& P = args ? *args : mine;  // (what finish_kernel takes)
     P.e = e, P.whole = plan ? plan->whole : INT32_MAX, P.shares = plan ? plan->shares : 1, P.part = plan ? plan->part : nullptr;
     const int nt = plan ? plan->nt : many_tile(M, N);
-    if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_half_rows(&P.tx, half, M, K, (long long)pitch, nt / 2)) return FXPQ_ERR_CUDA;
+    if (!encode_rows(&P.tw, d_w, N, K, w_stride, 128) || !encode_half_rows(&P.tx, half, EPI == PARTS ? 2 * M : M, K, (long long)pitch, nt / 2))
+        return FXPQ_ERR_CUDA;
     P.sx = d_sx, P.sw = d_sw, P.bias = d_bias, P.y = d_y, P.ys = y_stride, P.M = M, P.N = N, P.K = K, P.y_type = y_type;
     P.status = status_ptr();
     const auto go = [&](auto form) {
@@ -720,6 +737,8 @@ fxpq_status product_many(const __half* half, size_t pitch, const float* d_sx, co
         // (a gate that is cut, the rarest form, has no kernel of its own)
         P.e.fast = y_type != FXPQ_FT_F32 && P.e.vec == 7 && N % (EPI == GATED ? 4 : 2) == 0 && !(e.pre && e.pre_f32) &&
                    !(EPI == GATED && e.act == FXPQ_ACT_RELU);
+    }
+    if constexpr (EPI == LAYER || EPI == GATED) {
         if (e.act == FXPQ_ACT_GELU) return go(std::integral_constant<int, NORMAL>());
         if (EPI == GATED || e.act == FXPQ_ACT_SILU || e.act == FXPQ_ACT_GELU_TANH) return go(std::integral_constant<int, SIGMOID>());
     }
