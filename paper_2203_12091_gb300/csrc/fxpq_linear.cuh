@@ -160,8 +160,9 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
     sxs += odd;
     const float ps = P.e.pre_scale;
     // (addresses that walk along the tokens: computed from the token each, they took more registers than there are)
-    const long long y_step = 2 * P.ys * 2, p_step = 2 * P.e.pre_stride * 2;
-    char* pre = P.e.pre ? static_cast<char*>(P.e.pre) + ((m0 + odd) * P.e.pre_stride + c0) * 2 : nullptr;
+    const int kept = P.e.pre_f32 ? 4 : 2;
+    const long long y_step = 2 * P.ys * 2, p_step = 2 * P.e.pre_stride * kept;
+    char* pre = P.e.pre ? static_cast<char*>(P.e.pre) + ((m0 + odd) * P.e.pre_stride + c0) * kept : nullptr;
     auto act = [&](float z) { return FORM == SIGMOID ? sig(z) : FORM == NORMAL ? gelu(z) : cut(z, low); };
     auto pack = [&](float a, float b) {
         if (f16) return h2_bits(__floats2half2_rn(a, b));
@@ -184,7 +185,12 @@ __device__ __forceinline__ void epilogue_fast(const ManyArgs& P, Sum&& sum, cons
         if (P.e.pre) {
 #pragma unroll
             for (int i = 0; i < STEP; ++i) {
-                if (2 * (i0 + i) < cols) *reinterpret_cast<__half2*>(pre) = __floats2half2_rn(a[i] * ps, b[i] * ps);
+                if (2 * (i0 + i) < cols) {
+                    if (P.e.pre_f32)
+                        *reinterpret_cast<float2*>(pre) = make_float2(a[i], b[i]);
+                    else
+                        *reinterpret_cast<__half2*>(pre) = __floats2half2_rn(a[i] * ps, b[i] * ps);
+                }
                 pre += p_step;
             }
         }
@@ -735,8 +741,7 @@ fxpq_status product_many(const __half* half, size_t pitch, const float* d_sx, co
         P.e.vec = (aligned(d_y, 2 * type) && y_stride % 2 == 0 ? 1 : 0) | (aligned(e.res, 2 * type) && e.res_stride % 2 == 0 ? 2 : 0) |
                   (aligned(e.pre, 2 * kept) && e.pre_stride % 2 == 0 ? 4 : 0);
         // (a gate that is cut, the rarest form, has no kernel of its own)
-        P.e.fast = y_type != FXPQ_FT_F32 && P.e.vec == 7 && N % (EPI == GATED ? 4 : 2) == 0 && !(e.pre && e.pre_f32) &&
-                   !(EPI == GATED && e.act == FXPQ_ACT_RELU);
+        P.e.fast = y_type != FXPQ_FT_F32 && P.e.vec == 7 && N % (EPI == GATED ? 4 : 2) == 0 && !(EPI == GATED && e.act == FXPQ_ACT_RELU);
     }
     if constexpr (EPI == LAYER || EPI == GATED) {
         if (e.act == FXPQ_ACT_GELU) return go(std::integral_constant<int, NORMAL>());

@@ -135,9 +135,9 @@ def _activation(name, activation):
     return act
 
 
-def _kept_row(N, wide):
-    """Bytes of a row of kept sums."""
-    return (N + 7) // 8 * 8 * (4 if wide else 2)
+def _kept_row(N):
+    """Bytes of a row of kept sums: in 32 bits, so that a slope is taken at the forward pass's own z."""
+    return (N + 7) // 8 * 8 * 4
 
 
 class _Layer8:
@@ -187,14 +187,14 @@ class _Layer8:
             r = _float_rows(name + ": residual", residual)
             res, res_stride = r.data_ptr(), r.stride(0)
         y = _empty((M, wide), dtype=dtype, device=dev)
-        kept, pre_t = None, L.FT_F32 if xt == L.FT_F32 or yt == L.FT_F32 else L.FT_F16
+        kept = None
         if keep and act:
-            room = M * _kept_row(N, pre_t == L.FT_F32)
+            room = M * _kept_row(N)
             kept = _empty(room + 4 * M, dtype=_u8, device=dev)
             pre_at = kept.data_ptr()
             sx_at = pre_at + room
         desc = _LAYER(rows.data_ptr(), rows.stride(0), nrm, w.data_ptr(), _pitch(w, K), self.w_scale.data_ptr(), 0 if bias is None else bias.data_ptr(),
-                      res, res_stride, y.data_ptr(), wide, pre_at, sx_at, M, N, K, xt, yt, act, self.gated, pre_t, eps)
+                      res, res_stride, y.data_ptr(), wide, pre_at, sx_at, M, N, K, xt, yt, act, self.gated, L.FT_F32, eps)
         lib = L.lib()
         need = lib.fxpq_layer_workspace(desc)
         ws = _empty(need, dtype=_u8, device=dev) if need else None
@@ -215,11 +215,10 @@ class _Layer8:
         M, (N, K), wt, bias = rows.shape[0], self.w.shape, self.wt, self.bias
         dx = _empty((M, K), dtype=dtype, device=dy.device)
         xt, yt = _FT[dtype], _FT[dy.dtype]
-        wide32 = xt == L.FT_F32 or yt == L.FT_F32
         pre = 0 if kept is None else kept.data_ptr()
-        desc = _LAYER_GRAD(rows.data_ptr(), rows.stride(0), pre, pre and pre + M * _kept_row(N, wide32), self.w_scale.data_ptr(),
+        desc = _LAYER_GRAD(rows.data_ptr(), rows.stride(0), pre, pre and pre + M * _kept_row(N), self.w_scale.data_ptr(),
                            0 if bias is None else bias.data_ptr(), wt.data_ptr(), _pitch(wt, N), dx.data_ptr(), K, M, N, K, yt, xt, act, self.gated,
-                           L.FT_F32 if wide32 else L.FT_F16, 0)
+                           L.FT_F32, 0)
         lib = L.lib()
         need = lib.fxpq_layer_gradient_workspace(desc)
         ws = _empty(need, dtype=_u8, device=dy.device)

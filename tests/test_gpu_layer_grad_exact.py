@@ -1,9 +1,11 @@
-"""Gradients of 8-bit layers held to what 32 bits give: the rows dz * sw to 2^-23 of the row's largest value, sums exact."""
+"""Gradients of 8-bit layers held to what 32 bits give: the rows dz * sw to 2^-23 of the row's largest value, sums exact, activations' slopes
+of the forward pass's own z."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_layer import TYPES, Weights, check, host, ops, rows, status_is_clear  # noqa: F401
+from oracle import llm as O
+from test_gpu_layer import ACTS, TYPES, Weights, act_spread, argument, check, host, ops, rows, status_is_clear  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +57,68 @@ def test_small_values_beside_a_large_one(ops, M, N, K, x):
     dy[:, 5] = 2.0 ** 20
     dx = torch.autograd.grad(layer(leaf, torch.float32), leaf, dy)[0]
     check_rows(dx, host(dy), 0.0 * host(dy), W, x)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 512, 300), (40, 512, 300), (300, 512, 256), (700, 300, 512)])
+@pytest.mark.parametrize("act", ACTS[2:])
+@pytest.mark.parametrize("is_gated", [False, True])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_slopes_are_those_of_the_forward_pass(ops, M, N, K, act, is_gated, kind):
+    """z as the forward pass had it, not of rounded sums: what is left is the arithmetic of the slopes."""
+    rng = np.random.default_rng(M + N + K)
+    N = N // 2 if is_gated else N
+    W = small(rng, N, K, True, 2 if is_gated else 1)
+    layer = (W.gated(ops, act) if is_gated else W.layer(ops)).with_gradient()
+    leaf = rows(rng, M, K, kind).requires_grad_()
+    y = layer(leaf) if is_gated else layer(leaf, activation=act)
+    dy = rows(rng, M, N, kind)
+    dx = torch.autograd.grad(y, leaf, dy)[0]
+    z, e, _ = W.sums(leaf)
+    d = host(dy)
+    # slopes bend by less than 0.8 a unit of z; their exponentials and quotients are good to some steps of 2^-22 of what they are made of
+    slope_err = 0.8 * e + np.minimum((16 + 8 * argument(z, act)) * 2.0 ** -22, 1) * (1 + np.abs(z))
+    if is_gated:
+        g, u, eg, eu = z[:, ::2], z[:, 1::2], e[:, ::2], e[:, 1::2]
+        f, slope = O.activation(g, act)
+        err = np.empty_like(z)
+        err[:, ::2] = np.abs(d) * (np.abs(slope) * eu + (np.abs(u) + eu) * slope_err[:, ::2])
+        err[:, 1::2] = np.abs(d) * (act_spread(g, eg, act) + np.abs(f) * 2.0 ** -23)
+    else:
+        err = np.abs(d) * slope_err
+    check_rows(dx, O.layer_slopes(z, d, act, is_gated), err, W, kind)
+
+
+@pytest.mark.parametrize("M", [3, 40, 300, 1300])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("is_gated", [False, True])
+def test_relu_passes_a_gradient_where_its_own_output_is_positive(ops, M, out, is_gated):
+    """Biases that take back one row's sums but for their rounding, so that z lies next to 0 on either side there."""
+    rng = np.random.default_rng(M)
+    N, K = 512, 2048
+    W = small(rng, N // 2 if is_gated else N, K, True, 2 if is_gated else 1)
+    leaf = rows(rng, M, K, "bf16").requires_grad_()
+    codes, sx = O.quantize_tokens(leaf.detach().float().cpu().numpy())
+    at = M // 2
+    near = -(O.layer_sums(codes[at:at + 1], W.w)[0][0].astype(np.float32) * np.float32(sx[at]) * W.sw)
+    if is_gated:
+        W.b[::2], W.b[1::2] = near[::2], 1
+    else:
+        W.b[:] = near
+    layer = (W.gated(ops, "relu") if is_gated else W.layer(ops)).with_gradient()
+    y = layer(leaf, TYPES[out]) if is_gated else layer(leaf, TYPES[out], activation="relu")
+    dy = rows(rng, M, y.shape[1], out)
+    dx = torch.autograd.grad(y, leaf, dy)[0]
+    z, e, _ = W.sums(leaf)
+    d = host(dy)
+    if is_gated:
+        g, u = z[:, ::2], z[:, 1::2]
+        on = (host(y) * u > 0) | (g > 1)  # (y = relu(g) u, and no u is 0 here)
+        assert np.all(u != 0)
+        dz, err = np.empty_like(z), np.empty_like(z)
+        dz[:, ::2], dz[:, 1::2] = d * u * on, d * np.maximum(g, 0)
+        err[:, ::2], err[:, 1::2] = np.abs(d) * e[:, 1::2], np.abs(d) * e[:, ::2]
+    else:
+        on = host(y) > 0
+        dz, err = d * on, 0 * d
+    assert 0.1 < on[at].mean() < 0.9 and np.all(np.abs(z[at, :: 2 if is_gated else 1]) < 1e-5)
+    check_rows(dx, dz, err, W, "bf16")
