@@ -579,7 +579,9 @@ FXPQ_API fxpq_status fxpq_layer_forward(const fxpq_layer* layer, void* d_ws, siz
  * identity:
  *   dz[m, n] = dy[m, n] act'(z[m, n]);   gated: dz[m, 2 j] = dy[m, j] z[m, 2 j + 1] act'(z[m, 2 j]), dz[m, 2 j + 1] = dy[m, j] act(z[m, 2 j])
  *   dx[m, k] = sum_n dz[m, n] d_sw[n] w[n, k]
- * d_dy: rows of N (gated: N / 2) values of y_type; d_pre, pre_type, d_sx: what fxpq_layer_forward left (not read without activation);
+ * d_dy: rows of N (gated: N / 2) values of y_type; d_pre, pre_type, d_sx: what fxpq_layer_forward left (not read without activation).
+ * With sums kept in F32 act' is taken at the forward pass's own z, with F16 at one that is off by up to 2^-11 of sum * sx * d_sw; ReLU, whose
+ * derivative steps, needs F32.
  * d_wt: the weights' codes transposed, [K][N], 16-byte aligned rows a multiple of 16 bytes apart; d_dx: rows of K values of dx_type.
  * A row's dz * sw is taken in two parts of fp16 with a power of two of its own: to 2^-23 of the row's largest value, or to 2^-12 of each value
  * (2^-47 of the largest) where that is less; products are exact, sums fp32.  ReLU's derivative at 0 is 0.  A row with a

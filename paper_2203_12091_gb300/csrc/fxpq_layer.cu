@@ -210,6 +210,8 @@ extern "C" fxpq_status fxpq_layer_gradient(const fxpq_layer_grad* grad, void* d_
         return FXPQ_ERR_INVALID_ARG;
     if (d.N > 0 && d.activation != FXPQ_ACT_NONE && (!d.d_pre || !d.d_sx || !aligned(d.d_pre, ftype_bytes(d.pre_type)) || !aligned(d.d_sx, 4)))
         return FXPQ_ERR_INVALID_ARG;
+    // (sums rounded to 16 bits may lie on the other side of the step than the forward pass's z: gradients where y is 0)
+    if (d.N > 0 && d.activation == FXPQ_ACT_RELU && d.pre_type == FXPQ_FT_F16) return FXPQ_ERR_INVALID_ARG;
     const GradSpace at(d);
     if (!d_ws || ws_bytes < at.end || !aligned(d_ws, 256)) return FXPQ_ERR_WORKSPACE;
     char* ws = static_cast<char*>(d_ws);

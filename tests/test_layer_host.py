@@ -151,6 +151,15 @@ def test_gradient_refuses(lib, bad):
     assert run_grad(lib, grad(**bad)) == L.ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("gated", [0, 1])
+def test_relus_gradient_refuses_rounded_sums(lib, gated):
+    """z > 0 of a rounded sum is not what the forward pass cut."""
+    bad = grad(act=L.ACT_RELU, gated=gated)
+    assert run_grad(lib, bad) == L.ERR_INVALID_ARG
+    assert run_grad(lib, grad(act=L.ACT_RELU, gated=gated, pt=L.FT_F32), short=1) == L.ERR_WORKSPACE  # (past that check)
+    assert run_grad(lib, grad(act=L.ACT_RELU, gated=gated, N=0, dy=None, pre=None), short=1) == L.ERR_WORKSPACE  # (nothing to cut)
+
+
 def test_gradient_refuses_workspaces(lib):
     assert run_grad(lib, grad(), work=None) == run_grad(lib, grad(), short=1) == run_grad(lib, grad(), work=4112) == L.ERR_WORKSPACE
     assert run_grad(lib, grad(M=0)) == run_grad(lib, grad(K=0)) == L.OK
