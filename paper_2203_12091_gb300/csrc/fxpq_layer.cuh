@@ -11,6 +11,12 @@ __device__ __forceinline__ float cut(float z, float low) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(z), "f"(low));
     return y;
 }
+// z between -limit and limit; NaN stays NaN.
+__device__ __forceinline__ float within(float z, float limit) {
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(cut(z, -limit)), "f"(limit));
+    return y;
+}
 inline bool act_ok(int a) { return a >= FXPQ_ACT_NONE && a <= FXPQ_ACT_GELU_TANH; }
 
 // 1 / (1 + e^-z).  (__expf and __fdividef: 2^-21 of the result where it is 2^-8 or more; past e^88 the quotient is 0.)
@@ -37,7 +43,7 @@ __device__ __forceinline__ float normal_tail(float a, float& e) {
 __device__ __forceinline__ float gelu(float z) {
     float e;
     const float q = normal_tail(fabsf(z), e);
-    return fmaxf(z, -40.0f) * (z > 0.0f ? 1.0f - q : q);  // (far below, a tail of 0 meets no inf)
+    return cut(z, -40.0f) * (z > 0.0f ? 1.0f - q : q);  // (far below, a tail of 0 meets no inf)
 }
 __device__ __forceinline__ float activate(float z, int act) {
     switch (act) {
@@ -48,24 +54,24 @@ __device__ __forceinline__ float activate(float z, int act) {
         default: return z;
     }
 }
-// act(z) and its derivative.  Where the derivative has reached its limits z is cut off, so that no inf meets a zero.
+// act(z) and its derivative.  Where the derivative has reached its limits z is cut off, so that no inf meets a zero; both are NaN where z is.
 __device__ __forceinline__ float activate_slope(float z, int act, float& slope) {
     switch (act) {
-        case FXPQ_ACT_RELU: slope = z > 0.0f ? 1.0f : 0.0f; return cut(z, 0.0f);
+        case FXPQ_ACT_RELU: slope = z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z; return cut(z, 0.0f);
         case FXPQ_ACT_SILU: {
-            const float c = fminf(fmaxf(z, -100.0f), 100.0f), s = sigmoid(c);
+            const float c = within(z, 100.0f), s = sigmoid(c);
             slope = s * fmaf(c, 1.0f - s, 1.0f);
             return z * s;
         }
         case FXPQ_ACT_GELU: {
-            const float c = fminf(fmaxf(z, -40.0f), 40.0f);
+            const float c = within(z, 40.0f);
             float e;
             const float q = normal_tail(fabsf(c), e), p = z > 0.0f ? 1.0f - q : q;
             slope = fmaf(c * 0.3989422804014327f, e, p);
-            return fmaxf(z, -40.0f) * p;
+            return cut(z, -40.0f) * p;
         }
         case FXPQ_ACT_GELU_TANH: {
-            const float c = fminf(fmaxf(z, -30.0f), 30.0f), p = sigmoid(GELU_A * c * fmaf(GELU_B, c * c, 1.0f));
+            const float c = within(z, 30.0f), p = sigmoid(GELU_A * c * fmaf(GELU_B, c * c, 1.0f));
             slope = p * fmaf(c * (1.0f - p), GELU_A * fmaf(3.0f * GELU_B, c * c, 1.0f), 1.0f);
             return z * p;
         }

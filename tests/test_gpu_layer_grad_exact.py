@@ -5,6 +5,8 @@ import pytest
 import torch
 
 from oracle import llm as O
+from paper_2203_12091_gb300 import _lib as L
+from paper_2203_12091_gb300 import fxpq as F
 from test_gpu_layer import ACTS, TYPES, Weights, act_spread, argument, check, host, ops, rows, status_is_clear  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -122,3 +124,27 @@ def test_relu_passes_a_gradient_where_its_own_output_is_positive(ops, M, out, is
         dz, err = d * on, 0 * d
     assert 0.1 < on[at].mean() < 0.9 and np.all(np.abs(z[at, :: 2 if is_gated else 1]) < 1e-5)
     check_rows(dx, dz, err, W, "bf16")
+
+
+@pytest.mark.parametrize("M", [3, 40, 300])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("is_gated", [False, True])
+def test_nan_in_a_bias_reaches_the_gradient(ops, M, act, is_gated):
+    """z is NaN in one channel: so is every slope there, and with it every row's gradient, dy of 0 or not."""
+    if is_gated and act is None:
+        return
+    rng = np.random.default_rng(M)
+    for bad in (6, 7):  # (of a gate, and of a value)
+        W = small(rng, 64, 200, True, 2)
+        W.b[bad] = np.nan
+        layer = (W.gated(ops, act) if is_gated else W.layer(ops)).with_gradient()
+        leaf = rows(rng, M, 200, "bf16").requires_grad_()
+        y = layer(leaf) if is_gated else layer(leaf, activation=act)
+        dy = rows(rng, M, y.shape[1], "bf16")
+        dy[0] = 0
+        dx = torch.autograd.grad(y, leaf, dy)[0]
+        if act is None:  # (dz = dy: no z in it)
+            assert bool(dx.isfinite().all())
+        else:
+            assert F.fxpq_get_device_status() == L.ERR_NONFINITE
+            assert bool(dx.isnan().all())
