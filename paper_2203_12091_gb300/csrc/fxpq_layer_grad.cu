@@ -68,12 +68,15 @@ __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kerne
     constexpr int D = GATE ? 4 : 8;  // values of dy to eight channels
     const long long m = blockIdx.x;
     const int t = threadIdx.x, N = G.N, groups = (N + 7) / 8, pre_type = PRE == 4 ? FXPQ_FT_F32 : FXPQ_FT_F16;
-    const float sx = NEEDS ? __ldg(G.sx + m) * (PRE == 4 ? 1.0f : G.pre_unit) : 0.0f;  // (a power of two: z as in the forward pass)
+    const float sx = NEEDS ? __ldg(G.sx + m) : 0.0f;
     const long long pitch = pre_pitch(N);
     auto compute = [&](const float (&d)[D], float (&a)[8], const float (&w)[8], const float (&b)[8], float (&v)[8]) {
         if constexpr (NEEDS) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] = fmaf(a[e] * sx, w[e], G.bias ? b[e] : 0.0f);
+            for (int e = 0; e < 8; ++e) {
+                const float sum = PRE == 4 ? a[e] : a[e] * G.pre_unit;  // (a power of two; its product with sx instead can pass fp32 where z does not)
+                a[e] = fmaf(sum * sx, w[e], G.bias ? b[e] : 0.0f);
+            }
         }
 #pragma unroll
         for (int e = 0; e < 8; e += GATE ? 2 : 1) {

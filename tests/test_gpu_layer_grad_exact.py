@@ -148,3 +148,33 @@ def test_nan_in_a_bias_reaches_the_gradient(ops, M, act, is_gated):
         else:
             assert F.fxpq_get_device_status() == L.ERR_NONFINITE
             assert bool(dx.isnan().all())
+
+
+@pytest.mark.parametrize("act", [L.ACT_SILU, L.ACT_GELU, L.ACT_GELU_TANH])
+@pytest.mark.parametrize("is_gated", [0, 1])
+@pytest.mark.parametrize("M", [3, 300])
+def test_kept_sums_of_rows_next_to_the_largest_float(ops, M, act, is_gated):
+    """A row's scale times the power of two of sums kept in fp16 can pass fp32 where z does not: sums of few bits, exact in either form,
+    give the same gradients in both."""
+    rng = np.random.default_rng(M)
+    N, K = 64, 4096
+    W = Weights(rng, N, K, True)
+    W.w = rng.integers(-7, 8, W.w.shape, dtype=np.int8)
+    W.sw[:] = 2.0 ** -126
+    layer = W.layer(ops).with_gradient()
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    x[:, 0] = 2.0 ** 125  # (a scale of 2^118.01; sums of 127 times 0 to 7, below 2^9.8; the power of two is 2^10)
+    wide = N // 2 if is_gated else N
+    dy, got = rows(rng, M, wide, "f32"), []
+    for pre_type, kept in ((L.FT_F16, torch.float16), (L.FT_F32, torch.float32)):
+        y, pre, sx = torch.empty(M, wide, device="cuda"), torch.zeros(M, N, dtype=kept, device="cuda"), torch.empty(M, device="cuda")
+        d = L.LayerDesc(x.data_ptr(), K, None, layer.w.data_ptr(), K, layer.w_scale.data_ptr(), layer.bias.data_ptr(), None, 0, y.data_ptr(), wide,
+                        pre.data_ptr(), sx.data_ptr(), M, N, K, L.FT_BF16, L.FT_F32, act, is_gated, pre_type, 0.0)
+        F.fxpq_layer_forward(d, torch.empty(F.fxpq_layer_workspace(d), dtype=torch.uint8, device="cuda"))
+        assert bool(y.isfinite().all())
+        dx = torch.empty(M, K, device="cuda")
+        g = L.LayerGradDesc(dy.data_ptr(), wide, pre.data_ptr(), sx.data_ptr(), layer.w_scale.data_ptr(), layer.bias.data_ptr(),
+                            layer.wt.data_ptr(), layer.wt.stride(0), dx.data_ptr(), K, M, N, K, L.FT_F32, L.FT_F32, act, is_gated, pre_type, 0)
+        F.fxpq_layer_gradient(g, torch.empty(F.fxpq_layer_gradient_workspace(g), dtype=torch.uint8, device="cuda"))
+        got.append(dx)
+    assert bool(got[1].isfinite().all()) and bool((got[1] != 0).any()) and torch.equal(*got)
