@@ -520,23 +520,19 @@ fxpq_status launch_few(FewArgs& P, cudaStream_t st) {
     // each left one for a second round (251 x 1001 of 4090: 19.4 us, 13.3 with clusters of 4).
     int shares = 1;
     for (; shares < 8 && P.n_kb >= (tn * tm * shares * 4 <= num_sms() ? 8 : 16) * shares; shares *= 2) {
-        static std::atomic<int> room[9][4];  // clusters that run at once, by tile width and size, asked for once
-        const int w = P.cols / 16, l = shares == 1 ? 1 : shares == 2 ? 2 : 3;
-        int n = room[w][l].load(std::memory_order_relaxed);
-        if (n == 0) {
-            at[1].val.clusterDim.x = 2 * shares;
-            c.gridDim = dim3(2 * shares, 1024, 1);
-            (void)two_fit(2 * shares);
-            c.dynamicSmemBytes = smem_for(2 * shares);
-            c.numAttrs = 2;
-            if (cudaOccupancyMaxActiveClusters(&n, kernel, &c) != cudaSuccess || n <= 0) {
-                (void)cudaGetLastError();
-                n = -1;
-            }
-            room[w][l].store(n, std::memory_order_relaxed);
-        }
+        const int blocks = (P.n_kb + 2 * shares - 1) / (2 * shares), l = shares == 1 ? 1 : shares == 2 ? 2 : 3;
+        if (TOK == FLOATS && blocks > LF_MOST) continue;  // (no CTA holds their codes)
+        // By what their shared memory goes by: tile width, or floats' groups of rows and blocks of a share; and by their size.
+        static std::atomic<int> room[TOK == FLOATS ? 2 * (LF_MOST + 1) : 9][4][DEVICES];
+        const int w = TOK == FLOATS ? (P.rows > 8 ? LF_MOST + 1 : 0) + blocks : P.cols / 16;
+        const bool two = two_fit(2 * shares);
+        at[1].val.clusterDim.x = 2 * shares;
+        c.gridDim = dim3(2 * shares, 1024, 1);
+        c.dynamicSmemBytes = smem_for(2 * shares);
+        c.numAttrs = 2;
+        const int n = clusters_at_once(kernel, c, room[w][l]);
         // (the query counts one CTA to an SM: it says 15 clusters of 8 where 32 of two CTAs to an SM ran at once)
-        if (tn * tm > (two_fit(2 * shares) ? 2 * n + 2 : n)) break;
+        if (tn * tm > (two ? 2 * n + 2 : n)) break;
     }
     if (TOK == FLOATS)
         while (P.n_kb > LF_MOST * shares) shares *= 2;

@@ -703,6 +703,24 @@ bool allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& set, int regs =
     return true;
 }
 
+// Clusters of c that run at once on the current device, at least one, or -1.  Asked for once on each device (the call takes some us): a `known`, zeros at
+// first, belongs to one kernel, cluster size and amount of shared memory, for a choice may rest on sizes alone, not on the calls before.
+constexpr int DEVICES = 16;
+template <typename Kernel>
+int clusters_at_once(Kernel kernel, const cudaLaunchConfig_t& c, std::atomic<int> (&known)[DEVICES]) {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return -1;
+    if (dev < DEVICES) n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &c) != cudaSuccess || n <= 0) {
+            (void)cudaGetLastError();
+            n = -1;
+        }
+        if (dev < DEVICES) known[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 template <int NT, int EPI, int FORM>
 fxpq_status launch_many(ManyArgs& P, cudaStream_t st) {
     const auto kernel = linear_many_kernel<NT, EPI, FORM>;
