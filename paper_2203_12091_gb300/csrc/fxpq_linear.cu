@@ -392,12 +392,8 @@ __global__ void __launch_bounds__(LS_THREADS) linear_few_kernel(const __grid_con
 
 template <bool HALF>
 fxpq_status launch_few(LinArgs& P, cudaStream_t st) {
-    static bool set = false;
-    if (!set) {
-        if (cudaFuncSetAttribute(linear_few_kernel<HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, ls_smem(128, 4, HALF)) != cudaSuccess)
-            return FXPQ_ERR_CUDA;
-        set = true;
-    }
+    static std::atomic<uint64_t> set{0};
+    if (!allow_smem(linear_few_kernel<HALF>, ls_smem(128, 4, HALF), set)) return FXPQ_ERR_CUDA;
     const long long tn = (P.N + 127) / 128, tm = (P.M + P.rows - 1) / P.rows;
     if (tn > 65535 || tm > 65535) return FXPQ_ERR_UNSUPPORTED;
     P.stages = P.cols <= 32 || P.cols > 64 ? 4 : 3;
@@ -416,19 +412,11 @@ fxpq_status launch_few(LinArgs& P, cudaStream_t st) {
     // each left one for a second round (251 x 1001 of 4090: 19.4 us, 13.3 with clusters of 4).
     int shares = 1;
     for (; shares < 8 && P.n_kb >= (tn * tm * shares * 4 <= num_sms() ? 8 : 16) * shares; shares *= 2) {
-        static std::atomic<int> room[2][9][4];  // clusters that run at once, by tile width and size, asked for once
-        const int w = P.cols / 16, l = shares == 1 ? 1 : shares == 2 ? 2 : 3;
-        int n = room[HALF][w][l].load(std::memory_order_relaxed);
-        if (n == 0) {
-            at[1].val.clusterDim.x = 2 * shares;
-            c.gridDim = dim3(2 * shares, 1024, 1);
-            c.numAttrs = 2;
-            if (cudaOccupancyMaxActiveClusters(&n, linear_few_kernel<HALF>, &c) != cudaSuccess || n <= 0) {
-                (void)cudaGetLastError();
-                n = -1;
-            }
-            room[HALF][w][l].store(n, std::memory_order_relaxed);
-        }
+        static std::atomic<int> room[9][4][DEVICES];  // by tile width and cluster size
+        at[1].val.clusterDim.x = 2 * shares;
+        c.gridDim = dim3(2 * shares, 1024, 1);
+        c.numAttrs = 2;
+        const int n = clusters_at_once(linear_few_kernel<HALF>, c, room[P.cols / 16][shares == 1 ? 1 : shares == 2 ? 2 : 3]);
         // (the query counts one CTA to an SM: it says 15 clusters of 8 where 32 of two CTAs to an SM ran at once)
         if (tn * tm > (P.cols <= 64 ? 2 * n + 2 : n)) break;
     }
