@@ -110,6 +110,8 @@ def _check_layer(name, w, w_scale, bias, K):
     _want(f"{name}: w_scale", w_scale, _f32, 1)
     if bias is not None:
         _want(f"{name}: bias", bias, _f32, 1)
+    if w_scale.device != w.device or (bias is not None and bias.device != w.device):
+        raise ValueError(f"{name}: weights, scales and biases must be on one device")
     if w_scale.shape[0] != w.shape[0] or (bias is not None and bias.shape[0] != w.shape[0]):
         raise ValueError(f"{name}: one scale and bias for each channel are needed")
 
@@ -295,6 +297,11 @@ class Linear8(_Layer8):
         if x.requires_grad:
             _no_grad("Linear8", x)
         rows = _float_rows("Linear8", x)
+        if x.device != self.w.device:
+            raise ValueError(f"Linear8: rows and weights must be on one device, rows are on {x.device}, weights on {self.w.device}")
+        if x.device.index != torch.cuda.current_device():
+            with torch.cuda.device(x.device):  # (its current stream)
+                return self(x, out_dtype)
         M, K = rows.shape
         if K != self.K:
             raise ValueError(f"Linear8: rows of {self.K} values are needed, got {tuple(x.shape)}")

@@ -170,3 +170,74 @@ def test_gradient_refuses_workspaces(lib):
 def test_unknown_activations_are_refused(name):
     with pytest.raises(ValueError):
         llm._activation("layer", name)
+
+
+class OnDevice:
+    """As much of a CUDA tensor as the checks look at."""
+    requires_grad = False
+    is_cuda = True
+
+    def __init__(self, shape, dtype, index):
+        self.shape, self.dtype, self.device, self.nbytes = torch.Size(shape), dtype, torch.device("cuda", index), 0
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, i=None):
+        s = (*self.shape[1:], 1)
+        return s if i is None else s[i]
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 4096
+
+    def detach(self):
+        return self
+
+
+def test_a_layers_tensors_are_on_one_device():
+    w, scale = OnDevice((32, 64), torch.int8, 1), OnDevice((32,), torch.float32, 1)
+    llm._check_layer("layer", w, scale, scale, 64)
+    for bad in ((w, OnDevice((32,), torch.float32, 0), None), (w, scale, OnDevice((32,), torch.float32, 0))):
+        with pytest.raises(ValueError):
+            llm._check_layer("layer", *bad, 64)
+        with pytest.raises(ValueError):
+            llm.Linear8(*bad)
+    with pytest.raises(ValueError):
+        llm.GatedLinear8(w, scale, w, OnDevice((32,), torch.float32, 0))
+
+
+def test_rows_on_another_device(monkeypatch):
+    """Rows on another device than the weights are refused; on another than the current one the call is made there."""
+    current, calls = [0], []
+
+    class Device:
+        def __init__(self, device):
+            self.to = device.index
+
+        def __enter__(self):
+            self.was, current[0] = current[0], self.to
+
+        def __exit__(self, *_):
+            current[0] = self.was
+
+    class Lib:
+        def fxpq_linear_tokens_workspace(self, *_):
+            return 0
+
+        def fxpq_linear_tokens(self, *_):
+            calls.append(current[0])
+            return 0
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(L, "lib", Lib)
+    monkeypatch.setattr(llm.F, "_s", lambda _: 0)
+    monkeypatch.setattr(llm, "_empty", lambda shape, dtype, device: OnDevice(shape if isinstance(shape, tuple) else (shape,), dtype, device.index))
+    layer = llm.Linear8(OnDevice((32, 64), torch.int8, 1), OnDevice((32,), torch.float32, 1))
+    y = layer(OnDevice((5, 64), torch.float32, 1))
+    assert y.shape == (5, 32) and y.device.index == 1 and calls == [1] and current == [0]
+    with pytest.raises(ValueError):
+        layer(OnDevice((5, 64), torch.float32, 0))
+    assert calls == [1]
