@@ -679,3 +679,18 @@ def test_kept_sums_of_any_type_with_a_gradient_of_any(ops, N, is_gated, dx_type)
             F.fxpq_layer_gradient(g, torch.empty(F.fxpq_layer_gradient_workspace(g), dtype=torch.uint8, device="cuda"))
             got.append(dx)
         assert torch.equal(*got) and bool(got[0].isfinite().all()) and bool((got[0] != 0).any())
+
+
+@pytest.mark.parametrize("M,K", [(1, 32768), (1, 32769), (2, 16384), (2, 16385), (3, 10922), (3, 10923), (4, 8192), (8, 4096), (8, 4097), (9, 1820),
+                                 (9, 1821), (16, 1024), (16, 1025), (13, 1260), (5, 6553), (1, 16896)])
+@pytest.mark.parametrize("x", ["bf16", "f16", "f32"])
+def test_both_sides_of_the_rule_for_rows_whose_codes_the_product_forms(ops, M, K, x):
+    """At most 32768 values of up to 8 rows, or 16384 of up to 16: the last size of that form, the first of the other, and shares of 32 blocks."""
+    rng = np.random.default_rng(M + K)
+    need = F.fxpq_layer_workspace(L.LayerDesc(None, K, None, None, (K + 15) // 16 * 16, None, None, None, 0, None, 130, None, None, M, 130, K, L.FT_BF16,
+                                              L.FT_BF16, L.ACT_RELU, 0, L.FT_F16, 0.0))
+    assert (need == 0) == (M * K <= (32768 if M <= 8 else 16384))
+    for N in (130, 512):
+        check_layer(ops, rng, M, N, K, x, "f32", "silu", True, True, True)
+        check_layer(ops, rng, M, N, K, x, "bf16", None, False, False, True)
+        check_gated(ops, rng, M, N // 2, K, x, "bf16", "silu", True, False)

@@ -120,3 +120,12 @@ def test_the_kernel_waits_in_that_order():
     src = open(SRC).read()
     converters = src[src.index("const int grp = "):]
     assert converters.index("wait_warp(conv_empty + 8 * c.at") < converters.index("wait_warp(raw_full + 8 * s.at, s.phase")
+
+
+def test_what_would_not_do():
+    """Each of the comment's conditions by itself: more operands than stages fail although the waits are in order, and as many fail with the
+    copy waited for first but not in order."""
+    rng = random.Random(1)
+    assert not all(simulate(rng, 3, 4, 30, False) for _ in range(3000))
+    assert not all(simulate(rng, 3, 3, 30, False, empty_first=False) for _ in range(3000))
+    assert all(simulate(rng, 3, 3, 30, False) for _ in range(3000))
