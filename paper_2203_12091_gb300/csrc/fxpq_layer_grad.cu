@@ -56,10 +56,10 @@ struct Words {
 // fp16, as are its products' sums below 2^24), and what h leaves of v (up to 2^11, to 2^-12 of itself), M rows further on.  So a value
 // loses 2^-23 of the row's largest at most, or 2^-12 of its own size where that is less.  (In one part of 11 bits gradients of 16 bits came
 // out 3e-4 to 1e-3 from those of 32-bit products, in their last places.)
-// Bytes bound it (dy and the sums in, the row out): 8192 rows of 2 x 5632 460 MB, 68 us.  Rows stay in registers between their maximum
+// Bytes bound it (dy and the sums in, both parts out): 8192 rows of 2 x 5632 830 MB, 125 us, 6.6 TB/s.  Rows stay in registers between their maximum
 // and the rounding, GR_KEEP groups of eight channels a thread, which are also on their way together; what does not fit, the last
-// group of some, and all of constants or sums that are not aligned, is formed again.  (A group at a time, kept in shared memory, the same rows took 185 us.)
-// ALL: every group is kept; without the code for the others, and what it holds of registers, those rows took 94 us, not 107.
+// group of some, and all of constants or sums that are not aligned, is formed again.  (A group at a time, kept in shared memory, the rows took
+// twice as long.)  ALL: every group is kept; with the code for the others, and what it holds of registers, those rows took 158 us.
 constexpr int GR_KEEP = 3;
 template <bool GATE, int ACT, int DY, int PRE, int GR_THREADS, bool ALL>
 __global__ void __launch_bounds__(GR_THREADS, 1024 / GR_THREADS) grad_rows_kernel(const __grid_constant__ GradRows G, int y_type) {
@@ -213,17 +213,17 @@ fxpq_status grad_rows(const GradRows& G, int y_type, int gated, cudaStream_t st)
             const auto run = [&](auto dy, auto pre) {
                 constexpr int DY = decltype(dy)::value, PRE = decltype(pre)::value;
                 constexpr bool NEEDS = GATE || ACT != FXPQ_ACT_NONE;
-                const bool fits = DY == 2 && PRE == 2 && G.N % 8 == 0 && G.N <= 8 * GR_KEEP * 1024 &&
+                const bool fits = DY == 2 && G.N % 8 == 0 && G.N <= 8 * GR_KEEP * 1024 &&
                                   (G.vec | 1 | (NEEDS ? 0 : 2) | (G.bias ? 0 : 8)) == 15;
                 const auto go = [&](auto threads) {
                     constexpr int THREADS = decltype(threads)::value;
                     const auto with = [&](auto kernel) { launch_pdl(kernel, dim3((unsigned)G.M), dim3(THREADS), 0, st, G, y_type); };
-                    if constexpr (DY == 2 && PRE == 2)
+                    if constexpr (DY == 2)
                         if (fits) return with(grad_rows_kernel<GATE, ACT, DY, PRE, THREADS, true>);
                     if constexpr (THREADS <= 512) with(grad_rows_kernel<GATE, ACT, DY, PRE, THREADS, false>);
                 };
-                // As many threads as the row's groups need, so that more rows are under way (3990 rows of 549 channels 54 us with 512), or all
-                // there are where that keeps the row (7999 rows of 22400: 231 us, with 512 and the rest formed again 254).
+                // As many threads as the row's groups need, so that more rows are under way (3990 rows of 549 channels in fp32: 12 us), or all
+                // there are where that keeps the row (7999 rows of 22400: 293 us, with 512 and the rest formed again a tenth more).
                 if (G.N <= 8 * GR_KEEP * 128)
                     go(std::integral_constant<int, 128>());
                 else if (G.N <= 8 * GR_KEEP * 256)
@@ -235,10 +235,12 @@ fxpq_status grad_rows(const GradRows& G, int y_type, int gated, cudaStream_t st)
             };
             using Two = std::integral_constant<int, 2>;
             using Four = std::integral_constant<int, 4>;
-            if (y_type == FXPQ_FT_F32)
-                G.pre_f32 ? run(Four(), Four()) : run(Four(), Two());
-            else
-                G.pre_f32 ? run(Two(), Four()) : run(Two(), Two());
+            const auto kept = [&](auto dy) {
+                if constexpr (GATE || ACT != FXPQ_ACT_NONE)  // (else none are read)
+                    if (G.pre_f32) return run(dy, Four());
+                run(dy, Two());
+            };
+            y_type == FXPQ_FT_F32 ? kept(Four()) : kept(Two());
         };
         if (!gated) return sized(std::false_type());
         if constexpr (ACT != FXPQ_ACT_NONE) sized(std::true_type());
