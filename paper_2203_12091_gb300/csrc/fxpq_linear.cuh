@@ -66,10 +66,6 @@ __device__ __forceinline__ void store_some(void* p, int type, long long at, cons
             if (i < count) store_y(p, type, at + i, v[i]);
     }
 }
-__device__ __forceinline__ float load_y(const void* p, int type, long long at) {
-    return type == FXPQ_FT_F32 ? static_cast<const float*>(p)[at]
-                               : type == FXPQ_FT_F16 ? __half2float(static_cast<const __half*>(p)[at]) : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]);
-}
 __device__ __forceinline__ float2 pair_f32(uint32_t w, int type) {
     return type == FXPQ_FT_F16 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w));
 }
