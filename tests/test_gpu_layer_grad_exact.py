@@ -178,3 +178,26 @@ def test_kept_sums_of_rows_next_to_the_largest_float(ops, M, act, is_gated):
         F.fxpq_layer_gradient(g, torch.empty(F.fxpq_layer_gradient_workspace(g), dtype=torch.uint8, device="cuda"))
         got.append(dx)
     assert bool(got[1].isfinite().all()) and bool((got[1] != 0).any()) and torch.equal(*got)
+
+
+@pytest.mark.parametrize("M,N,K,x", [(239, 1462, 158, "bf16"), (464, 180, 2700, "f16"), (1638, 153, 1064, "bf16"), (712, 1055, 3173, "bf16"), (224, 6872, 2541, "f16"),
+                                     (599, 1128, 4017, "f32"), (819, 3243, 1427, "f32"), (1605, 3787, 691, "bf16"), (3000, 4000, 1000, "bf16"),
+                                     (1659, 204, 646, "f32"), (80, 8000, 6000, "f32"), (130, 8192, 4096, "bf16")])
+def test_both_parts_in_the_tiles_of_pairs(ops, M, N, K, x):
+    """Tiles of either width, reductions split and whole, rows and channels past the last tile's, outputs in pairs and one by one: into rows
+    with a stride of their own, of which nothing else is written."""
+    rng = np.random.default_rng(M)
+    W = Weights(rng, N, K, False)
+    W.w = rng.integers(-1, 2, W.w.shape, dtype=np.int8)
+    W.sw *= np.float32(100)
+    layer = W.layer(ops).with_gradient()
+    dy = rows(rng, M, N, "f32")
+    dy[M // 2] = 0
+    out = torch.full((M + 3, K + 6), 7.0, dtype=TYPES[x], device="cuda")
+    g = L.LayerGradDesc(dy.data_ptr(), N, None, None, layer.w_scale.data_ptr(), None, layer.wt.data_ptr(), layer.wt.stride(0), out.data_ptr(), K + 6, M, N, K,
+                        L.FT_F32, {"f32": L.FT_F32, "f16": L.FT_F16, "bf16": L.FT_BF16}[x], L.ACT_NONE, 0, L.FT_F32, 0)
+    F.fxpq_layer_gradient(g, torch.empty(F.fxpq_layer_gradient_workspace(g), dtype=torch.uint8, device="cuda"))
+    check_rows(out[:M, :K], host(dy), 0.0 * host(dy), W, x)
+    assert bool((out[M:] == 7).all()) and bool((out[:, K:] == 7).all())
+    leaf = rows(rng, M, K, x).requires_grad_()
+    assert torch.equal(torch.autograd.grad(layer(leaf, torch.float32), leaf, dy)[0], out[:M, :K])
